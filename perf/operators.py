@@ -123,7 +123,10 @@ def _quantise(x):
     lo, hi = g.amin(-1).clamp(max=0.0), g.amax(-1).clamp(min=0.0)
     # the divisor as a tensor: torch multiplies by the reciprocal of a number, which is not the same
     bits = ((hi * 0.5 - lo * 0.5) / torch.full_like(lo, 7.5)).view(torch.int32)
-    s = ((bits + 0xFFFFF) & -0x100000).view(torch.float32).clamp(min=2.0 ** -126)
+    bits = (bits + 0xFFFFF) & -0x100000
+    # one step up where a difference that float rounds off leaves hi - lo above 15 s
+    bits += (hi * 0.5 - bits.view(torch.float32) * 7.5 > lo * 0.5).int() << 20
+    s = bits.view(torch.float32).clamp(min=2.0 ** -126)
     z = torch.round(-lo / s)
     c = (torch.round(g / s[..., None]) + z[..., None]).clamp(0, 15)
     c = torch.where(finite[..., None], c, torch.zeros_like(c)).to(torch.uint8).flatten(-2).unflatten(-1, (-1, 8))
