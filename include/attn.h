@@ -412,6 +412,64 @@ int attn_w4bf16_gemm(const void* w_tiles, const uint16_t* x, int T, int N, int K
  * when K is not a positive multiple of 128 or too large to stage (host only). */
 int attn_w4bf16_rows_per_launch(int K);
 
+/*
+ * The 4-bit KV cache (no counterpart in the paper, whose caches are bf16; its weights are at 4 bits, and at
+ * long histories the cache is what a decode step reads): 4.5 bits per value instead of 16, for the
+ * stages of a context.  The D values of a slot are quantised in groups of 32.  A group x has
+ *   lo = min(x, 0), hi = max(x, 0)
+ *   s  = the smallest number of 4 significant bits that is >= (hi - lo) / 15, at least 2^-126
+ *   z  = rint(-lo / s), c = min(max(rint(x / s) + z, 0), 15)     (ties to even)
+ * and stands for (c - z) s, which is a bf16 exactly (infinite where that passes the largest bf16, from |x|
+ * of about 2^127).  A group with an infinity or a NaN has c = z = 0 and s = NaN: it reads as NaN.  Device
+ * memory of the caller, 16-byte aligned, Lp = attn_kv4_slots(max_len) slots:
+ *   k_codes, v_codes    [batch][n_kv_heads][Lp][head_dim / 2] bytes: little-endian 32-bit words of 8
+ *                       values, the code of value j at bit (0, 16, 4, 20, 8, 24, 12, 28)[j];
+ *   k_scales, v_scales  [batch][n_kv_heads][Lp][head_dim / 32]: s as a bf16, whose four lowest bits are
+ *                       zero, with z in their place.
+ * Keys are quantised after RoPE, from the bf16 that the bf16 cache would hold (attn_prefill_kv, attn_decode).
+ * Whatever attends to a token sees the values its slot stands for, the token itself included, so
+ * a prompt's outputs do not depend on how it is cut into chunks (up to the order of float sums).  Slots past
+ * the tokens written may hold anything.  The calls enqueue on `stream`, allocate nothing and use the
+ * context's scratch as the other stages do.
+ */
+typedef struct attn_kv4 {
+    uint8_t* k_codes;
+    uint16_t* k_scales;
+    uint8_t* v_codes;
+    uint16_t* v_scales;
+} attn_kv4;
+
+/* Slots per (sequence, kv head) of a 4-bit cache: max_len rounded up to a multiple of 64; 0 for a max_len that
+ * no context has (host only). */
+int attn_kv4_slots(int max_len);
+
+/* Quantise chunk_len new tokens (k, v [batch][chunk_len][n_kv_heads][head_dim], k before RoPE) into slots
+ * hist_len .. hist_len + chunk_len - 1 of every sequence; no other slot is written.  hist_len >= 0, chunk_len
+ * >= 1, hist_len + chunk_len <= max_len.  Returns ATTN_OK, ATTN_EINVAL or ATTN_ECUDA. */
+int attn_kv4_append(attn_ctx* ctx, const uint16_t* k, const uint16_t* v, int hist_len, int chunk_len,
+                    const attn_kv4* cache, attn_stream_t stream);
+
+/* The values of slots first .. first + count - 1 as bf16: k, v [batch][n_kv_heads][count][head_dim], 16-byte
+ * aligned.  first, count >= 0, first + count <= max_len; nothing is enqueued for count 0. */
+int attn_kv4_read(attn_ctx* ctx, const attn_kv4* cache, int first, int count, uint16_t* k, uint16_t* v,
+                  attn_stream_t stream);
+
+/* attn_decode_multi over a 4-bit cache: n_new (1 .. 16) tokens per sequence at positions d_hist_len[b] + i are
+ * quantised into their slots and attend to slots [0, d_hist_len[b] + i].  A sequence with a position
+ * outside [0, max_len - 1] is skipped (cache and out not written) and sets ATTN_DEVERR_HIST_RANGE.  The other
+ * arguments and the errors are those of attn_decode_multi. */
+int attn_kv4_decode(attn_ctx* ctx, const uint16_t* q, const uint16_t* k, const uint16_t* v,
+                    const int32_t* d_hist_len, int n_new, const attn_kv4* cache, uint16_t* out, attn_stream_t stream);
+
+/* attn_prefill_kv over a 4-bit cache (hist_len = 0: a prefill): the chunk is quantised into its slots and attends
+ * causally to slots [0, hist_len + i].  workspace: device memory of at least attn_kv4_workspace(ctx,
+ * hist_len + chunk_len) bytes, 256-byte aligned, which holds the bf16 values of those slots during the call
+ * (one workspace serves every layer).  The other arguments and the errors are those of attn_prefill_kv. */
+size_t attn_kv4_workspace(const attn_ctx* ctx, int tokens);
+int attn_kv4_prefill_kv(attn_ctx* ctx, const uint16_t* q, const uint16_t* k, const uint16_t* v, int hist_len,
+                        int chunk_len, const attn_kv4* cache, uint16_t* out, void* workspace, size_t workspace_bytes,
+                        attn_stream_t stream);
+
 /* Static text for an ATTN_* code. */
 const char* attn_strerror(int code);
 

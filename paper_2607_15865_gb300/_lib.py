@@ -22,7 +22,8 @@ EXPORTED = ("attn_create", "attn_destroy", "attn_prefill", "attn_prefill_kv", "a
             "attn_timing_enable", "attn_timing_read",
             "attn_strerror", "attn_last_cuda_error_string", "attn_decode_noalloc", "attn_w4bf16_gemv",
             "attn_w4bf16_rows_per_launch", "attn_w4bf16_gemv_fused", "attn_decode_layer",
-            "attn_w4bf16_gemm", "attn_prefill_layer", "attn_prefill_layer_workspace")
+            "attn_w4bf16_gemm", "attn_prefill_layer", "attn_prefill_layer_workspace", "attn_kv4_slots",
+            "attn_kv4_append", "attn_kv4_read", "attn_kv4_decode", "attn_kv4_workspace", "attn_kv4_prefill_kv")
 NOALLOC_SCRATCH_FLOATS = 1 << 20
 # attn_timing_read's slots; no kernel runs as decode_combine (the decode merges itself): it reads 0
 KERNELS = ("rope_append", "flash_fwd", "decode_split", "decode_combine")
@@ -31,6 +32,11 @@ KERNELS = ("rope_append", "flash_fwd", "decode_split", "decode_combine")
 class AttnCfg(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int), ("n_q_heads", ctypes.c_int), ("n_kv_heads", ctypes.c_int),
                 ("head_dim", ctypes.c_int), ("max_len", ctypes.c_int), ("rope_theta", ctypes.c_double)]
+
+
+class AttnKv4(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p)]
 
 
 class AttnError(RuntimeError):
@@ -100,6 +106,19 @@ def load(path: str = LIB_PATH):
     lib.attn_w4bf16_gemm.restype = i32
     lib.attn_w4bf16_rows_per_launch.argtypes = [i32]
     lib.attn_w4bf16_rows_per_launch.restype = i32
+    kv4 = ctypes.POINTER(AttnKv4)
+    lib.attn_kv4_slots.argtypes = [i32]
+    lib.attn_kv4_slots.restype = i32
+    lib.attn_kv4_append.argtypes = [vp, u16p, u16p, i32, i32, kv4, vp]
+    lib.attn_kv4_append.restype = i32
+    lib.attn_kv4_read.argtypes = [vp, kv4, i32, i32, u16p, u16p, vp]
+    lib.attn_kv4_read.restype = i32
+    lib.attn_kv4_decode.argtypes = [vp, u16p, u16p, u16p, vp, i32, kv4, u16p, vp]
+    lib.attn_kv4_decode.restype = i32
+    lib.attn_kv4_workspace.argtypes = [vp, i32]
+    lib.attn_kv4_workspace.restype = ctypes.c_size_t
+    lib.attn_kv4_prefill_kv.argtypes = [vp, u16p, u16p, u16p, i32, i32, kv4, u16p, vp, ctypes.c_size_t, vp]
+    lib.attn_kv4_prefill_kv.restype = i32
     lib.attn_strerror.argtypes = [i32]
     lib.attn_strerror.restype = ctypes.c_char_p
     lib.attn_last_cuda_error_string.argtypes = []

@@ -12,6 +12,8 @@ and the stage driver of Sections 4.1 and 4.5:
   prompt        a prompt of any length in segments: 1 prefill (or prefill_kv) + N prefill_kv
   decode_steps  n decode steps in a row, step t at positions hist_len + t (step-major inputs)
 
+and the stages over a cache held in 4 bits (kv4.Kv4Cache): kv4_append, kv4_read, kv4_decode, kv4_prefill_kv.
+
 Caches are [B,Hkv,L,D] bf16 tensors owned by the caller and updated in place.
 All calls are asynchronous on the given (default: current) torch CUDA stream.
 """
@@ -22,6 +24,7 @@ import ctypes
 import torch
 
 from . import _lib
+from .kv4 import Kv4Cache
 
 _BF16_LIKE = (torch.bfloat16, torch.int16, torch.uint16)
 
@@ -240,6 +243,75 @@ class Attention:
                                         _ptr(v_cache, "v_cache", self._cache_shape()), _ptr(out, "out", qs),
                                         _stream(stream))
         self._check(rc, "attn_decode_steps")
+        return out
+
+    def kv4_cache(self, device="cuda") -> Kv4Cache:
+        """An empty (zeroed) 4-bit cache of this context's shape."""
+        return Kv4Cache.empty(self.batch, self.n_kv_heads, self.max_len, self.head_dim, device)
+
+    def _kv4(self, cache):
+        if not isinstance(cache, Kv4Cache):
+            raise TypeError("cache must be a Kv4Cache")
+        if cache.shape != self._cache:
+            raise ValueError(f"cache is for [B, Hkv, max_len, D] = {cache.shape}, expected {self._cache}")
+        return cache.ref
+
+    def kv4_append(self, k, v, hist_len: int, cache, stream=None) -> None:
+        """Quantise new tokens k, v [B,S,Hkv,D] (k before RoPE) into slots hist_len .. hist_len + S - 1."""
+        S = k.shape[1]
+        ks = (self.batch, S, self.n_kv_heads, self.head_dim)
+        rc = self.lib.attn_kv4_append(self._ctx, _ptr(k, "k", ks), _ptr(v, "v", ks), int(hist_len), S,
+                                      self._kv4(cache), _stream(stream))
+        self._check(rc, "attn_kv4_append")
+
+    def kv4_read(self, cache, first: int = 0, count: int | None = None, out=None, stream=None):
+        """The bf16 values (k, v), each [B,Hkv,count,D], of slots first .. first + count - 1 (default: all from
+        first on).  out: a pair of such tensors to write to."""
+        count = self.max_len - int(first) if count is None else int(count)
+        ref = self._kv4(cache)
+        shape = (self.batch, self.n_kv_heads, max(count, 0), self.head_dim)
+        if out is None:
+            out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=cache.k_codes.device) for _ in range(2))
+        k, v = out
+        rc = self.lib.attn_kv4_read(self._ctx, ref, int(first), count, _ptr(k, "k", shape), _ptr(v, "v", shape),
+                                    _stream(stream))
+        self._check(rc, "attn_kv4_read")
+        return out
+
+    def kv4_decode(self, q, k, v, hist_len: torch.Tensor, cache, out=None, stream=None) -> torch.Tensor:
+        """decode / decode_multi over a 4-bit cache: n = q.shape[1] (1 .. 16) new tokens per sequence."""
+        n = q.shape[1]
+        qs = (self.batch, n, self.n_q_heads, self.head_dim)
+        ks = (self.batch, n, self.n_kv_heads, self.head_dim)
+        if not _is_len(hist_len, self.batch):
+            raise TypeError("hist_len must be a contiguous int32 CUDA tensor of shape [batch]")
+        out = self._new_out(q, out)
+        rc = self.lib.attn_kv4_decode(self._ctx, _ptr(q, "q", qs), _ptr(k, "k", ks), _ptr(v, "v", ks),
+                                      hist_len.data_ptr(), n, self._kv4(cache), _ptr(out, "out", qs), _stream(stream))
+        self._check(rc, "attn_kv4_decode")
+        return out
+
+    def kv4_workspace(self, tokens: int) -> int:
+        """Bytes of device workspace kv4_prefill_kv needs for hist_len + chunk = tokens (host only)."""
+        return int(self.lib.attn_kv4_workspace(self._ctx, int(tokens)))
+
+    def kv4_prefill_kv(self, q, k, v, hist_len: int, cache, workspace=None, out=None, stream=None) -> torch.Tensor:
+        """prefill_kv (hist_len = 0: prefill) over a 4-bit cache.  workspace: a uint8 CUDA tensor of at least
+        kv4_workspace(hist_len + S) bytes (allocated here when None)."""
+        S = q.shape[1]
+        qs = (self.batch, S, self.n_q_heads, self.head_dim)
+        ks = (self.batch, S, self.n_kv_heads, self.head_dim)
+        args = (_ptr(q, "q", qs), _ptr(k, "k", ks), _ptr(v, "v", ks))
+        need = self.kv4_workspace(int(hist_len) + S)
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        if not (isinstance(workspace, torch.Tensor) and workspace.is_cuda and workspace.dtype == torch.uint8
+                and workspace.is_contiguous() and workspace.numel() >= need):
+            raise TypeError(f"workspace must be a contiguous uint8 CUDA tensor of at least {need} bytes")
+        out = self._new_out(q, out)
+        rc = self.lib.attn_kv4_prefill_kv(self._ctx, *args, int(hist_len), S, self._kv4(cache), _ptr(out, "out", qs),
+                                          workspace.data_ptr(), workspace.numel(), _stream(stream))
+        self._check(rc, "attn_kv4_prefill_kv")
         return out
 
     def timing_enable(self, max_launches: int):

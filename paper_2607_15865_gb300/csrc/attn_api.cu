@@ -137,6 +137,42 @@ int encode_map(const attn_ctx* c, CUtensorMap* map, const void* gaddr, cuuint32_
     return ATTN_OK;
 }
 
+// The tensor maps of flash_fwd for `chunk` queries at positions hist.. over slots [0, hist + chunk) of caches
+// with `rows` slots per (sequence, kv head); ATTN_EINVAL where the chunk's work items would not fit their counters.
+int flash_maps(const attn_ctx* c, const uint16_t* q, int hist, int chunk, int seq_stride, const uint16_t* kc,
+               const uint16_t* vc, int rows, attn::FlashMaps* maps) {
+    const attn::Shape& s = c->shape;
+    // flash_fwd's work items (pairs of 128-row query tiles x query heads x sequences) are
+    // counted in int: keep them well inside it
+    if ((static_cast<long long>(chunk) + 255) / 256 * s.n_q_heads * s.batch > (1LL << 30)) return ATTN_EINVAL;
+    const cuuint64_t D = static_cast<cuuint64_t>(s.head_dim);
+    {
+        const cuuint64_t dims[4] = {D, static_cast<cuuint64_t>(s.n_q_heads), static_cast<cuuint64_t>(chunk),
+                                    static_cast<cuuint64_t>(s.batch)};
+        const cuuint64_t strides[3] = {D * 2, D * 2 * s.n_q_heads,
+                                       D * 2 * s.n_q_heads * static_cast<cuuint64_t>(seq_stride)};
+        const cuuint32_t heads = static_cast<cuuint32_t>(attn::flash_pack_heads(s, hist, chunk, c->num_sms));
+        const cuuint32_t box[4] = {64, heads, 128 / heads, 1};
+        const int rc = encode_map(c, &maps->q, q, 4, dims, strides, box);
+        if (rc != ATTN_OK) return rc;
+    }
+    const cuuint64_t dims[3] = {D, static_cast<cuuint64_t>(hist + chunk),
+                                static_cast<cuuint64_t>(s.batch) * s.n_kv_heads};
+    const cuuint64_t strides[2] = {D * 2, D * 2 * static_cast<cuuint64_t>(rows)};
+    const cuuint32_t box[3] = {64, 128, 1};
+    const int rc = encode_map(c, &maps->k, kc, 3, dims, strides, box);
+    return rc == ATTN_OK ? encode_map(c, &maps->v, vc, 3, dims, strides, box) : rc;
+}
+
+int run_flash(attn_ctx* c, const attn::FlashMaps& maps, int hist, int chunk, int seq_stride, uint16_t* out,
+              cudaStream_t st) {
+    const cudaError_t e = timed(c, ATTN_KERNEL_FLASH_FWD, st, [&](int* n) {
+        return attn::launch_flash_fwd(c->shape, maps, hist, chunk, seq_stride, c->d_cos_t, c->d_sin_t, out, c->d_flash_o,
+                                      c->d_flash_ml, c->d_err, c->num_sms, st, n, c->wait_ns);
+    });
+    return e == cudaSuccess ? ATTN_OK : cuda_fail(e, "flash_fwd launch");
+}
+
 // The prefill stages: validate, K1, build the maps over [0, hist+chunk), K2.  q/k/v/out
 // hold `chunk` tokens of each sequence, sequence b starting at token b * seq_stride
 // (seq_stride = chunk for a dense chunk; the prompt length for a segment of a prompt).
@@ -150,42 +186,16 @@ int run_prefill(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uint16_
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(kc) || !aligned16(vc) || !aligned16(out))
         return ATTN_EINVAL;
     const attn::Shape& s = c->shape;
-    // flash_fwd's work items (pairs of 128-row query tiles x query heads x sequences) are
-    // counted in int: keep them well inside it
-    if ((static_cast<long long>(chunk) + 255) / 256 * s.n_q_heads * s.batch > (1LL << 30)) return ATTN_EINVAL;
-    const cuuint64_t D = static_cast<cuuint64_t>(s.head_dim);
     attn::FlashMaps maps;
-    {
-        const cuuint64_t dims[4] = {D, static_cast<cuuint64_t>(s.n_q_heads), static_cast<cuuint64_t>(chunk),
-                                    static_cast<cuuint64_t>(s.batch)};
-        const cuuint64_t strides[3] = {D * 2, D * 2 * s.n_q_heads,
-                                       D * 2 * s.n_q_heads * static_cast<cuuint64_t>(seq_stride)};
-        const cuuint32_t heads = static_cast<cuuint32_t>(attn::flash_pack_heads(s, hist, chunk, c->num_sms));
-        const cuuint32_t box[4] = {64, heads, 128 / heads, 1};
-        const int rc = encode_map(c, &maps.q, q, 4, dims, strides, box);
-        if (rc != ATTN_OK) return rc;
-    }
-    {
-        const cuuint64_t dims[3] = {D, static_cast<cuuint64_t>(hist + chunk),
-                                    static_cast<cuuint64_t>(s.batch) * s.n_kv_heads};
-        const cuuint64_t strides[2] = {D * 2, D * 2 * static_cast<cuuint64_t>(s.max_len)};
-        const cuuint32_t box[3] = {64, 128, 1};
-        int rc = encode_map(c, &maps.k, kc, 3, dims, strides, box);
-        if (rc == ATTN_OK) rc = encode_map(c, &maps.v, vc, 3, dims, strides, box);
-        if (rc != ATTN_OK) return rc;
-    }
-    cudaError_t e = timed(c, ATTN_KERNEL_ROPE_APPEND, st, [&](int*) {
+    const int rc = flash_maps(c, q, hist, chunk, seq_stride, kc, vc, s.max_len, &maps);
+    if (rc != ATTN_OK) return rc;
+    const cudaError_t e = timed(c, ATTN_KERNEL_ROPE_APPEND, st, [&](int*) {
         return attn::launch_rope_append(s, k, v, hist, nullptr, chunk, seq_stride, c->d_cos, c->d_sin, c->d_cos_t,
                                         c->d_sin_t, kc, vc, c->d_err,
                                         st);
     });
     if (e != cudaSuccess) return cuda_fail(e, "rope_append launch");
-    e = timed(c, ATTN_KERNEL_FLASH_FWD, st, [&](int* n) {
-        return attn::launch_flash_fwd(s, maps, hist, chunk, seq_stride, c->d_cos_t, c->d_sin_t, out, c->d_flash_o,
-                                      c->d_flash_ml, c->d_err, c->num_sms, st, n, c->wait_ns);
-    });
-    if (e != cudaSuccess) return cuda_fail(e, "flash_fwd launch");
-    return ATTN_OK;
+    return run_flash(c, maps, hist, chunk, seq_stride, out, st);
 }
 
 }  // namespace
@@ -679,6 +689,94 @@ int attn_w4bf16_gemv(const void* w_tiles, const uint16_t* x, int M, int N, int K
                      int flags, attn_stream_t stream) {
     return attn_w4bf16_gemv_fused(w_tiles, x, M, N, K, nullptr, 0.f, nullptr, y, 0, nullptr, 0, nullptr, d_err, flags,
                                   stream);
+}
+
+// ------------------------------------------------------------------ the 4-bit cache
+
+namespace {
+
+bool kv4_ok(const attn_kv4* c) {
+    return c != nullptr && c->k_codes != nullptr && c->k_scales != nullptr && c->v_codes != nullptr &&
+           c->v_scales != nullptr && aligned16(c->k_codes) && aligned16(c->k_scales) && aligned16(c->v_codes) &&
+           aligned16(c->v_scales);
+}
+
+attn::Kv4Cache kv4_of(const attn_kv4* c) { return {c->k_codes, c->k_scales, c->v_codes, c->v_scales}; }
+
+// Bytes of one of the two bf16 copies (k, v) of `tokens` slots that the prefill over a 4-bit cache reads.
+size_t kv4_plain_bytes(const attn_cfg& cfg, int tokens) {
+    return (static_cast<size_t>(cfg.batch) * cfg.n_kv_heads * tokens * cfg.head_dim * 2 + 255) & ~static_cast<size_t>(255);
+}
+
+}  // namespace
+
+int attn_kv4_slots(int max_len) { return max_len < 1 || max_len > (1 << 20) ? 0 : attn::kv4_slots(max_len); }
+
+int attn_kv4_append(attn_ctx* c, const uint16_t* k, const uint16_t* v, int hist_len, int chunk_len,
+                    const attn_kv4* cache, attn_stream_t stream) {
+    if (c == nullptr || k == nullptr || v == nullptr || !kv4_ok(cache) || !aligned16(k) || !aligned16(v))
+        return ATTN_EINVAL;
+    if (chunk_len < 1 || hist_len < 0 || static_cast<long>(hist_len) + chunk_len > c->cfg.max_len) return ATTN_EINVAL;
+    const attn::Kv4New a{k, v, nullptr, hist_len, chunk_len, c->cfg.batch};
+    const cudaError_t e = attn::launch_kv4_append(c->shape, a, c->d_cos, c->d_sin, kv4_of(cache),
+                                                  attn::Kv4Plain{nullptr, nullptr, 0}, c->d_err,
+                                                  reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? ATTN_OK : cuda_fail(e, "kv4 append launch");
+}
+
+int attn_kv4_read(attn_ctx* c, const attn_kv4* cache, int first, int count, uint16_t* k, uint16_t* v,
+                  attn_stream_t stream) {
+    if (c == nullptr || !kv4_ok(cache) || first < 0 || count < 0 || static_cast<long>(first) + count > c->cfg.max_len)
+        return ATTN_EINVAL;
+    if (count == 0) return ATTN_OK;
+    if (k == nullptr || v == nullptr || !aligned16(k) || !aligned16(v)) return ATTN_EINVAL;
+    const cudaError_t e = attn::launch_kv4_read(c->shape, first, count, kv4_of(cache), attn::Kv4Plain{k, v, count},
+                                                reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? ATTN_OK : cuda_fail(e, "kv4 read launch");
+}
+
+int attn_kv4_decode(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uint16_t* v, const int32_t* d_hist_len,
+                    int n_new, const attn_kv4* cache, uint16_t* out, attn_stream_t stream) {
+    if (c == nullptr || q == nullptr || k == nullptr || v == nullptr || d_hist_len == nullptr || out == nullptr ||
+        !kv4_ok(cache))
+        return ATTN_EINVAL;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) ||
+        (reinterpret_cast<uintptr_t>(d_hist_len) & 3u))
+        return ATTN_EINVAL;
+    if (n_new < 1 || n_new > kMaxDraftTokens || n_new > c->cfg.max_len) return ATTN_EINVAL;
+    const cudaError_t e = attn::launch_kv4_decode(c->shape, q, k, v, d_hist_len, n_new, kv4_of(cache), c->d_cos, c->d_sin,
+                                                  out, c->d_err, reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? ATTN_OK : cuda_fail(e, "kv4 decode launch");
+}
+
+size_t attn_kv4_workspace(const attn_ctx* c, int tokens) {
+    if (c == nullptr || tokens < 1 || tokens > c->cfg.max_len) return 0;
+    return 2 * kv4_plain_bytes(c->cfg, tokens);
+}
+
+int attn_kv4_prefill_kv(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uint16_t* v, int hist_len,
+                        int chunk_len, const attn_kv4* cache, uint16_t* out, void* workspace, size_t workspace_bytes,
+                        attn_stream_t stream) {
+    if (c == nullptr || q == nullptr || k == nullptr || v == nullptr || out == nullptr || workspace == nullptr ||
+        !kv4_ok(cache))
+        return ATTN_EINVAL;
+    if (chunk_len < 1 || hist_len < 0 || static_cast<long>(hist_len) + chunk_len > c->cfg.max_len) return ATTN_EINVAL;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) ||
+        (reinterpret_cast<uintptr_t>(workspace) & 255u))
+        return ATTN_EINVAL;
+    const int tokens = hist_len + chunk_len;
+    if (workspace_bytes < attn_kv4_workspace(c, tokens)) return ATTN_EINVAL;
+    uint16_t* kp = static_cast<uint16_t*>(workspace);
+    uint16_t* vp = kp + kv4_plain_bytes(c->cfg, tokens) / 2;
+    attn::FlashMaps maps;
+    const int rc = flash_maps(c, q, hist_len, chunk_len, chunk_len, kp, vp, tokens, &maps);
+    if (rc != ATTN_OK) return rc;
+    const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const attn::Kv4New a{k, v, nullptr, hist_len, chunk_len, c->cfg.batch};
+    const cudaError_t e = attn::launch_kv4_append(c->shape, a, c->d_cos, c->d_sin, kv4_of(cache),
+                                                  attn::Kv4Plain{kp, vp, tokens}, c->d_err, st);
+    if (e != cudaSuccess) return cuda_fail(e, "kv4 append launch");
+    return run_flash(c, maps, hist_len, chunk_len, chunk_len, out, st);
 }
 
 // Exported for the tests, not part of attn.h: how the library cuts a call on this device (out[4] as

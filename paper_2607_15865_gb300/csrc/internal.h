@@ -125,6 +125,39 @@ cudaError_t launch_decode_tc(const Shape& s, const DecodeMaps& maps, const uint1
                              int* counters, int nsplit, uint16_t* out, int* err, bool after_decode, int ntok,
                              int seq_tok, cudaStream_t st, bool producer_early, uint64_t wait_ns, int num_sms);
 
+// The 4-bit KV cache (format: kv4.cuh).  Slots per (sequence, kv head): whole tiles of the decode.
+inline int kv4_slots(int max_len) { return (max_len + 63) / 64 * 64; }
+struct Kv4Cache {
+    uint8_t* k_codes;    // [B][Hkv][kv4_slots][D / 2]
+    uint16_t* k_scales;  // [B][Hkv][kv4_slots][D / 32]
+    uint8_t* v_codes;
+    uint16_t* v_scales;
+};
+// New tokens of the cache: k and v [batch][chunk][Hkv][D] for slots hist .. hist + chunk - 1, hist read from
+// d_hist[b] where that is not null (a sequence it puts outside the cache is flagged and skipped).
+struct Kv4New {
+    const uint16_t* k;
+    const uint16_t* v;
+    const int32_t* d_hist;
+    int hist, chunk, batch;
+};
+// bf16 rows that the cache's values go to: [B * Hkv][rows][D].
+struct Kv4Plain {
+    uint16_t* k;
+    uint16_t* v;
+    int rows;
+};
+// Appends the new tokens; with plain.k also writes slots [0, hist + chunk) as bf16 there (row p: slot p).
+cudaError_t launch_kv4_append(const Shape& s, const Kv4New& a, const float* cos_tab, const float* sin_tab,
+                              const Kv4Cache& c, const Kv4Plain& plain, int* err, cudaStream_t st);
+// Slots first .. first + count - 1 as bf16 (row i: slot first + i).
+cudaError_t launch_kv4_read(const Shape& s, int first, int count, const Kv4Cache& c, const Kv4Plain& plain,
+                            cudaStream_t st);
+// Decode over the 4-bit cache: ntok new tokens per sequence at positions d_hist[b] + i, appended and attended to.
+cudaError_t launch_kv4_decode(const Shape& s, const uint16_t* q, const uint16_t* k_new, const uint16_t* v_new,
+                              const int32_t* d_hist, int ntok, const Kv4Cache& c, const float* cos_tab,
+                              const float* sin_tab, uint16_t* out, int* err, cudaStream_t st);
+
 // W4BF16 GEMV (w4_gemv.cu): y[m, n] = sum_k x[m, k] (q[n, k] - z[n, k/128]) s[n, k/128] for
 // the activation rows of one launch.  tiles: the tile
 // stream of attn_w4bf16_gemv (16-byte aligned); x: bf16 [M][K] (16-byte aligned);

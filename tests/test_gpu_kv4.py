@@ -1,0 +1,389 @@
+"""The 4-bit cache on the GPU: append, read, decode and prefill_kv against 64 bits (bars: kv4_util)."""
+import numpy as np
+import pytest
+
+from oracle import kv4_oracle as K
+from tests import kv4_util as U
+
+pytestmark = pytest.mark.gpu
+
+DEV_ERR_HIST = 1
+
+
+def context(B, Hq, Hkv, D, L, theta=1.0e6):
+    from paper_2607_15865_gb300.attention import Attention
+    return Attention(B, Hq, Hkv, D, L, theta)
+
+
+def slots(L):
+    return (L + 63) // 64 * 64
+
+
+def run_append(attn, cache, ref, tag, hist, n, k=None, v=None):
+    """Append n tokens on the device and in ref (a K.Cache, updated)."""
+    B, Hkv, D = attn.batch, attn.n_kv_heads, attn.head_dim
+    _, k0, v0 = U.new_tokens(tag, B, n, Hkv, Hkv, D)
+    k, v = k0 if k is None else k, v0 if v is None else v
+    attn.kv4_append(U.dev_bf16(k), U.dev_bf16(v), hist, cache)
+    tab = K.tables(attn.max_len, D, attn.rope_theta)
+    pos = np.arange(hist, hist + n)
+    for b in range(B):
+        ref.write(b, pos, K.rope(k[b], pos, tab), v[b])
+
+
+# ------------------------------------------------------------------ append and read
+
+@pytest.mark.parametrize("B,Hkv,D,L,hist,n", [
+    (1, 1, 64, 1, 0, 1),         # one slot
+    (1, 2, 64, 32, 16, 8),
+    (2, 3, 128, 100, 37, 63),    # up to the last slot, odd
+    (1, 8, 128, 2048, 0, 777),
+    (5, 1, 64, 129, 1, 127),
+    (3, 4, 128, 65, 64, 1),
+])
+def test_append_is_bit_exact_and_leaves_other_slots(B, Hkv, D, L, hist, n):
+    attn = context(B, Hkv, Hkv, D, L)
+    ref = U.history(f"app{B}{Hkv}{D}", B, Hkv, slots(L), D, [hist] * B)
+    cache = U.to_dev(ref, L)
+    run_append(attn, cache, ref, f"app{B}{Hkv}{D}", hist, n)
+    U.same_cache(cache, ref, "append")
+    assert attn.device_error() == 0
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_append_of_special_values(D):
+    """Zeros, one-signed groups, infinities, NaN, subnormal and very large values, in v (k keeps its bits
+    at position 0, where RoPE is the identity)."""
+    n, Hkv, L = 12, 2, 16
+    v = U.bf16("special", "v", (1, n, Hkv, D))
+    f = K.bf16_to_f64(v)
+    f[0, 0] = 0.0
+    f[0, 1] = np.abs(f[0, 1])
+    f[0, 2] = -np.abs(f[0, 2])
+    f[0, 3, 0, 5], f[0, 3, 1, 40] = np.inf, -np.inf
+    f[0, 4, 0, 33] = np.nan
+    f[0, 5] *= 2.0 ** -130
+    f[0, 6] *= 2.0 ** 120
+    f[0, 7] = 0.0
+    f[0, 7, :, 1::32] = 15.0
+    f[0, 8] = -0.0
+    f[0, 9] *= 2.0 ** -40
+    f[0, 9, 0, 3] = 7.5
+    f[0, 10] = 3.0
+    f[0, 11, :, ::2] = 1e-40
+    v = K.f32_to_bf16(f)
+    for t in range(n):
+        attn = context(1, Hkv, Hkv, D, L)
+        ref = K.Cache(1, Hkv, slots(L), D)
+        cache = U.to_dev(ref, L)
+        run_append(attn, cache, ref, "special", 0, 1, v[:, t:t + 1], v[:, t:t + 1])
+        U.same_cache(cache, ref, f"token {t}")
+        k, w = attn.kv4_read(cache, 0, 1)
+        for t2, got in enumerate((k, w)):
+            want = K.values(ref.codes[t2][:, :, :1], ref.scales[t2][:, :, :1])
+            got = K.bf16_to_f64(U.host_bits(got))
+            assert ((got == want) | (np.isnan(got) & np.isnan(want))).all(), f"token {t}"
+
+
+@pytest.mark.parametrize("B,Hkv,D,L,first,count", [
+    (1, 1, 64, 1, 0, 1), (2, 3, 128, 100, 37, 63), (1, 8, 128, 2048, 0, 2048), (3, 2, 64, 130, 129, 1),
+    (2, 2, 128, 65, 3, 0),
+])
+def test_read_gives_the_values(B, Hkv, D, L, first, count):
+    import torch
+    attn = context(B, Hkv, Hkv, D, L)
+    ref = U.history(f"read{D}", B, Hkv, slots(L), D, [L - L // 3] * B)  # NaN groups in the last third
+    cache = U.to_dev(ref, L)
+    got = attn.kv4_read(cache, first, count)
+    for t in range(2):
+        want = K.values(ref.codes[t][:, :, first:first + count], ref.scales[t][:, :, first:first + count])
+        g = K.bf16_to_f64(U.host_bits(got[t]))
+        assert g.shape == want.shape and ((g == want) | (np.isnan(g) & np.isnan(want))).all()
+    assert len(attn.kv4_read(cache)) == 2 and attn.kv4_read(cache)[0].shape == (B, Hkv, L, D)
+    U.same_cache(cache, ref, "read")
+    torch.cuda.synchronize()
+
+
+# ------------------------------------------------------------------ decode
+
+def run_decode(attn, ref, tag, hist, n, kv=None, what="decode"):
+    """One decode of n tokens per sequence at the lengths hist; compares outputs and cache; returns out."""
+    import torch
+    B, Hq, Hkv, D, L = attn.batch, attn.n_q_heads, attn.n_kv_heads, attn.head_dim, attn.max_len
+    q, k, v = U.new_tokens(tag, B, n, Hq, Hkv, D)
+    if kv is not None:
+        kv(k, v)
+    cache = U.to_dev(ref, L)
+    out = torch.full((B, n, Hq, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    lens = torch.tensor(hist, dtype=torch.int32, device="cuda")
+    attn.kv4_decode(U.dev_bf16(q), U.dev_bf16(k), U.dev_bf16(v), lens, cache, out=out)
+    tab = K.tables(L, D, attn.rope_theta)
+    want, mass = np.full(out.shape, 7.0), np.full(out.shape, 7.0)
+    bad = False
+    for b, h in enumerate(hist):
+        if h < 0 or h + n > L:
+            bad = True
+            continue
+        pos = np.arange(h, h + n)
+        ref.write(b, pos, K.rope(k[b], pos, tab), v[b])
+        want[b], mass[b] = K.attend(K.rope(q[b], pos, tab), pos, ref, b)
+    torch.cuda.synchronize()
+    assert attn.device_error() == (DEV_ERR_HIST if bad else 0)
+    U.close(out, want, mass, what)
+    U.same_cache(cache, ref, what)
+    return out
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (4, 2), (5, 1), (14, 2), (16, 1), (32, 8), (8, 8)])
+def test_decode_group_sizes(D, Hq, Hkv):
+    attn = context(2, Hq, Hkv, D, 300)
+    hist = [213, 64]
+    run_decode(attn, U.history(f"dg{D}", 2, Hkv, slots(300), D, hist), f"dg{Hq}{Hkv}{D}", hist, 1)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("hist", [[0], [1], [31], [32], [33], [63, 64, 65], [127, 128, 129, 0], [998, 0, 999, 500, 1],
+                                  [7] * 40])
+def test_decode_lengths(D, hist):
+    B = len(hist)
+    attn = context(B, 8, 2, D, 1000)
+    run_decode(attn, U.history(f"dl{D}", B, 2, slots(1000), D, hist), f"dl{D}", hist, 1)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv,n", [(4, 2, 2), (8, 2, 5), (8, 1, 16), (16, 1, 16), (5, 1, 3), (7, 7, 4), (8, 4, 8),
+                                      (14, 2, 11)])
+def test_decode_several_tokens(D, Hq, Hkv, n):
+    hist = [150, 0, 31, 96 - n]
+    attn = context(4, Hq, Hkv, D, 200)
+    run_decode(attn, U.history(f"dm{D}", 4, Hkv, slots(200), D, hist), f"dm{Hq}{Hkv}{n}{D}", hist, n)
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,D,L,hist,n", [
+    (1, 8, 2, 128, 8192, [8191], 1), (1, 40, 8, 128, 6000, [5999], 1), (2, 8, 1, 64, 9000, [8999, 4444], 1),
+    (1, 8, 2, 128, 5000, [4990], 7), (9, 4, 2, 128, 4000, [3999, 17, 2048, 0, 1000, 3500, 33, 64, 1], 1),
+])
+def test_decode_long(B, Hq, Hkv, D, L, hist, n):
+    attn = context(B, Hq, Hkv, D, L)
+    run_decode(attn, U.history(f"long{B}{D}", B, Hkv, slots(L), D, hist), f"long{B}{D}", hist, n)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [1, 3])
+def test_decode_skips_and_flags_lengths_outside(D, n):
+    hist = [10, -1, 65 - n, 66 - n, 2 ** 31 - 1, -2 ** 31, 0]
+    attn = context(7, 4, 2, D, 65)
+    ref = U.history(f"skip{D}", 7, 2, slots(65), D, [min(max(h, 0), 65) for h in hist])
+    out = run_decode(attn, ref, f"skip{D}", hist, n)
+    assert (out[1] == 7).all() and (out[3] == 7).all() and (out[5] == 7).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_decode_of_sharp_and_far_scores(D):
+    """Scores of hundreds, rising and falling along the history: the running maximum moves often."""
+    hist = [700]
+    attn = context(1, 4, 1, D, 800)
+    ref = U.history(f"sharp{D}", 1, 1, slots(800), D, hist)
+    c, s = K.quantise(K.f32_to_bf16(K.values(ref.codes[0][:, :, :700], ref.scales[0][:, :, :700])
+                                    * np.linspace(0.1, 30, 700)[None, None, :, None]))
+    ref.codes[0][:, :, :700], ref.scales[0][:, :, :700] = K.pack(c), s
+    run_decode(attn, ref, f"sharp{D}", hist, 2)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_decode_nan_in_the_history(D):
+    """A NaN group of a key makes the heads that read it NaN; one of a value its 32 outputs."""
+    hist = [300, 300]
+    attn = context(2, 4, 2, D, 400)
+    ref = U.history(f"nan{D}", 2, 2, slots(400), D, hist)
+    ref.scales[0][0, 1, 17, 1] = K.NAN_SCALE
+    ref.scales[1][1, 0, 299, D // 32 - 1] = K.NAN_SCALE
+    out = run_decode(attn, ref, f"nan{D}", hist, 1)
+    assert out[0, 0, 2:].isnan().all() and not out[0, 0, :2].isnan().any()
+    assert out[1, 0, :2, D - 32:].isnan().all() and not out[1, 0, :, :D - 32].isnan().any()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq,n", [(2, 4), (8, 5)])
+def test_decode_nan_in_a_new_token_reaches_only_later_ones(D, Hq, n):
+    """Token 2's infinite k and NaN v are seen by tokens 2 .. n - 1 and not by 0 and 1."""
+    hist = [61]
+    attn = context(1, Hq, 2, D, 100)
+    def odd(k, v):
+        k[0, 2, 0, 5] = 0x7F80
+        v[0, 2, 1, 33] = 0x7FC0
+    out = run_decode(attn, U.history(f"late{D}", 1, 2, slots(100), D, hist), f"late{D}", hist, n, odd)
+    assert not out[0, :2].isnan().any() and out[0, 2:, :Hq // 2].isnan().all()
+    assert out[0, 2:, Hq // 2:, 32:64].isnan().all() and not out[0, 2:, Hq // 2:, :32].isnan().any()
+
+
+# ------------------------------------------------------------------ prefill
+
+def run_prefill(attn, cache, ref, tag, hist, n, workspace=None, what="prefill"):
+    B, Hq, Hkv, D, L = attn.batch, attn.n_q_heads, attn.n_kv_heads, attn.head_dim, attn.max_len
+    q, k, v = U.new_tokens(tag, B, n, Hq, Hkv, D)
+    out = attn.kv4_prefill_kv(U.dev_bf16(q), U.dev_bf16(k), U.dev_bf16(v), hist, cache, workspace)
+    tab, pos = K.tables(L, D, attn.rope_theta), np.arange(hist, hist + n)
+    want, mass = np.zeros(out.shape), np.zeros(out.shape)
+    for b in range(B):
+        ref.write(b, pos, K.rope(k[b], pos, tab), v[b])
+        want[b], mass[b] = K.attend(K.rope(q[b], pos, tab), pos, ref, b)
+    U.close(out, want, mass, what)
+    U.same_cache(cache, ref, what)
+    assert attn.device_error() == 0
+    return out
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,D,L,hist,n", [
+    (1, 4, 2, 64, 32, 0, 16), (1, 4, 2, 64, 32, 16, 8), (1, 1, 1, 128, 1, 0, 1), (2, 14, 2, 128, 300, 77, 130),
+    (1, 16, 1, 64, 700, 500, 77), (3, 5, 5, 128, 260, 1, 259), (1, 28, 4, 128, 512, 0, 300),
+])
+def test_prefill(B, Hq, Hkv, D, L, hist, n):
+    attn = context(B, Hq, Hkv, D, L)
+    ref = U.history(f"pre{B}{D}", B, Hkv, slots(L), D, [hist] * B)
+    run_prefill(attn, U.to_dev(ref, L), ref, f"pre{B}{Hq}{D}", hist, n)
+
+
+def test_a_prompt_in_chunks_then_decodes_equals_its_cache():
+    """Two chunks in one workspace, single and several tokens: each step is the stage over the cache so far."""
+    import torch
+    attn = context(2, 8, 2, 128, 256)
+    ref = K.Cache(2, 2, slots(256), 128)
+    cache = attn.kv4_cache()
+    ws = torch.empty(attn.kv4_workspace(200), dtype=torch.uint8, device="cuda")
+    run_prefill(attn, cache, ref, "chain0", 0, 150, ws, "first chunk")
+    run_prefill(attn, cache, ref, "chain1", 150, 37, ws, "second chunk")
+    tab = K.tables(256, 128, attn.rope_theta)
+    for t, n in ((187, 1), (188, 3), (191, 1)):
+        q, k, v = U.new_tokens(f"chain{t}", 2, n, 8, 2, 128)
+        lens = torch.full((2,), t, dtype=torch.int32, device="cuda")
+        out = attn.kv4_decode(U.dev_bf16(q), U.dev_bf16(k), U.dev_bf16(v), lens, cache)
+        pos = np.arange(t, t + n)
+        for b in range(2):
+            ref.write(b, pos, K.rope(k[b], pos, tab), v[b])
+            U.close(out[b], *K.attend(K.rope(q[b], pos, tab), pos, ref, b), f"step {t}")
+    U.same_cache(cache, ref, "chain")
+
+
+def test_the_cache_is_the_bf16_cache_quantised():
+    """kv4_append writes what quantising attn_prefill's bf16 cache gives."""
+    import torch
+    attn = context(1, 8, 4, 128, 200, 5.0e5)
+    q, k, v = (U.dev_bf16(x) for x in U.new_tokens("bf16", 1, 200, 8, 4, 128))
+    kc, vc = (torch.zeros(1, 4, 200, 128, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    attn.prefill(q, k, v, kc, vc)
+    cache = attn.kv4_cache()
+    attn.kv4_append(k, v, 0, cache)
+    for t, (x, codes, scales) in enumerate(((kc, cache.k_codes, cache.k_scales), (vc, cache.v_codes, cache.v_scales))):
+        c, s = K.quantise(U.host_bits(x))
+        assert (codes[:, :, :200].cpu().numpy() == K.pack(c)).all(), "kv"[t]
+        assert (scales[:, :, :200].cpu().numpy().view(np.uint16) == s).all(), "kv"[t]
+
+
+def test_calls_on_another_stream():
+    import torch
+    attn = context(1, 8, 2, 128, 500)
+    ref = U.history("stream", 1, 2, slots(500), 128, [300])
+    cache = U.to_dev(ref, 500)
+    st = torch.cuda.Stream()
+    q, k, v = U.new_tokens("stream", 1, 1, 8, 2, 128)
+    lens = torch.tensor([300], dtype=torch.int32, device="cuda")
+    dq, dk, dv = (U.dev_bf16(x) for x in (q, k, v))
+    out = torch.empty_like(dq)
+    st.wait_stream(torch.cuda.current_stream())
+    attn.kv4_decode(dq, dk, dv, lens, cache, out=out, stream=st)
+    kr, vr = torch.empty(2, 1, 2, 301, 128, dtype=torch.bfloat16, device="cuda")
+    attn.kv4_read(cache, 0, 301, out=(kr, vr), stream=st)
+    st.synchronize()
+    tab, pos = K.tables(500, 128, attn.rope_theta), np.array([300])
+    ref.write(0, pos, K.rope(k[0], pos, tab), v[0])
+    U.close(out[0], *K.attend(K.rope(q[0], pos, tab), pos, ref, 0), "stream")
+    assert (K.bf16_to_f64(U.host_bits(kr)) == K.values(ref.codes[0][:, :, :301], ref.scales[0][:, :, :301])).all()
+
+
+def test_offsets_past_32_bits():
+    """A cache of 80 heads of a million slots: the last head's codes lie 5.3 GB in."""
+    import torch
+
+    from paper_2607_15865_gb300.kv4 import Kv4Cache
+    L, B, Hkv, D = 1 << 20, 10, 8, 128
+    attn = context(B, Hkv, Hkv, D, L)
+    cache = Kv4Cache.empty(B, Hkv, L, D)
+    h = L - 40
+    q, k, v = U.new_tokens("far", B, 1, Hkv, Hkv, D)
+    dk, dv = U.dev_bf16(k), U.dev_bf16(v)
+    lens = torch.tensor([5] * (B - 1) + [h], dtype=torch.int32, device="cuda")
+    kc, kvv = U.new_tokens("farc", B, 40, Hkv, Hkv, D)[1:]
+    attn.kv4_append(U.dev_bf16(kc), U.dev_bf16(kvv), h, cache)
+    out = attn.kv4_decode(U.dev_bf16(q), dk, dv, lens, cache)
+    got_k, got_v = attn.kv4_read(cache, h, 40)
+    ref = K.Cache(1, Hkv, 64, D)
+    tab = K.tables(1, D, attn.rope_theta)
+    ang = np.arange(h, L, dtype=np.float64)[:, None] * np.array([attn.rope_theta ** (-2.0 * j / D) for j in range(D // 2)])
+    tab = np.cos(ang).astype(np.float32), np.sin(ang).astype(np.float32)
+    b = B - 1
+    ref.write(0, np.arange(40), K.rope(kc[b], np.arange(40), tab), kvv[b])
+    ref.write(0, np.array([0]), K.rope(k[b], np.array([0]), tab), v[b])
+    for t, got in enumerate((got_k, got_v)):
+        want = K.values(ref.codes[t][0, :, :40], ref.scales[t][0, :, :40])
+        assert (K.bf16_to_f64(U.host_bits(got[b])) == want).all()
+    # the history is zeros: h keys of score 0 and value 0, and the new one (slot h)
+    kn, vn = K.values(ref.codes[0][0, :, 0], ref.scales[0][0, :, 0]), K.values(ref.codes[1][0, :, 0], ref.scales[1][0, :, 0])
+    s = (K.bf16_to_f64(K.rope(q[b], np.array([0]), tab))[0] * kn).sum(-1) / np.sqrt(D)
+    w = np.exp(s) / (np.exp(s) + h)
+    U.close(out[b, 0], w[:, None] * vn, np.abs(w[:, None] * vn), "far")
+
+
+# ------------------------------------------------------------------ refusals
+
+def test_refusals():
+    import torch
+
+    from paper_2607_15865_gb300 import _lib
+    from paper_2607_15865_gb300.kv4 import Kv4Cache
+    attn = context(1, 4, 2, 64, 100)
+    cache = attn.kv4_cache()
+    q, k, v = (U.dev_bf16(x) for x in U.new_tokens("ref", 1, 4, 4, 2, 64))
+    lens = torch.tensor([3], dtype=torch.int32, device="cuda")
+    before = [t.clone() for t in (cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales)]
+    for bad in (dict(hist_len=97), dict(hist_len=-1)):
+        with pytest.raises(_lib.AttnError):
+            attn.kv4_append(k, v, cache=cache, **bad)
+        with pytest.raises((_lib.AttnError, TypeError)):
+            attn.kv4_prefill_kv(q, k, v, cache=cache, **bad)
+    for first, count in ((-1, 2), (0, 101), (100, 1), (0, -1)):
+        with pytest.raises(_lib.AttnError):
+            attn.kv4_read(cache, first, count)
+    with pytest.raises(ValueError):
+        attn.kv4_append(k[:, :, :1], v, 0, cache)                      # shape
+    with pytest.raises(ValueError):
+        attn.kv4_append(k.transpose(1, 2).contiguous().transpose(1, 2), v, 0, cache)  # strides
+    with pytest.raises(TypeError):
+        attn.kv4_append(k.float(), v, 0, cache)
+    with pytest.raises(TypeError):
+        attn.kv4_decode(q, k, v, lens.long(), cache)
+    with pytest.raises(TypeError):
+        attn.kv4_decode(q, k, v, lens, cache.k_codes)
+    with pytest.raises(ValueError):
+        attn.kv4_decode(q, k, v, lens, Kv4Cache.empty(1, 2, 99, 64))   # another max_len
+    with pytest.raises(ValueError):
+        attn.kv4_decode(q, k, v, lens, Kv4Cache.empty(1, 2, 100, 128))
+    with pytest.raises(TypeError):
+        attn.kv4_prefill_kv(q, k, v, 0, cache, torch.empty(attn.kv4_workspace(4) - 1, dtype=torch.uint8, device="cuda"))
+    q17, k17, v17 = (U.dev_bf16(x) for x in U.new_tokens("ref", 1, 17, 4, 2, 64))
+    with pytest.raises(_lib.AttnError):
+        attn.kv4_decode(q17, k17, v17, lens, cache)
+    c = [t.clone() for t in before]
+    with pytest.raises(ValueError):
+        Kv4Cache(200, *c)
+    with pytest.raises(TypeError):
+        Kv4Cache(100, c[0], c[1].float(), c[2], c[3])
+    with pytest.raises(ValueError):
+        Kv4Cache(100, c[0].transpose(2, 3), c[1], c[2], c[3])
+    odd = torch.empty(c[0].numel() + 1, dtype=torch.uint8, device="cuda")[1:].view(c[0].shape)
+    with pytest.raises(_lib.AttnError):
+        attn.kv4_append(k, v, 0, Kv4Cache(100, odd, c[1], c[2], c[3]))  # 16-byte alignment
+    torch.cuda.synchronize()
+    assert all((x == y).all() for x, y in zip(before, (cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales)))
+    assert attn.device_error() == 0
