@@ -233,6 +233,7 @@ int attn_create(const attn_cfg* cfg, attn_ctx** out) {
     c->encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
     e = attn::configure_flash_fwd();
     if (e == cudaSuccess) e = attn::configure_decode_tc();
+    if (e == cudaSuccess) e = attn::configure_kv4_decode();
     if (e != cudaSuccess) {
         delete c;
         return cuda_fail(e, "configure kernels");
@@ -745,7 +746,8 @@ int attn_kv4_decode(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uin
         return ATTN_EINVAL;
     if (n_new < 1 || n_new > kMaxDraftTokens || n_new > c->cfg.max_len) return ATTN_EINVAL;
     const cudaError_t e = attn::launch_kv4_decode(c->shape, q, k, v, d_hist_len, n_new, kv4_of(cache), c->d_cos, c->d_sin,
-                                                  out, c->d_err, reinterpret_cast<cudaStream_t>(stream));
+                                                  c->d_flash_o, c->d_flash_ml, c->d_counters, out, c->d_err, c->num_sms,
+                                                  reinterpret_cast<cudaStream_t>(stream), c->wait_ns);
     return e == cudaSuccess ? ATTN_OK : cuda_fail(e, "kv4 decode launch");
 }
 

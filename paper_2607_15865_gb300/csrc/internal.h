@@ -153,10 +153,15 @@ cudaError_t launch_kv4_append(const Shape& s, const Kv4New& a, const float* cos_
 // Slots first .. first + count - 1 as bf16 (row i: slot first + i).
 cudaError_t launch_kv4_read(const Shape& s, int first, int count, const Kv4Cache& c, const Kv4Plain& plain,
                             cudaStream_t st);
-// Decode over the 4-bit cache: ntok new tokens per sequence at positions d_hist[b] + i, appended and attended to.
+// Decode over the 4-bit cache (kv4_decode.cu): ntok (1 .. 16) new tokens per sequence at positions d_hist[b] + i,
+// appended and attended to; a sequence with a position outside the cache is flagged and skipped.  part_o
+// [num_sms * 32][D] and part_ml [num_sms * 36][2] hold the parts of items that CTAs share; counters:
+// an int per item (sequence, kv head, 16 columns) of up to 1024 sequences, zero before and after every launch.
+cudaError_t configure_kv4_decode();
 cudaError_t launch_kv4_decode(const Shape& s, const uint16_t* q, const uint16_t* k_new, const uint16_t* v_new,
                               const int32_t* d_hist, int ntok, const Kv4Cache& c, const float* cos_tab,
-                              const float* sin_tab, uint16_t* out, int* err, cudaStream_t st);
+                              const float* sin_tab, float* part_o, float* part_ml, int* counters, uint16_t* out, int* err,
+                              int num_sms, cudaStream_t st, uint64_t wait_ns);
 
 // W4BF16 GEMV (w4_gemv.cu): y[m, n] = sum_k x[m, k] (q[n, k] - z[n, k/128]) s[n, k/128] for
 // the activation rows of one launch.  tiles: the tile
