@@ -2,32 +2,38 @@
 // append of the new tokens and the merge of the splits fused in.
 //
 // A (sequence, kv head) has G query heads x ntok new tokens = columns, taken 16 at a time (an item).
-// An item's slots are cut into blocks of 32 (head_dim 128) or 64 slots; the blocks of all items, in order, are
-// cut into equal runs, one per CTA, whatever the lengths (they are read on the device), so that mixed lengths load
-// the SMs evenly.  Within a CTA the warps take its blocks in turn, each through a private ring of bulk
-// copies with one mbarrier per stage and with its own running maximum, sum and accumulators; they meet
-// once per item, in shared memory.  An item that several CTAs share is merged by the last of them to finish.
+// An item's slots are cut into blocks of 32 (head_dim 128) or 64 slots.  The lengths are read on the device, and so
+// every CTA works out the same cut of the work: where the items are at most the SMs, each is cut into pieces of
+// at most `target` blocks, the least target for which the pieces are at most the SMs, a piece per CTA; where
+// they are more, the blocks of all items, in order, are cut into equal runs.  Within a CTA the warps take its
+// blocks in turn, each through a private ring of bulk copies with one mbarrier per stage and with its own
+// running maximum, sum and accumulators; they meet once per item, in shared memory.  An item that several CTAs
+// share is merged by the last of them to finish, in the order of its pieces.
 //
 // Per 16 slots, with mma.sync m16n8k16 (A from registers: a tcgen05 operand would have to be written
 // back to shared or tensor memory at four times the packed bytes, for products 8 or 16 columns wide):
-//   S [16 cols x 16 slots]  = Q [16 x D] K^T         B fragments: a lane's 16 bytes of a slot's codes
-//   O^T [D x cols]         += V^T [D x 16] P^T       A fragments: 8 bytes of four slots; P^T is S's layout
+//   S^T [16 slots x cols]   = K [16 x D] Q^T         A fragments: a lane's 16 bytes of two slots' codes
+//   O^T [D x cols]         += V^T [D x 16] P^T       A fragments: 8 bytes of four slots
+// P^T goes from the layout of the first's result to the operand of the second by an 8 x 8 transpose
+// (movmatrix) per 8 slots.  (With S [cols x slots] it needs none, but its Q fragments are half zeros for
+// up to 8 columns, and the moves that set them up cost more than the products.)
 // Decoding is a shift and a masked OR of the pair (128 + c, 128 + c').  For k one fma with (s, -128 s) then
 // gives c s exactly (kv4.cuh), and the zero points go as a product of their own, one further mma:
 //   S -= sum over groups of (z s) (sum of q over the group), those sums in three bf16 parts.
 // For v it is the difference with 128 + z and the product with s, both exact: a v that is small
-// beside its group must not be what is left of two larger sums.  A row of ones in place of V^T gives the
+// beside its group must not be what is left of two larger sums.  Rows of ones in place of V^T give the
 // softmax sum, of the same rounded P that weighs V.
 // The running maximum moves lazily: only when a score passes it by 2^8 are O and the sum rescaled.
 //
-// The new tokens: the warp that holds the block of their slots rotates, quantises and writes them, to the
-// cache and to its copy of the block.  Slots past the last one are masked by position and by a scale of 0;
-// a NaN group of a new token's v counts from that token on, so its scale is taken as 0 too and the
-// columns that see it are set to NaN when they are written.
+// The new tokens: before its item's blocks a CTA that holds their slots rotates and quantises them, a warp per
+// row, writes them to the cache and stages them for the warp that has their block.  Slots past the last
+// one are masked by position and by a scale of 0; a NaN group of a new token's v counts from that token on, so its
+// scale is taken as 0 too and the columns that see it are set to NaN when they are written.
 // Every wait is bounded: on expiry a warp records kDevErrTimeout, issues and computes nothing more, lets its
 // copies land and takes part in the barriers and counts.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "internal.h"
 #include "kv4.cuh"
@@ -37,6 +43,7 @@ namespace attn {
 namespace {
 
 constexpr int kMaxSeqs = 1024;  // sequences of one launch (their block counts are summed in shared memory)
+constexpr int kMaxNew = 16;     // new tokens per sequence
 constexpr int kNone = 1 << 20;  // no new token with a NaN group
 
 template <int D_, int NT_>
@@ -54,15 +61,18 @@ struct Cfg {
     static constexpr int COLS = 8 * NT;
     static constexpr int QS = D + 8;             // row stride of q in shared memory (bf16)
     static constexpr int OS = D + 4;             // row stride of a warp's O (floats)
+    static constexpr int NEW = ROW + 2 * GR;     // bytes of a staged row: codes, scales
     static constexpr int OFF_O = W * STAGES * STAGE;            // float [W][COLS][OS]
     static constexpr int OFF_ML = OFF_O + W * COLS * OS * 4;    // float [W][COLS][2]
-    static constexpr int OFF_Q = OFF_ML + W * COLS * 8;         // bf16 [16][QS]
-    static constexpr int OFF_PRE = OFF_Q + 16 * QS * 2;         // int [kMaxSeqs + 1]
-    static constexpr int OFF_BAR = (OFF_PRE + (kMaxSeqs + 1) * 4 + 7) & ~7;
+    static constexpr int OFF_Q = OFF_ML + W * COLS * 8;         // bf16 [COLS][QS]
+    static constexpr int OFF_NEW = OFF_Q + COLS * QS * 2;       // [kMaxNew][k, v][NEW]
+    static constexpr int OFF_PRE = OFF_NEW + kMaxNew * 2 * NEW;  // int [kMaxSeqs + 1]: blocks before a sequence
+    static constexpr int OFF_PIECES = OFF_PRE + (kMaxSeqs + 1) * 4;  // int [kMaxSeqs + 1]: pieces before it
+    static constexpr int OFF_BAR = (OFF_PIECES + (kMaxSeqs + 1) * 4 + 7) & ~7;
     static constexpr int OFF_NAN = OFF_BAR + W * STAGES * 8;    // int [4]: first new token with a NaN group of v
-    static constexpr int OFF_FLAG = OFF_NAN + 16;
+    static constexpr int OFF_FLAG = OFF_NAN + 16;               // int [4]: last CTA, target (0: runs), items
     static constexpr int BYTES = OFF_FLAG + 16;
-    static_assert(CODES == 2048 && SCALES == 256 && BYTES <= 232448, "shared memory");
+    static_assert(CODES == 2048 && SCALES == 256 && NEW % 4 == 0 && BYTES <= 232448, "shared memory");
 };
 
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -99,31 +109,39 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     return d;
 }
 
-constexpr uint32_t kOnes = 0x3F803F80u, kMinus128 = 0xC300C300u;
+constexpr uint32_t kOnes = 0x3F803F80u, kMinus128 = 0xC300C300u, k128 = 0x43004300u;
+
+// The pair of codes in bits 0 .. 3 and 16 .. 19 as bf16 128 + c: one LOP3, which takes one constant as an
+// immediate and the other from a register (left to the compiler it is two).
+__device__ __forceinline__ uint32_t codes_of(uint32_t w, uint32_t k128reg) {
+    uint32_t d;
+    asm("lop3.b32 %0, %1, 0x000F000F, %2, 0xEA;" : "=r"(d) : "r"(w), "r"(k128reg));
+    return d;
+}
 
 // The scales of a pair of values: s and -128 s (for decode2), and z s.
 struct Pair {
     uint32_t s, n;
 };
-__device__ __forceinline__ Pair pair_of(uint32_t m2, uint32_t& zs) {
+__device__ __forceinline__ Pair pair_of(uint32_t m2, uint32_t& zs, uint32_t magic) {
     Pair p;
     p.s = m2 & 0x7FF07FF0u;
     p.n = mul2(p.s, kMinus128);
-    zs = fma2((m2 & 0x000F000Fu) | 0x43004300u, p.s, p.n);
+    zs = fma2(codes_of(m2, magic), p.s, p.n);
     return p;
 }
 struct ZPair {  // the scales s of a pair and 128 + z
     uint32_t s, z;
 };
-__device__ __forceinline__ ZPair zpair_of(uint32_t m2) {
-    return {m2 & 0x7FF07FF0u, (m2 & 0x000F000Fu) | 0x43004300u};
+__device__ __forceinline__ ZPair zpair_of(uint32_t m2, uint32_t magic) {
+    return {m2 & 0x7FF07FF0u, codes_of(m2, magic)};
 }
-__device__ __forceinline__ uint32_t value2(uint32_t w, int i, const ZPair& p) {
-    return mul2(sub2(((w >> (4 * i)) & 0x000F000Fu) | 0x43004300u, p.z), p.s);
+__device__ __forceinline__ uint32_t value2(uint32_t w, int i, const ZPair& p, uint32_t magic) {
+    return mul2(sub2(codes_of(w >> (4 * i), magic), p.z), p.s);
 }
 // Pair i of a word: the two codes at bit 4 i of its halves, times s.
-__device__ __forceinline__ uint32_t decode2(uint32_t w, int i, const Pair& p) {
-    return fma2(((w >> (4 * i)) & 0x000F000Fu) | 0x43004300u, p.s, p.n);
+__device__ __forceinline__ uint32_t decode2(uint32_t w, int i, const Pair& p, uint32_t magic) {
+    return fma2(codes_of(w >> (4 * i), magic), p.s, p.n);
 }
 
 __device__ __forceinline__ uint32_t lds32(uint32_t a) {
@@ -150,6 +168,12 @@ __device__ __forceinline__ void lds(uint32_t a, uint32_t (&v)[N]) {
         v[0] = lds32(a);
 }
 
+__device__ __forceinline__ uint32_t transpose8(uint32_t a) {
+    uint32_t d;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
+}
+
 struct Args {
     const uint16_t* q;
     const uint16_t* k_new;
@@ -165,15 +189,15 @@ struct Args {
     int* counters;   // per item, zero between launches
     int* err;
     uint64_t wait_ns;
-    float scale_log2;
+    float scale_log2, move;  // log2 e / sqrt D, and the lead of a score that moves the maximum (2^8)
     int batch, ntok, Hq, Hkv, max_len, lp, ncg, min_blocks;
 };
 
 // One warp: quantise the E values x that each lane holds of a row of D = 32 E, write the row's codes and
-// scales to the cache and to the block's copy in shared memory.  Returns whether the lane's group is NaN.
+// scales to the cache and to a staged row (codes, then scales).  Returns whether the lane's group is NaN.
 template <int D>
 __device__ __forceinline__ bool put_row(const float (&x)[D / 32], int lane, uint8_t* codes, uint16_t* scales,
-                                        uint8_t* s_codes, uint16_t* s_scales) {
+                                        uint8_t* staged) {
     constexpr int E = D / 32, LANES = kKv4Group / E, WL = 8 / E;  // lanes of a group and of a word
     float lo = 0.f, hi = 0.f;
     bool odd = false;
@@ -206,11 +230,11 @@ __device__ __forceinline__ bool put_row(const float (&x)[D / 32], int lane, uint
     for (int mask = 1; mask < WL; mask <<= 1) w |= __shfl_xor_sync(0xFFFFFFFFu, w, mask);
     if ((lane & (WL - 1)) == 0) {
         reinterpret_cast<uint32_t*>(codes)[lane / WL] = w;
-        reinterpret_cast<uint32_t*>(s_codes)[lane / WL] = w;
+        reinterpret_cast<uint32_t*>(staged)[lane / WL] = w;
     }
     if ((lane & (LANES - 1)) == 0) {
         scales[lane / LANES] = static_cast<uint16_t>(scale);
-        s_scales[lane / LANES] = static_cast<uint16_t>(scale);
+        reinterpret_cast<uint16_t*>(staged + D / 2)[lane / LANES] = static_cast<uint16_t>(scale);
     }
     return nan;
 }
@@ -218,19 +242,111 @@ __device__ __forceinline__ bool put_row(const float (&x)[D / 32], int lane, uint
 template <int E>
 __device__ __forceinline__ void load_row(const uint16_t* p, int lane, float (&x)[E]) {
     if constexpr (E == 4) {
-        const uint2 w = *reinterpret_cast<const uint2*>(p + 4 * lane);
+        const uint2 w = __ldg(reinterpret_cast<const uint2*>(p + 4 * lane));
         x[0] = __uint_as_float(w.x << 16);
         x[1] = __uint_as_float(w.x & 0xFFFF0000u);
         x[2] = __uint_as_float(w.y << 16);
         x[3] = __uint_as_float(w.y & 0xFFFF0000u);
     } else {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(p + 2 * lane);
+        const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(p + 2 * lane));
         x[0] = __uint_as_float(w << 16);
         x[1] = __uint_as_float(w & 0xFFFF0000u);
     }
 }
 
 __device__ __forceinline__ float round_bf16(float x) { return __bfloat162float(__float2bfloat16_rn(x)); }
+
+// Inclusive sum over the lanes of a warp.
+__device__ __forceinline__ int warp_scan(int v, int lane) {
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int u = __shfl_up_sync(0xFFFFFFFFu, v, d);
+        if (lane >= d) v += u;
+    }
+    return v;
+}
+
+// One warp: the cut of the work from the blocks of each sequence (pre[b + 1] on entry).  On return pre[b] are
+// the blocks, and pieces[b] the pieces, of an item of each sequence before b, summed; returns the blocks per piece,
+// or 0 where the items are more than the CTAs (runs of equal length).
+__device__ __forceinline__ int cut_work(int* pre, int* pieces, int batch, int hc, int ctas, int min_blocks, int lane) {
+    int sum = 0, items = 0, longest = 0, shortest = INT32_MAX;
+    for (int b0 = 0; b0 < batch; b0 += 32) {
+        const int T = b0 + lane < batch ? pre[b0 + lane + 1] : 0;
+        const int v = warp_scan(T, lane);
+        if (b0 + lane < batch) pre[b0 + lane + 1] = sum + v;
+        sum += __shfl_sync(0xFFFFFFFFu, v, 31);
+        items += __popc(__ballot_sync(0xFFFFFFFFu, T > 0));
+        longest = max(longest, __reduce_max_sync(0xFFFFFFFFu, T));
+        shortest = min(shortest, __reduce_min_sync(0xFFFFFFFFu, T > 0 ? T : INT32_MAX));
+    }
+    if (lane == 0) pre[0] = pieces[0] = 0;
+    __syncwarp();
+    if (items == 0 || static_cast<long long>(items) * hc > ctas) return 0;
+    auto pieces_of = [&](int target) {  // of an item of every sequence
+        int n = 0;
+        for (int b = lane; b < batch; b += 32) n += (pre[b + 1] - pre[b] + target - 1) / target;
+        return __reduce_add_sync(0xFFFFFFFFu, n);
+    };
+    const int per = ctas / hc;                                        // pieces that fit, per head and column group
+    int hi = max(min_blocks, (longest + per / items - 1) / (per / items));  // fits
+    int lo = max(min_blocks, (sum + per - 1) / per);                  // no less does
+    if (shortest < longest)
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (pieces_of(mid) <= per) hi = mid;
+            else lo = mid + 1;
+        }
+    int before = 0;
+    for (int b0 = 0; b0 < batch; b0 += 32) {
+        const int n = b0 + lane < batch ? (pre[b0 + lane + 1] - pre[b0 + lane] + hi - 1) / hi : 0;
+        const int v = warp_scan(n, lane);
+        if (b0 + lane < batch) pieces[b0 + lane + 1] = before + v;
+        before += __shfl_sync(0xFFFFFFFFu, v, 31);
+    }
+    return hi;
+}
+
+// The first b with sums[b + 1] * hc > r.
+__device__ __forceinline__ int search(const int* sums, int batch, int hc, int r) {
+    int lo = 0, hi = batch - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (sums[mid + 1] * hc > r) hi = mid;
+        else lo = mid + 1;
+    }
+    return lo;
+}
+
+// The merge of up to N parts (m, l, o[4]) with a running (m, l, o[4]); parts of weight 0 are left out.
+struct Merged {
+    float m = -INFINITY, l = 0.f, o[4] = {};
+    template <int N>
+    __device__ __forceinline__ void add(const float2 (&ml)[N], const float4 (&x)[N]) {
+        float mx = m;
+#pragma unroll
+        for (int i = 0; i < N; ++i) mx = fmaxf(mx, ml[i].x);
+        const float mu = mx == -INFINITY ? 0.f : mx, f0 = exp2_fast(m - mu);
+        m = mx;
+        l *= f0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] *= f0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float f = exp2_fast(ml[i].x - mu);
+            if (f == 0.f) continue;
+            l += f * ml[i].y;
+            o[0] += f * x[i].x;
+            o[1] += f * x[i].y;
+            o[2] += f * x[i].z;
+            o[3] += f * x[i].w;
+        }
+    }
+    __device__ __forceinline__ uint2 result(bool nan) const {
+        if (nan) return make_uint2(0x7FC07FC0u, 0x7FC07FC0u);
+        return make_uint2(pack2(o[0] / l, o[1] / l), pack2(o[2] / l, o[3] / l));
+    }
+};
 
 template <int D, int NT>
 __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(const __grid_constant__ Args a) {
@@ -242,11 +358,12 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
     const uint32_t base = smem_u32(smem);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     int* pre = reinterpret_cast<int*>(smem + C::OFF_PRE);
+    int* pieces = reinterpret_cast<int*>(smem + C::OFF_PIECES);
     int* s_nan = reinterpret_cast<int*>(smem + C::OFF_NAN);
     int* flag = reinterpret_cast<int*>(smem + C::OFF_FLAG);
     uint16_t* s_q = reinterpret_cast<uint16_t*>(smem + C::OFF_Q);
     float* s_o = reinterpret_cast<float*>(smem + C::OFF_O);
-    float* s_ml = reinterpret_cast<float*>(smem + C::OFF_ML);
+    float2* s_ml = reinterpret_cast<float2*>(smem + C::OFF_ML);
     auto bar = [&](int stage) { return base + C::OFF_BAR + 8u * static_cast<uint32_t>(warp * C::STAGES + stage); };
     auto stage_at = [&](int stage) { return static_cast<uint32_t>((warp * C::STAGES + stage) * C::STAGE); };
     if (lane == 0) {
@@ -257,86 +374,86 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
     griddep_wait();
     griddep_launch_dependents();
 
-    // blocks of each sequence, and their running sums.  The blocks of a launch are counted in int: a cache of 2^31
-    // of them would take 2^31 x 4.5 KB / 16 column groups.
+    // The blocks of a launch are counted in int: a cache of 2^31 of them would take 2^31 x 4.5 KB / 16 column groups.
+    const int hc = a.Hkv * a.ncg;  // items of a sequence
+    const int cta = static_cast<int>(blockIdx.x);
     for (int b = tid; b < a.batch; b += C::THREADS) {
         const int h = a.d_hist[b];
         const bool ok = h >= 0 && h <= a.max_len - a.ntok;
-        if (!ok && blockIdx.x == 0) atomicOr(a.err, kDevErrHistRange);
+        if (!ok && cta == 0) atomicOr(a.err, kDevErrHistRange);
         pre[b + 1] = ok ? (h + a.ntok + KB - 1) / KB : 0;
     }
-    __syncthreads();
+    if (a.batch > 32) __syncthreads();  // up to 32 sequences are warp 0's own
     if (warp == 0) {
-        int sum = 0;
-        for (int b0 = 0; b0 < a.batch; b0 += 32) {
-            int v = b0 + lane < a.batch ? pre[b0 + lane + 1] : 0;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int u = __shfl_up_sync(0xFFFFFFFFu, v, d);
-                if (lane >= d) v += u;
-            }
-            if (b0 + lane < a.batch) pre[b0 + lane + 1] = sum + v;
-            sum += __shfl_sync(0xFFFFFFFFu, v, 31);
-        }
-        if (lane == 0) pre[0] = 0;
+        __syncwarp();
+        const int target = cut_work(pre, pieces, a.batch, hc, static_cast<int>(gridDim.x), a.min_blocks, lane);
+        if (lane == 0) flag[1] = target;
     }
     __syncthreads();
-    const int hc = a.Hkv * a.ncg;  // items of a sequence
-    const int total = pre[a.batch] * hc;
-    const int nc = min(static_cast<int>(gridDim.x), max(1, (total + a.min_blocks - 1) / a.min_blocks));
-    const int cta = static_cast<int>(blockIdx.x);
-    if (total == 0 || cta >= nc) return;
-    auto start = [&](int j) { return static_cast<int>(static_cast<long long>(total) * j / nc); };
-    auto cta_of = [&](int r) { return static_cast<int>((static_cast<long long>(r + 1) * nc - 1) / total); };
-    const int r0 = start(cta), r1 = start(cta + 1);
-
-    // where block r lies: sequence, item of the sequence, block of the item
-    auto find = [&](int r, int& b) {
-        while (r >= pre[b + 1] * hc) ++b;
-    };
-    int b_first = 0;
-    {
-        int hi = a.batch - 1;  // the first sequence that ends past r0
-        while (b_first < hi) {
-            const int mid = (b_first + hi) >> 1;
-            if (pre[mid + 1] * hc > r0) hi = mid;
-            else b_first = mid + 1;
-        }
+    const int total = pre[a.batch] * hc, target = flag[1];
+    int r0, r1, nc = 0, piece = 0, b_first;
+    if (target > 0) {
+        if (cta >= pieces[a.batch] * hc) return;
+        b_first = search(pieces, a.batch, hc, cta);
+        const int T = pre[b_first + 1] - pre[b_first], n = pieces[b_first + 1] - pieces[b_first];
+        const int rem = cta - pieces[b_first] * hc, i0 = pre[b_first] * hc + rem / n * T;
+        piece = rem % n;
+        r0 = i0 + T * piece / n;
+        r1 = i0 + T * (piece + 1) / n;
+    } else {
+        nc = min(static_cast<int>(gridDim.x), max(1, (total + a.min_blocks - 1) / a.min_blocks));
+        if (total == 0 || cta >= nc) return;
+        r0 = static_cast<int>(static_cast<long long>(total) * cta / nc);
+        r1 = static_cast<int>(static_cast<long long>(total) * (cta + 1) / nc);
+        b_first = search(pre, a.batch, hc, r0);
     }
+    auto cta_of = [&](int r) { return static_cast<int>((static_cast<long long>(r + 1) * nc - 1) / total); };
 
-    // the warp's blocks: r0 + warp, + W, ...; copies run up to STAGES blocks ahead
-    int next = r0 + warp, b_next = b_first;
+    // The warp's blocks: r0 + warp, + W, ...; copies run up to STAGES blocks ahead.  (b_next, head x column group,
+    // block) is where block `next` lies.
+    int next = r0 + warp, b_next = b_first, T_next = pre[b_first + 1] - pre[b_first];
+    int item_next = (r0 - pre[b_first] * hc) / T_next, blk_next = r0 - pre[b_first] * hc - item_next * T_next + warp;
     uint32_t issued = 0;
     bool dead = false;
     auto issue = [&]() {
         if (next >= r1 || dead) return;
-        find(next, b_next);
-        const int rem = next - pre[b_next] * hc, T = pre[b_next + 1] - pre[b_next];
-        const int blk = rem % T, head = rem / T / a.ncg;
+        while (blk_next >= T_next) {
+            blk_next -= T_next;
+            if (++item_next == hc) {
+                item_next = 0;
+                do ++b_next;
+                while (pre[b_next + 1] == pre[b_next]);
+                T_next = pre[b_next + 1] - pre[b_next];
+            }
+        }
         if (lane == 0) {
             const int st = static_cast<int>(issued % C::STAGES);
-            const size_t slot = (static_cast<size_t>(b_next) * a.Hkv + head) * a.lp + static_cast<size_t>(blk) * KB;
+            const int head = a.ncg == 1 ? item_next : item_next / a.ncg;
+            const size_t slot = (static_cast<size_t>(b_next) * a.Hkv + head) * a.lp + static_cast<size_t>(blk_next) * KB;
             const uint32_t dst = base + stage_at(st);
             mbar_arrive_expect_tx(bar(st), C::STAGE);
             bulk_g2s(dst, a.c.k_codes + slot * C::ROW, C::CODES, bar(st));
-            bulk_g2s(dst + C::CODES, a.c.v_codes + slot * C::ROW, C::CODES, bar(st));
             bulk_g2s(dst + 2 * C::CODES, a.c.k_scales + slot * GR, C::SCALES, bar(st));
+            bulk_g2s(dst + C::CODES, a.c.v_codes + slot * C::ROW, C::CODES, bar(st));
             bulk_g2s(dst + 2 * C::CODES + C::SCALES, a.c.v_scales + slot * GR, C::SCALES, bar(st));
         }
         ++issued;
         next += W;
+        blk_next += W;
     };
     __syncwarp();
 #pragma unroll
     for (int s = 0; s < C::STAGES; ++s) issue();
 
+    uint32_t magic;  // 0x43004300, kept in a register
+    asm volatile("mov.u32 %0, %1;" : "=r"(magic) : "n"(k128));
     uint32_t done = 0;
-    int b_seg = b_first;
+    int b = b_first;
     for (int seg = r0; seg < r1;) {
         // the item of block `seg`, up to where it or the CTA's run ends
-        find(seg, b_seg);
-        const int b = b_seg, T = pre[b + 1] - pre[b];
-        const int rem = seg - pre[b] * hc, item = rem / T, head = item / a.ncg, cg = item % a.ncg;
+        while (seg >= pre[b + 1] * hc) ++b;
+        const int T = pre[b + 1] - pre[b];
+        const int item = (seg - pre[b] * hc) / T, head = item / a.ncg, cg = item % a.ncg;
         const int i0 = pre[b] * hc + item * T;  // the item's first block
         const int end = min(r1, i0 + T);
         const int hist = a.d_hist[b], G = a.Hq / a.Hkv;
@@ -345,55 +462,88 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
         auto row_of = [&](int col) {  // of q and out, in rows of D
             return (static_cast<size_t>(b) * a.ntok + token(col)) * a.Hq + head * G + (c0 + col) % G;
         };
+        if (tid < 4) s_nan[tid] = kNone;
         // q of the columns, rotated and rounded to bf16; columns that do not exist are 0
-        for (int u = tid; u < 16 * (D / 2); u += C::THREADS) {
+        for (int u = tid; u < C::COLS * (D / 2); u += C::THREADS) {
             const int col = u / (D / 2), j = u % (D / 2);
             uint16_t lo = 0, hi = 0;
             if (col < ncol) {
                 const uint16_t* src = a.q + row_of(col) * D;
                 const size_t p = static_cast<size_t>(hist + token(col)) * (D / 2) + j;
-                const float x = __uint_as_float(static_cast<uint32_t>(src[j]) << 16);
-                const float y = __uint_as_float(static_cast<uint32_t>(src[j + D / 2]) << 16);
-                const float cs = a.cos_tab[p], sn = a.sin_tab[p];
+                const float x = __uint_as_float(static_cast<uint32_t>(__ldg(src + j)) << 16);
+                const float y = __uint_as_float(static_cast<uint32_t>(__ldg(src + j + D / 2)) << 16);
+                const float cs = __ldg(a.cos_tab + p), sn = __ldg(a.sin_tab + p);
                 lo = __bfloat16_as_ushort(__float2bfloat16_rn(__fsub_rn(__fmul_rn(x, cs), __fmul_rn(y, sn))));
                 hi = __bfloat16_as_ushort(__float2bfloat16_rn(__fadd_rn(__fmul_rn(y, cs), __fmul_rn(x, sn))));
             }
             s_q[col * C::QS + j] = lo;
             s_q[col * C::QS + j + D / 2] = hi;
         }
-        if (tid < 4) s_nan[tid] = kNone;
+        // the new tokens whose slots lie in the segment's blocks, a warp per row of k or v
+        const int new0 = max(hist, (seg - i0) * KB), new1 = min(hist + a.ntok, (end - i0) * KB);
+        if (new0 < new1) {
+            __syncthreads();  // s_nan is set
+            for (int u = W - 1 - warp; u < 2 * (new1 - new0); u += W) {
+                const int p = new0 + u / 2, i = p - hist;
+                const size_t src = ((static_cast<size_t>(b) * a.ntok + i) * a.Hkv + head) * D;
+                const size_t slot = (static_cast<size_t>(b) * a.Hkv + head) * a.lp + p;
+                uint8_t* staged = smem + C::OFF_NEW + (2 * i + (u & 1)) * C::NEW;
+                float x[E];
+                load_row<E>(((u & 1) ? a.v_new : a.k_new) + src, lane, x);
+                if (u & 1) {
+                    const bool nan = put_row<D>(x, lane, a.c.v_codes + slot * C::ROW, a.c.v_scales + slot * GR, staged);
+                    if (nan && lane % (kKv4Group / E) == 0) atomicMin(&s_nan[lane / (kKv4Group / E)], i);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const size_t j = static_cast<size_t>(p) * (D / 2) + (lane & 15) * E + e;
+                        const float other = __shfl_xor_sync(0xFFFFFFFFu, x[e], 16);
+                        const float cs = __ldg(a.cos_tab + j), sn = __ldg(a.sin_tab + j);
+                        x[e] = round_bf16(lane < 16 ? __fsub_rn(__fmul_rn(x[e], cs), __fmul_rn(other, sn))
+                                                    : __fadd_rn(__fmul_rn(x[e], cs), __fmul_rn(other, sn)));
+                    }
+                    put_row<D>(x, lane, a.c.k_codes + slot * C::ROW, a.c.k_scales + slot * GR, staged);
+                }
+            }
+        }
         __syncthreads();
 
-        // Q's A fragments: lane (g, t) holds values D/4 t .. D/4 t + D/4 - 1 of columns g (and g + 8); step (w, h)
-        // of the products takes values 8 w + 4 h .. + 3 of them.  qz: minus their sum in three parts.
-        uint32_t qa[NT][2 * KW][2], qz[NT][2];
+        // Q^T's B fragments: lane (g, t) holds values D/4 t .. D/4 t + D/4 - 1 of column g (+ 8 n); step s of the
+        // products takes values 4 s .. 4 s + 3 of them.  qz: minus their sum in three parts.
+        uint32_t qb[NT][2 * KW][2], qz[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const uint32_t row = base + C::OFF_Q + ((g + 8 * n) * C::QS + (D / 4) * t) * 2;
-            float total_q = 0.f;
+            float sum_q = 0.f;
 #pragma unroll
-            for (int s = 0; s < 2 * KW; ++s)
+            for (int s = 0; s < 2 * KW; ++s) {
+                lds<2>(row + 8 * s, qb[n][s]);
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const uint32_t w = lds32(row + 8 * s + 4 * e);
-                    qa[n][s][e] = w;
-                    total_q += __uint_as_float(w << 16) + __uint_as_float(w & 0xFFFF0000u);
-                }
-            const float p0 = round_bf16(-total_q), p1 = round_bf16(-total_q - p0), p2 = (-total_q - p0) - p1;
+                for (int e = 0; e < 2; ++e)
+                    sum_q += __uint_as_float(qb[n][s][e] << 16) + __uint_as_float(qb[n][s][e] & 0xFFFF0000u);
+            }
+            const float p0 = round_bf16(-sum_q), p1 = round_bf16(-sum_q - p0), p2 = (-sum_q - p0) - p1;
             qz[n][0] = pack2(p0, p1);
             qz[n][1] = pack2(p2, 0.f);
         }
-        float o[NT][4 * VW][4] = {}, sum[NT][4] = {};  // sum: rows 8 .. 15 the softmax sum
-        float m[NT], ml[NT];                          // running maximum of the column (scaled by log2 e / sqrt D)
-        int lim[NT];                                  // last slot that the column sees
+        float o[NT][4 * VW][4] = {}, sum[NT][4] = {};
+        // of columns 2 t and 2 t + 1 (+ 8 n): the running maximum m of the scores, m log2 e / sqrt D (0 while m
+        // is -inf), and the last slot that the column sees
+        float m[NT][2], ms[NT][2];
+        int lim[NT][2];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            m[n] = -INFINITY;
-            ml[n] = 0.f;  // m, or 0 while that is -inf
-            lim[n] = hist + (g + 8 * n < ncol ? token(g + 8 * n) : a.ntok - 1);
-        }
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int col = 8 * n + 2 * t + e;
+                m[n][e] = -INFINITY;
+                ms[n][e] = 0.f;
+                lim[n][e] = hist + (col < ncol ? token(col) : a.ntok - 1);
+            }
 
-        for (int r = r0 + warp + static_cast<int>(done) * W; r < end; r += W) {
+        int r = r0 + warp + static_cast<int>(done) * W;
+        const bool has_blocks = r < end;
+        for (; r < end; r += W) {
             const int st = static_cast<int>(done % C::STAGES);
             const int k0 = (r - i0) * KB;
             if (!dead && !mbar_wait(bar(st), (done / C::STAGES) & 1u, nullptr, a.wait_ns)) {
@@ -405,169 +555,183 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
             if (dead) continue;
             const uint32_t s_k = base + stage_at(st), s_v = s_k + C::CODES, s_ks = s_v + C::CODES, s_vs = s_ks + C::SCALES;
             const bool tail = k0 + KB > hist;  // the block holds slots of new tokens, or none at all
-            if (tail) {
+            if (tail) {  // the staged rows into the block
                 const int lo = max(k0, hist), hi = min(k0 + KB, hist + a.ntok);
-                uint8_t* gs = smem + stage_at(st);
-                for (int p = lo; p < hi; ++p) {
-                    const size_t src = ((static_cast<size_t>(b) * a.ntok + (p - hist)) * a.Hkv + head) * D;
-                    const size_t slot = (static_cast<size_t>(b) * a.Hkv + head) * a.lp + p;
-                    float x[E], y[E], v[E];
-                    load_row<E>(a.k_new + src, lane, x);
-                    load_row<E>(a.v_new + src, lane, v);
+                for (int p = lo; p < hi; ++p)
 #pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const size_t j = static_cast<size_t>(p) * (D / 2) + (lane & 15) * E + e;
-                        const float other = __shfl_xor_sync(0xFFFFFFFFu, x[e], 16), cs = a.cos_tab[j], sn = a.sin_tab[j];
-                        y[e] = round_bf16(lane < 16 ? __fsub_rn(__fmul_rn(x[e], cs), __fmul_rn(other, sn))
-                                                    : __fadd_rn(__fmul_rn(x[e], cs), __fmul_rn(other, sn)));
+                    for (int kind = 0; kind < 2; ++kind) {
+                        const uint32_t* src =
+                            reinterpret_cast<const uint32_t*>(smem + C::OFF_NEW + (2 * (p - hist) + kind) * C::NEW);
+                        uint8_t* blk = smem + stage_at(st);
+                        if (lane < C::ROW / 4)
+                            reinterpret_cast<uint32_t*>(blk + kind * C::CODES + (p - k0) * C::ROW)[lane] = src[lane];
+                        else if (lane < C::NEW / 4)
+                            reinterpret_cast<uint32_t*>(blk + 2 * C::CODES + kind * C::SCALES + (p - k0) * GR * 2)[lane - C::ROW / 4] =
+                                src[lane];
                     }
-                    const int i = p - k0;
-                    put_row<D>(y, lane, a.c.k_codes + slot * C::ROW, a.c.k_scales + slot * GR, gs + i * C::ROW,
-                               reinterpret_cast<uint16_t*>(gs + 2 * C::CODES) + i * GR);
-                    const bool nan = put_row<D>(v, lane, a.c.v_codes + slot * C::ROW, a.c.v_scales + slot * GR,
-                                                gs + C::CODES + i * C::ROW,
-                                                reinterpret_cast<uint16_t*>(gs + 2 * C::CODES + C::SCALES) + i * GR);
-                    if (nan && lane % (kKv4Group / E) == 0) atomicMin(&s_nan[lane / (kKv4Group / E)], p - hist);
-                }
                 __syncwarp();
             }
             const int last = hist + a.ntok - 1 - k0;  // last slot of the block that holds a token
+            auto attend = [&](auto is_tail) {
+                constexpr bool TAIL = decltype(is_tail)::value;
 #pragma unroll
-            for (int half = 0; half < KB / 32; ++half) {
-                if (half > 0 && 32 * half > last) break;
-                // scores of 32 slots: lane (g, t) has columns g, g + 8 at slots 2 t, 2 t + 1 of each 8
-                float s[4][4];
+                for (int half = 0; half < KB / 32; ++half) {
+                    if (TAIL && half > 0 && 32 * half > last) break;
+                    // scores of 32 slots: lane (g, t) has slots g, g + 8 of each 16, columns 2 t, 2 t + 1 (+ 8 n)
+                    float s[2][NT][4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int key = 32 * half + 8 * j + g;
-                    uint32_t w[KW], zs;
-                    lds<KW>(s_k + key * C::ROW + t * (KW * 4), w);
-                    const uint32_t sc = lds16(s_ks + (key * GR + t * GR / 4) * 2);
-                    const Pair p = pair_of(sc * 0x10001u, zs);
-                    s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
-                    mma(s[j], qz[0][0], NT == 2 ? qz[NT - 1][0] : 0u, qz[0][1], NT == 2 ? qz[NT - 1][1] : 0u, zs, zs);
-#pragma unroll
-                    for (int e = 0; e < 2 * KW; ++e)
-                        mma(s[j], qa[0][e][0], NT == 2 ? qa[NT - 1][e][0] : 0u, qa[0][e][1], NT == 2 ? qa[NT - 1][e][1] : 0u,
-                            decode2(w[e / 2], 2 * (e % 2), p), decode2(w[e / 2], 2 * (e % 2) + 1, p));
-                }
-                bool moves = false;
-                float mx[NT];
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    mx[n] = -INFINITY;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
+                    for (int j = 0; j < 2; ++j) {
+                        uint32_t w[2][KW], zs[2];
+                        Pair p[2];
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            float& x = s[j][2 * n + e];
-                            x *= a.scale_log2;
-                            if (tail && k0 + 32 * half + 8 * j + 2 * t + e > lim[n]) x = -INFINITY;
-                            mx[n] = fmaxf(mx[n], x);
+                            const int key = 32 * half + 16 * j + 8 * e + g;
+                            lds<KW>(s_k + key * C::ROW + t * (KW * 4), w[e]);
+                            p[e] = pair_of(__byte_perm(lds16(s_ks + (key * GR + t * GR / 4) * 2), 0, 0x1010), zs[e], magic);
                         }
-                    moves |= mx[n] > m[n] + 8.f;
-                }
-                if (__any_sync(0xFFFFFFFFu, moves)) {
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        float x = fmaxf(mx[n], __shfl_xor_sync(0xFFFFFFFFu, mx[n], 1));
-                        x = fmaxf(fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 2)), m[n]);
-                        const float f = m[n] == x ? 1.f : exp2_fast(m[n] - x);
-                        m[n] = x;
-                        ml[n] = x == -INFINITY ? 0.f : x;
-                        const float f0 = __shfl_sync(0xFFFFFFFFu, f, 8 * t), f1 = __shfl_sync(0xFFFFFFFFu, f, 8 * t + 4);
+                        for (int n = 0; n < NT; ++n) {
+                            s[j][n][0] = s[j][n][1] = s[j][n][2] = s[j][n][3] = 0.f;
+                            mma(s[j][n], zs[0], zs[1], zs[0], zs[1], qz[n][0], qz[n][1]);
+                        }
 #pragma unroll
-                        for (int i = 0; i <= 4 * VW; ++i) {
-                            float(&acc)[4] = i == 4 * VW ? sum[n] : o[n][i < 4 * VW ? i : 0];
-                            acc[0] *= f0;
-                            acc[1] *= f1;
-                            acc[2] *= f0;
-                            acc[3] *= f1;
+                        for (int i = 0; i < 2 * KW; ++i) {
+                            const uint32_t x0 = decode2(w[0][i / 2], 2 * (i % 2), p[0], magic),
+                                           x1 = decode2(w[1][i / 2], 2 * (i % 2), p[1], magic),
+                                           x2 = decode2(w[0][i / 2], 2 * (i % 2) + 1, p[0], magic),
+                                           x3 = decode2(w[1][i / 2], 2 * (i % 2) + 1, p[1], magic);
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) mma(s[j][n], x0, x1, x2, x3, qb[n][i][0], qb[n][i][1]);
+                        }
+                    }
+                    bool moves = false;
+                    float mx[NT][2];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            if (TAIL)
+#pragma unroll
+                                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                                    for (int h = 0; h < 2; ++h)
+                                        if (k0 + 32 * half + 16 * j + 8 * h + g > lim[n][e]) s[j][n][2 * h + e] = -INFINITY;
+                            mx[n][e] = fmaxf(fmaxf(s[0][n][e], s[0][n][2 + e]), fmaxf(s[1][n][e], s[1][n][2 + e]));
+                            moves |= mx[n][e] > m[n][e] + a.move;
+                        }
+                    if (__any_sync(0xFFFFFFFFu, moves)) {
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                float x = mx[n][e];
+#pragma unroll
+                                for (int mask = 4; mask <= 16; mask <<= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, mask));
+                                x = fmaxf(x, m[n][e]);
+                                const float f = m[n][e] == x ? 1.f : exp2_fast((m[n][e] - x) * a.scale_log2);
+                                m[n][e] = x;
+                                ms[n][e] = x == -INFINITY ? 0.f : x * a.scale_log2;
+                                sum[n][e] *= f;
+#pragma unroll
+                                for (int i = 0; i < 4 * VW; ++i) {
+                                    o[n][i][e] *= f;
+                                    o[n][i][2 + e] *= f;
+                                }
+                            }
+                    }
+                    uint32_t pb[NT][4];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float* x = &s[j / 2][n][2 * (j % 2)];
+                            pb[n][j] = transpose8(pack2(exp2_fast(fmaf(x[0], a.scale_log2, -ms[n][0])),
+                                                        exp2_fast(fmaf(x[1], a.scale_log2, -ms[n][1]))));
+                        }
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {  // 16 slots
+                        const int key = 32 * half + 16 * k + 2 * t;
+                        uint32_t w[4][VW], sc[4];  // slots 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int row = key + (e & 1) + 8 * (e >> 1);
+                            lds<VW>(s_v + row * C::ROW + g * (VW * 4), w[e]);
+                            sc[e] = lds16(s_vs + (row * GR + g * GR / 8) * 2);
+                            if (TAIL && (row > last || (sc[e] == kKv4NanScale && k0 + row > hist))) sc[e] = 0;
+                        }
+                        const ZPair p01 = zpair_of(__byte_perm(sc[0], sc[1], 0x5410), magic),
+                                    p23 = zpair_of(__byte_perm(sc[2], sc[3], 0x5410), magic);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) mma(sum[n], kOnes, kOnes, kOnes, kOnes, pb[n][2 * k], pb[n][2 * k + 1]);
+#pragma unroll
+                        for (int v = 0; v < VW; ++v) {
+                            const uint32_t a01 = __byte_perm(w[0][v], w[1][v], 0x5410), b01 = __byte_perm(w[0][v], w[1][v], 0x7632);
+                            const uint32_t a23 = __byte_perm(w[2][v], w[3][v], 0x5410), b23 = __byte_perm(w[2][v], w[3][v], 0x7632);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const uint32_t x0 = value2(a01, i, p01, magic), x1 = value2(b01, i, p01, magic),
+                                               x2 = value2(a23, i, p23, magic), x3 = value2(b23, i, p23, magic);
+#pragma unroll
+                                for (int n = 0; n < NT; ++n)
+                                    mma(o[n][4 * v + i], x0, x1, x2, x3, pb[n][2 * k], pb[n][2 * k + 1]);
+                            }
                         }
                     }
                 }
-                uint32_t pb[NT][4];
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        pb[n][j] = pack2(exp2_fast(s[j][2 * n] - ml[n]), exp2_fast(s[j][2 * n + 1] - ml[n]));
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {  // 16 slots
-                    const int key = 32 * half + 16 * k + 2 * t;
-                    uint32_t w[4][VW], sc[4];  // slots 2 t, 2 t + 1, 2 t + 8, 2 t + 9
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int row = key + (e & 1) + 8 * (e >> 1);
-                        lds<VW>(s_v + row * C::ROW + g * (VW * 4), w[e]);
-                        sc[e] = lds16(s_vs + (row * GR + g * GR / 8) * 2);
-                        if (tail && (row > last || (sc[e] == kKv4NanScale && k0 + row > hist))) sc[e] = 0;
-                    }
-                    const ZPair p01 = zpair_of(sc[0] | (sc[1] << 16)), p23 = zpair_of(sc[2] | (sc[3] << 16));
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) mma(sum[n], 0u, kOnes, 0u, kOnes, pb[n][2 * k], pb[n][2 * k + 1]);
-#pragma unroll
-                    for (int v = 0; v < VW; ++v) {
-                        const uint32_t a01 = __byte_perm(w[0][v], w[1][v], 0x5410), b01 = __byte_perm(w[0][v], w[1][v], 0x7632);
-                        const uint32_t a23 = __byte_perm(w[2][v], w[3][v], 0x5410), b23 = __byte_perm(w[2][v], w[3][v], 0x7632);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t x0 = value2(a01, i, p01), x1 = value2(b01, i, p01), x2 = value2(a23, i, p23),
-                                           x3 = value2(b23, i, p23);
-#pragma unroll
-                            for (int n = 0; n < NT; ++n) mma(o[n][4 * v + i], x0, x1, x2, x3, pb[n][2 * k], pb[n][2 * k + 1]);
-                        }
-                    }
-                }
-            }
+            };
+            if (tail) attend(std::true_type{});
+            else attend(std::false_type{});
             if (tail) fence_proxy_async_smem();  // this warp wrote to the stage that the next copy fills
             __syncwarp();
             issue();
         }
 
-        // The warps' parts meet.  Lane (g, t) holds columns 2 t, 2 t + 1 (+ 8 n) of values D/8 g .. D/8 g + D/8 - 1
-        // and m of column g.
+        // The warps' parts meet.  Lane (g, t) holds columns 2 t, 2 t + 1 (+ 8 n) of values D/8 g .. D/8 g + D/8 - 1.
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const float m0 = __shfl_sync(0xFFFFFFFFu, m[n], 8 * t), m1 = __shfl_sync(0xFFFFFFFFu, m[n], 8 * t + 4);
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int col = warp * C::COLS + 8 * n + 2 * t + e;
-                float* dst = s_o + col * C::OS + (D / 8) * g;
+                if (has_blocks) {
+                    float* dst = s_o + col * C::OS + (D / 8) * g;
 #pragma unroll
-                for (int i = 0; i < 4 * VW; ++i)
-                    *reinterpret_cast<float2*>(dst + 2 * i) = make_float2(o[n][i][e], o[n][i][2 + e]);
-                if (g == 0) {
-                    s_ml[2 * col] = e ? m1 : m0;
-                    s_ml[2 * col + 1] = sum[n][2 + e];
+                    for (int i = 0; i < 2 * VW; ++i)
+                        *reinterpret_cast<float4*>(dst + 4 * i) =
+                            make_float4(o[n][2 * i][e], o[n][2 * i][2 + e], o[n][2 * i + 1][e], o[n][2 * i + 1][2 + e]);
                 }
+                if (g == 0) s_ml[col] = make_float2(m[n][e] * a.scale_log2, sum[n][e]);
             }
-        }
         __syncthreads();
-        const int j0 = cta_of(i0), j1 = cta_of(i0 + T - 1);  // the CTAs that share the item
-        const int part = 2 * cta + (i0 >= r0 ? 1 : 0);
-        for (int u = tid; u < ncol * D; u += C::THREADS) {
-            const int col = u / D, d = u % D;
-            float mx = -INFINITY;
+        int j0, j1;  // the CTAs that share the item
+        if (target > 0) {
+            j0 = cta - piece;
+            j1 = j0 + pieces[b + 1] - pieces[b] - 1;
+        } else {
+            j0 = cta_of(i0);
+            j1 = cta_of(i0 + T - 1);
+        }
+        const int part = 2 * cta + (cta == j0 ? 1 : 0);
+        for (int u = tid; u < ncol * (D / 4); u += C::THREADS) {
+            const int col = u / (D / 4), d = u % (D / 4) * 4;
+            Merged acc;
 #pragma unroll
-            for (int w = 0; w < W; ++w) mx = fmaxf(mx, s_ml[2 * (w * C::COLS + col)]);
-            const float mu = mx == -INFINITY ? 0.f : mx;
-            float acc = 0.f, l = 0.f;
+            for (int w0 = 0; w0 < W; w0 += 4) {
+                float2 ml[4];
+                float4 x[4];
 #pragma unroll
-            for (int w = 0; w < W; ++w) {
-                const float f = exp2_fast(s_ml[2 * (w * C::COLS + col)] - mu);
-                l += f * s_ml[2 * (w * C::COLS + col) + 1];
-                acc += f * s_o[(w * C::COLS + col) * C::OS + d];
+                for (int w = 0; w < 4; ++w) {
+                    ml[w] = s_ml[(w0 + w) * C::COLS + col];
+                    x[w] = *reinterpret_cast<const float4*>(s_o + ((w0 + w) * C::COLS + col) * C::OS + d);
+                }
+                acc.add(ml, x);
             }
             if (j0 == j1) {
-                const bool nan = s_nan[d / kKv4Group] <= token(col) && s_nan[d / kKv4Group] > 0;
-                a.out[row_of(col) * D + d] = nan ? 0x7FC0 : __bfloat16_as_ushort(__float2bfloat16_rn(acc / l));
+                const int first = s_nan[d / kKv4Group];
+                *reinterpret_cast<uint2*>(a.out + row_of(col) * D + d) = acc.result(first > 0 && first <= token(col));
             } else {
-                a.part_o[(static_cast<size_t>(part) * 16 + col) * D + d] = acc;
-                if (d == 0) {
-                    a.part_ml[2 * (part * 16 + col)] = mx;
-                    a.part_ml[2 * (part * 16 + col) + 1] = l;
-                }
+                *reinterpret_cast<float4*>(a.part_o + (static_cast<size_t>(part) * 16 + col) * D + d) =
+                    make_float4(acc.o[0], acc.o[1], acc.o[2], acc.o[3]);
+                if (d == 0) reinterpret_cast<float2*>(a.part_ml)[part * 16 + col] = make_float2(acc.m, acc.l);
             }
         }
         if (j0 != j1) {
@@ -575,32 +739,31 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
             __threadfence();
             __syncthreads();
             int* count = a.counters + static_cast<size_t>(b) * hc + item;
-            if (tid == 0) *flag = atomicAdd(count, 1) == j1 - j0;
+            if (tid == 0) flag[0] = atomicAdd(count, 1) == j1 - j0;
             __syncthreads();
-            if (*flag) {  // the last of the item's CTAs merges them, in order
+            if (flag[0]) {  // the last of the item's CTAs merges them, in order
                 __threadfence();
                 if (tid == 0) *count = 0;
-                auto part_of = [&](int j) { return 2 * j + (j == j0 ? 1 : 0); };
-                for (int u = tid; u < ncol * D; u += C::THREADS) {
-                    const int col = u / D, d = u % D;
-                    float mx = -INFINITY;
+                for (int u = tid; u < ncol * (D / 4); u += C::THREADS) {
+                    const int col = u / (D / 4), d = u % (D / 4) * 4;
+                    Merged acc;
                     int nan = kNone;
-                    for (int j = j0; j <= j1; ++j) {
-                        mx = fmaxf(mx, __ldcg(a.part_ml + 2 * (part_of(j) * 16 + col)));
-                        const int first = __ldcg(a.part_nan + 4 * part_of(j) + d / kKv4Group);
-                        nan = min(nan, first);
+                    for (int j = j0; j <= j1; j += 8) {
+                        float2 ml[8];
+                        float4 x[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            ml[i] = make_float2(-INFINITY, 0.f);
+                            x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                            if (j + i > j1) continue;
+                            const int from = 2 * (j + i) + (j + i == j0 ? 1 : 0), row = from * 16 + col;
+                            ml[i] = __ldcg(reinterpret_cast<const float2*>(a.part_ml) + row);
+                            x[i] = __ldcg(reinterpret_cast<const float4*>(a.part_o + static_cast<size_t>(row) * D + d));
+                            if (a.ntok > 1) nan = min(nan, __ldcg(a.part_nan + 4 * from + d / kKv4Group));
+                        }
+                        acc.add(ml, x);
                     }
-                    const float mu = mx == -INFINITY ? 0.f : mx;
-                    float acc = 0.f, l = 0.f;
-                    for (int j = j0; j <= j1; ++j) {
-                        const int row = part_of(j) * 16 + col;
-                        const float f = exp2_fast(__ldcg(a.part_ml + 2 * row) - mu);
-                        l += f * __ldcg(a.part_ml + 2 * row + 1);
-                        acc += f * __ldcg(a.part_o + static_cast<size_t>(row) * D + d);
-                    }
-                    a.out[row_of(col) * D + d] = nan <= token(col) && nan > 0
-                                                     ? 0x7FC0
-                                                     : __bfloat16_as_ushort(__float2bfloat16_rn(acc / l));
+                    *reinterpret_cast<uint2*>(a.out + row_of(col) * D + d) = acc.result(nan > 0 && nan <= token(col));
                 }
             }
         }
@@ -617,11 +780,9 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
 template <int D, int NT>
 cudaError_t launch(const Args& a, int num_sms, cudaStream_t st) {
     using C = Cfg<D, NT>;
-    // a run of fewer than W blocks leaves warps idle, but spreads a short history over more SMs
     const long long most = static_cast<long long>(a.batch) * a.Hkv * a.ncg * ((a.max_len + C::KB - 1) / C::KB);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(
-        std::max(1LL, std::min<long long>(num_sms, (most + a.min_blocks - 1) / a.min_blocks))));
+    cfg.gridDim = dim3(static_cast<unsigned>(std::min<long long>(num_sms, most)));
     cfg.blockDim = dim3(C::THREADS);
     cfg.dynamicSmemBytes = C::BYTES;
     cfg.stream = st;
@@ -675,6 +836,7 @@ cudaError_t launch_kv4_decode(const Shape& s, const uint16_t* q, const uint16_t*
         a.err = err;
         a.wait_ns = wait_ns;
         a.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(s.head_dim)));
+        a.move = 8.f / a.scale_log2;
         a.batch = std::min(kMaxSeqs, s.batch - b0);
         a.ntok = ntok;
         a.Hq = s.n_q_heads;
