@@ -17,12 +17,16 @@
 // P^T goes from the layout of the first's result to the operand of the second by an 8 x 8 transpose
 // (movmatrix) per 8 slots.  (With S [cols x slots] it needs none, but its Q fragments are half zeros for
 // up to 8 columns, and the moves that set them up cost more than the products.)
-// Decoding is a shift and a masked OR of the pair (128 + c, 128 + c').  For k one fma with (s, -128 s) then
-// gives c s exactly (kv4.cuh), and the zero points go as a product of their own, one further mma:
+// Decoding: a code in bits 0 .. 3 of a bf16 that is otherwise 0 is the subnormal c 2^-133, and in bits 4 .. 7 it is
+// 16 c 2^-133 (where the exponent's first bit comes in, the spacing is still that of the subnormals).  So one AND
+// makes a pair of numbers, without a shift for every other pair, and one product with s 2^60, or s 2^56,
+// makes c s 2^-73, exactly (kv4.cuh); scales of 2^-53 to 2^67 stay in the range of bf16.  Scores are in units of
+// 2^-73; P and its sum are 2^60 times as large, so that small weights of small values stay above the
+// least float.  For k the zero points go as a product of their own, one further mma:
 //   S -= sum over groups of (z s) (sum of q over the group), those sums in three bf16 parts.
-// For v it is the difference with 128 + z and the product with s, both exact: a v that is small
-// beside its group must not be what is left of two larger sums.  Rows of ones in place of V^T give the
-// softmax sum, of the same rounded P that weighs V.
+// For v it is one fma with - z s instead of the product: a v that is small beside its group must not be
+// what is left of two larger sums.  Rows of ones in place of V^T give the softmax sum, of the same rounded P
+// that weighs V.
 // The running maximum moves lazily: only when a score passes it by 2^8 are O and the sum rescaled.
 //
 // The new tokens: before its item's blocks a CTA that holds their slots rotates and quantises them, a warp per
@@ -83,19 +87,14 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-__device__ __forceinline__ uint32_t fma2(uint32_t a, uint32_t b, uint32_t c) {
+__device__ __forceinline__ uint32_t fms2(uint32_t a, uint32_t b, uint32_t c) {  // a b - c
     uint32_t d;
-    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    asm("{.reg .b32 n;\n\tneg.bf16x2 n, %3;\n\tfma.rn.bf16x2 %0, %1, %2, n;}" : "=r"(d) : "r"(a), "r"(b), "r"(c));
     return d;
 }
 __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
     uint32_t d;
     asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
-__device__ __forceinline__ uint32_t sub2(uint32_t a, uint32_t b) {
-    uint32_t d;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
     return d;
 }
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -109,39 +108,31 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     return d;
 }
 
-constexpr uint32_t kOnes = 0x3F803F80u, kMinus128 = 0xC300C300u, k128 = 0x43004300u;
+constexpr uint32_t kOnes = 0x3F803F80u;                       // 1
+constexpr uint32_t kUp = 0x5D805D80u, kSixteenth = 0x3D803D80u;  // 2^60, 2^-4
+constexpr float kUnit = 9.44473296573929e21f;                // 2^73
+constexpr float kLift = 60.f;                                // P is 2^60 times the weights
 
-// The pair of codes in bits 0 .. 3 and 16 .. 19 as bf16 128 + c: one LOP3, which takes one constant as an
-// immediate and the other from a register (left to the compiler it is two).
-__device__ __forceinline__ uint32_t codes_of(uint32_t w, uint32_t k128reg) {
-    uint32_t d;
-    asm("lop3.b32 %0, %1, 0x000F000F, %2, 0xEA;" : "=r"(d) : "r"(w), "r"(k128reg));
-    return d;
-}
-
-// The scales of a pair of values: s and -128 s (for decode2), and z s.
+// The scales of a pair of values, for codes in the low and in the high four bits of a byte, and z s (in
+// units of 2^-73).
 struct Pair {
-    uint32_t s, n;
+    uint32_t lo, hi, zs;
 };
-__device__ __forceinline__ Pair pair_of(uint32_t m2, uint32_t& zs, uint32_t magic) {
+__device__ __forceinline__ Pair pair_of(uint32_t m2) {
     Pair p;
-    p.s = m2 & 0x7FF07FF0u;
-    p.n = mul2(p.s, kMinus128);
-    zs = fma2(codes_of(m2, magic), p.s, p.n);
+    p.lo = mul2(m2 & 0x7FF07FF0u, kUp);
+    p.hi = mul2(p.lo, kSixteenth);
+    p.zs = mul2(m2 & 0x000F000Fu, p.lo);
     return p;
 }
-struct ZPair {  // the scales s of a pair and 128 + z
-    uint32_t s, z;
-};
-__device__ __forceinline__ ZPair zpair_of(uint32_t m2, uint32_t magic) {
-    return {m2 & 0x7FF07FF0u, codes_of(m2, magic)};
+// Pair i of a word and of the same word shifted right by 8: c s, and (c - z) s.
+__device__ __forceinline__ uint32_t code2(uint32_t w, uint32_t w8, int i, const Pair& p) {
+    const uint32_t x = i < 2 ? w : w8;
+    return i % 2 == 0 ? mul2(x & 0x000F000Fu, p.lo) : mul2(x & 0x00F000F0u, p.hi);
 }
-__device__ __forceinline__ uint32_t value2(uint32_t w, int i, const ZPair& p, uint32_t magic) {
-    return mul2(sub2(codes_of(w >> (4 * i), magic), p.z), p.s);
-}
-// Pair i of a word: the two codes at bit 4 i of its halves, times s.
-__device__ __forceinline__ uint32_t decode2(uint32_t w, int i, const Pair& p, uint32_t magic) {
-    return fma2(codes_of(w >> (4 * i), magic), p.s, p.n);
+__device__ __forceinline__ uint32_t value2(uint32_t w, uint32_t w8, int i, const Pair& p) {
+    const uint32_t x = i < 2 ? w : w8;
+    return i % 2 == 0 ? fms2(x & 0x000F000Fu, p.lo, p.zs) : fms2(x & 0x00F000F0u, p.hi, p.zs);
 }
 
 __device__ __forceinline__ uint32_t lds32(uint32_t a) {
@@ -189,7 +180,7 @@ struct Args {
     int* counters;   // per item, zero between launches
     int* err;
     uint64_t wait_ns;
-    float scale_log2, move;  // log2 e / sqrt D, and the lead of a score that moves the maximum (2^8)
+    float scale_log2, move;  // log2 e / sqrt D in units of 2^-73, and the lead of a score that moves the maximum (2^8)
     int batch, ntok, Hq, Hkv, max_len, lp, ncg, min_blocks;
 };
 
@@ -344,7 +335,8 @@ struct Merged {
     }
     __device__ __forceinline__ uint2 result(bool nan) const {
         if (nan) return make_uint2(0x7FC07FC0u, 0x7FC07FC0u);
-        return make_uint2(pack2(o[0] / l, o[1] / l), pack2(o[2] / l, o[3] / l));
+        const float f = kUnit / l;
+        return make_uint2(pack2(o[0] * f, o[1] * f), pack2(o[2] * f, o[3] * f));
     }
 };
 
@@ -445,8 +437,6 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
 #pragma unroll
     for (int s = 0; s < C::STAGES; ++s) issue();
 
-    uint32_t magic;  // 0x43004300, kept in a register
-    asm volatile("mov.u32 %0, %1;" : "=r"(magic) : "n"(k128));
     uint32_t done = 0;
     int b = b_first;
     for (int seg = r0; seg < r1;) {
@@ -528,7 +518,7 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
         }
         float o[NT][4 * VW][4] = {}, sum[NT][4] = {};
         // of columns 2 t and 2 t + 1 (+ 8 n): the running maximum m of the scores, m log2 e / sqrt D (0 while m
-        // is -inf), and the last slot that the column sees
+        // is -inf) less kLift, and the last slot that the column sees
         float m[NT][2], ms[NT][2];
         int lim[NT][2];
 #pragma unroll
@@ -537,7 +527,7 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
             for (int e = 0; e < 2; ++e) {
                 const int col = 8 * n + 2 * t + e;
                 m[n][e] = -INFINITY;
-                ms[n][e] = 0.f;
+                ms[n][e] = -kLift;
                 lim[n][e] = hist + (col < ncol ? token(col) : a.ntok - 1);
             }
 
@@ -581,25 +571,25 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
                     float s[2][NT][4];
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        uint32_t w[2][KW], zs[2];
+                        uint32_t w[2][KW];
                         Pair p[2];
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             const int key = 32 * half + 16 * j + 8 * e + g;
                             lds<KW>(s_k + key * C::ROW + t * (KW * 4), w[e]);
-                            p[e] = pair_of(__byte_perm(lds16(s_ks + (key * GR + t * GR / 4) * 2), 0, 0x1010), zs[e], magic);
+                            p[e] = pair_of(__byte_perm(lds16(s_ks + (key * GR + t * GR / 4) * 2), 0, 0x1010));
                         }
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
                             s[j][n][0] = s[j][n][1] = s[j][n][2] = s[j][n][3] = 0.f;
-                            mma(s[j][n], zs[0], zs[1], zs[0], zs[1], qz[n][0], qz[n][1]);
+                            mma(s[j][n], p[0].zs, p[1].zs, p[0].zs, p[1].zs, qz[n][0], qz[n][1]);
                         }
 #pragma unroll
                         for (int i = 0; i < 2 * KW; ++i) {
-                            const uint32_t x0 = decode2(w[0][i / 2], 2 * (i % 2), p[0], magic),
-                                           x1 = decode2(w[1][i / 2], 2 * (i % 2), p[1], magic),
-                                           x2 = decode2(w[0][i / 2], 2 * (i % 2) + 1, p[0], magic),
-                                           x3 = decode2(w[1][i / 2], 2 * (i % 2) + 1, p[1], magic);
+                            const uint32_t w0 = w[0][i / 2], w1 = w[1][i / 2];
+                            const uint32_t x0 = code2(w0, w0 >> 8, 2 * (i % 2), p[0]), x1 = code2(w1, w1 >> 8, 2 * (i % 2), p[1]),
+                                           x2 = code2(w0, w0 >> 8, 2 * (i % 2) + 1, p[0]),
+                                           x3 = code2(w1, w1 >> 8, 2 * (i % 2) + 1, p[1]);
 #pragma unroll
                             for (int n = 0; n < NT; ++n) mma(s[j][n], x0, x1, x2, x3, qb[n][i][0], qb[n][i][1]);
                         }
@@ -630,7 +620,7 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
                                 x = fmaxf(x, m[n][e]);
                                 const float f = m[n][e] == x ? 1.f : exp2_fast((m[n][e] - x) * a.scale_log2);
                                 m[n][e] = x;
-                                ms[n][e] = x == -INFINITY ? 0.f : x * a.scale_log2;
+                                ms[n][e] = (x == -INFINITY ? 0.f : x * a.scale_log2) - kLift;
                                 sum[n][e] *= f;
 #pragma unroll
                                 for (int i = 0; i < 4 * VW; ++i) {
@@ -659,8 +649,8 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
                             sc[e] = lds16(s_vs + (row * GR + g * GR / 8) * 2);
                             if (TAIL && (row > last || (sc[e] == kKv4NanScale && k0 + row > hist))) sc[e] = 0;
                         }
-                        const ZPair p01 = zpair_of(__byte_perm(sc[0], sc[1], 0x5410), magic),
-                                    p23 = zpair_of(__byte_perm(sc[2], sc[3], 0x5410), magic);
+                        const Pair p01 = pair_of(__byte_perm(sc[0], sc[1], 0x5410)),
+                                   p23 = pair_of(__byte_perm(sc[2], sc[3], 0x5410));
 #pragma unroll
                         for (int n = 0; n < NT; ++n) mma(sum[n], kOnes, kOnes, kOnes, kOnes, pb[n][2 * k], pb[n][2 * k + 1]);
 #pragma unroll
@@ -669,8 +659,8 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
                             const uint32_t a23 = __byte_perm(w[2][v], w[3][v], 0x5410), b23 = __byte_perm(w[2][v], w[3][v], 0x7632);
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                const uint32_t x0 = value2(a01, i, p01, magic), x1 = value2(b01, i, p01, magic),
-                                               x2 = value2(a23, i, p23, magic), x3 = value2(b23, i, p23, magic);
+                                const uint32_t x0 = value2(a01, a01 >> 8, i, p01), x1 = value2(b01, b01 >> 8, i, p01),
+                                               x2 = value2(a23, a23 >> 8, i, p23), x3 = value2(b23, b23 >> 8, i, p23);
 #pragma unroll
                                 for (int n = 0; n < NT; ++n)
                                     mma(o[n][4 * v + i], x0, x1, x2, x3, pb[n][2 * k], pb[n][2 * k + 1]);
@@ -835,7 +825,7 @@ cudaError_t launch_kv4_decode(const Shape& s, const uint16_t* q, const uint16_t*
         a.counters = counters;
         a.err = err;
         a.wait_ns = wait_ns;
-        a.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(s.head_dim)));
+        a.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(s.head_dim))) * kUnit;
         a.move = 8.f / a.scale_log2;
         a.batch = std::min(kMaxSeqs, s.batch - b0);
         a.ntok = ntok;

@@ -192,6 +192,22 @@ def test_decode_of_sharp_and_far_scores(D):
 
 
 @pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("k_exp,v_exp", [(0, 40), (0, -40), (-20, 0), (3, 60), (-45, -30)])
+def test_decode_of_large_and_small_values(D, k_exp, v_exp):
+    """Keys and values 2^k_exp and 2^v_exp times as large as the others'."""
+    hist = [100]
+    attn = context(1, 4, 2, D, 200)
+    ref = U.history(f"mag{D}", 1, 2, slots(200), D, hist)
+    for t, e in enumerate((k_exp, v_exp)):
+        c, s = K.quantise(K.f32_to_bf16(K.values(ref.codes[t][:, :, :100], ref.scales[t][:, :, :100]) * 2.0 ** e))
+        ref.codes[t][:, :, :100], ref.scales[t][:, :, :100] = K.pack(c), s
+    def scaled(k, v):
+        k[:] = K.f32_to_bf16(K.bf16_to_f64(k) * 2.0 ** k_exp)
+        v[:] = K.f32_to_bf16(K.bf16_to_f64(v) * 2.0 ** v_exp)
+    run_decode(attn, ref, f"mag{D}", hist, 2, scaled)
+
+
+@pytest.mark.parametrize("D", [64, 128])
 def test_decode_nan_in_the_history(D):
     """A NaN group of a key makes the heads that read it NaN; one of a value its 32 outputs."""
     hist = [300, 300]
