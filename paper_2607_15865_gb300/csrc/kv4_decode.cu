@@ -357,7 +357,6 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
     float* s_o = reinterpret_cast<float*>(smem + C::OFF_O);
     float2* s_ml = reinterpret_cast<float2*>(smem + C::OFF_ML);
     auto bar = [&](int stage) { return base + C::OFF_BAR + 8u * static_cast<uint32_t>(warp * C::STAGES + stage); };
-    auto stage_at = [&](int stage) { return static_cast<uint32_t>((warp * C::STAGES + stage) * C::STAGE); };
     if (lane == 0) {
 #pragma unroll
         for (int s = 0; s < C::STAGES; ++s) mbar_init(bar(s), 1);
@@ -401,43 +400,48 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
     }
     auto cta_of = [&](int r) { return static_cast<int>((static_cast<long long>(r + 1) * nc - 1) / total); };
 
-    // The warp's blocks: r0 + warp, + W, ...; copies run up to STAGES blocks ahead.  (b_next, head x column group,
-    // block) is where block `next` lies.
+    // The warp's blocks: r0 + warp, + W, ...; copies run two blocks ahead.  (b_next, head x column group, block) is
+    // where block `next` lies, off_next its byte in the codes (an eighth of it: in the scales).
+    static_assert(C::STAGES == 2 && C::ROW == 8 * 2 * GR, "stages alternate; codes and scales share an offset");
+    const uint32_t s_warp = base + static_cast<uint32_t>(warp * C::STAGES * C::STAGE), bar0 = bar(0);
     int next = r0 + warp, b_next = b_first, T_next = pre[b_first + 1] - pre[b_first];
     int item_next = (r0 - pre[b_first] * hc) / T_next, blk_next = r0 - pre[b_first] * hc - item_next * T_next + warp;
-    uint32_t issued = 0;
-    bool dead = false;
-    auto issue = [&]() {
-        if (next >= r1 || dead) return;
-        while (blk_next >= T_next) {
-            blk_next -= T_next;
-            if (++item_next == hc) {
-                item_next = 0;
-                do ++b_next;
-                while (pre[b_next + 1] == pre[b_next]);
-                T_next = pre[b_next + 1] - pre[b_next];
+    size_t off_next = 0;
+    bool placed = false, dead = false;
+    auto issue = [&](uint32_t stage, uint32_t barrier) {
+        if (next >= r1) return;
+        if (!placed || blk_next >= T_next) {
+            while (blk_next >= T_next) {
+                blk_next -= T_next;
+                if (++item_next == hc) {
+                    item_next = 0;
+                    do ++b_next;
+                    while (pre[b_next + 1] == pre[b_next]);
+                    T_next = pre[b_next + 1] - pre[b_next];
+                }
             }
+            const int head = a.ncg == 1 ? item_next : item_next / a.ncg;
+            off_next = ((static_cast<size_t>(b_next) * a.Hkv + head) * a.lp + static_cast<size_t>(blk_next) * KB) * C::ROW;
+            placed = true;
         }
         if (lane == 0) {
-            const int st = static_cast<int>(issued % C::STAGES);
-            const int head = a.ncg == 1 ? item_next : item_next / a.ncg;
-            const size_t slot = (static_cast<size_t>(b_next) * a.Hkv + head) * a.lp + static_cast<size_t>(blk_next) * KB;
-            const uint32_t dst = base + stage_at(st);
-            mbar_arrive_expect_tx(bar(st), C::STAGE);
-            bulk_g2s(dst, a.c.k_codes + slot * C::ROW, C::CODES, bar(st));
-            bulk_g2s(dst + 2 * C::CODES, a.c.k_scales + slot * GR, C::SCALES, bar(st));
-            bulk_g2s(dst + C::CODES, a.c.v_codes + slot * C::ROW, C::CODES, bar(st));
-            bulk_g2s(dst + 2 * C::CODES + C::SCALES, a.c.v_scales + slot * GR, C::SCALES, bar(st));
+            mbar_arrive_expect_tx(barrier, C::STAGE);
+            bulk_g2s(stage, a.c.k_codes + off_next, C::CODES, barrier);
+            bulk_g2s(stage + 2 * C::CODES, reinterpret_cast<const uint8_t*>(a.c.k_scales) + (off_next >> 3), C::SCALES, barrier);
+            bulk_g2s(stage + C::CODES, a.c.v_codes + off_next, C::CODES, barrier);
+            bulk_g2s(stage + 2 * C::CODES + C::SCALES, reinterpret_cast<const uint8_t*>(a.c.v_scales) + (off_next >> 3),
+                     C::SCALES, barrier);
         }
-        ++issued;
         next += W;
         blk_next += W;
+        off_next += static_cast<size_t>(W) * C::CODES;
     };
     __syncwarp();
 #pragma unroll
-    for (int s = 0; s < C::STAGES; ++s) issue();
+    for (int s = 0; s < C::STAGES; ++s) issue(s_warp + s * C::STAGE, bar0 + 8 * s);
 
-    uint32_t done = 0;
+    uint32_t st_off = 0, bar_off = 0, phase = 0;  // of the warp's next block
+    int mine = r0 + warp;                         // that block
     int b = b_first;
     for (int seg = r0; seg < r1;) {
         // the item of block `seg`, up to where it or the CTA's run ends
@@ -531,19 +535,17 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
                 lim[n][e] = hist + (col < ncol ? token(col) : a.ntok - 1);
             }
 
-        int r = r0 + warp + static_cast<int>(done) * W;
-        const bool has_blocks = r < end;
-        for (; r < end; r += W) {
-            const int st = static_cast<int>(done % C::STAGES);
-            const int k0 = (r - i0) * KB;
-            if (!dead && !mbar_wait(bar(st), (done / C::STAGES) & 1u, nullptr, a.wait_ns)) {
-                dead = true;
+        const bool has_blocks = !dead && mine < end;
+        for (; !dead && mine < end; mine += W) {
+            const int k0 = (mine - i0) * KB;
+            const uint32_t s_k = s_warp + st_off, full = bar0 + bar_off;
+            if (!__all_sync(0xFFFFFFFFu, mbar_wait(full, phase, nullptr, a.wait_ns))) {
                 if (lane == 0) record_dev_err(a.err, kDevErrTimeout);
+                dead = true;
+                break;
             }
-            ++done;
-            dead = __any_sync(0xFFFFFFFFu, dead);
-            if (dead) continue;
-            const uint32_t s_k = base + stage_at(st), s_v = s_k + C::CODES, s_ks = s_v + C::CODES, s_vs = s_ks + C::SCALES;
+            phase ^= bar_off >> 3;
+            const uint32_t s_v = s_k + C::CODES, s_ks = s_v + C::CODES, s_vs = s_ks + C::SCALES;
             const bool tail = k0 + KB > hist;  // the block holds slots of new tokens, or none at all
             if (tail) {  // the staged rows into the block
                 const int lo = max(k0, hist), hi = min(k0 + KB, hist + a.ntok);
@@ -552,7 +554,7 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
                     for (int kind = 0; kind < 2; ++kind) {
                         const uint32_t* src =
                             reinterpret_cast<const uint32_t*>(smem + C::OFF_NEW + (2 * (p - hist) + kind) * C::NEW);
-                        uint8_t* blk = smem + stage_at(st);
+                        uint8_t* blk = smem + (s_k - base);
                         if (lane < C::ROW / 4)
                             reinterpret_cast<uint32_t*>(blk + kind * C::CODES + (p - k0) * C::ROW)[lane] = src[lane];
                         else if (lane < C::NEW / 4)
@@ -673,7 +675,9 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
             else attend(std::false_type{});
             if (tail) fence_proxy_async_smem();  // this warp wrote to the stage that the next copy fills
             __syncwarp();
-            issue();
+            issue(s_k, full);
+            st_off = C::STAGE - st_off;
+            bar_off ^= 8u;
         }
 
         // The warps' parts meet.  Lane (g, t) holds columns 2 t, 2 t + 1 (+ 8 n) of values D/8 g .. D/8 g + D/8 - 1.
@@ -760,11 +764,10 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
         seg = end;
         if (seg < r1) __syncthreads();  // the merge buffers and q are written again
     }
-    if (dead)  // copies still in flight land before the CTA's shared memory is given up
-        for (uint32_t s = 0; s < C::STAGES; ++s) {
-            const uint32_t i = issued > C::STAGES ? issued - C::STAGES + s : s;
-            if (i < issued) mbar_wait(bar(static_cast<int>(i % C::STAGES)), (i / C::STAGES) & 1u, nullptr);
-        }
+    if (dead) {  // the copies still in flight, of blocks `mine` and the next, land before the shared memory is given up
+        if (mine < next) mbar_wait(bar0 + bar_off, phase, nullptr);
+        if (mine + W < next) mbar_wait(bar0 + (bar_off ^ 8u), phase ^ (bar_off >> 3), nullptr);
+    }
 }
 
 template <int D, int NT>
