@@ -3,12 +3,12 @@
 //
 // A (sequence, kv head) has G query heads x ntok new tokens = columns, taken 16 at a time (an item).
 // An item's slots are cut into blocks of 32 (head_dim 128) or 64 slots.  The lengths are read on the device, and so
-// every CTA works out the same cut of the work: where the items are at most the SMs, each is cut into pieces of
-// at most `target` blocks, the least target for which the pieces are at most the SMs, a piece per CTA; where
-// they are more, the blocks of all items, in order, are cut into equal runs.  Within a CTA the warps take its
-// blocks in turn, each through a private ring of bulk copies with one mbarrier per stage and with its own
-// running maximum, sum and accumulators; they meet once per item, in shared memory.  An item that several CTAs
-// share is merged by the last of them to finish, in the order of its pieces.
+// every CTA works out the same cut of the work: where the items are at most the SMs (of up to 32 sequences), each
+// is cut into pieces of at most `target` blocks, a piece per CTA, with the least target (of 32 tried) for which the
+// pieces are at most the SMs; otherwise the blocks of all items, in order, are cut into equal runs.  Within a
+// CTA the warps take its blocks in turn, each through a private ring of bulk copies with one mbarrier per stage and
+// with its own running maximum, sum and accumulators; they meet once per item, in shared memory.  An item that
+// several CTAs share is merged by the last of them to finish, in a fixed order.
 //
 // Per 16 slots, with mma.sync m16n8k16 (A from registers: a tcgen05 operand would have to be written
 // back to shared or tensor memory at four times the packed bytes, for products 8 or 16 columns wide):
@@ -29,15 +29,14 @@
 // that weighs V.
 // The running maximum moves lazily: only when a score passes it by 2^8 are O and the sum rescaled.
 //
-// The new tokens: before its item's blocks a CTA that holds their slots rotates and quantises them, a warp per
-// row, writes them to the cache and stages them for the warp that has their block.  Slots past the last
+// The new tokens: a CTA that holds their slots rotates and quantises them, a warp per row, before its own
+// blocks, writes them to the cache and stages them for the warp that has their block.  Slots past the last
 // one are masked by position and by a scale of 0; a NaN group of a new token's v counts from that token on, so its
 // scale is taken as 0 too and the columns that see it are set to NaN when they are written.
 // Every wait is bounded: on expiry a warp records kDevErrTimeout, issues and computes nothing more, lets its
 // copies land and takes part in the barriers and counts.
 #include <algorithm>
 #include <cmath>
-#include <type_traits>
 
 #include "internal.h"
 #include "kv4.cuh"
@@ -71,11 +70,11 @@ struct Cfg {
     static constexpr int OFF_Q = OFF_ML + W * COLS * 8;         // bf16 [COLS][QS]
     static constexpr int OFF_NEW = OFF_Q + COLS * QS * 2;       // [kMaxNew][k, v][NEW]
     static constexpr int OFF_PRE = OFF_NEW + kMaxNew * 2 * NEW;  // int [kMaxSeqs + 1]: blocks before a sequence
-    static constexpr int OFF_PIECES = OFF_PRE + (kMaxSeqs + 1) * 4;  // int [kMaxSeqs + 1]: pieces before it
-    static constexpr int OFF_BAR = (OFF_PIECES + (kMaxSeqs + 1) * 4 + 7) & ~7;
-    static constexpr int OFF_NAN = OFF_BAR + W * STAGES * 8;    // int [4]: first new token with a NaN group of v
-    static constexpr int OFF_FLAG = OFF_NAN + 16;               // int [4]: last CTA, target (0: runs), items
-    static constexpr int BYTES = OFF_FLAG + 16;
+    static constexpr int OFF_BAR = (OFF_PRE + (kMaxSeqs + 1) * 4 + 7) & ~7;  // rings, then the staged rows
+    static constexpr int OFF_NAN = OFF_BAR + (W * STAGES + 1) * 8;  // int [4]: first new token with a NaN group of v
+    static constexpr int OFF_FLAG = OFF_NAN + 16;               // int: whether this CTA merges the item
+    static constexpr int OFF_SHARE = OFF_FLAG + 8;              // Share
+    static constexpr int BYTES = OFF_SHARE + 40;
     static_assert(CODES == 2048 && SCALES == 256 && NEW % 4 == 0 && BYTES <= 232448, "shared memory");
 };
 
@@ -85,6 +84,15 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
         "{%0, %1, %2, %3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// The same on zeros.
+__device__ __forceinline__ void mma_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                          uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+        "{%10, %10, %10, %10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 
 __device__ __forceinline__ uint32_t fms2(uint32_t a, uint32_t b, uint32_t c) {  // a b - c
@@ -181,7 +189,7 @@ struct Args {
     int* err;
     uint64_t wait_ns;
     float scale_log2, move;  // log2 e / sqrt D in units of 2^-73, and the lead of a score that moves the maximum (2^8)
-    int batch, ntok, Hq, Hkv, max_len, lp, ncg, min_blocks;
+    int batch, ntok, Hq, Hkv, max_len, lp, ncg, min_blocks, per;  // per: CTAs per (kv head, column group)
 };
 
 // One warp: quantise the E values x that each lane holds of a row of D = 32 E, write the row's codes and
@@ -257,45 +265,58 @@ __device__ __forceinline__ int warp_scan(int v, int lane) {
     return v;
 }
 
-// One warp: the cut of the work from the blocks of each sequence (pre[b + 1] on entry).  On return pre[b] are
-// the blocks, and pieces[b] the pieces, of an item of each sequence before b, summed; returns the blocks per piece,
-// or 0 where the items are more than the CTAs (runs of equal length).
-__device__ __forceinline__ int cut_work(int* pre, int* pieces, int batch, int hc, int ctas, int min_blocks, int lane) {
-    int sum = 0, items = 0, longest = 0, shortest = INT32_MAX;
-    for (int b0 = 0; b0 < batch; b0 += 32) {
-        const int T = b0 + lane < batch ? pre[b0 + lane + 1] : 0;
-        const int v = warp_scan(T, lane);
-        if (b0 + lane < batch) pre[b0 + lane + 1] = sum + v;
-        sum += __shfl_sync(0xFFFFFFFFu, v, 31);
-        items += __popc(__ballot_sync(0xFFFFFFFFu, T > 0));
-        longest = max(longest, __reduce_max_sync(0xFFFFFFFFu, T));
-        shortest = min(shortest, __reduce_min_sync(0xFFFFFFFFu, T > 0 ? T : INT32_MAX));
+// x / y for 0 <= x < 2^20, y > 0: (x + 1/2) / y is at least 1 / 2y from an integer, twice what the float quotient
+// may be off by.
+__device__ __forceinline__ int small_div(int x, int y) {
+    return static_cast<int>(__fdividef(static_cast<float>(x) + 0.5f, static_cast<float>(y)));
+}
+__device__ __forceinline__ int small_ceil_div(int x, int y) { return small_div(x - 1, y) + 1; }  // x > 0
+
+// A CTA's part of the work: blocks r0 .. r1 - 1 of one item, its piece `piece` of n; or (n = 0) of the blocks of all
+// items, in order.
+struct Share {
+    int b, item, T, hist;  // the sequence, its item and that one's blocks
+    int r0, r1, piece, n;
+    int nc, total;         // CTAs and blocks of a cut into runs
+};
+
+// One warp: the share of CTA `cta` for up to 32 sequences, lane b holding the blocks T of sequence b's items (0:
+// skipped).  hc: items of a sequence, per * hc CTAs.  pre: filled where the cut is into runs.
+__device__ __forceinline__ Share piece_of(int T, int hist, int hc, int per, int min_blocks, int cta, int* pre, int lane) {
+    Share sh = {};
+    const uint32_t live = __ballot_sync(0xFFFFFFFFu, T > 0);
+    const int items = __popc(live), sum = __reduce_add_sync(0xFFFFFFFFu, T), longest = __reduce_max_sync(0xFFFFFFFFu, T);
+    if (items == 0) return sh;
+    if (items > per) {
+        pre[lane + 1] = warp_scan(T, lane);
+        if (lane == 0) pre[0] = 0;
+        sh.total = sum * hc;
+        return sh;
     }
-    if (lane == 0) pre[0] = pieces[0] = 0;
-    __syncwarp();
-    if (items == 0 || static_cast<long long>(items) * hc > ctas) return 0;
-    auto pieces_of = [&](int target) {  // of an item of every sequence
-        int n = 0;
-        for (int b = lane; b < batch; b += 32) n += (pre[b + 1] - pre[b] + target - 1) / target;
-        return __reduce_add_sync(0xFFFFFFFFu, n);
-    };
-    const int per = ctas / hc;                                        // pieces that fit, per head and column group
-    int hi = max(min_blocks, (longest + per / items - 1) / (per / items));  // fits
-    int lo = max(min_blocks, (sum + per - 1) / per);                  // no less does
-    if (shortest < longest)
-        while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (pieces_of(mid) <= per) hi = mid;
-            else lo = mid + 1;
-        }
-    int before = 0;
-    for (int b0 = 0; b0 < batch; b0 += 32) {
-        const int n = b0 + lane < batch ? (pre[b0 + lane + 1] - pre[b0 + lane] + hi - 1) / hi : 0;
-        const int v = warp_scan(n, lane);
-        if (b0 + lane < batch) pieces[b0 + lane + 1] = before + v;
-        before += __shfl_sync(0xFFFFFFFFu, v, 31);
+    int target = max(min_blocks, small_ceil_div(longest, small_div(per, items)));  // fits
+    if (longest * items != sum) {
+        const int lo = max(min_blocks, (sum + per - 1) / per);  // no less fits
+        const int mine = lo + (((target - lo) * lane) >> 5);
+        int pieces = 0;
+        for (uint32_t rest = live; rest != 0; rest &= rest - 1)
+            pieces += small_ceil_div(__shfl_sync(0xFFFFFFFFu, T, __ffs(rest) - 1), mine);
+        const uint32_t fits = __ballot_sync(0xFFFFFFFFu, pieces <= per);
+        if (fits != 0) target = __shfl_sync(0xFFFFFFFFu, mine, __ffs(fits) - 1);
     }
-    return hi;
+    const int n = T > 0 ? small_ceil_div(T, target) : 0, upto = warp_scan(n, lane);
+    const uint32_t past = __ballot_sync(0xFFFFFFFFu, T > 0 && upto * hc > cta);
+    if (past == 0) return sh;
+    sh.b = __ffs(past) - 1;
+    sh.T = __shfl_sync(0xFFFFFFFFu, T, sh.b);
+    sh.hist = __shfl_sync(0xFFFFFFFFu, hist, sh.b);
+    sh.n = __shfl_sync(0xFFFFFFFFu, n, sh.b);
+    const int rem = cta - __shfl_sync(0xFFFFFFFFu, upto - n, sh.b) * hc;
+    sh.item = small_div(rem, sh.n);
+    sh.piece = rem - sh.item * sh.n;
+    const int each = small_div(sh.T, sh.n), more = sh.T - each * sh.n;
+    sh.r0 = sh.piece * each + min(sh.piece, more);
+    sh.r1 = sh.r0 + each + (sh.piece < more ? 1 : 0);
+    return sh;
 }
 
 // The first b with sums[b + 1] * hc > r.
@@ -350,16 +371,18 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
     const uint32_t base = smem_u32(smem);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     int* pre = reinterpret_cast<int*>(smem + C::OFF_PRE);
-    int* pieces = reinterpret_cast<int*>(smem + C::OFF_PIECES);
     int* s_nan = reinterpret_cast<int*>(smem + C::OFF_NAN);
     int* flag = reinterpret_cast<int*>(smem + C::OFF_FLAG);
     uint16_t* s_q = reinterpret_cast<uint16_t*>(smem + C::OFF_Q);
     float* s_o = reinterpret_cast<float*>(smem + C::OFF_O);
     float2* s_ml = reinterpret_cast<float2*>(smem + C::OFF_ML);
+    Share* share = reinterpret_cast<Share*>(smem + C::OFF_SHARE);
     auto bar = [&](int stage) { return base + C::OFF_BAR + 8u * static_cast<uint32_t>(warp * C::STAGES + stage); };
+    const uint32_t new_full = base + C::OFF_BAR + 8u * (W * C::STAGES);
     if (lane == 0) {
 #pragma unroll
         for (int s = 0; s < C::STAGES; ++s) mbar_init(bar(s), 1);
+        if (warp == 0) mbar_init(new_full, W);
         fence_mbar_init();
     }
     griddep_wait();
@@ -368,44 +391,63 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
     // The blocks of a launch are counted in int: a cache of 2^31 of them would take 2^31 x 4.5 KB / 16 column groups.
     const int hc = a.Hkv * a.ncg;  // items of a sequence
     const int cta = static_cast<int>(blockIdx.x);
-    for (int b = tid; b < a.batch; b += C::THREADS) {
-        const int h = a.d_hist[b];
+    auto blocks_of = [&](int b, int& h) {
+        h = a.d_hist[b];
         const bool ok = h >= 0 && h <= a.max_len - a.ntok;
         if (!ok && cta == 0) atomicOr(a.err, kDevErrHistRange);
-        pre[b + 1] = ok ? (h + a.ntok + KB - 1) / KB : 0;
+        return ok ? (h + a.ntok + KB - 1) / KB : 0;
+    };
+    if (a.batch > 32) {
+        for (int b = tid; b < a.batch; b += C::THREADS) {
+            int h;
+            pre[b + 1] = blocks_of(b, h);
+        }
+        __syncthreads();
     }
-    if (a.batch > 32) __syncthreads();  // up to 32 sequences are warp 0's own
     if (warp == 0) {
-        __syncwarp();
-        const int target = cut_work(pre, pieces, a.batch, hc, static_cast<int>(gridDim.x), a.min_blocks, lane);
-        if (lane == 0) flag[1] = target;
+        Share sh = {};
+        if (a.batch <= 32) {
+            int h = 0;
+            const int T = lane < a.batch ? blocks_of(lane, h) : 0;
+            sh = piece_of(T, h, hc, a.per, a.min_blocks, cta, pre, lane);
+        } else {
+            int sum = 0;
+            for (int b0 = 0; b0 < a.batch; b0 += 32) {
+                const int v = warp_scan(b0 + lane < a.batch ? pre[b0 + lane + 1] : 0, lane);
+                if (b0 + lane < a.batch) pre[b0 + lane + 1] = sum + v;
+                sum += __shfl_sync(0xFFFFFFFFu, v, 31);
+            }
+            if (lane == 0) pre[0] = 0;
+            sh.total = sum * hc;
+        }
+        if (sh.n == 0) {
+            sh.nc = min(static_cast<int>(gridDim.x), max(1, (sh.total + a.min_blocks - 1) / a.min_blocks));
+            if (cta < sh.nc) {
+                sh.r0 = static_cast<int>(static_cast<long long>(sh.total) * cta / sh.nc);
+                sh.r1 = static_cast<int>(static_cast<long long>(sh.total) * (cta + 1) / sh.nc);
+            }
+        }
+        if (lane == 0) *share = sh;
     }
     __syncthreads();
-    const int total = pre[a.batch] * hc, target = flag[1];
-    int r0, r1, nc = 0, piece = 0, b_first;
-    if (target > 0) {
-        if (cta >= pieces[a.batch] * hc) return;
-        b_first = search(pieces, a.batch, hc, cta);
-        const int T = pre[b_first + 1] - pre[b_first], n = pieces[b_first + 1] - pieces[b_first];
-        const int rem = cta - pieces[b_first] * hc, i0 = pre[b_first] * hc + rem / n * T;
-        piece = rem % n;
-        r0 = i0 + T * piece / n;
-        r1 = i0 + T * (piece + 1) / n;
-    } else {
-        nc = min(static_cast<int>(gridDim.x), max(1, (total + a.min_blocks - 1) / a.min_blocks));
-        if (total == 0 || cta >= nc) return;
-        r0 = static_cast<int>(static_cast<long long>(total) * cta / nc);
-        r1 = static_cast<int>(static_cast<long long>(total) * (cta + 1) / nc);
-        b_first = search(pre, a.batch, hc, r0);
-    }
-    auto cta_of = [&](int r) { return static_cast<int>((static_cast<long long>(r + 1) * nc - 1) / total); };
+    const int r0 = share->r0, r1 = share->r1;
+    const bool runs = share->n == 0;
+    if (r0 >= r1) return;
+    auto cta_of = [&](int r) {
+        return static_cast<int>((static_cast<long long>(r + 1) * share->nc - 1) / share->total);
+    };
 
     // The warp's blocks: r0 + warp, + W, ...; copies run two blocks ahead.  (b_next, head x column group, block) is
     // where block `next` lies, off_next its byte in the codes (an eighth of it: in the scales).
     static_assert(C::STAGES == 2 && C::ROW == 8 * 2 * GR, "stages alternate; codes and scales share an offset");
     const uint32_t s_warp = base + static_cast<uint32_t>(warp * C::STAGES * C::STAGE), bar0 = bar(0);
-    int next = r0 + warp, b_next = b_first, T_next = pre[b_first + 1] - pre[b_first];
-    int item_next = (r0 - pre[b_first] * hc) / T_next, blk_next = r0 - pre[b_first] * hc - item_next * T_next + warp;
+    int next = r0 + warp, b_next = share->b, T_next = share->T, item_next = share->item, blk_next = next;
+    if (runs) {
+        b_next = search(pre, a.batch, hc, r0);
+        T_next = pre[b_next + 1] - pre[b_next];
+        item_next = (r0 - pre[b_next] * hc) / T_next;
+        blk_next = next - pre[b_next] * hc - item_next * T_next;
+    }
     size_t off_next = 0;
     bool placed = false, dead = false;
     auto issue = [&](uint32_t stage, uint32_t barrier) {
@@ -442,15 +484,22 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
 
     uint32_t st_off = 0, bar_off = 0, phase = 0;  // of the warp's next block
     int mine = r0 + warp;                         // that block
-    int b = b_first;
+    uint32_t new_phase = 0;
+    int b = share->b;
+    if (runs) b = search(pre, a.batch, hc, r0);
     for (int seg = r0; seg < r1;) {
         // the item of block `seg`, up to where it or the CTA's run ends
-        while (seg >= pre[b + 1] * hc) ++b;
-        const int T = pre[b + 1] - pre[b];
-        const int item = (seg - pre[b] * hc) / T, head = item / a.ncg, cg = item % a.ncg;
-        const int i0 = pre[b] * hc + item * T;  // the item's first block
+        int T = share->T, item = share->item, hist = share->hist, i0 = 0;  // i0: the item's first block
+        if (runs) {
+            while (seg >= pre[b + 1] * hc) ++b;
+            T = pre[b + 1] - pre[b];
+            item = (seg - pre[b] * hc) / T;
+            i0 = pre[b] * hc + item * T;
+            hist = a.d_hist[b];
+        }
+        const int head = a.ncg == 1 ? item : item / a.ncg, cg = a.ncg == 1 ? 0 : item % a.ncg;
         const int end = min(r1, i0 + T);
-        const int hist = a.d_hist[b], G = a.Hq / a.Hkv;
+        const int G = a.Hq / a.Hkv;
         const int c0 = cg * 16, ncol = min(16, G * a.ntok - c0);
         auto token = [&](int col) { return (c0 + col) / G; };
         auto row_of = [&](int col) {  // of q and out, in rows of D
@@ -473,10 +522,10 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
             s_q[col * C::QS + j] = lo;
             s_q[col * C::QS + j + D / 2] = hi;
         }
+        __syncthreads();
         // the new tokens whose slots lie in the segment's blocks, a warp per row of k or v
         const int new0 = max(hist, (seg - i0) * KB), new1 = min(hist + a.ntok, (end - i0) * KB);
         if (new0 < new1) {
-            __syncthreads();  // s_nan is set
             for (int u = W - 1 - warp; u < 2 * (new1 - new0); u += W) {
                 const int p = new0 + u / 2, i = p - hist;
                 const size_t src = ((static_cast<size_t>(b) * a.ntok + i) * a.Hkv + head) * D;
@@ -499,8 +548,9 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
                     put_row<D>(x, lane, a.c.k_codes + slot * C::ROW, a.c.k_scales + slot * GR, staged);
                 }
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(new_full);
         }
-        __syncthreads();
 
         // Q^T's B fragments: lane (g, t) holds values D/4 t .. D/4 t + D/4 - 1 of column g (+ 8 n); step s of the
         // products takes values 4 s .. 4 s + 3 of them.  qz: minus their sum in three parts.
@@ -544,10 +594,14 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
                 dead = true;
                 break;
             }
-            phase ^= bar_off >> 3;
             const uint32_t s_v = s_k + C::CODES, s_ks = s_v + C::CODES, s_vs = s_ks + C::SCALES;
             const bool tail = k0 + KB > hist;  // the block holds slots of new tokens, or none at all
             if (tail) {  // the staged rows into the block
+                if (!__all_sync(0xFFFFFFFFu, mbar_wait(new_full, new_phase, nullptr))) {
+                    if (lane == 0) record_dev_err(a.err, kDevErrTimeout);
+                    dead = true;
+                    break;
+                }
                 const int lo = max(k0, hist), hi = min(k0 + KB, hist + a.ntok);
                 for (int p = lo; p < hi; ++p)
 #pragma unroll
@@ -564,119 +618,120 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
                 __syncwarp();
             }
             const int last = hist + a.ntok - 1 - k0;  // last slot of the block that holds a token
-            auto attend = [&](auto is_tail) {
-                constexpr bool TAIL = decltype(is_tail)::value;
+#pragma unroll 1
+            for (int half = 0; half < KB / 32; ++half) {
+                if (32 * half > last) break;
+                // scores of 32 slots: lane (g, t) has slots g, g + 8 of each 16, columns 2 t, 2 t + 1 (+ 8 n)
+                float s[2][NT][4];
 #pragma unroll
-                for (int half = 0; half < KB / 32; ++half) {
-                    if (TAIL && half > 0 && 32 * half > last) break;
-                    // scores of 32 slots: lane (g, t) has slots g, g + 8 of each 16, columns 2 t, 2 t + 1 (+ 8 n)
-                    float s[2][NT][4];
+                for (int j = 0; j < 2; ++j) {
+                    uint32_t w[2][KW];
+                    Pair p[2];
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        uint32_t w[2][KW];
-                        Pair p[2];
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const int key = 32 * half + 16 * j + 8 * e + g;
-                            lds<KW>(s_k + key * C::ROW + t * (KW * 4), w[e]);
-                            p[e] = pair_of(__byte_perm(lds16(s_ks + (key * GR + t * GR / 4) * 2), 0, 0x1010));
-                        }
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            s[j][n][0] = s[j][n][1] = s[j][n][2] = s[j][n][3] = 0.f;
-                            mma(s[j][n], p[0].zs, p[1].zs, p[0].zs, p[1].zs, qz[n][0], qz[n][1]);
-                        }
-#pragma unroll
-                        for (int i = 0; i < 2 * KW; ++i) {
-                            const uint32_t w0 = w[0][i / 2], w1 = w[1][i / 2];
-                            const uint32_t x0 = code2(w0, w0 >> 8, 2 * (i % 2), p[0]), x1 = code2(w1, w1 >> 8, 2 * (i % 2), p[1]),
-                                           x2 = code2(w0, w0 >> 8, 2 * (i % 2) + 1, p[0]),
-                                           x3 = code2(w1, w1 >> 8, 2 * (i % 2) + 1, p[1]);
-#pragma unroll
-                            for (int n = 0; n < NT; ++n) mma(s[j][n], x0, x1, x2, x3, qb[n][i][0], qb[n][i][1]);
-                        }
+                    for (int e = 0; e < 2; ++e) {
+                        const int key = 32 * half + 16 * j + 8 * e + g;
+                        lds<KW>(s_k + key * C::ROW + t * (KW * 4), w[e]);
+                        p[e] = pair_of(__byte_perm(lds16(s_ks + (key * GR + t * GR / 4) * 2), 0, 0x1010));
                     }
-                    bool moves = false;
-                    float mx[NT][2];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        mma_first(s[j][n], p[0].zs, p[1].zs, p[0].zs, p[1].zs, qz[n][0], qz[n][1]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2 * KW; ++i) {
+                        const uint32_t w0 = w[0][i / 2], w1 = w[1][i / 2];
+                        const uint32_t x0 = code2(w0, w0 >> 8, 2 * (i % 2), p[0]), x1 = code2(w1, w1 >> 8, 2 * (i % 2), p[1]),
+                                       x2 = code2(w0, w0 >> 8, 2 * (i % 2) + 1, p[0]),
+                                       x3 = code2(w1, w1 >> 8, 2 * (i % 2) + 1, p[1]);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) mma(s[j][n], x0, x1, x2, x3, qb[n][i][0], qb[n][i][1]);
+                    }
+                }
+                bool moves = false;
+                float mx[NT][2];
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        if (tail)
+#pragma unroll
+                            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                                for (int h = 0; h < 2; ++h)
+                                    if (k0 + 32 * half + 16 * j + 8 * h + g > lim[n][e]) s[j][n][2 * h + e] = -INFINITY;
+                        mx[n][e] = fmaxf(fmaxf(s[0][n][e], s[0][n][2 + e]), fmaxf(s[1][n][e], s[1][n][2 + e]));
+                        moves |= mx[n][e] > m[n][e] + a.move;
+                    }
+                if (__any_sync(0xFFFFFFFFu, moves)) {
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            if (TAIL)
+                            float x = mx[n][e];
 #pragma unroll
-                                for (int j = 0; j < 2; ++j)
+                            for (int mask = 4; mask <= 16; mask <<= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, mask));
+                            x = fmaxf(x, m[n][e]);
+                            const float f = m[n][e] == x ? 1.f : exp2_fast((m[n][e] - x) * a.scale_log2);
+                            m[n][e] = x;
+                            ms[n][e] = (x == -INFINITY ? 0.f : x * a.scale_log2) - kLift;
+                            sum[n][e] *= f;
 #pragma unroll
-                                    for (int h = 0; h < 2; ++h)
-                                        if (k0 + 32 * half + 16 * j + 8 * h + g > lim[n][e]) s[j][n][2 * h + e] = -INFINITY;
-                            mx[n][e] = fmaxf(fmaxf(s[0][n][e], s[0][n][2 + e]), fmaxf(s[1][n][e], s[1][n][2 + e]));
-                            moves |= mx[n][e] > m[n][e] + a.move;
-                        }
-                    if (__any_sync(0xFFFFFFFFu, moves)) {
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                float x = mx[n][e];
-#pragma unroll
-                                for (int mask = 4; mask <= 16; mask <<= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, mask));
-                                x = fmaxf(x, m[n][e]);
-                                const float f = m[n][e] == x ? 1.f : exp2_fast((m[n][e] - x) * a.scale_log2);
-                                m[n][e] = x;
-                                ms[n][e] = (x == -INFINITY ? 0.f : x * a.scale_log2) - kLift;
-                                sum[n][e] *= f;
-#pragma unroll
-                                for (int i = 0; i < 4 * VW; ++i) {
-                                    o[n][i][e] *= f;
-                                    o[n][i][2 + e] *= f;
-                                }
+                            for (int i = 0; i < 4 * VW; ++i) {
+                                o[n][i][e] *= f;
+                                o[n][i][2 + e] *= f;
                             }
-                    }
-                    uint32_t pb[NT][4];
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const float* x = &s[j / 2][n][2 * (j % 2)];
-                            pb[n][j] = transpose8(pack2(exp2_fast(fmaf(x[0], a.scale_log2, -ms[n][0])),
-                                                        exp2_fast(fmaf(x[1], a.scale_log2, -ms[n][1]))));
                         }
+                }
+                uint32_t pb[NT][4];
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {  // 16 slots
-                        const int key = 32 * half + 16 * k + 2 * t;
-                        uint32_t w[4][VW], sc[4];  // slots 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float* x = &s[j / 2][n][2 * (j % 2)];
+                        pb[n][j] = transpose8(pack2(exp2_fast(fmaf(x[0], a.scale_log2, -ms[n][0])),
+                                                    exp2_fast(fmaf(x[1], a.scale_log2, -ms[n][1]))));
+                    }
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {  // 16 slots
+                    const int key = 32 * half + 16 * k + 2 * t;
+                    uint32_t w[4][VW], sc[4];  // slots 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int row = key + (e & 1) + 8 * (e >> 1);
+                        lds<VW>(s_v + row * C::ROW + g * (VW * 4), w[e]);
+                        sc[e] = lds16(s_vs + (row * GR + g * GR / 8) * 2);
+                    }
+                    if (tail) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const int row = key + (e & 1) + 8 * (e >> 1);
-                            lds<VW>(s_v + row * C::ROW + g * (VW * 4), w[e]);
-                            sc[e] = lds16(s_vs + (row * GR + g * GR / 8) * 2);
-                            if (TAIL && (row > last || (sc[e] == kKv4NanScale && k0 + row > hist))) sc[e] = 0;
+                            if (row > last || (sc[e] == kKv4NanScale && k0 + row > hist)) sc[e] = 0;
                         }
-                        const Pair p01 = pair_of(__byte_perm(sc[0], sc[1], 0x5410)),
-                                   p23 = pair_of(__byte_perm(sc[2], sc[3], 0x5410));
+                    }
+                    const Pair p01 = pair_of(__byte_perm(sc[0], sc[1], 0x5410)),
+                               p23 = pair_of(__byte_perm(sc[2], sc[3], 0x5410));
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) mma(sum[n], kOnes, kOnes, kOnes, kOnes, pb[n][2 * k], pb[n][2 * k + 1]);
+                    for (int n = 0; n < NT; ++n) mma(sum[n], kOnes, kOnes, kOnes, kOnes, pb[n][2 * k], pb[n][2 * k + 1]);
 #pragma unroll
-                        for (int v = 0; v < VW; ++v) {
-                            const uint32_t a01 = __byte_perm(w[0][v], w[1][v], 0x5410), b01 = __byte_perm(w[0][v], w[1][v], 0x7632);
-                            const uint32_t a23 = __byte_perm(w[2][v], w[3][v], 0x5410), b23 = __byte_perm(w[2][v], w[3][v], 0x7632);
+                    for (int v = 0; v < VW; ++v) {
+                        const uint32_t a01 = __byte_perm(w[0][v], w[1][v], 0x5410), b01 = __byte_perm(w[0][v], w[1][v], 0x7632);
+                        const uint32_t a23 = __byte_perm(w[2][v], w[3][v], 0x5410), b23 = __byte_perm(w[2][v], w[3][v], 0x7632);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const uint32_t x0 = value2(a01, a01 >> 8, i, p01), x1 = value2(b01, b01 >> 8, i, p01),
-                                               x2 = value2(a23, a23 >> 8, i, p23), x3 = value2(b23, b23 >> 8, i, p23);
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t x0 = value2(a01, a01 >> 8, i, p01), x1 = value2(b01, b01 >> 8, i, p01),
+                                           x2 = value2(a23, a23 >> 8, i, p23), x3 = value2(b23, b23 >> 8, i, p23);
 #pragma unroll
-                                for (int n = 0; n < NT; ++n)
-                                    mma(o[n][4 * v + i], x0, x1, x2, x3, pb[n][2 * k], pb[n][2 * k + 1]);
-                            }
+                            for (int n = 0; n < NT; ++n)
+                                mma(o[n][4 * v + i], x0, x1, x2, x3, pb[n][2 * k], pb[n][2 * k + 1]);
                         }
                     }
                 }
-            };
-            if (tail) attend(std::true_type{});
-            else attend(std::false_type{});
+            }
             if (tail) fence_proxy_async_smem();  // this warp wrote to the stage that the next copy fills
             __syncwarp();
             issue(s_k, full);
             st_off = C::STAGE - st_off;
+            phase ^= bar_off >> 3;
             bar_off ^= 8u;
         }
 
@@ -696,26 +751,28 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
                 if (g == 0) s_ml[col] = make_float2(m[n][e] * a.scale_log2, sum[n][e]);
             }
         __syncthreads();
-        int j0, j1;  // the CTAs that share the item
-        if (target > 0) {
-            j0 = cta - piece;
-            j1 = j0 + pieces[b + 1] - pieces[b] - 1;
-        } else {
+        if (new0 < new1) new_phase ^= 1u;
+        int j0 = cta - share->piece, j1 = j0 + share->n - 1;  // the CTAs that share the item
+        if (runs) {
             j0 = cta_of(i0);
             j1 = cta_of(i0 + T - 1);
         }
         const int part = 2 * cta + (cta == j0 ? 1 : 0);
+        const int used = min(W, end - seg), first_warp = (seg - r0) % W;  // the warps that had blocks
         for (int u = tid; u < ncol * (D / 4); u += C::THREADS) {
             const int col = u / (D / 4), d = u % (D / 4) * 4;
             Merged acc;
-#pragma unroll
-            for (int w0 = 0; w0 < W; w0 += 4) {
+#pragma unroll 1
+            for (int w0 = 0; w0 < used; w0 += 4) {
                 float2 ml[4];
                 float4 x[4];
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    ml[w] = s_ml[(w0 + w) * C::COLS + col];
-                    x[w] = *reinterpret_cast<const float4*>(s_o + ((w0 + w) * C::COLS + col) * C::OS + d);
+                for (int i = 0; i < 4; ++i) {
+                    int w = first_warp + min(w0 + i, used - 1);
+                    w = w >= W ? w - W : w;
+                    ml[i] = s_ml[w * C::COLS + col];
+                    x[i] = *reinterpret_cast<const float4*>(s_o + (w * C::COLS + col) * C::OS + d);
+                    if (w0 + i >= used) ml[i].x = -INFINITY;
                 }
                 acc.add(ml, x);
             }
@@ -730,34 +787,56 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
         }
         if (j0 != j1) {
             if (tid < 4) a.part_nan[4 * part + tid] = s_nan[tid];
-            __threadfence();
             __syncthreads();
             int* count = a.counters + static_cast<size_t>(b) * hc + item;
-            if (tid == 0) flag[0] = atomicAdd(count, 1) == j1 - j0;
+            if (tid == 0) {
+                __threadfence();  // the CTA's part, and then its count
+                *flag = atomicAdd(count, 1) == j1 - j0;
+                __threadfence();  // the count, and then the others' parts
+            }
             __syncthreads();
-            if (flag[0]) {  // the last of the item's CTAs merges them, in order
-                __threadfence();
+            if (*flag) {  // the last of the item's CTAs merges them: `subs` threads per four values, every subs-th part each
                 if (tid == 0) *count = 0;
-                for (int u = tid; u < ncol * (D / 4); u += C::THREADS) {
+                const int vals = ncol * (D / 4), subs = max(1, min(C::THREADS / vals, j1 - j0 + 1));
+                float4* s_x = reinterpret_cast<float4*>(s_o);
+                float2* s_y = reinterpret_cast<float2*>(s_x + C::THREADS);
+                for (int u0 = 0; u0 < vals; u0 += C::THREADS) {  // one turn where subs > 1
+                    const int sub = subs > 1 ? tid / vals : 0, u = u0 + tid - sub * vals;
                     const int col = u / (D / 4), d = u % (D / 4) * 4;
                     Merged acc;
                     int nan = kNone;
-                    for (int j = j0; j <= j1; j += 8) {
-                        float2 ml[8];
-                        float4 x[8];
+                    if (sub < subs && u < vals)
+#pragma unroll 1
+                        for (int j = j0 + sub; j <= j1; j += 8 * subs) {
+                            float2 ml[8];
+                            float4 x[8];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            ml[i] = make_float2(-INFINITY, 0.f);
-                            x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                            if (j + i > j1) continue;
-                            const int from = 2 * (j + i) + (j + i == j0 ? 1 : 0), row = from * 16 + col;
-                            ml[i] = __ldcg(reinterpret_cast<const float2*>(a.part_ml) + row);
-                            x[i] = __ldcg(reinterpret_cast<const float4*>(a.part_o + static_cast<size_t>(row) * D + d));
-                            if (a.ntok > 1) nan = min(nan, __ldcg(a.part_nan + 4 * from + d / kKv4Group));
+                            for (int i = 0; i < 8; ++i) {
+                                const int from = min(j + i * subs, j1), row = (2 * from + (from == j0 ? 1 : 0)) * 16 + col;
+                                ml[i] = __ldcg(reinterpret_cast<const float2*>(a.part_ml) + row);
+                                x[i] = __ldcg(reinterpret_cast<const float4*>(a.part_o + static_cast<size_t>(row) * D + d));
+                                if (a.ntok > 1) nan = min(nan, __ldcg(a.part_nan + 4 * (row / 16) + d / kKv4Group));
+                                if (j + i * subs > j1) ml[i].x = -INFINITY;
+                            }
+                            acc.add(ml, x);
                         }
-                        acc.add(ml, x);
+                    if (subs > 1) {
+                        if (sub > 0 && sub < subs) {
+                            s_x[tid] = make_float4(acc.o[0], acc.o[1], acc.o[2], acc.o[3]);
+                            s_y[tid] = make_float2(acc.m, acc.l);
+                            if (nan < kNone) atomicMin(&s_nan[d / kKv4Group], nan);
+                        }
+                        __syncthreads();
+                        if (sub == 0)
+                            for (int i = 1; i < subs; ++i) {
+                                const float2 ml[1] = {s_y[tid + i * vals]};
+                                const float4 x[1] = {s_x[tid + i * vals]};
+                                acc.add(ml, x);
+                            }
+                        nan = min(nan, s_nan[d / kKv4Group]);
                     }
-                    *reinterpret_cast<uint2*>(a.out + row_of(col) * D + d) = acc.result(nan > 0 && nan <= token(col));
+                    if (sub == 0 && u < vals)
+                        *reinterpret_cast<uint2*>(a.out + row_of(col) * D + d) = acc.result(nan > 0 && nan <= token(col));
                 }
             }
         }
@@ -771,11 +850,10 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
 }
 
 template <int D, int NT>
-cudaError_t launch(const Args& a, int num_sms, cudaStream_t st) {
+cudaError_t launch(const Args& a, int grid, cudaStream_t st) {
     using C = Cfg<D, NT>;
-    const long long most = static_cast<long long>(a.batch) * a.Hkv * a.ncg * ((a.max_len + C::KB - 1) / C::KB);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(std::min<long long>(num_sms, most)));
+    cfg.gridDim = dim3(static_cast<unsigned>(grid));
     cfg.blockDim = dim3(C::THREADS);
     cfg.dynamicSmemBytes = C::BYTES;
     cfg.stream = st;
@@ -837,8 +915,11 @@ cudaError_t launch_kv4_decode(const Shape& s, const uint16_t* q, const uint16_t*
         a.max_len = s.max_len;
         a.ncg = (cols + 15) / 16;
         a.min_blocks = 8;
-        const cudaError_t e = D == 128 ? (cols <= 8 ? launch<128, 1>(a, num_sms, st) : launch<128, 2>(a, num_sms, st))
-                                       : (cols <= 8 ? launch<64, 1>(a, num_sms, st) : launch<64, 2>(a, num_sms, st));
+        const int grid = static_cast<int>(std::min<long long>(
+            num_sms, static_cast<long long>(a.batch) * a.Hkv * a.ncg * ((a.max_len + (D == 128 ? 31 : 63)) / (D == 128 ? 32 : 64))));
+        a.per = grid / (a.Hkv * a.ncg);
+        const cudaError_t e = D == 128 ? (cols <= 8 ? launch<128, 1>(a, grid, st) : launch<128, 2>(a, grid, st))
+                                       : (cols <= 8 ? launch<64, 1>(a, grid, st) : launch<64, 2>(a, grid, st));
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
