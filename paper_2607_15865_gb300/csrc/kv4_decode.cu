@@ -2,13 +2,15 @@
 // append of the new tokens and the merge of the splits fused in.
 //
 // A (sequence, kv head) has G query heads x ntok new tokens = columns, taken 16 at a time (an item).
-// An item's slots are cut into blocks of 32 (head_dim 128) or 64 slots.  The lengths are read on the device, and so
-// every CTA works out the same cut of the work: where the items are at most the SMs (of up to 32 sequences), each
-// is cut into pieces of at most `target` blocks, a piece per CTA, with the least target (of 32 tried) for which the
-// pieces are at most the SMs; otherwise the blocks of all items, in order, are cut into equal runs.  Within a
-// CTA the warps take its blocks in turn, each through a private ring of bulk copies with one mbarrier per stage and
-// with its own running maximum, sum and accumulators; they meet once per item, in shared memory.  An item that
-// several CTAs share is merged by the last of them to finish, in a fixed order.
+// An item's slots are cut into blocks of 32 (head_dim 128) or 64 slots; the lengths are read on the device.
+//   one sequence     each item's blocks in equal pieces, one per CTA, as many as the SMs allow: CTAs of all
+//                    the warps that an SM's registers hold, so that an item has few parts to merge
+//   several          the blocks of all items, in order, in equal runs, whatever the lengths: each item counts
+//                    kItemCost blocks more than it has, for what it costs to begin and to end one.  CTAs of
+//                    four warps, several per SM: while one begins or ends an item the others walk
+// Within a CTA the warps take an item's blocks in turn, each through a private ring of bulk copies with one
+// mbarrier per stage and with its own running maximum, sum and accumulators; they meet once per item, in shared
+// memory.  An item that several CTAs share is merged by the last of them to finish, in a fixed order.
 //
 // Per 16 slots, with mma.sync m16n8k16 (A from registers: a tcgen05 operand would have to be written
 // back to shared or tensor memory at four times the packed bytes, for products 8 or 16 columns wide):
@@ -45,14 +47,18 @@
 namespace attn {
 namespace {
 
-constexpr int kMaxSeqs = 1024;  // sequences of one launch (their block counts are summed in shared memory)
+constexpr int kMaxSeqs = 128;   // sequences of one launch (their block counts are summed in shared memory)
+constexpr int kItemCost = 16;    // blocks
 constexpr int kMaxNew = 16;     // new tokens per sequence
+constexpr int kBatch = 8;       // parts of an item that a merging thread loads at once
 constexpr int kNone = 1 << 20;  // no new token with a NaN group
 
-template <int D_, int NT_>
+template <int D_, int NT_, bool WIDE_>
 struct Cfg {
     static constexpr int D = D_, NT = NT_;       // NT: tiles of 8 columns
-    static constexpr int W = NT == 1 ? 16 : 12;  // warps: what the registers allow
+    static constexpr bool WIDE = WIDE_;          // one CTA per SM
+    static constexpr int W = !WIDE ? 4 : NT == 1 ? 16 : 8;  // warps
+    static constexpr int CTAS = WIDE ? 1 : NT == 1 ? 4 : D == 128 ? 2 : 3;  // per SM: what registers and shared memory allow
     static constexpr int THREADS = 32 * W;
     static constexpr int KB = 32 * 128 / D;      // slots per block
     static constexpr int ROW = D / 2;            // bytes of a slot's codes
@@ -64,18 +70,19 @@ struct Cfg {
     static constexpr int COLS = 8 * NT;
     static constexpr int QS = D + 8;             // row stride of q in shared memory (bf16)
     static constexpr int OS = D + 4;             // row stride of a warp's O (floats)
+    static constexpr int O_BYTES = COLS * OS * 4;  // of a warp
     static constexpr int NEW = ROW + 2 * GR;     // bytes of a staged row: codes, scales
-    static constexpr int OFF_O = W * STAGES * STAGE;            // float [W][COLS][OS]
-    static constexpr int OFF_ML = OFF_O + W * COLS * OS * 4;    // float [W][COLS][2]
+    static constexpr int OFF_O = W * STAGES * STAGE;            // float [W][COLS][OS]; before that staged rows (stage_row)
+    static constexpr int OFF_ML = OFF_O + W * O_BYTES;          // float [W][COLS][2]
     static constexpr int OFF_Q = OFF_ML + W * COLS * 8;         // bf16 [COLS][QS]
-    static constexpr int OFF_NEW = OFF_Q + COLS * QS * 2;       // [kMaxNew][k, v][NEW]
-    static constexpr int OFF_PRE = OFF_NEW + kMaxNew * 2 * NEW;  // int [kMaxSeqs + 1]: blocks before a sequence
+    static constexpr int OFF_PRE = OFF_Q + COLS * QS * 2;       // int [kMaxSeqs + 1]: blocks and costs before a sequence
     static constexpr int OFF_BAR = (OFF_PRE + (kMaxSeqs + 1) * 4 + 7) & ~7;  // rings, then the staged rows
     static constexpr int OFF_NAN = OFF_BAR + (W * STAGES + 1) * 8;  // int [4]: first new token with a NaN group of v
-    static constexpr int OFF_FLAG = OFF_NAN + 16;               // int: whether this CTA merges the item
-    static constexpr int OFF_SHARE = OFF_FLAG + 8;              // Share
-    static constexpr int BYTES = OFF_SHARE + 40;
-    static_assert(CODES == 2048 && SCALES == 256 && NEW % 4 == 0 && BYTES <= 232448, "shared memory");
+    static constexpr int OFF_FLAG = OFF_NAN + 16;               // int [2]: whether this CTA merges its first, its last item
+    static constexpr int OFF_SEG = OFF_FLAG + 8;                // Segment [2]: of this turn, and a held one
+    static constexpr int BYTES = OFF_SEG + 2 * 40;
+    static_assert(CODES == 2048 && SCALES == 256 && NEW % 4 == 0 && 2 * kMaxNew * NEW <= O_BYTES, "layout");
+    static_assert(BYTES <= 232448 && CTAS * (BYTES + 1024) <= 233472, "shared memory");
 };
 
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -189,7 +196,7 @@ struct Args {
     int* err;
     uint64_t wait_ns;
     float scale_log2, move;  // log2 e / sqrt D in units of 2^-73, and the lead of a score that moves the maximum (2^8)
-    int batch, ntok, Hq, Hkv, max_len, lp, ncg, min_blocks, per;  // per: CTAs per (kv head, column group)
+    int batch, ntok, Hq, Hkv, max_len, lp, ncg, min_blocks;
 };
 
 // One warp: quantise the E values x that each lane holds of a row of D = 32 E, write the row's codes and
@@ -265,59 +272,19 @@ __device__ __forceinline__ int warp_scan(int v, int lane) {
     return v;
 }
 
+// The part of an item that a CTA walks: its blocks lo .. hi - 1 of T.
+struct Segment {
+    int b, item, head, T, hist;
+    int c0, ncol;      // the item's columns
+    int lo, hi, base;  // base: the item's block 0 in the order that runs are cut from
+};
+
 // x / y for 0 <= x < 2^20, y > 0: (x + 1/2) / y is at least 1 / 2y from an integer, twice what the float quotient
 // may be off by.
 __device__ __forceinline__ int small_div(int x, int y) {
     return static_cast<int>(__fdividef(static_cast<float>(x) + 0.5f, static_cast<float>(y)));
 }
 __device__ __forceinline__ int small_ceil_div(int x, int y) { return small_div(x - 1, y) + 1; }  // x > 0
-
-// A CTA's part of the work: blocks r0 .. r1 - 1 of one item, its piece `piece` of n; or (n = 0) of the blocks of all
-// items, in order.
-struct Share {
-    int b, item, T, hist;  // the sequence, its item and that one's blocks
-    int r0, r1, piece, n;
-    int nc, total;         // CTAs and blocks of a cut into runs
-};
-
-// One warp: the share of CTA `cta` for up to 32 sequences, lane b holding the blocks T of sequence b's items (0:
-// skipped).  hc: items of a sequence, per * hc CTAs.  pre: filled where the cut is into runs.
-__device__ __forceinline__ Share piece_of(int T, int hist, int hc, int per, int min_blocks, int cta, int* pre, int lane) {
-    Share sh = {};
-    const uint32_t live = __ballot_sync(0xFFFFFFFFu, T > 0);
-    const int items = __popc(live), sum = __reduce_add_sync(0xFFFFFFFFu, T), longest = __reduce_max_sync(0xFFFFFFFFu, T);
-    if (items == 0) return sh;
-    if (items > per) {
-        pre[lane + 1] = warp_scan(T, lane);
-        if (lane == 0) pre[0] = 0;
-        sh.total = sum * hc;
-        return sh;
-    }
-    int target = max(min_blocks, small_ceil_div(longest, small_div(per, items)));  // fits
-    if (longest * items != sum) {
-        const int lo = max(min_blocks, (sum + per - 1) / per);  // no less fits
-        const int mine = lo + (((target - lo) * lane) >> 5);
-        int pieces = 0;
-        for (uint32_t rest = live; rest != 0; rest &= rest - 1)
-            pieces += small_ceil_div(__shfl_sync(0xFFFFFFFFu, T, __ffs(rest) - 1), mine);
-        const uint32_t fits = __ballot_sync(0xFFFFFFFFu, pieces <= per);
-        if (fits != 0) target = __shfl_sync(0xFFFFFFFFu, mine, __ffs(fits) - 1);
-    }
-    const int n = T > 0 ? small_ceil_div(T, target) : 0, upto = warp_scan(n, lane);
-    const uint32_t past = __ballot_sync(0xFFFFFFFFu, T > 0 && upto * hc > cta);
-    if (past == 0) return sh;
-    sh.b = __ffs(past) - 1;
-    sh.T = __shfl_sync(0xFFFFFFFFu, T, sh.b);
-    sh.hist = __shfl_sync(0xFFFFFFFFu, hist, sh.b);
-    sh.n = __shfl_sync(0xFFFFFFFFu, n, sh.b);
-    const int rem = cta - __shfl_sync(0xFFFFFFFFu, upto - n, sh.b) * hc;
-    sh.item = small_div(rem, sh.n);
-    sh.piece = rem - sh.item * sh.n;
-    const int each = small_div(sh.T, sh.n), more = sh.T - each * sh.n;
-    sh.r0 = sh.piece * each + min(sh.piece, more);
-    sh.r1 = sh.r0 + each + (sh.piece < more ? 1 : 0);
-    return sh;
-}
 
 // The first b with sums[b + 1] * hc > r.
 __device__ __forceinline__ int search(const int* sums, int batch, int hc, int r) {
@@ -361,12 +328,14 @@ struct Merged {
     }
 };
 
-template <int D, int NT>
-__global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(const __grid_constant__ Args a) {
-    using C = Cfg<D, NT>;
+template <int D, int NT, bool WIDE>
+__global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::CTAS) kv4_decode_kernel(
+    const __grid_constant__ Args a) {
+    using C = Cfg<D, NT, WIDE>;
     constexpr int W = C::W, KB = C::KB, GR = C::GR, E = D / 32;
     constexpr int KW = D / 32;   // words of a lane's part of a k row (D / 4 values)
     constexpr int VW = D / 64;   // words of a lane's part of a v row (D / 8 values)
+    constexpr int V = C::THREADS >= 256 && NT == 1 ? 2 : 4;  // values of a thread where the warps' parts meet
     extern __shared__ __align__(128) uint8_t smem[];
     const uint32_t base = smem_u32(smem);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
@@ -376,19 +345,21 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
     uint16_t* s_q = reinterpret_cast<uint16_t*>(smem + C::OFF_Q);
     float* s_o = reinterpret_cast<float*>(smem + C::OFF_O);
     float2* s_ml = reinterpret_cast<float2*>(smem + C::OFF_ML);
-    Share* share = reinterpret_cast<Share*>(smem + C::OFF_SHARE);
-    auto bar = [&](int stage) { return base + C::OFF_BAR + 8u * static_cast<uint32_t>(warp * C::STAGES + stage); };
+    Segment* segs = reinterpret_cast<Segment*>(smem + C::OFF_SEG);
+    static_assert(sizeof(Segment) == 40, "shared memory");
+    const uint32_t bar0 = base + C::OFF_BAR + 8u * static_cast<uint32_t>(warp * C::STAGES);
     const uint32_t new_full = base + C::OFF_BAR + 8u * (W * C::STAGES);
     if (lane == 0) {
 #pragma unroll
-        for (int s = 0; s < C::STAGES; ++s) mbar_init(bar(s), 1);
+        for (int s = 0; s < C::STAGES; ++s) mbar_init(bar0 + 8 * s, 1);
         if (warp == 0) mbar_init(new_full, W);
         fence_mbar_init();
     }
     griddep_wait();
     griddep_launch_dependents();
 
-    // The blocks of a launch are counted in int: a cache of 2^31 of them would take 2^31 x 4.5 KB / 16 column groups.
+    // The CTA's share: from block first.lo of item `first` on, and as far as `stop` in the order of the runs.  (Blocks are
+    // counted in int: a cache of 2^31 of them would take 2^31 x 4.5 KB / 16 column groups.)
     const int hc = a.Hkv * a.ncg;  // items of a sequence
     const int cta = static_cast<int>(blockIdx.x);
     auto blocks_of = [&](int b, int& h) {
@@ -397,71 +368,96 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
         if (!ok && cta == 0) atomicOr(a.err, kDevErrHistRange);
         return ok ? (h + a.ntok + KB - 1) / KB : 0;
     };
-    if (a.batch > 32) {
-        for (int b = tid; b < a.batch; b += C::THREADS) {
-            int h;
-            pre[b + 1] = blocks_of(b, h);
+    Segment first;
+    int stop = 0, each = 0, more = 0;  // runs: CTA j has each blocks, the first `more` one more
+    int n = 0;                         // pieces of an item, 0 for runs
+    if (WIDE) {
+        const int T = blocks_of(0, first.hist), per = static_cast<int>(gridDim.x) / hc;
+        if (T == 0) return;
+        n = small_ceil_div(T, max(a.min_blocks, small_ceil_div(T, per)));
+        first.b = 0;
+        first.T = T;
+        first.item = small_div(cta, n);
+        if (first.item >= hc) return;
+        const int piece = cta - first.item * n, whole = small_div(T, n), rest = T - whole * n;
+        first.lo = piece * whole + min(piece, rest);
+        first.hi = first.lo + whole + (piece < rest ? 1 : 0);
+        first.base = piece;
+    } else {
+        auto cost = [](int T) { return T > 0 ? T + kItemCost : 0; };
+        if (a.batch > 32) {
+            for (int b = tid; b < a.batch; b += C::THREADS) {
+                int h;
+                pre[b + 1] = cost(blocks_of(b, h));
+            }
+            __syncthreads();
         }
-        __syncthreads();
-    }
-    if (warp == 0) {
-        Share sh = {};
-        if (a.batch <= 32) {
-            int h = 0;
-            const int T = lane < a.batch ? blocks_of(lane, h) : 0;
-            sh = piece_of(T, h, hc, a.per, a.min_blocks, cta, pre, lane);
-        } else {
+        if (warp == 0) {
             int sum = 0;
             for (int b0 = 0; b0 < a.batch; b0 += 32) {
-                const int v = warp_scan(b0 + lane < a.batch ? pre[b0 + lane + 1] : 0, lane);
+                int h, v = 0;
+                if (b0 + lane < a.batch) v = a.batch > 32 ? pre[b0 + lane + 1] : cost(blocks_of(lane, h));
+                v = warp_scan(v, lane);
                 if (b0 + lane < a.batch) pre[b0 + lane + 1] = sum + v;
                 sum += __shfl_sync(0xFFFFFFFFu, v, 31);
             }
             if (lane == 0) pre[0] = 0;
-            sh.total = sum * hc;
         }
-        if (sh.n == 0) {
-            sh.nc = min(static_cast<int>(gridDim.x), max(1, (sh.total + a.min_blocks - 1) / a.min_blocks));
-            if (cta < sh.nc) {
-                sh.r0 = static_cast<int>(static_cast<long long>(sh.total) * cta / sh.nc);
-                sh.r1 = static_cast<int>(static_cast<long long>(sh.total) * (cta + 1) / sh.nc);
-            }
-        }
-        if (lane == 0) *share = sh;
+        __syncthreads();
+        const int total = pre[a.batch] * hc;
+        const int nc = min(static_cast<int>(gridDim.x), (total + a.min_blocks - 1) / a.min_blocks);
+        if (cta >= nc) return;
+        each = total / nc;
+        more = total - each * nc;
+        const int r0 = cta * each + min(cta, more);
+        stop = r0 + each + (cta < more ? 1 : 0);
+        first.b = search(pre, a.batch, hc, r0);
+        const int whole = pre[first.b + 1] - pre[first.b], rem = r0 - pre[first.b] * hc;
+        first.T = whole - kItemCost;
+        first.item = rem / whole;
+        first.base = r0 - (rem - first.item * whole) + kItemCost;
+        first.lo = max(0, r0 - first.base);
+        first.hi = min(first.T, stop - first.base);
+        if (first.lo >= first.hi) return;  // the run ends in what the item counts beside its blocks
+        first.hist = a.d_hist[first.b];
     }
-    __syncthreads();
-    const int r0 = share->r0, r1 = share->r1;
-    const bool runs = share->n == 0;
-    if (r0 >= r1) return;
-    auto cta_of = [&](int r) {
-        return static_cast<int>((static_cast<long long>(r + 1) * share->nc - 1) / share->total);
+    auto cta_of = [&](int r) {  // whose run has block r
+        const int cut = more * (each + 1);
+        return r < cut ? r / (each + 1) : more + (r - cut) / each;
+    };
+    // The item after (b, item), its blocks in the run: false where the run has none of it.
+    auto following = [&](int& b, int& item, int& T, int& at, int& hi) {
+        at += T + kItemCost;
+        if (WIDE || at >= stop) return false;
+        if (++item == hc) {
+            item = 0;
+            do ++b;
+            while (pre[b + 1] == pre[b]);
+            T = pre[b + 1] - pre[b] - kItemCost;
+        }
+        hi = min(T, stop - at);
+        return true;
     };
 
-    // The warp's blocks: r0 + warp, + W, ...; copies run two blocks ahead.  (b_next, head x column group, block) is
-    // where block `next` lies, off_next its byte in the codes (an eighth of it: in the scales).
+    // The warp's copies run two blocks ahead of it: block blk_next of an item is next, off_next its byte in
+    // the codes (an eighth of it: in the scales).
     static_assert(C::STAGES == 2 && C::ROW == 8 * 2 * GR, "stages alternate; codes and scales share an offset");
-    const uint32_t s_warp = base + static_cast<uint32_t>(warp * C::STAGES * C::STAGE), bar0 = bar(0);
-    int next = r0 + warp, b_next = share->b, T_next = share->T, item_next = share->item, blk_next = next;
-    if (runs) {
-        b_next = search(pre, a.batch, hc, r0);
-        T_next = pre[b_next + 1] - pre[b_next];
-        item_next = (r0 - pre[b_next] * hc) / T_next;
-        blk_next = next - pre[b_next] * hc - item_next * T_next;
-    }
+    const uint32_t s_warp = base + static_cast<uint32_t>(warp * C::STAGES * C::STAGE);
+    int b_next = first.b, item_next = first.item, T_next = first.T, base_next = first.base, hi_next = first.hi;
+    int blk_next = first.lo + warp, pending = 0;
     size_t off_next = 0;
-    bool placed = false, dead = false;
+    bool placed = false, ended = false, dead = false;
     auto issue = [&](uint32_t stage, uint32_t barrier) {
-        if (next >= r1) return;
-        if (!placed || blk_next >= T_next) {
-            while (blk_next >= T_next) {
-                blk_next -= T_next;
-                if (++item_next == hc) {
-                    item_next = 0;
-                    do ++b_next;
-                    while (pre[b_next + 1] == pre[b_next]);
-                    T_next = pre[b_next + 1] - pre[b_next];
-                }
+        if (ended) return;
+        while (blk_next >= hi_next) {
+            if (!following(b_next, item_next, T_next, base_next, hi_next)) {
+                ended = true;
+                return;
             }
+            blk_next = warp;
+            placed = false;
+        }
+        if (!placed) {
             const int head = a.ncg == 1 ? item_next : item_next / a.ncg;
             off_next = ((static_cast<size_t>(b_next) * a.Hkv + head) * a.lp + static_cast<size_t>(blk_next) * KB) * C::ROW;
             placed = true;
@@ -474,7 +470,7 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
             bulk_g2s(stage + 2 * C::CODES + C::SCALES, reinterpret_cast<const uint8_t*>(a.c.v_scales) + (off_next >> 3),
                      C::SCALES, barrier);
         }
-        next += W;
+        ++pending;
         blk_next += W;
         off_next += static_cast<size_t>(W) * C::CODES;
     };
@@ -483,74 +479,134 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
     for (int s = 0; s < C::STAGES; ++s) issue(s_warp + s * C::STAGE, bar0 + 8 * s);
 
     uint32_t st_off = 0, bar_off = 0, phase = 0;  // of the warp's next block
-    int mine = r0 + warp;                         // that block
     uint32_t new_phase = 0;
-    int b = share->b;
-    if (runs) b = search(pre, a.batch, hc, r0);
-    for (int seg = r0; seg < r1;) {
-        // the item of block `seg`, up to where it or the CTA's run ends
-        int T = share->T, item = share->item, hist = share->hist, i0 = 0;  // i0: the item's first block
-        if (runs) {
-            while (seg >= pre[b + 1] * hc) ++b;
-            T = pre[b + 1] - pre[b];
-            item = (seg - pre[b] * hc) / T;
-            i0 = pre[b] * hc + item * T;
-            hist = a.d_hist[b];
-        }
-        const int head = a.ncg == 1 ? item : item / a.ncg, cg = a.ncg == 1 ? 0 : item % a.ncg;
-        const int end = min(r1, i0 + T);
-        const int G = a.Hq / a.Hkv;
-        const int c0 = cg * 16, ncol = min(16, G * a.ntok - c0);
-        auto token = [&](int col) { return (c0 + col) / G; };
-        auto row_of = [&](int col) {  // of q and out, in rows of D
-            return (static_cast<size_t>(b) * a.ntok + token(col)) * a.Hq + head * G + (c0 + col) % G;
-        };
-        if (tid < 4) s_nan[tid] = kNone;
-        // q of the columns, rotated and rounded to bf16; columns that do not exist are 0
-        for (int u = tid; u < C::COLS * (D / 2); u += C::THREADS) {
-            const int col = u / (D / 2), j = u % (D / 2);
-            uint16_t lo = 0, hi = 0;
-            if (col < ncol) {
-                const uint16_t* src = a.q + row_of(col) * D;
-                const size_t p = static_cast<size_t>(hist + token(col)) * (D / 2) + j;
-                const float x = __uint_as_float(static_cast<uint32_t>(__ldg(src + j)) << 16);
-                const float y = __uint_as_float(static_cast<uint32_t>(__ldg(src + j + D / 2)) << 16);
-                const float cs = __ldg(a.cos_tab + p), sn = __ldg(a.sin_tab + p);
-                lo = __bfloat16_as_ushort(__float2bfloat16_rn(__fsub_rn(__fmul_rn(x, cs), __fmul_rn(y, sn))));
-                hi = __bfloat16_as_ushort(__float2bfloat16_rn(__fadd_rn(__fmul_rn(y, cs), __fmul_rn(x, sn))));
-            }
-            s_q[col * C::QS + j] = lo;
-            s_q[col * C::QS + j + D / 2] = hi;
-        }
-        __syncthreads();
-        // the new tokens whose slots lie in the segment's blocks, a warp per row of k or v
-        const int new0 = max(hist, (seg - i0) * KB), new1 = min(hist + a.ntok, (end - i0) * KB);
-        if (new0 < new1) {
-            for (int u = W - 1 - warp; u < 2 * (new1 - new0); u += W) {
-                const int p = new0 + u / 2, i = p - hist;
-                const size_t src = ((static_cast<size_t>(b) * a.ntok + i) * a.Hkv + head) * D;
-                const size_t slot = (static_cast<size_t>(b) * a.Hkv + head) * a.lp + p;
-                uint8_t* staged = smem + C::OFF_NEW + (2 * i + (u & 1)) * C::NEW;
-                float x[E];
-                load_row<E>(((u & 1) ? a.v_new : a.k_new) + src, lane, x);
-                if (u & 1) {
-                    const bool nan = put_row<D>(x, lane, a.c.v_codes + slot * C::ROW, a.c.v_scales + slot * GR, staged);
-                    if (nan && lane % (kKv4Group / E) == 0) atomicMin(&s_nan[lane / (kKv4Group / E)], i);
-                } else {
+    const int G = a.Hq / a.Hkv;
+    auto token = [&](const Segment& w, int col) { return small_div(w.c0 + col, G); };
+    auto row_of = [&](const Segment& w, int col) {  // of q and out, in rows of D
+        const int i = token(w, col);
+        return (static_cast<size_t>(w.b) * a.ntok + i) * a.Hq + w.head * G + (w.c0 + col - i * G);
+    };
+    // Staged row of new token i, k (0) or v (1): in the O buffer, not yet written, of the warp that has its block.
+    auto staged_row = [&](const Segment& w, int i, int kind) {
+        const int owner = (((w.hist + i) / KB) - w.lo) % W;
+        return smem + C::OFF_O + owner * C::O_BYTES + (2 * i + kind) * C::NEW;
+    };
+    // The merge of an item's parts by its last CTA: `subs` threads per four values, every subs-th part each.
+    auto merge = [&](const Segment& w, int j0, int j1) {
+        if (tid == 0) a.counters[static_cast<size_t>(w.b) * hc + w.item] = 0;
+        const int vals = w.ncol * (D / 4), subs = max(1, min(C::THREADS / vals, j1 - j0 + 1));
+        float4* s_x = reinterpret_cast<float4*>(s_o);
+        float2* s_y = reinterpret_cast<float2*>(s_x + C::THREADS);
+        for (int u0 = 0; u0 < vals; u0 += C::THREADS) {  // one turn where subs > 1
+            const int sub = subs > 1 ? tid / vals : 0, u = u0 + tid - sub * vals;
+            const int col = u / (D / 4), d = u % (D / 4) * 4;
+            Merged acc;
+            int nan = kNone;
+            if (sub < subs && u < vals)
+#pragma unroll 1
+                for (int j = j0 + sub; j <= j1; j += kBatch * subs) {
+                    float2 ml[kBatch];
+                    float4 x[kBatch];
 #pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const size_t j = static_cast<size_t>(p) * (D / 2) + (lane & 15) * E + e;
-                        const float other = __shfl_xor_sync(0xFFFFFFFFu, x[e], 16);
-                        const float cs = __ldg(a.cos_tab + j), sn = __ldg(a.sin_tab + j);
-                        x[e] = round_bf16(lane < 16 ? __fsub_rn(__fmul_rn(x[e], cs), __fmul_rn(other, sn))
-                                                    : __fadd_rn(__fmul_rn(x[e], cs), __fmul_rn(other, sn)));
+                    for (int i = 0; i < kBatch; ++i) {
+                        const int from = min(j + i * subs, j1), row = (2 * from + (from == j0 ? 1 : 0)) * 16 + col;
+                        ml[i] = __ldcg(reinterpret_cast<const float2*>(a.part_ml) + row);
+                        x[i] = __ldcg(reinterpret_cast<const float4*>(a.part_o + static_cast<size_t>(row) * D + d));
+                        if (a.ntok > 1) nan = min(nan, __ldcg(a.part_nan + 4 * (row / 16) + d / kKv4Group));
+                        if (j + i * subs > j1) ml[i].x = -INFINITY;
                     }
-                    put_row<D>(x, lane, a.c.k_codes + slot * C::ROW, a.c.k_scales + slot * GR, staged);
+                    acc.add(ml, x);
                 }
+            if (subs > 1) {
+                if (sub > 0 && sub < subs) {
+                    s_x[tid] = make_float4(acc.o[0], acc.o[1], acc.o[2], acc.o[3]);
+                    s_y[tid] = make_float2(acc.m, acc.l);
+                    if (nan < kNone) atomicMin(&s_nan[d / kKv4Group], nan);
+                }
+                __syncthreads();
+                if (sub == 0)
+                    for (int i = 1; i < subs; ++i) {
+                        const float2 ml[1] = {s_y[tid + i * vals]};
+                        const float4 x[1] = {s_x[tid + i * vals]};
+                        acc.add(ml, x);
+                    }
+                nan = min(nan, s_nan[d / kKv4Group]);
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(new_full);
+            if (sub == 0 && u < vals)
+                *reinterpret_cast<uint2*>(a.out + row_of(w, col) * D + d) = acc.result(nan > 0 && nan <= token(w, col));
         }
+    };
+
+    if (tid == 0) {
+        segs[0] = first;
+        segs[1].b = -1;
+    }
+    for (bool final_turn = false; !final_turn;) {
+        __syncthreads();  // segs[0]; the buffers of the item before are free
+        Segment& now = segs[0];
+        {
+            Segment w = now;
+            w.head = a.ncg == 1 ? w.item : w.item / a.ncg;
+            w.c0 = a.ncg == 1 ? 0 : (w.item - w.head * a.ncg) * 16;
+            w.ncol = min(16, G * a.ntok - w.c0);
+            // q of the columns, rotated and rounded to bf16; columns that do not exist are 0
+            for (int u = tid; u < C::COLS * (D / 4); u += C::THREADS) {
+                const int col = u / (D / 4), j = u % (D / 4) * 2;
+                uint32_t lo = 0, hi = 0;
+                if (col < w.ncol) {
+                    const uint16_t* src = a.q + row_of(w, col) * D + j;
+                    const size_t p = static_cast<size_t>(w.hist + token(w, col)) * (D / 2) + j;
+                    const uint32_t x = __ldg(reinterpret_cast<const uint32_t*>(src));
+                    const uint32_t y = __ldg(reinterpret_cast<const uint32_t*>(src + D / 2));
+                    const float2 cs = __ldg(reinterpret_cast<const float2*>(a.cos_tab + p));
+                    const float2 sn = __ldg(reinterpret_cast<const float2*>(a.sin_tab + p));
+                    const float x0 = __uint_as_float(x << 16), x1 = __uint_as_float(x & 0xFFFF0000u);
+                    const float y0 = __uint_as_float(y << 16), y1 = __uint_as_float(y & 0xFFFF0000u);
+                    lo = pack2(__fsub_rn(__fmul_rn(x0, cs.x), __fmul_rn(y0, sn.x)),
+                               __fsub_rn(__fmul_rn(x1, cs.y), __fmul_rn(y1, sn.y)));
+                    hi = pack2(__fadd_rn(__fmul_rn(y0, cs.x), __fmul_rn(x0, sn.x)),
+                               __fadd_rn(__fmul_rn(y1, cs.y), __fmul_rn(x1, sn.y)));
+                }
+                *reinterpret_cast<uint32_t*>(s_q + col * C::QS + j) = lo;
+                *reinterpret_cast<uint32_t*>(s_q + col * C::QS + j + D / 2) = hi;
+            }
+            if (tid < 4) s_nan[tid] = kNone;
+            __syncthreads();
+            if (tid == 0) {
+                now.head = w.head;
+                now.c0 = w.c0;
+                now.ncol = w.ncol;
+            }
+            // the new tokens whose slots lie in the segment's blocks, a warp per row of k or v
+            const int new0 = max(w.hist, w.lo * KB), new1 = min(w.hist + a.ntok, w.hi * KB);
+            if (new0 < new1) {
+                for (int u = W - 1 - warp; u < 2 * (new1 - new0); u += W) {
+                    const int p = new0 + u / 2, i = p - w.hist;
+                    const size_t src = ((static_cast<size_t>(w.b) * a.ntok + i) * a.Hkv + w.head) * D;
+                    const size_t slot = (static_cast<size_t>(w.b) * a.Hkv + w.head) * a.lp + p;
+                    uint8_t* staged = staged_row(w, i, u & 1);
+                    float x[E];
+                    load_row<E>(((u & 1) ? a.v_new : a.k_new) + src, lane, x);
+                    if (u & 1) {
+                        const bool nan = put_row<D>(x, lane, a.c.v_codes + slot * C::ROW, a.c.v_scales + slot * GR, staged);
+                        if (nan && lane % (kKv4Group / E) == 0) atomicMin(&s_nan[lane / (kKv4Group / E)], i);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < E; ++e) {
+                            const size_t j = static_cast<size_t>(p) * (D / 2) + (lane & 15) * E + e;
+                            const float other = __shfl_xor_sync(0xFFFFFFFFu, x[e], 16);
+                            const float cs = __ldg(a.cos_tab + j), sn = __ldg(a.sin_tab + j);
+                            x[e] = round_bf16(lane < 16 ? __fsub_rn(__fmul_rn(x[e], cs), __fmul_rn(other, sn))
+                                                        : __fadd_rn(__fmul_rn(x[e], cs), __fmul_rn(other, sn)));
+                        }
+                        put_row<D>(x, lane, a.c.k_codes + slot * C::ROW, a.c.k_scales + slot * GR, staged);
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(new_full);
+            }
+        }
+        const int hist = now.hist, hi = now.hi;
 
         // Q^T's B fragments: lane (g, t) holds values D/4 t .. D/4 t + D/4 - 1 of column g (+ 8 n); step s of the
         // products takes values 4 s .. 4 s + 3 of them.  qz: minus their sum in three parts.
@@ -582,19 +638,20 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
                 const int col = 8 * n + 2 * t + e;
                 m[n][e] = -INFINITY;
                 ms[n][e] = -kLift;
-                lim[n][e] = hist + (col < ncol ? token(col) : a.ntok - 1);
+                lim[n][e] = hist + min(small_div((a.ncg == 1 ? 0 : now.item % a.ncg * 16) + col, G), a.ntok - 1);
             }
 
-        const bool has_blocks = !dead && mine < end;
-        for (; !dead && mine < end; mine += W) {
-            const int k0 = (mine - i0) * KB;
+        int blk = now.lo + warp;
+        const bool has_blocks = !dead && blk < hi;
+        for (; !dead && blk < hi; blk += W) {
+            const int k0 = blk * KB;
             const uint32_t s_k = s_warp + st_off, full = bar0 + bar_off;
+            const uint32_t s_v = s_k + C::CODES, s_ks = s_v + C::CODES, s_vs = s_ks + C::SCALES;
             if (!__all_sync(0xFFFFFFFFu, mbar_wait(full, phase, nullptr, a.wait_ns))) {
                 if (lane == 0) record_dev_err(a.err, kDevErrTimeout);
                 dead = true;
                 break;
             }
-            const uint32_t s_v = s_k + C::CODES, s_ks = s_v + C::CODES, s_vs = s_ks + C::SCALES;
             const bool tail = k0 + KB > hist;  // the block holds slots of new tokens, or none at all
             if (tail) {  // the staged rows into the block
                 if (!__all_sync(0xFFFFFFFFu, mbar_wait(new_full, new_phase, nullptr))) {
@@ -606,14 +663,13 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
                 for (int p = lo; p < hi; ++p)
 #pragma unroll
                     for (int kind = 0; kind < 2; ++kind) {
-                        const uint32_t* src =
-                            reinterpret_cast<const uint32_t*>(smem + C::OFF_NEW + (2 * (p - hist) + kind) * C::NEW);
-                        uint8_t* blk = smem + (s_k - base);
+                        const uint32_t* src = reinterpret_cast<const uint32_t*>(staged_row(now, p - hist, kind));
+                        uint8_t* dst = smem + (s_k - base);
                         if (lane < C::ROW / 4)
-                            reinterpret_cast<uint32_t*>(blk + kind * C::CODES + (p - k0) * C::ROW)[lane] = src[lane];
+                            reinterpret_cast<uint32_t*>(dst + kind * C::CODES + (p - k0) * C::ROW)[lane] = src[lane];
                         else if (lane < C::NEW / 4)
-                            reinterpret_cast<uint32_t*>(blk + 2 * C::CODES + kind * C::SCALES + (p - k0) * GR * 2)[lane - C::ROW / 4] =
-                                src[lane];
+                            reinterpret_cast<uint32_t*>(dst + 2 * C::CODES + kind * C::SCALES +
+                                                        (p - k0) * GR * 2)[lane - C::ROW / 4] = src[lane];
                     }
                 __syncwarp();
             }
@@ -729,6 +785,7 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
             }
             if (tail) fence_proxy_async_smem();  // this warp wrote to the stage that the next copy fills
             __syncwarp();
+            --pending;
             issue(s_k, full);
             st_off = C::STAGE - st_off;
             phase ^= bar_off >> 3;
@@ -751,109 +808,80 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1) kv4_decode_kernel(cons
                 if (g == 0) s_ml[col] = make_float2(m[n][e] * a.scale_log2, sum[n][e]);
             }
         __syncthreads();
-        if (new0 < new1) new_phase ^= 1u;
-        int j0 = cta - share->piece, j1 = j0 + share->n - 1;  // the CTAs that share the item
-        if (runs) {
-            j0 = cta_of(i0);
-            j1 = cta_of(i0 + T - 1);
-        }
+        if (max(hist, now.lo * KB) < min(hist + a.ntok, hi * KB)) new_phase ^= 1u;
+        const int j0 = WIDE ? cta - now.base : cta_of(now.base);  // the CTAs that share the item
+        const int j1 = WIDE ? j0 + n - 1 : cta_of(now.base + now.T - 1);
         const int part = 2 * cta + (cta == j0 ? 1 : 0);
-        const int used = min(W, end - seg), first_warp = (seg - r0) % W;  // the warps that had blocks
-        for (int u = tid; u < ncol * (D / 4); u += C::THREADS) {
-            const int col = u / (D / 4), d = u % (D / 4) * 4;
-            Merged acc;
-#pragma unroll 1
-            for (int w0 = 0; w0 < used; w0 += 4) {
-                float2 ml[4];
-                float4 x[4];
+        for (int u = tid; u < now.ncol * (D / V); u += C::THREADS) {
+            const int col = u / (D / V), d = u % (D / V) * V;
+            float f[W], mx = -INFINITY, l = 0.f, acc[V] = {};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    int w = first_warp + min(w0 + i, used - 1);
-                    w = w >= W ? w - W : w;
-                    ml[i] = s_ml[w * C::COLS + col];
-                    x[i] = *reinterpret_cast<const float4*>(s_o + (w * C::COLS + col) * C::OS + d);
-                    if (w0 + i >= used) ml[i].x = -INFINITY;
-                }
-                acc.add(ml, x);
+            for (int w = 0; w < W; ++w) {
+                f[w] = s_ml[w * C::COLS + col].x;
+                mx = fmaxf(mx, f[w]);
+            }
+            const float mu = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                f[w] = exp2_fast(f[w] - mu);
+                if (f[w] == 0.f) continue;  // a warp without blocks wrote nothing else
+                l += f[w] * s_ml[w * C::COLS + col].y;
+                const float* x = s_o + (w * C::COLS + col) * C::OS + d;
+#pragma unroll
+                for (int e = 0; e < V; ++e) acc[e] += f[w] * x[e];
             }
             if (j0 == j1) {
-                const int first = s_nan[d / kKv4Group];
-                *reinterpret_cast<uint2*>(a.out + row_of(col) * D + d) = acc.result(first > 0 && first <= token(col));
-            } else {
-                *reinterpret_cast<float4*>(a.part_o + (static_cast<size_t>(part) * 16 + col) * D + d) =
-                    make_float4(acc.o[0], acc.o[1], acc.o[2], acc.o[3]);
-                if (d == 0) reinterpret_cast<float2*>(a.part_ml)[part * 16 + col] = make_float2(acc.m, acc.l);
-            }
-        }
-        if (j0 != j1) {
-            if (tid < 4) a.part_nan[4 * part + tid] = s_nan[tid];
-            __syncthreads();
-            int* count = a.counters + static_cast<size_t>(b) * hc + item;
-            if (tid == 0) {
-                __threadfence();  // the CTA's part, and then its count
-                *flag = atomicAdd(count, 1) == j1 - j0;
-                __threadfence();  // the count, and then the others' parts
-            }
-            __syncthreads();
-            if (*flag) {  // the last of the item's CTAs merges them: `subs` threads per four values, every subs-th part each
-                if (tid == 0) *count = 0;
-                const int vals = ncol * (D / 4), subs = max(1, min(C::THREADS / vals, j1 - j0 + 1));
-                float4* s_x = reinterpret_cast<float4*>(s_o);
-                float2* s_y = reinterpret_cast<float2*>(s_x + C::THREADS);
-                for (int u0 = 0; u0 < vals; u0 += C::THREADS) {  // one turn where subs > 1
-                    const int sub = subs > 1 ? tid / vals : 0, u = u0 + tid - sub * vals;
-                    const int col = u / (D / 4), d = u % (D / 4) * 4;
-                    Merged acc;
-                    int nan = kNone;
-                    if (sub < subs && u < vals)
-#pragma unroll 1
-                        for (int j = j0 + sub; j <= j1; j += 8 * subs) {
-                            float2 ml[8];
-                            float4 x[8];
+                const int from = s_nan[d / kKv4Group];
+                const bool nan = from > 0 && from <= token(now, col);
+                const float r = kUnit / l;
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                const int from = min(j + i * subs, j1), row = (2 * from + (from == j0 ? 1 : 0)) * 16 + col;
-                                ml[i] = __ldcg(reinterpret_cast<const float2*>(a.part_ml) + row);
-                                x[i] = __ldcg(reinterpret_cast<const float4*>(a.part_o + static_cast<size_t>(row) * D + d));
-                                if (a.ntok > 1) nan = min(nan, __ldcg(a.part_nan + 4 * (row / 16) + d / kKv4Group));
-                                if (j + i * subs > j1) ml[i].x = -INFINITY;
-                            }
-                            acc.add(ml, x);
-                        }
-                    if (subs > 1) {
-                        if (sub > 0 && sub < subs) {
-                            s_x[tid] = make_float4(acc.o[0], acc.o[1], acc.o[2], acc.o[3]);
-                            s_y[tid] = make_float2(acc.m, acc.l);
-                            if (nan < kNone) atomicMin(&s_nan[d / kKv4Group], nan);
-                        }
-                        __syncthreads();
-                        if (sub == 0)
-                            for (int i = 1; i < subs; ++i) {
-                                const float2 ml[1] = {s_y[tid + i * vals]};
-                                const float4 x[1] = {s_x[tid + i * vals]};
-                                acc.add(ml, x);
-                            }
-                        nan = min(nan, s_nan[d / kKv4Group]);
-                    }
-                    if (sub == 0 && u < vals)
-                        *reinterpret_cast<uint2*>(a.out + row_of(col) * D + d) = acc.result(nan > 0 && nan <= token(col));
-                }
+                for (int e = 0; e < V; e += 2)
+                    *reinterpret_cast<uint32_t*>(a.out + row_of(now, col) * D + d + e) =
+                        nan ? 0x7FC07FC0u : pack2(acc[e] * r, acc[e + 1] * r);
+            } else {
+                float* dst = a.part_o + (static_cast<size_t>(part) * 16 + col) * D + d;
+#pragma unroll
+                for (int e = 0; e < V; e += 2) *reinterpret_cast<float2*>(dst + e) = make_float2(acc[e], acc[e + 1]);
+                if (d == 0) reinterpret_cast<float2*>(a.part_ml)[part * 16 + col] = make_float2(mx, l);
             }
         }
-        seg = end;
-        if (seg < r1) __syncthreads();  // the merge buffers and q are written again
+        if (j0 != j1 && tid < 4) a.part_nan[4 * part + tid] = s_nan[tid];
+        int b = now.b, item = now.item, T = now.T, at = now.base, hi_after;
+        final_turn = !following(b, item, T, at, hi_after);
+        __syncthreads();  // the part is complete
+        if (tid == 0) {
+            if (j0 != j1) {
+                __threadfence();  // the CTA's part, and then its count
+                flag[final_turn] = atomicAdd(a.counters + static_cast<size_t>(now.b) * hc + now.item, 1) == j1 - j0;
+                __threadfence();  // the count, and then the others' parts
+                if (!final_turn) segs[1] = now;  // an item that began in an earlier CTA: looked at again at the end
+            }
+            if (!final_turn) now = Segment{b, item, 0, T, a.d_hist[b], 0, 0, 0, hi_after, at};
+        }
+        if (final_turn) {
+            __syncthreads();
+            if (j0 != j1 && flag[1]) merge(now, j0, j1);
+            const Segment& held = segs[1];
+            if (held.b >= 0 && flag[0]) {
+                __syncthreads();
+                if (tid < 4) s_nan[tid] = kNone;
+                __syncthreads();
+                merge(held, cta_of(held.base), cta_of(held.base + held.T - 1));
+            }
+        }
     }
-    if (dead) {  // the copies still in flight, of blocks `mine` and the next, land before the shared memory is given up
-        if (mine < next) mbar_wait(bar0 + bar_off, phase, nullptr);
-        if (mine + W < next) mbar_wait(bar0 + (bar_off ^ 8u), phase ^ (bar_off >> 3), nullptr);
+    if (dead) {  // copies still in flight land before the shared memory is given up
+        if (pending > 0) mbar_wait(bar0 + bar_off, phase, nullptr);
+        if (pending > 1) mbar_wait(bar0 + (bar_off ^ 8u), phase ^ (bar_off >> 3), nullptr);
     }
 }
 
-template <int D, int NT>
-cudaError_t launch(const Args& a, int grid, cudaStream_t st) {
-    using C = Cfg<D, NT>;
+template <int D, int NT, bool WIDE>
+cudaError_t launch(const Args& a, int num_sms, cudaStream_t st) {
+    using C = Cfg<D, NT, WIDE>;
+    const long long most = static_cast<long long>(a.batch) * a.Hkv * a.ncg * ((a.max_len + C::KB - 1) / C::KB + kItemCost);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(grid));
+    cfg.gridDim = dim3(static_cast<unsigned>(std::min<long long>(num_sms * C::CTAS, most)));
     cfg.blockDim = dim3(C::THREADS);
     cfg.dynamicSmemBytes = C::BYTES;
     cfg.stream = st;
@@ -862,21 +890,29 @@ cudaError_t launch(const Args& a, int grid, cudaStream_t st) {
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kv4_decode_kernel<D, NT>, a);
+    return cudaLaunchKernelEx(&cfg, kv4_decode_kernel<D, NT, WIDE>, a);
+}
+
+template <int D, int NT, bool WIDE>
+cudaError_t configure() {
+    return cudaFuncSetAttribute(kv4_decode_kernel<D, NT, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                Cfg<D, NT, WIDE>::BYTES);
 }
 
 template <int D, int NT>
-cudaError_t configure() {
-    return cudaFuncSetAttribute(kv4_decode_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D, NT>::BYTES);
+cudaError_t launch_for(const Args& a, int num_sms, cudaStream_t st) {
+    // pieces need a CTA per item
+    const bool wide = a.batch == 1 && a.Hkv * a.ncg <= num_sms;
+    return wide ? launch<D, NT, true>(a, num_sms, st) : launch<D, NT, false>(a, num_sms, st);
 }
 
 }  // namespace
 
 cudaError_t configure_kv4_decode() {
-    cudaError_t e = configure<128, 1>();
-    if (e == cudaSuccess) e = configure<128, 2>();
-    if (e == cudaSuccess) e = configure<64, 1>();
-    if (e == cudaSuccess) e = configure<64, 2>();
+    cudaError_t e = cudaSuccess;
+    for (auto fn : {configure<128, 1, false>, configure<128, 1, true>, configure<128, 2, false>, configure<128, 2, true>,
+                    configure<64, 1, false>, configure<64, 1, true>, configure<64, 2, false>, configure<64, 2, true>})
+        if (e == cudaSuccess) e = fn();
     return e;
 }
 
@@ -902,7 +938,7 @@ cudaError_t launch_kv4_decode(const Shape& s, const uint16_t* q, const uint16_t*
         a.sin_tab = sin_tab;
         a.part_o = part_o;
         a.part_ml = part_ml;
-        a.part_nan = reinterpret_cast<int*>(part_ml + static_cast<size_t>(num_sms) * 2 * 16 * 2);
+        a.part_nan = reinterpret_cast<int*>(part_ml + static_cast<size_t>(num_sms) * 4 * 2 * 16 * 2);
         a.counters = counters;
         a.err = err;
         a.wait_ns = wait_ns;
@@ -914,12 +950,9 @@ cudaError_t launch_kv4_decode(const Shape& s, const uint16_t* q, const uint16_t*
         a.Hkv = s.n_kv_heads;
         a.max_len = s.max_len;
         a.ncg = (cols + 15) / 16;
-        a.min_blocks = 8;
-        const int grid = static_cast<int>(std::min<long long>(
-            num_sms, static_cast<long long>(a.batch) * a.Hkv * a.ncg * ((a.max_len + (D == 128 ? 31 : 63)) / (D == 128 ? 32 : 64))));
-        a.per = grid / (a.Hkv * a.ncg);
-        const cudaError_t e = D == 128 ? (cols <= 8 ? launch<128, 1>(a, grid, st) : launch<128, 2>(a, grid, st))
-                                       : (cols <= 8 ? launch<64, 1>(a, grid, st) : launch<64, 2>(a, grid, st));
+        a.min_blocks = a.batch == 1 ? 8 : 4;
+        const cudaError_t e = D == 128 ? (cols <= 8 ? launch_for<128, 1>(a, num_sms, st) : launch_for<128, 2>(a, num_sms, st))
+                                       : (cols <= 8 ? launch_for<64, 1>(a, num_sms, st) : launch_for<64, 2>(a, num_sms, st));
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
