@@ -102,9 +102,9 @@ __device__ __forceinline__ void mma_first(float (&c)[4], uint32_t a0, uint32_t a
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 
-__device__ __forceinline__ uint32_t fms2(uint32_t a, uint32_t b, uint32_t c) {  // a b - c
+__device__ __forceinline__ uint32_t fma2(uint32_t a, uint32_t b, uint32_t c) {
     uint32_t d;
-    asm("{.reg .b32 n;\n\tneg.bf16x2 n, %3;\n\tfma.rn.bf16x2 %0, %1, %2, n;}" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
     return d;
 }
 __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
@@ -140,14 +140,14 @@ __device__ __forceinline__ Pair pair_of(uint32_t m2) {
     p.zs = mul2(m2 & 0x000F000Fu, p.lo);
     return p;
 }
-// Pair i of a word and of the same word shifted right by 8: c s, and (c - z) s.
+// Pair i of a word and of the same word shifted right by 8: c s, and (c - z) s with p.zs negated.
 __device__ __forceinline__ uint32_t code2(uint32_t w, uint32_t w8, int i, const Pair& p) {
     const uint32_t x = i < 2 ? w : w8;
     return i % 2 == 0 ? mul2(x & 0x000F000Fu, p.lo) : mul2(x & 0x00F000F0u, p.hi);
 }
 __device__ __forceinline__ uint32_t value2(uint32_t w, uint32_t w8, int i, const Pair& p) {
     const uint32_t x = i < 2 ? w : w8;
-    return i % 2 == 0 ? fms2(x & 0x000F000Fu, p.lo, p.zs) : fms2(x & 0x00F000F0u, p.hi, p.zs);
+    return i % 2 == 0 ? fma2(x & 0x000F000Fu, p.lo, p.zs) : fma2(x & 0x00F000F0u, p.hi, p.zs);
 }
 
 __device__ __forceinline__ uint32_t lds32(uint32_t a) {
@@ -439,6 +439,70 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
         return true;
     };
 
+    const int G = a.Hq / a.Hkv;
+    auto columns = [&](Segment& w) {
+        w.head = a.ncg == 1 ? w.item : w.item / a.ncg;
+        w.c0 = a.ncg == 1 ? 0 : (w.item - w.head * a.ncg) * 16;
+        w.ncol = min(16, G * a.ntok - w.c0);
+    };
+    auto token = [&](const Segment& w, int col) { return small_div(w.c0 + col, G); };
+    auto row_of = [&](const Segment& w, int col) {  // of q and out, in rows of D
+        const int i = token(w, col);
+        return (static_cast<size_t>(w.b) * a.ntok + i) * a.Hq + w.head * G + (w.c0 + col - i * G);
+    };
+    // q of an item's columns and its rows of the tables: loaded early, a load waits behind the copies in flight
+    constexpr int QN = (C::COLS * (D / 4) + C::THREADS - 1) / C::THREADS;
+    uint32_t qx[QN], qy[QN];
+    float2 qc[QN], qs[QN];
+    auto load_q = [&](const Segment& w) {
+#pragma unroll
+        for (int i = 0; i < QN; ++i) {
+            const int u = tid + i * C::THREADS, col = u / (D / 4), j = u % (D / 4) * 2;
+            qx[i] = qy[i] = 0;  // columns that do not exist
+            qc[i] = qs[i] = make_float2(0.f, 0.f);
+            if (col < w.ncol) {
+                const uint16_t* src = a.q + row_of(w, col) * D + j;
+                const size_t p = static_cast<size_t>(w.hist + token(w, col)) * (D / 2) + j;
+                qx[i] = __ldg(reinterpret_cast<const uint32_t*>(src));
+                qy[i] = __ldg(reinterpret_cast<const uint32_t*>(src + D / 2));
+                qc[i] = __ldg(reinterpret_cast<const float2*>(a.cos_tab + p));
+                qs[i] = __ldg(reinterpret_cast<const float2*>(a.sin_tab + p));
+            }
+        }
+    };
+    auto store_q = [&]() {  // rotated and rounded to bf16
+#pragma unroll
+        for (int i = 0; i < QN; ++i) {
+            const int u = tid + i * C::THREADS, col = u / (D / 4), j = u % (D / 4) * 2;
+            if (col >= C::COLS) break;
+            const float x0 = __uint_as_float(qx[i] << 16), x1 = __uint_as_float(qx[i] & 0xFFFF0000u);
+            const float y0 = __uint_as_float(qy[i] << 16), y1 = __uint_as_float(qy[i] & 0xFFFF0000u);
+            *reinterpret_cast<uint32_t*>(s_q + col * C::QS + j) =
+                pack2(__fsub_rn(__fmul_rn(x0, qc[i].x), __fmul_rn(y0, qs[i].x)),
+                      __fsub_rn(__fmul_rn(x1, qc[i].y), __fmul_rn(y1, qs[i].y)));
+            *reinterpret_cast<uint32_t*>(s_q + col * C::QS + j + D / 2) =
+                pack2(__fadd_rn(__fmul_rn(y0, qc[i].x), __fmul_rn(x0, qs[i].x)),
+                      __fadd_rn(__fmul_rn(y1, qc[i].y), __fmul_rn(x1, qs[i].y)));
+        }
+    };
+    // One warp: an item's q, table rows and new k and v into L2.
+    auto prefetch = [&](const Segment& w) {
+        constexpr int LINES = D / 64;  // of a row of D bf16 or D / 2 floats
+        auto line = [](const void* p, int i) {
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint8_t*>(p) + 128 * i));
+        };
+        for (int i = lane; i < w.ncol * LINES; i += 32) line(a.q + row_of(w, i / LINES) * D, i % LINES);
+        for (int i = lane; i < a.ntok * 4 * LINES; i += 32) {
+            const int tok = i / (4 * LINES), kind = i / LINES % 4;
+            const size_t row = (static_cast<size_t>(w.b) * a.ntok + tok) * a.Hkv + w.head, p = static_cast<size_t>(w.hist) + tok;
+            if (kind < 2) line((kind == 0 ? a.cos_tab : a.sin_tab) + p * (D / 2), i % LINES);
+            else if (w.hi == w.T) line((kind == 2 ? a.k_new : a.v_new) + row * D, i % LINES);
+        }
+    };
+    columns(first);
+    load_q(first);
+    if (warp == W - 1) prefetch(first);
+
     // The warp's copies run two blocks ahead of it: block blk_next of an item is next, off_next its byte in
     // the codes (an eighth of it: in the scales).
     static_assert(C::STAGES == 2 && C::ROW == 8 * 2 * GR, "stages alternate; codes and scales share an offset");
@@ -475,17 +539,10 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
         off_next += static_cast<size_t>(W) * C::CODES;
     };
     __syncwarp();
-#pragma unroll
-    for (int s = 0; s < C::STAGES; ++s) issue(s_warp + s * C::STAGE, bar0 + 8 * s);
+    issue(s_warp, bar0);
 
     uint32_t st_off = 0, bar_off = 0, phase = 0;  // of the warp's next block
     uint32_t new_phase = 0;
-    const int G = a.Hq / a.Hkv;
-    auto token = [&](const Segment& w, int col) { return small_div(w.c0 + col, G); };
-    auto row_of = [&](const Segment& w, int col) {  // of q and out, in rows of D
-        const int i = token(w, col);
-        return (static_cast<size_t>(w.b) * a.ntok + i) * a.Hq + w.head * G + (w.c0 + col - i * G);
-    };
     // Staged row of new token i, k (0) or v (1): in the O buffer, not yet written, of the warp that has its block.
     auto staged_row = [&](const Segment& w, int i, int kind) {
         const int owner = (((w.hist + i) / KB) - w.lo) % W;
@@ -537,46 +594,21 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
         }
     };
 
-    if (tid == 0) {
-        segs[0] = first;
-        segs[1].b = -1;
-    }
+    if (tid == 0) segs[1].b = -1;
+    Segment w = first;
+    bool first_turn = true;
     for (bool final_turn = false; !final_turn;) {
-        __syncthreads();  // segs[0]; the buffers of the item before are free
-        Segment& now = segs[0];
+        __syncthreads();  // the buffers of the item before are free
+        store_q();
+        if (tid < 4) s_nan[tid] = kNone;
+        if (tid == 0) segs[0] = w;
+        __syncthreads();
+        if (first_turn) {
+            issue(s_warp + C::STAGE, bar0 + 8);
+            first_turn = false;
+        }
+        const Segment& now = segs[0];  // what the walk needs no more is read again after it
         {
-            Segment w = now;
-            w.head = a.ncg == 1 ? w.item : w.item / a.ncg;
-            w.c0 = a.ncg == 1 ? 0 : (w.item - w.head * a.ncg) * 16;
-            w.ncol = min(16, G * a.ntok - w.c0);
-            // q of the columns, rotated and rounded to bf16; columns that do not exist are 0
-            for (int u = tid; u < C::COLS * (D / 4); u += C::THREADS) {
-                const int col = u / (D / 4), j = u % (D / 4) * 2;
-                uint32_t lo = 0, hi = 0;
-                if (col < w.ncol) {
-                    const uint16_t* src = a.q + row_of(w, col) * D + j;
-                    const size_t p = static_cast<size_t>(w.hist + token(w, col)) * (D / 2) + j;
-                    const uint32_t x = __ldg(reinterpret_cast<const uint32_t*>(src));
-                    const uint32_t y = __ldg(reinterpret_cast<const uint32_t*>(src + D / 2));
-                    const float2 cs = __ldg(reinterpret_cast<const float2*>(a.cos_tab + p));
-                    const float2 sn = __ldg(reinterpret_cast<const float2*>(a.sin_tab + p));
-                    const float x0 = __uint_as_float(x << 16), x1 = __uint_as_float(x & 0xFFFF0000u);
-                    const float y0 = __uint_as_float(y << 16), y1 = __uint_as_float(y & 0xFFFF0000u);
-                    lo = pack2(__fsub_rn(__fmul_rn(x0, cs.x), __fmul_rn(y0, sn.x)),
-                               __fsub_rn(__fmul_rn(x1, cs.y), __fmul_rn(y1, sn.y)));
-                    hi = pack2(__fadd_rn(__fmul_rn(y0, cs.x), __fmul_rn(x0, sn.x)),
-                               __fadd_rn(__fmul_rn(y1, cs.y), __fmul_rn(x1, sn.y)));
-                }
-                *reinterpret_cast<uint32_t*>(s_q + col * C::QS + j) = lo;
-                *reinterpret_cast<uint32_t*>(s_q + col * C::QS + j + D / 2) = hi;
-            }
-            if (tid < 4) s_nan[tid] = kNone;
-            __syncthreads();
-            if (tid == 0) {
-                now.head = w.head;
-                now.c0 = w.c0;
-                now.ncol = w.ncol;
-            }
             // the new tokens whose slots lie in the segment's blocks, a warp per row of k or v
             const int new0 = max(w.hist, w.lo * KB), new1 = min(w.hist + a.ntok, w.hi * KB);
             if (new0 < new1) {
@@ -604,6 +636,11 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(new_full);
+            }
+            if (warp == 0 && following(w.b, w.item, w.T, w.base, w.hi)) {
+                w.hist = a.d_hist[w.b];
+                columns(w);
+                prefetch(w);
             }
         }
         const int hist = now.hist, hi = now.hi;
@@ -764,8 +801,9 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
                             if (row > last || (sc[e] == kKv4NanScale && k0 + row > hist)) sc[e] = 0;
                         }
                     }
-                    const Pair p01 = pair_of(__byte_perm(sc[0], sc[1], 0x5410)),
-                               p23 = pair_of(__byte_perm(sc[2], sc[3], 0x5410));
+                    Pair p01 = pair_of(__byte_perm(sc[0], sc[1], 0x5410)), p23 = pair_of(__byte_perm(sc[2], sc[3], 0x5410));
+                    p01.zs ^= 0x80008000u;
+                    p23.zs ^= 0x80008000u;
 #pragma unroll
                     for (int n = 0; n < NT; ++n) mma(sum[n], kOnes, kOnes, kOnes, kOnes, pb[n][2 * k], pb[n][2 * k + 1]);
 #pragma unroll
@@ -807,6 +845,14 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
                 }
                 if (g == 0) s_ml[col] = make_float2(m[n][e] * a.scale_log2, sum[n][e]);
             }
+        w = now;
+        final_turn = !following(w.b, w.item, w.T, w.base, w.hi);
+        if (!final_turn) {
+            w.lo = 0;
+            w.hist = a.d_hist[w.b];
+            columns(w);
+            load_q(w);
+        }
         __syncthreads();
         if (max(hist, now.lo * KB) < min(hist + a.ntok, hi * KB)) new_phase ^= 1u;
         const int j0 = WIDE ? cta - now.base : cta_of(now.base);  // the CTAs that share the item
@@ -846,28 +892,30 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
             }
         }
         if (j0 != j1 && tid < 4) a.part_nan[4 * part + tid] = s_nan[tid];
-        int b = now.b, item = now.item, T = now.T, at = now.base, hi_after;
-        final_turn = !following(b, item, T, at, hi_after);
-        __syncthreads();  // the part is complete
-        if (tid == 0) {
-            if (j0 != j1) {
-                __threadfence();  // the CTA's part, and then its count
-                flag[final_turn] = atomicAdd(a.counters + static_cast<size_t>(now.b) * hc + now.item, 1) == j1 - j0;
-                __threadfence();  // the count, and then the others' parts
-                if (!final_turn) segs[1] = now;  // an item that began in an earlier CTA: looked at again at the end
-            }
-            if (!final_turn) now = Segment{b, item, 0, T, a.d_hist[b], 0, 0, 0, hi_after, at};
+        if (!final_turn) {
+            // a part of an item that began in an earlier CTA is counted at the end: a fence here would hold up the walk
+            if (tid == 0 && j0 != j1) segs[1] = now;
+            continue;
         }
-        if (final_turn) {
+        __syncthreads();  // the CTA's parts are complete
+        const Segment& held = segs[1];
+        if (j0 == j1 && held.b < 0) break;
+        if (tid == 0) {
+            auto last = [&](const Segment& x, int parts) {
+                return atomicAdd(a.counters + static_cast<size_t>(x.b) * hc + x.item, 1) == parts - 1;
+            };
+            __threadfence();  // the parts, and then their counts
+            flag[0] = held.b >= 0 && last(held, cta_of(held.base + held.T - 1) - cta_of(held.base) + 1);
+            flag[1] = j0 != j1 && last(now, j1 - j0 + 1);
+            __threadfence();  // the counts, and then the others' parts
+        }
+        __syncthreads();
+        if (flag[1]) merge(now, j0, j1);
+        if (flag[0]) {
             __syncthreads();
-            if (j0 != j1 && flag[1]) merge(now, j0, j1);
-            const Segment& held = segs[1];
-            if (held.b >= 0 && flag[0]) {
-                __syncthreads();
-                if (tid < 4) s_nan[tid] = kNone;
-                __syncthreads();
-                merge(held, cta_of(held.base), cta_of(held.base + held.T - 1));
-            }
+            if (tid < 4) s_nan[tid] = kNone;
+            __syncthreads();
+            merge(held, cta_of(held.base), cta_of(held.base + held.T - 1));
         }
     }
     if (dead) {  // copies still in flight land before the shared memory is given up
