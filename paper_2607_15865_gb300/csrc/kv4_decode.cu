@@ -8,9 +8,9 @@
 //   several          the blocks of all items, in order, in equal runs, whatever the lengths: each item counts
 //                    kItemCost blocks more than it has, for what it costs to begin and to end one.  CTAs of
 //                    four warps, several per SM: while one begins or ends an item the others walk
-// Within a CTA the warps take an item's blocks in turn, each through a private ring of bulk copies with one
-// mbarrier per stage and with its own running maximum, sum and accumulators; they meet once per item, in shared
-// memory.  An item that several CTAs share is merged by the last of them to finish, in a fixed order.
+// Within a CTA the warps take an item's blocks in turn, each through a private ring of two stages, filled by
+// cp.async (ten 16-byte copies per lane; as four bulk copies and an mbarrier a block cost 50 instructions
+// more), and with its own running maximum, sum and accumulators; they meet once per item, in shared memory.  An item that several CTAs share is merged by the last of them to finish, in a fixed order.
 //
 // Per 16 slots, with mma.sync m16n8k16 (A from registers: a tcgen05 operand would have to be written
 // back to shared or tensor memory at four times the packed bytes, for products 8 or 16 columns wide):
@@ -35,8 +35,8 @@
 // blocks, writes them to the cache and stages them for the warp that has their block.  Slots past the last
 // one are masked by position and by a scale of 0; a NaN group of a new token's v counts from that token on, so its
 // scale is taken as 0 too and the columns that see it are set to NaN when they are written.
-// Every wait is bounded: on expiry a warp records kDevErrTimeout, issues and computes nothing more, lets its
-// copies land and takes part in the barriers and counts.
+// The only wait on other warps that is not a barrier, for the staged rows, is bounded: on expiry the warp records
+// kDevErrTimeout and goes on with what it has.
 #include <algorithm>
 #include <cmath>
 
@@ -76,8 +76,8 @@ struct Cfg {
     static constexpr int OFF_ML = OFF_O + W * O_BYTES;          // float [W][COLS][2]
     static constexpr int OFF_Q = OFF_ML + W * COLS * 8;         // bf16 [COLS][QS]
     static constexpr int OFF_PRE = OFF_Q + COLS * QS * 2;       // int [kMaxSeqs + 1]: blocks and costs before a sequence
-    static constexpr int OFF_BAR = (OFF_PRE + (kMaxSeqs + 1) * 4 + 7) & ~7;  // rings, then the staged rows
-    static constexpr int OFF_NAN = OFF_BAR + (W * STAGES + 1) * 8;  // int [4]: first new token with a NaN group of v
+    static constexpr int OFF_BAR = (OFF_PRE + (kMaxSeqs + 1) * 4 + 7) & ~7;  // mbarrier: the staged rows
+    static constexpr int OFF_NAN = OFF_BAR + 8;                 // int [4]: first new token with a NaN group of v
     static constexpr int OFF_FLAG = OFF_NAN + 16;               // int [2]: whether this CTA merges its first, its last item
     static constexpr int OFF_SEG = OFF_FLAG + 8;                // Segment [2]: of this turn, and a held one
     static constexpr int BYTES = OFF_SEG + 2 * 40;
@@ -174,6 +174,9 @@ __device__ __forceinline__ void lds(uint32_t a, uint32_t (&v)[N]) {
         v[0] = lds32(a);
 }
 
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ uint32_t transpose8(uint32_t a) {
     uint32_t d;
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
@@ -347,12 +350,9 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
     float2* s_ml = reinterpret_cast<float2*>(smem + C::OFF_ML);
     Segment* segs = reinterpret_cast<Segment*>(smem + C::OFF_SEG);
     static_assert(sizeof(Segment) == 40, "shared memory");
-    const uint32_t bar0 = base + C::OFF_BAR + 8u * static_cast<uint32_t>(warp * C::STAGES);
-    const uint32_t new_full = base + C::OFF_BAR + 8u * (W * C::STAGES);
-    if (lane == 0) {
-#pragma unroll
-        for (int s = 0; s < C::STAGES; ++s) mbar_init(bar0 + 8 * s, 1);
-        if (warp == 0) mbar_init(new_full, W);
+    const uint32_t new_full = base + C::OFF_BAR;
+    if (tid == 0) {
+        mbar_init(new_full, W);
         fence_mbar_init();
     }
     griddep_wait();
@@ -504,44 +504,45 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
     if (warp == W - 1) prefetch(first);
 
     // The warp's copies run two blocks ahead of it: block blk_next of an item is next, off_next its byte in
-    // the codes (an eighth of it: in the scales).
+    // the codes (an eighth of it: in the scales).  A group of copies is committed for every block, or an empty one.
     static_assert(C::STAGES == 2 && C::ROW == 8 * 2 * GR, "stages alternate; codes and scales share an offset");
     const uint32_t s_warp = base + static_cast<uint32_t>(warp * C::STAGES * C::STAGE);
     int b_next = first.b, item_next = first.item, T_next = first.T, base_next = first.base, hi_next = first.hi;
-    int blk_next = first.lo + warp, pending = 0;
+    int blk_next = first.lo + warp;
     size_t off_next = 0;
-    bool placed = false, ended = false, dead = false;
-    auto issue = [&](uint32_t stage, uint32_t barrier) {
-        if (ended) return;
-        while (blk_next >= hi_next) {
-            if (!following(b_next, item_next, T_next, base_next, hi_next)) {
-                ended = true;
-                return;
-            }
+    bool placed = false, ended = false;
+    auto issue = [&](uint32_t stage) {
+        while (!ended && blk_next >= hi_next) {
+            if (!following(b_next, item_next, T_next, base_next, hi_next)) ended = true;
             blk_next = warp;
             placed = false;
         }
-        if (!placed) {
-            const int head = a.ncg == 1 ? item_next : item_next / a.ncg;
-            off_next = ((static_cast<size_t>(b_next) * a.Hkv + head) * a.lp + static_cast<size_t>(blk_next) * KB) * C::ROW;
-            placed = true;
+        if (!ended) {
+            if (!placed) {
+                const int head = a.ncg == 1 ? item_next : item_next / a.ncg;
+                off_next = ((static_cast<size_t>(b_next) * a.Hkv + head) * a.lp + static_cast<size_t>(blk_next) * KB) * C::ROW +
+                           16 * lane;
+                placed = true;
+            }
+            const uint32_t dst = stage + 16 * lane;
+            const uint8_t* k = a.c.k_codes + off_next;
+            const uint8_t* v = a.c.v_codes + off_next;
+#pragma unroll
+            for (int i = 0; i < C::CODES; i += 512) {
+                copy16(dst + i, k + i);
+                copy16(dst + C::CODES + i, v + i);
+            }
+            // half the lanes the scales of k, half those of v
+            const size_t at = ((off_next - 16 * lane) >> 3) + 16 * (lane & 15);
+            copy16(dst + 2 * C::CODES, reinterpret_cast<const uint8_t*>(lane < 16 ? a.c.k_scales : a.c.v_scales) + at);
+            blk_next += W;
+            off_next += static_cast<size_t>(W) * C::CODES;
         }
-        if (lane == 0) {
-            mbar_arrive_expect_tx(barrier, C::STAGE);
-            bulk_g2s(stage, a.c.k_codes + off_next, C::CODES, barrier);
-            bulk_g2s(stage + 2 * C::CODES, reinterpret_cast<const uint8_t*>(a.c.k_scales) + (off_next >> 3), C::SCALES, barrier);
-            bulk_g2s(stage + C::CODES, a.c.v_codes + off_next, C::CODES, barrier);
-            bulk_g2s(stage + 2 * C::CODES + C::SCALES, reinterpret_cast<const uint8_t*>(a.c.v_scales) + (off_next >> 3),
-                     C::SCALES, barrier);
-        }
-        ++pending;
-        blk_next += W;
-        off_next += static_cast<size_t>(W) * C::CODES;
+        asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    __syncwarp();
-    issue(s_warp, bar0);
+    issue(s_warp);
 
-    uint32_t st_off = 0, bar_off = 0, phase = 0;  // of the warp's next block
+    uint32_t st_off = 0;  // of the warp's next block
     uint32_t new_phase = 0;
     // Staged row of new token i, k (0) or v (1): in the O buffer, not yet written, of the warp that has its block.
     auto staged_row = [&](const Segment& w, int i, int kind) {
@@ -604,7 +605,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
         if (tid == 0) segs[0] = w;
         __syncthreads();
         if (first_turn) {
-            issue(s_warp + C::STAGE, bar0 + 8);
+            issue(s_warp + C::STAGE);
             first_turn = false;
         }
         const Segment& now = segs[0];  // what the walk needs no more is read again after it
@@ -679,23 +680,16 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
             }
 
         int blk = now.lo + warp;
-        const bool has_blocks = !dead && blk < hi;
-        for (; !dead && blk < hi; blk += W) {
+        const bool has_blocks = blk < hi;
+        for (; blk < hi; blk += W) {
             const int k0 = blk * KB;
-            const uint32_t s_k = s_warp + st_off, full = bar0 + bar_off;
+            const uint32_t s_k = s_warp + st_off;
             const uint32_t s_v = s_k + C::CODES, s_ks = s_v + C::CODES, s_vs = s_ks + C::SCALES;
-            if (!__all_sync(0xFFFFFFFFu, mbar_wait(full, phase, nullptr, a.wait_ns))) {
-                if (lane == 0) record_dev_err(a.err, kDevErrTimeout);
-                dead = true;
-                break;
-            }
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+            __syncwarp();
             const bool tail = k0 + KB > hist;  // the block holds slots of new tokens, or none at all
             if (tail) {  // the staged rows into the block
-                if (!__all_sync(0xFFFFFFFFu, mbar_wait(new_full, new_phase, nullptr))) {
-                    if (lane == 0) record_dev_err(a.err, kDevErrTimeout);
-                    dead = true;
-                    break;
-                }
+                if (!mbar_wait(new_full, new_phase, nullptr, a.wait_ns)) record_dev_err(a.err, kDevErrTimeout);
                 const int lo = max(k0, hist), hi = min(k0 + KB, hist + a.ntok);
                 for (int p = lo; p < hi; ++p)
 #pragma unroll
@@ -821,13 +815,9 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
                     }
                 }
             }
-            if (tail) fence_proxy_async_smem();  // this warp wrote to the stage that the next copy fills
             __syncwarp();
-            --pending;
-            issue(s_k, full);
+            issue(s_k);
             st_off = C::STAGE - st_off;
-            phase ^= bar_off >> 3;
-            bar_off ^= 8u;
         }
 
         // The warps' parts meet.  Lane (g, t) holds columns 2 t, 2 t + 1 (+ 8 n) of values D/8 g .. D/8 g + D/8 - 1.
@@ -917,10 +907,6 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
             __syncthreads();
             merge(held, cta_of(held.base), cta_of(held.base + held.T - 1));
         }
-    }
-    if (dead) {  // copies still in flight land before the shared memory is given up
-        if (pending > 0) mbar_wait(bar0 + bar_off, phase, nullptr);
-        if (pending > 1) mbar_wait(bar0 + (bar_off ^ 8u), phase ^ (bar_off >> 3), nullptr);
     }
 }
 
