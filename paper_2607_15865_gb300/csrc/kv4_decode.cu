@@ -3,9 +3,10 @@
 //
 // A (sequence, kv head) has G query heads x ntok new tokens = columns, taken 16 at a time (an item).
 // An item's slots are cut into blocks of 32 (head_dim 128) or 64 slots; the lengths are read on the device.
-//   one sequence     each item's blocks in equal pieces, one per CTA, as many as the SMs allow: CTAs of all
-//                    the warps that an SM's registers hold, so that an item has few parts to merge
-//   several          the blocks of all items, in order, in equal runs, whatever the lengths: each item counts
+//   few items        (up to half the SMs) each item's blocks in equal pieces, one per CTA, as many as the SMs allow and
+//                    in proportion to the lengths: CTAs of all the warps that an SM's registers hold, so that
+//                    an item has few parts to merge
+//   many             the blocks of all items, in order, in equal runs, whatever the lengths: each item counts
 //                    kItemCost blocks more than it has, for what it costs to begin and to end one.  CTAs of
 //                    four warps, several per SM: while one begins or ends an item the others walk
 // Within a CTA the warps take an item's blocks in turn, each through a private ring of two stages, filled by
@@ -50,7 +51,6 @@ namespace {
 constexpr int kMaxSeqs = 128;   // sequences of one launch (their block counts are summed in shared memory)
 constexpr int kItemCost = 16;    // blocks
 constexpr int kMaxNew = 16;     // new tokens per sequence
-constexpr int kBatch = 8;       // parts of an item that a merging thread loads at once
 constexpr int kNone = 1 << 20;  // no new token with a NaN group
 
 template <int D_, int NT_, bool WIDE_>
@@ -60,6 +60,7 @@ struct Cfg {
     static constexpr int W = !WIDE ? 4 : NT == 1 ? 16 : 8;  // warps
     static constexpr int CTAS = WIDE ? 1 : NT == 1 ? 4 : D == 128 ? 2 : 3;  // per SM: what registers and shared memory allow
     static constexpr int THREADS = 32 * W;
+    static constexpr int BATCH = NT == 1 ? 8 : WIDE ? 20 : D == 128 ? 16 : 12;  // parts that a merging thread loads at once
     static constexpr int KB = 32 * 128 / D;      // slots per block
     static constexpr int ROW = D / 2;            // bytes of a slot's codes
     static constexpr int GR = D / kKv4Group;     // groups
@@ -76,7 +77,8 @@ struct Cfg {
     static constexpr int OFF_ML = OFF_O + W * O_BYTES;          // float [W][COLS][2]
     static constexpr int OFF_Q = OFF_ML + W * COLS * 8;         // bf16 [COLS][QS]
     static constexpr int OFF_PRE = OFF_Q + COLS * QS * 2;       // int [kMaxSeqs + 1]: blocks and costs before a sequence
-    static constexpr int OFF_BAR = (OFF_PRE + (kMaxSeqs + 1) * 4 + 7) & ~7;  // mbarrier: the staged rows
+    static constexpr int OFF_FREE = OFF_PRE + (kMaxSeqs + 1) * 4;  // uint8 [kMaxSeqs]: slots of the last block past the last token
+    static constexpr int OFF_BAR = (OFF_FREE + kMaxSeqs + 7) & ~7;  // mbarrier: the staged rows
     static constexpr int OFF_NAN = OFF_BAR + 8;                 // int [4]: first new token with a NaN group of v
     static constexpr int OFF_FLAG = OFF_NAN + 16;               // int [2]: whether this CTA merges its first, its last item
     static constexpr int OFF_SEG = OFF_FLAG + 8;                // Segment [2]: of this turn, and a held one
@@ -289,6 +291,41 @@ __device__ __forceinline__ int small_div(int x, int y) {
 }
 __device__ __forceinline__ int small_ceil_div(int x, int y) { return small_div(x - 1, y) + 1; }  // x > 0
 
+// One warp: piece `cta` where the items of up to 32 sequences are cut into pieces of at most `target` blocks, with the
+// least target (of 32 tried) for which the pieces are at most per for each of the hc items of a sequence.  Lane b
+// holds the blocks T of an item of sequence b (0: skipped).  The item's block 0 .. : T, hist, lo, hi; base:
+// the piece, c0: the pieces of the item (0: there is no piece `cta`).
+__device__ __forceinline__ Segment piece_of(int T, int hist, int hc, int per, int min_blocks, int cta, int lane) {
+    Segment w = {};
+    const uint32_t live = __ballot_sync(0xFFFFFFFFu, T > 0);
+    const int items = __popc(live), sum = __reduce_add_sync(0xFFFFFFFFu, T), longest = __reduce_max_sync(0xFFFFFFFFu, T);
+    if (items == 0) return w;
+    int target = max(min_blocks, small_ceil_div(longest, small_div(per, items)));  // fits
+    if (longest * items != sum) {
+        const int least = max(min_blocks, (sum + per - 1) / per);  // no less fits
+        const int mine = least + (((target - least) * lane) >> 5);
+        int pieces = 0;
+        for (uint32_t rest = live; rest != 0; rest &= rest - 1)
+            pieces += small_ceil_div(__shfl_sync(0xFFFFFFFFu, T, __ffs(rest) - 1), mine);
+        const uint32_t fits = __ballot_sync(0xFFFFFFFFu, pieces <= per);
+        if (fits != 0) target = __shfl_sync(0xFFFFFFFFu, mine, __ffs(fits) - 1);
+    }
+    const int n = T > 0 ? small_ceil_div(T, target) : 0, upto = warp_scan(n, lane);
+    const uint32_t past = __ballot_sync(0xFFFFFFFFu, T > 0 && upto * hc > cta);
+    if (past == 0) return w;
+    w.b = __ffs(past) - 1;
+    w.T = __shfl_sync(0xFFFFFFFFu, T, w.b);
+    w.hist = __shfl_sync(0xFFFFFFFFu, hist, w.b);
+    w.c0 = __shfl_sync(0xFFFFFFFFu, n, w.b);
+    const int rem = cta - __shfl_sync(0xFFFFFFFFu, upto - n, w.b) * hc;
+    w.item = small_div(rem, w.c0);
+    w.base = rem - w.item * w.c0;
+    const int whole = small_div(w.T, w.c0), more = w.T - whole * w.c0;
+    w.lo = w.base * whole + min(w.base, more);
+    w.hi = w.lo + whole + (w.base < more ? 1 : 0);
+    return w;
+}
+
 // The first b with sums[b + 1] * hc > r.
 __device__ __forceinline__ int search(const int* sums, int batch, int hc, int r) {
     int lo = 0, hi = batch - 1;
@@ -343,6 +380,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
     const uint32_t base = smem_u32(smem);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     int* pre = reinterpret_cast<int*>(smem + C::OFF_PRE);
+    uint8_t* s_free = smem + C::OFF_FREE;
     int* s_nan = reinterpret_cast<int*>(smem + C::OFF_NAN);
     int* flag = reinterpret_cast<int*>(smem + C::OFF_FLAG);
     uint16_t* s_q = reinterpret_cast<uint16_t*>(smem + C::OFF_Q);
@@ -370,8 +408,20 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
     };
     Segment first;
     int stop = 0, each = 0, more = 0;  // runs: CTA j has each blocks, the first `more` one more
-    int n = 0;                         // pieces of an item, 0 for runs
-    if (WIDE) {
+    int n = 0;                         // pieces of an item
+    auto hist_of = [&](int b, int T) { return T * KB - s_free[b] - a.ntok; };
+    if (WIDE && a.batch > 1) {
+        if (warp == 0) {
+            int h = 0;
+            const int T = lane < a.batch ? blocks_of(lane, h) : 0;
+            first = piece_of(T, h, hc, static_cast<int>(gridDim.x) / hc, a.min_blocks, cta, lane);
+            if (lane == 0) segs[0] = first;
+        }
+        __syncthreads();
+        first = segs[0];
+        n = first.c0;
+        if (n == 0) return;
+    } else if (WIDE) {
         const int T = blocks_of(0, first.hist), per = static_cast<int>(gridDim.x) / hc;
         if (T == 0) return;
         n = small_ceil_div(T, max(a.min_blocks, small_ceil_div(T, per)));
@@ -384,19 +434,21 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
         first.hi = first.lo + whole + (piece < rest ? 1 : 0);
         first.base = piece;
     } else {
-        auto cost = [](int T) { return T > 0 ? T + kItemCost : 0; };
+        auto cost_of = [&](int b) {  // with s_free
+            int h;
+            const int T = blocks_of(b, h);
+            s_free[b] = static_cast<uint8_t>(T * KB - h - a.ntok);
+            return T > 0 ? T + kItemCost : 0;
+        };
         if (a.batch > 32) {
-            for (int b = tid; b < a.batch; b += C::THREADS) {
-                int h;
-                pre[b + 1] = cost(blocks_of(b, h));
-            }
+            for (int b = tid; b < a.batch; b += C::THREADS) pre[b + 1] = cost_of(b);
             __syncthreads();
         }
         if (warp == 0) {
             int sum = 0;
             for (int b0 = 0; b0 < a.batch; b0 += 32) {
-                int h, v = 0;
-                if (b0 + lane < a.batch) v = a.batch > 32 ? pre[b0 + lane + 1] : cost(blocks_of(lane, h));
+                int v = 0;
+                if (b0 + lane < a.batch) v = a.batch > 32 ? pre[b0 + lane + 1] : cost_of(lane);
                 v = warp_scan(v, lane);
                 if (b0 + lane < a.batch) pre[b0 + lane + 1] = sum + v;
                 sum += __shfl_sync(0xFFFFFFFFu, v, 31);
@@ -419,7 +471,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
         first.lo = max(0, r0 - first.base);
         first.hi = min(first.T, stop - first.base);
         if (first.lo >= first.hi) return;  // the run ends in what the item counts beside its blocks
-        first.hist = a.d_hist[first.b];
+        first.hist = hist_of(first.b, first.T);
     }
     auto cta_of = [&](int r) {  // whose run has block r
         const int cut = more * (each + 1);
@@ -499,6 +551,8 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
             else if (w.hi == w.T) line((kind == 2 ? a.k_new : a.v_new) + row * D, i % LINES);
         }
     };
+    auto new_from = [&](const Segment& w) { return max(w.hist, w.lo * KB); };  // positions of the new tokens in its blocks
+    auto new_to = [&](const Segment& w) { return min(w.hist + a.ntok, w.hi * KB); };
     columns(first);
     load_q(first);
     if (warp == W - 1) prefetch(first);
@@ -562,11 +616,11 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
             int nan = kNone;
             if (sub < subs && u < vals)
 #pragma unroll 1
-                for (int j = j0 + sub; j <= j1; j += kBatch * subs) {
-                    float2 ml[kBatch];
-                    float4 x[kBatch];
+                for (int j = j0 + sub; j <= j1; j += C::BATCH * subs) {
+                    float2 ml[C::BATCH];
+                    float4 x[C::BATCH];
 #pragma unroll
-                    for (int i = 0; i < kBatch; ++i) {
+                    for (int i = 0; i < C::BATCH; ++i) {
                         const int from = min(j + i * subs, j1), row = (2 * from + (from == j0 ? 1 : 0)) * 16 + col;
                         ml[i] = __ldcg(reinterpret_cast<const float2*>(a.part_ml) + row);
                         x[i] = __ldcg(reinterpret_cast<const float4*>(a.part_o + static_cast<size_t>(row) * D + d));
@@ -604,14 +658,11 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
         if (tid < 4) s_nan[tid] = kNone;
         if (tid == 0) segs[0] = w;
         __syncthreads();
-        if (first_turn) {
-            issue(s_warp + C::STAGE);
-            first_turn = false;
-        }
+        if (first_turn) issue(s_warp + C::STAGE);
         const Segment& now = segs[0];  // what the walk needs no more is read again after it
         {
             // the new tokens whose slots lie in the segment's blocks, a warp per row of k or v
-            const int new0 = max(w.hist, w.lo * KB), new1 = min(w.hist + a.ntok, w.hi * KB);
+            const int new0 = new_from(w), new1 = new_to(w);
             if (new0 < new1) {
                 for (int u = W - 1 - warp; u < 2 * (new1 - new0); u += W) {
                     const int p = new0 + u / 2, i = p - w.hist;
@@ -638,8 +689,9 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
                 __syncwarp();
                 if (lane == 0) mbar_arrive(new_full);
             }
+            first_turn = false;
             if (warp == 0 && following(w.b, w.item, w.T, w.base, w.hi)) {
-                w.hist = a.d_hist[w.b];
+                w.hist = hist_of(w.b, w.T);
                 columns(w);
                 prefetch(w);
             }
@@ -839,12 +891,12 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
         final_turn = !following(w.b, w.item, w.T, w.base, w.hi);
         if (!final_turn) {
             w.lo = 0;
-            w.hist = a.d_hist[w.b];
+            w.hist = hist_of(w.b, w.T);
             columns(w);
             load_q(w);
         }
         __syncthreads();
-        if (max(hist, now.lo * KB) < min(hist + a.ntok, hi * KB)) new_phase ^= 1u;
+        if (new_from(now) < new_to(now)) new_phase ^= 1u;
         const int j0 = WIDE ? cta - now.base : cta_of(now.base);  // the CTAs that share the item
         const int j1 = WIDE ? j0 + n - 1 : cta_of(now.base + now.T - 1);
         const int part = 2 * cta + (cta == j0 ? 1 : 0);
@@ -933,10 +985,14 @@ cudaError_t configure() {
                                 Cfg<D, NT, WIDE>::BYTES);
 }
 
+// Pieces or runs.  Calls in a graph, 4 query heads per kv head, histories of 8000, pieces against runs: 8 items 9.1
+// and 14.8 us, 32 15.0 and 16.7, 64 21.9 and 23.7, 128 32.9 and 36.3; with mixed lengths up to 8000, which pieces
+// of whole blocks divide worse the fewer there are per item, 64 16.7 and 17.0, 128 28.3 and 24.1.
+bool is_wide(const Args& a, int num_sms) { return a.batch <= 32 && 2 * a.batch * a.Hkv * a.ncg <= num_sms; }
+
 template <int D, int NT>
 cudaError_t launch_for(const Args& a, int num_sms, cudaStream_t st) {
-    // pieces need a CTA per item
-    const bool wide = a.batch == 1 && a.Hkv * a.ncg <= num_sms;
+    const bool wide = is_wide(a, num_sms);
     return wide ? launch<D, NT, true>(a, num_sms, st) : launch<D, NT, false>(a, num_sms, st);
 }
 
@@ -984,7 +1040,7 @@ cudaError_t launch_kv4_decode(const Shape& s, const uint16_t* q, const uint16_t*
         a.Hkv = s.n_kv_heads;
         a.max_len = s.max_len;
         a.ncg = (cols + 15) / 16;
-        a.min_blocks = a.batch == 1 ? 8 : 4;
+        a.min_blocks = is_wide(a, num_sms) ? 8 : 4;
         const cudaError_t e = D == 128 ? (cols <= 8 ? launch_for<128, 1>(a, num_sms, st) : launch_for<128, 2>(a, num_sms, st))
                                        : (cols <= 8 ? launch_for<64, 1>(a, num_sms, st) : launch_for<64, 2>(a, num_sms, st));
         if (e != cudaSuccess) return e;
