@@ -285,10 +285,15 @@ class Attention:
         ks = (self.batch, n, self.n_kv_heads, self.head_dim)
         if not _is_len(hist_len, self.batch):
             raise TypeError("hist_len must be a contiguous int32 CUDA tensor of shape [batch]")
-        out = self._new_out(q, out)
-        rc = self.lib.attn_kv4_decode(self._ctx, _ptr(q, "q", qs), _ptr(k, "k", ks), _ptr(v, "v", ks),
-                                      hist_len.data_ptr(), n, self._kv4(cache), _ptr(out, "out", qs), _stream(stream))
-        self._check(rc, "attn_kv4_decode")
+        args = _ptr(q, "q", qs), _ptr(k, "k", ks), _ptr(v, "v", ks)
+        if out is None:
+            out = torch.empty_like(q)
+            o = out.data_ptr()
+        else:
+            o = _ptr(out, "out", qs)
+        rc = self.lib.attn_kv4_decode(self._ctx, *args, hist_len.data_ptr(), n, self._kv4(cache), o, _stream(stream))
+        if rc:
+            self._check(rc, "attn_kv4_decode")
         return out
 
     def kv4_workspace(self, tokens: int) -> int:

@@ -718,9 +718,9 @@ int attn_kv4_append(attn_ctx* c, const uint16_t* k, const uint16_t* v, int hist_
     if (c == nullptr || k == nullptr || v == nullptr || !kv4_ok(cache) || !aligned16(k) || !aligned16(v))
         return ATTN_EINVAL;
     if (chunk_len < 1 || hist_len < 0 || static_cast<long>(hist_len) + chunk_len > c->cfg.max_len) return ATTN_EINVAL;
-    const attn::Kv4New a{k, v, nullptr, hist_len, chunk_len, c->cfg.batch};
+    const attn::Kv4New a{k, v, hist_len, chunk_len, c->cfg.batch};
     const cudaError_t e = attn::launch_kv4_append(c->shape, a, c->d_cos, c->d_sin, kv4_of(cache),
-                                                  attn::Kv4Plain{nullptr, nullptr, 0}, c->d_err,
+                                                  attn::Kv4Plain{nullptr, nullptr, 0},
                                                   reinterpret_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? ATTN_OK : cuda_fail(e, "kv4 append launch");
 }
@@ -774,9 +774,9 @@ int attn_kv4_prefill_kv(attn_ctx* c, const uint16_t* q, const uint16_t* k, const
     const int rc = flash_maps(c, q, hist_len, chunk_len, chunk_len, kp, vp, tokens, &maps);
     if (rc != ATTN_OK) return rc;
     const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    const attn::Kv4New a{k, v, nullptr, hist_len, chunk_len, c->cfg.batch};
+    const attn::Kv4New a{k, v, hist_len, chunk_len, c->cfg.batch};
     const cudaError_t e = attn::launch_kv4_append(c->shape, a, c->d_cos, c->d_sin, kv4_of(cache),
-                                                  attn::Kv4Plain{kp, vp, tokens}, c->d_err, st);
+                                                  attn::Kv4Plain{kp, vp, tokens}, st);
     if (e != cudaSuccess) return cuda_fail(e, "kv4 append launch");
     return run_flash(c, maps, hist_len, chunk_len, chunk_len, out, st);
 }

@@ -133,12 +133,10 @@ struct Kv4Cache {
     uint8_t* v_codes;
     uint16_t* v_scales;
 };
-// New tokens of the cache: k and v [batch][chunk][Hkv][D] for slots hist .. hist + chunk - 1, hist read from
-// d_hist[b] where that is not null (a sequence it puts outside the cache is flagged and skipped).
+// New tokens of the cache: k and v [batch][chunk][Hkv][D] for slots hist .. hist + chunk - 1.
 struct Kv4New {
     const uint16_t* k;
     const uint16_t* v;
-    const int32_t* d_hist;
     int hist, chunk, batch;
 };
 // bf16 rows that the cache's values go to: [B * Hkv][rows][D].
@@ -149,7 +147,7 @@ struct Kv4Plain {
 };
 // Appends the new tokens; with plain.k also writes slots [0, hist + chunk) as bf16 there (row p: slot p).
 cudaError_t launch_kv4_append(const Shape& s, const Kv4New& a, const float* cos_tab, const float* sin_tab,
-                              const Kv4Cache& c, const Kv4Plain& plain, int* err, cudaStream_t st);
+                              const Kv4Cache& c, const Kv4Plain& plain, cudaStream_t st);
 // Slots first .. first + count - 1 as bf16 (row i: slot first + i).
 cudaError_t launch_kv4_read(const Shape& s, int first, int count, const Kv4Cache& c, const Kv4Plain& plain,
                             cudaStream_t st);

@@ -26,17 +26,36 @@ constexpr int kKv4Group = 32;
 constexpr uint32_t kKv4ScaleMask = 0x7FF0u, kKv4NanScale = 0x7FF0u;
 
 #ifdef __CUDACC__
-__device__ __forceinline__ float kv4_scale(uint32_t m) { return __uint_as_float((m & kKv4ScaleMask) << 16); }
+__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t sub2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+// The larger of each pair, NaN where either is.
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    uint32_t d;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// Eight values of a word as four bf16 pairs (values 2i and 2i + 1 in the halves of out[i]).
+// Eight values of a word as four bf16 pairs (values 2i and 2i + 1 in the halves of out[i]): 128 + c less 128 + z,
+// times s, all of it exact.
 __device__ __forceinline__ void kv4_values(uint32_t w, uint32_t m, uint32_t (&out)[4]) {
-    const float s = kv4_scale(m), z = static_cast<float>(m & 15u);
+    const uint32_t m2 = m * 0x10001u, s = m2 & 0x7FF07FF0u, z = (m2 & 0x000F000Fu) | 0x43004300u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float lo = static_cast<float>((w >> (4 * i)) & 15u), hi = static_cast<float>((w >> (16 + 4 * i)) & 15u);
-        const __nv_bfloat162 p = __floats2bfloat162_rn((lo - z) * s, (hi - z) * s);
-        out[i] = *reinterpret_cast<const uint32_t*>(&p);
-    }
+    for (int i = 0; i < 4; ++i) out[i] = mul2(sub2(((w >> (4 * i)) & 0x000F000Fu) | 0x43004300u, z), s);
 }
 
 // The scale (bits of a bf16, low four bits zero) of a group with extremes lo <= 0 <= hi.  The halves
@@ -50,45 +69,50 @@ __device__ __forceinline__ uint32_t kv4_scale_of(float lo, float hi) {
     return max(up, 0x00800000u) >> 16;
 }
 
-// rint(x / s) for a bf16 x and the reciprocal inv of a scale: x / s (8 bits over 4) is a tie or at least
-// 2^-10 away from one, so x * inv rounded to a multiple of 2^-11 (by adding and taking off
-// 1.5 * 2^12) is the tie itself or on its quotient's side of it.
+// rint(x / s) + 0x4B400000 for a bf16 x and the reciprocal inv of a scale: x / s (8 bits over 4) is a tie or at least
+// 2^-10 away from one, so x * inv rounded to a multiple of 2^-11 (by adding 1.5 * 2^12) is the tie itself
+// or on its quotient's side of it, and adding on to 1.5 * 2^23 leaves the integer in the low bits.
 __device__ __forceinline__ int kv4_round(float x, float inv) {
-    const float t = __fsub_rn(__fadd_rn(__fmul_rn(x, inv), 6144.0f), 6144.0f);
-    return __float_as_int(__fadd_rn(t, 12582912.0f)) - 0x4B400000;  // 1.5 * 2^23: the integer in the low bits
+    return __float_as_int(__fadd_rn(__fmaf_rn(x, inv, 6144.0f), 12582912.0f - 6144.0f));
+}
+constexpr int kKv4Round = 0x4B400000;
+
+// (hi, -lo) of eight values, given as bf16 pairs, in the halves of the result: at least 0, NaN where a value is.
+__device__ __forceinline__ uint32_t kv4_extremes(const uint32_t (&w)[4]) {
+    constexpr uint32_t kSign = 0x80008000u;
+    const uint32_t hi = max2(max2(w[0], w[1]), max2(w[2], w[3]));
+    const uint32_t lo = max2(max2(w[0] ^ kSign, w[1] ^ kSign), max2(w[2] ^ kSign, w[3] ^ kSign));
+    return max2(max2(__byte_perm(hi, lo, 0x5410), __byte_perm(hi, lo, 0x7632)), 0u);
 }
 
-// Eight neighbours of a group that four consecutive lanes of a full warp hold (lane & 3 = the word
-// of the group): the word of their codes, and the group's scale and zero point.
-__device__ __forceinline__ uint32_t kv4_quantise8(const float (&x)[8], uint32_t& scale) {
-    float lo = 0.f, hi = 0.f;
-    bool odd = false;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        lo = fminf(lo, x[j]);
-        hi = fmaxf(hi, x[j]);
-        odd |= (__float_as_uint(x[j]) & 0x7F800000u) == 0x7F800000u;
-    }
-#pragma unroll
-    for (int mask = 1; mask <= 2; mask <<= 1) {
-        lo = fminf(lo, __shfl_xor_sync(0xFFFFFFFFu, lo, mask));
-        hi = fmaxf(hi, __shfl_xor_sync(0xFFFFFFFFu, hi, mask));
-    }
-    const uint32_t odds = __ballot_sync(0xFFFFFFFFu, odd);
-    if ((odds >> (threadIdx.x & 28)) & 15u) {
-        scale = kKv4NanScale;
-        return 0;
-    }
-    const uint32_t s = kv4_scale_of(lo, hi);
-    const float inv = __frcp_rn(__uint_as_float(s << 16));
-    const int z = kv4_round(-lo, inv);
-    scale = s | static_cast<uint32_t>(z);
+// The scale and zero point of a group with those extremes, and the reciprocal of the scale.
+__device__ __forceinline__ uint32_t kv4_group(uint32_t extremes, float& inv) {
+    const uint32_t s = kv4_scale_of(-bf_hi(extremes), bf_lo(extremes));
+    inv = __frcp_rn(__uint_as_float(s << 16));
+    const bool odd = (extremes & 0x7F80u) == 0x7F80u || (extremes & 0x7F800000u) == 0x7F800000u;
+    return odd ? kKv4NanScale : s | static_cast<uint32_t>(kv4_round(bf_hi(extremes), inv) - kKv4Round);
+}
+
+// The code of x in a group: rint(x / s) + z, which is not negative (x >= lo), and at most 15 (both
+// roundings up may make 16).
+__device__ __forceinline__ uint32_t kv4_code(float x, float inv, int z) {
+    return static_cast<uint32_t>(min(kv4_round(x, inv) + (z - kKv4Round), 15));
+}
+
+// Eight neighbours, as bf16 pairs, of a group that four consecutive lanes of a full warp hold: the word of their
+// codes, and the group's scale and zero point.
+__device__ __forceinline__ uint32_t kv4_quantise8(const uint32_t (&x)[4], uint32_t& scale) {
+    uint32_t e = kv4_extremes(x);
+    e = max2(e, __shfl_xor_sync(0xFFFFFFFFu, e, 1));
+    e = max2(e, __shfl_xor_sync(0xFFFFFFFFu, e, 2));
+    float inv;
+    scale = kv4_group(e, inv);
+    if (scale == kKv4NanScale) return 0;
+    const int z = static_cast<int>(scale & 15u);
     uint32_t w = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int c = min(max(kv4_round(x[j], inv) + z, 0), 15);
-        w |= static_cast<uint32_t>(c) << (4 * (j >> 1) + 16 * (j & 1));
-    }
+    for (int i = 0; i < 4; ++i)
+        w |= (kv4_code(bf_lo(x[i]), inv, z) | kv4_code(bf_hi(x[i]), inv, z) << 16) << (4 * i);
     return w;
 }
 #endif

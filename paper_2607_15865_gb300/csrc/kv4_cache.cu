@@ -7,6 +7,8 @@
 //
 // All of it is bandwidth: 4 D bytes of new k and v in and 9/8 D out per token and kv head for
 // append, the reverse for read.
+#include <algorithm>
+
 #include "internal.h"
 #include "kv4.cuh"
 #include "sm100_ptx.cuh"
@@ -16,25 +18,12 @@ namespace {
 
 constexpr int kThreads = 256;
 
-__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
-__device__ __forceinline__ float round_bf16(float x) { return __bfloat162float(__float2bfloat16_rn(x)); }
-
-__device__ __forceinline__ void unpack8(const uint4& a, float (&x)[8]) {
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[2 * i] = bf_lo(w[i]);
-        x[2 * i + 1] = bf_hi(w[i]);
-    }
-}
-
 // The word of a row of D values at value index j (a multiple of 8), and its group's scale; with `out` (a
 // row of bf16) also the values that they stand for.
-__device__ __forceinline__ void put(const float (&x)[8], int j, bool mine, uint8_t* codes, uint16_t* scales,
-                                    uint16_t* out) {
+__device__ __forceinline__ void put(const uint4& x, int j, bool mine, uint8_t* codes, uint16_t* scales, uint16_t* out) {
+    const uint32_t pairs[4] = {x.x, x.y, x.z, x.w};
     uint32_t scale;
-    const uint32_t w = kv4_quantise8(x, scale);
+    const uint32_t w = kv4_quantise8(pairs, scale);
     if (!mine) return;
     *reinterpret_cast<uint32_t*>(codes + j / 2) = w;
     if (j % kKv4Group == 0) scales[j / kKv4Group] = static_cast<uint16_t>(scale);
@@ -45,10 +34,17 @@ __device__ __forceinline__ void put(const float (&x)[8], int j, bool mine, uint8
     }
 }
 
+// RoPE of two pairs: values j, j + 1 in x and their partners in y.
+__device__ __forceinline__ void turn(uint32_t& x, uint32_t& y, float c0, float c1, float s0, float s1) {
+    const float x0 = bf_lo(x), x1 = bf_hi(x), y0 = bf_lo(y), y1 = bf_hi(y);
+    x = pack2(__fsub_rn(__fmul_rn(x0, c0), __fmul_rn(y0, s0)), __fsub_rn(__fmul_rn(x1, c1), __fmul_rn(y1, s1)));
+    y = pack2(__fadd_rn(__fmul_rn(y0, c0), __fmul_rn(x0, s0)), __fadd_rn(__fmul_rn(y1, c1), __fmul_rn(x1, s1)));
+}
+
 // One thread per 16 values of k and of v (8 and their RoPE partners D / 2 further) of a (token, kv head).
 template <int D>
-__device__ __forceinline__ void append_unit(long long u, const Kv4New& a, int Hkv, int max_len, int lp, const float* cos_tab,
-                                            const float* sin_tab, const Kv4Cache& c, const Kv4Plain& plain, int* err) {
+__device__ __forceinline__ void append_unit(long long u, const Kv4New& a, int Hkv, int lp, const float* cos_tab,
+                                            const float* sin_tab, const Kv4Cache& c, const Kv4Plain& plain) {
     constexpr int PARTS = D / 16;
     const long long n = static_cast<long long>(a.batch) * a.chunk * Hkv * PARTS;
     const bool in = u < n;
@@ -58,95 +54,97 @@ __device__ __forceinline__ void append_unit(long long u, const Kv4New& a, int Hk
     const int g = static_cast<int>(row % Hkv);
     const int i = static_cast<int>(row / Hkv % a.chunk);
     const int b = static_cast<int>(row / Hkv / a.chunk);
-    int hist = a.hist;
-    bool mine = in;
-    if (a.d_hist != nullptr) {
-        hist = a.d_hist[b];
-        if (hist < 0 || hist > max_len - a.chunk) {
-            if (in && part == 0 && g == 0 && i == 0) atomicOr(err, kDevErrHistRange);
-            mine = false;
-            hist = 0;
-        }
-    }
-    const int p = hist + i, j = 8 * part;
+    const bool mine = in;
+    const int p = a.hist + i, j = 8 * part;
     const size_t src = static_cast<size_t>(row) * D + j;
     const size_t slot = (static_cast<size_t>(b) * Hkv + g) * lp + p;
     const size_t prow = (static_cast<size_t>(b) * Hkv + g) * plain.rows + p;
-    float xa[8], xb[8], cs[8], sn[8], ya[8], yb[8];
-    unpack8(*reinterpret_cast<const uint4*>(a.k + src), xa);
-    unpack8(*reinterpret_cast<const uint4*>(a.k + src + D / 2), xb);
+    uint4 ka = *reinterpret_cast<const uint4*>(a.k + src), kb = *reinterpret_cast<const uint4*>(a.k + src + D / 2);
     const uint4 va = *reinterpret_cast<const uint4*>(a.v + src), vb = *reinterpret_cast<const uint4*>(a.v + src + D / 2);
     const float4* ct = reinterpret_cast<const float4*>(cos_tab + static_cast<size_t>(p) * (D / 2) + j);
     const float4* st = reinterpret_cast<const float4*>(sin_tab + static_cast<size_t>(p) * (D / 2) + j);
-    *reinterpret_cast<float4*>(cs) = ct[0];
-    *reinterpret_cast<float4*>(cs + 4) = ct[1];
-    *reinterpret_cast<float4*>(sn) = st[0];
-    *reinterpret_cast<float4*>(sn + 4) = st[1];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        ya[e] = round_bf16(__fsub_rn(__fmul_rn(xa[e], cs[e]), __fmul_rn(xb[e], sn[e])));
-        yb[e] = round_bf16(__fadd_rn(__fmul_rn(xb[e], cs[e]), __fmul_rn(xa[e], sn[e])));
-    }
+    const float4 c0 = ct[0], c1 = ct[1], s0 = st[0], s1 = st[1];
+    turn(ka.x, kb.x, c0.x, c0.y, s0.x, s0.y);
+    turn(ka.y, kb.y, c0.z, c0.w, s0.z, s0.w);
+    turn(ka.z, kb.z, c1.x, c1.y, s1.x, s1.y);
+    turn(ka.w, kb.w, c1.z, c1.w, s1.z, s1.w);
     uint8_t* kc = c.k_codes + slot * (D / 2);
     uint8_t* vc = c.v_codes + slot * (D / 2);
     uint16_t* ks = c.k_scales + slot * (D / kKv4Group);
     uint16_t* vs = c.v_scales + slot * (D / kKv4Group);
     uint16_t* ko = plain.k == nullptr ? nullptr : plain.k + prow * D;
     uint16_t* vo = plain.v == nullptr ? nullptr : plain.v + prow * D;
-    put(ya, j, mine, kc, ks, ko);
-    put(yb, j + D / 2, mine, kc, ks, ko);
-    unpack8(va, xa);
-    unpack8(vb, xb);
-    put(xa, j, mine, vc, vs, vo);
-    put(xb, j + D / 2, mine, vc, vs, vo);
+    put(ka, j, mine, kc, ks, ko);
+    put(kb, j + D / 2, mine, kc, ks, ko);
+    put(va, j, mine, vc, vs, vo);
+    put(vb, j + D / 2, mine, vc, vs, vo);
 }
 
-// One thread per word of 8 values, of k and of v, of slots first .. first + count - 1.
+// One CTA reads kReadWords words of 8 values, of k or of v, of consecutive slots of a head, kReadEach per
+// thread, all of whose loads are in flight together.
+constexpr int kReadEach = 8, kReadWords = kThreads * kReadEach;
+struct ReadCut {
+    FastDiv parts;  // CTAs per head and array
+    int first, count, lp;
+};
 template <int D>
-__device__ __forceinline__ void read_unit(long long u, int first, int count, int heads, int lp, const Kv4Cache& c,
-                                          const Kv4Plain& plain) {
+ReadCut read_cut(int first, int count, int lp) {
+    return {make_fastdiv(static_cast<int>((static_cast<long long>(count) * (D / 8) + kReadWords - 1) / kReadWords)), first,
+            count, lp};
+}
+
+template <int D>
+__device__ __forceinline__ void read_part(int block, const ReadCut& r, const Kv4Cache& c, const Kv4Plain& plain) {
     constexpr int WORDS = D / 8;
-    if (u >= static_cast<long long>(heads) * count * WORDS) return;
-    const int word = static_cast<int>(u % WORDS);
-    const long long r = u / WORDS;
-    const int i = static_cast<int>(r % count), h = static_cast<int>(r / count);
-    const size_t slot = static_cast<size_t>(h) * lp + first + i;
-    const size_t out = (static_cast<size_t>(h) * plain.rows + i) * D + 8 * word;
+    const bool v = block & 1;
+    const int head = fdiv(block >> 1, r.parts), part = (block >> 1) - head * static_cast<int>(r.parts.d);
+    const size_t slot = static_cast<size_t>(head) * r.lp + r.first;
+    const uint32_t* codes = reinterpret_cast<const uint32_t*>((v ? c.v_codes : c.k_codes) + slot * (D / 2));
+    const uint16_t* scales = (v ? c.v_scales : c.k_scales) + slot * (D / kKv4Group);
+    uint4* out = reinterpret_cast<uint4*>((v ? plain.v : plain.k) + static_cast<size_t>(head) * plain.rows * D);
+    const int last = r.count * WORDS;  // count is at most 2^20
+    uint32_t w[kReadEach], m[kReadEach];
+    const int u0 = part * kReadWords + static_cast<int>(threadIdx.x);
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        const uint8_t* codes = t ? c.v_codes : c.k_codes;
-        const uint16_t* scales = t ? c.v_scales : c.k_scales;
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(codes + slot * (D / 2) + 4 * word);
-        uint32_t v[4];
-        kv4_values(w, scales[slot * (D / kKv4Group) + word / 4], v);
-        *reinterpret_cast<uint4*>((t ? plain.v : plain.k) + out) = make_uint4(v[0], v[1], v[2], v[3]);
+    for (int i = 0; i < kReadEach; ++i) {
+        const int u = u0 + i * kThreads;
+        if (u < last) {
+            w[i] = codes[u];
+            m[i] = scales[u / 4];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kReadEach; ++i) {
+        const int u = u0 + i * kThreads;
+        if (u < last) {
+            uint32_t x[4];
+            kv4_values(w[i], m[i], x);
+            out[u] = make_uint4(x[0], x[1], x[2], x[3]);
+        }
     }
 }
 
 template <int D>
-__global__ void __launch_bounds__(kThreads) kv4_append_kernel(Kv4New a, int Hkv, int max_len, int lp,
+__global__ void __launch_bounds__(kThreads) kv4_append_kernel(Kv4New a, int Hkv, int lp,
                                                               const float* __restrict__ cos_tab,
                                                               const float* __restrict__ sin_tab, Kv4Cache c, Kv4Plain plain,
-                                                              int append_blocks, int* __restrict__ err) {
+                                                              int append_blocks, ReadCut history) {
     // A dependent launch: it reads and writes only after the stream's previous kernel, and the kernel after it
     // (flash_fwd, whose prologue reads q) may be resident by then.
     griddep_wait();
     griddep_launch_dependents();
     const int block = static_cast<int>(blockIdx.x);
     if (block < append_blocks)
-        append_unit<D>(static_cast<long long>(block) * kThreads + threadIdx.x, a, Hkv, max_len, lp, cos_tab, sin_tab, c,
-                       plain, err);
+        append_unit<D>(static_cast<long long>(block) * kThreads + threadIdx.x, a, Hkv, lp, cos_tab, sin_tab, c, plain);
     else  // the history in front of the chunk, to the workspace
-        read_unit<D>(static_cast<long long>(block - append_blocks) * kThreads + threadIdx.x, 0, a.hist, a.batch * Hkv, lp,
-                     c, plain);
+        read_part<D>(block - append_blocks, history, c, plain);
 }
 
 template <int D>
-__global__ void __launch_bounds__(kThreads) kv4_read_kernel(int first, int count, int heads, int lp, Kv4Cache c,
-                                                            Kv4Plain plain) {
+__global__ void __launch_bounds__(kThreads) kv4_read_kernel(ReadCut cut, Kv4Cache c, Kv4Plain plain) {
     griddep_wait();
     griddep_launch_dependents();
-    read_unit<D>(static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x, first, count, heads, lp, c, plain);
+    read_part<D>(static_cast<int>(blockIdx.x), cut, c, plain);
 }
 
 cudaLaunchConfig_t dependent(long long blocks, cudaStream_t st, cudaLaunchAttribute* attr) {
@@ -166,27 +164,29 @@ long long blocks_for(long long units) { return (units + kThreads - 1) / kThreads
 }  // namespace
 
 cudaError_t launch_kv4_append(const Shape& s, const Kv4New& a, const float* cos_tab, const float* sin_tab, const Kv4Cache& c,
-                              const Kv4Plain& plain, int* err, cudaStream_t st) {
-    const long long tokens = static_cast<long long>(a.batch) * a.chunk;
-    const long long append = blocks_for(tokens * s.n_kv_heads * (s.head_dim / 16));
+                              const Kv4Plain& plain, cudaStream_t st) {
+    const bool d128 = s.head_dim == 128;
+    const long long append = blocks_for(static_cast<long long>(a.batch) * a.chunk * s.n_kv_heads * (s.head_dim / 16));
+    const int lp = kv4_slots(s.max_len);
+    const ReadCut history = d128 ? read_cut<128>(0, std::max(a.hist, 1), lp) : read_cut<64>(0, std::max(a.hist, 1), lp);
     const long long read =
-        plain.k == nullptr ? 0 : blocks_for(static_cast<long long>(a.batch) * s.n_kv_heads * a.hist * (s.head_dim / 8));
+        plain.k == nullptr || a.hist == 0 ? 0 : 2LL * a.batch * s.n_kv_heads * static_cast<long long>(history.parts.d);
     if (append + read > INT32_MAX) return cudaErrorInvalidConfiguration;
     cudaLaunchAttribute attr;
     const cudaLaunchConfig_t cfg = dependent(append + read, st, &attr);
-    return cudaLaunchKernelEx(&cfg, s.head_dim == 128 ? kv4_append_kernel<128> : kv4_append_kernel<64>, a, s.n_kv_heads,
-                              s.max_len, kv4_slots(s.max_len), cos_tab, sin_tab, c, plain, static_cast<int>(append), err);
+    return cudaLaunchKernelEx(&cfg, d128 ? kv4_append_kernel<128> : kv4_append_kernel<64>, a, s.n_kv_heads, lp,
+                              cos_tab, sin_tab, c, plain, static_cast<int>(append), history);
 }
 
 cudaError_t launch_kv4_read(const Shape& s, int first, int count, const Kv4Cache& c, const Kv4Plain& plain,
                             cudaStream_t st) {
-    const int heads = s.batch * s.n_kv_heads;
-    const long long blocks = blocks_for(static_cast<long long>(heads) * count * (s.head_dim / 8));
+    const int lp = kv4_slots(s.max_len);
+    const ReadCut cut = s.head_dim == 128 ? read_cut<128>(first, count, lp) : read_cut<64>(first, count, lp);
+    const long long blocks = 2LL * s.batch * s.n_kv_heads * static_cast<long long>(cut.parts.d);
     if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
     cudaLaunchAttribute attr;
     const cudaLaunchConfig_t cfg = dependent(blocks, st, &attr);
-    return cudaLaunchKernelEx(&cfg, s.head_dim == 128 ? kv4_read_kernel<128> : kv4_read_kernel<64>, first, count, heads,
-                              kv4_slots(s.max_len), c, plain);
+    return cudaLaunchKernelEx(&cfg, s.head_dim == 128 ? kv4_read_kernel<128> : kv4_read_kernel<64>, cut, c, plain);
 }
 
 }  // namespace attn

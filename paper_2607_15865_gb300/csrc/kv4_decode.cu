@@ -109,22 +109,11 @@ __device__ __forceinline__ uint32_t fma2(uint32_t a, uint32_t b, uint32_t c) {
     asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
     return d;
 }
-__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
-    uint32_t d;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-    uint32_t d;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
-    return d;
-}
-
 constexpr uint32_t kOnes = 0x3F803F80u;                       // 1
 constexpr uint32_t kUp = 0x5D805D80u, kSixteenth = 0x3D803D80u;  // 2^60, 2^-4
 constexpr float kUnit = 9.44473296573929e21f;                // 2^73
@@ -204,38 +193,25 @@ struct Args {
     int batch, ntok, Hq, Hkv, max_len, lp, ncg, min_blocks;
 };
 
-// One warp: quantise the E values x that each lane holds of a row of D = 32 E, write the row's codes and
-// scales to the cache and to a staged row (codes, then scales).  Returns whether the lane's group is NaN.
+// One warp: quantise the E = D / 32 values of a row that each lane holds (bf16 pairs; with E = 2 one pair), write
+// the row's codes and scales to the cache and to a staged row (codes, then scales).  Returns whether the lane's
+// group is NaN.
 template <int D>
-__device__ __forceinline__ bool put_row(const float (&x)[D / 32], int lane, uint8_t* codes, uint16_t* scales,
+__device__ __forceinline__ bool put_row(const uint32_t (&x)[D / 64], int lane, uint8_t* codes, uint16_t* scales,
                                         uint8_t* staged) {
     constexpr int E = D / 32, LANES = kKv4Group / E, WL = 8 / E;  // lanes of a group and of a word
-    float lo = 0.f, hi = 0.f;
-    bool odd = false;
+    const uint32_t all[4] = {x[0], x[E / 2 - 1], x[0], x[0]};
+    uint32_t e = kv4_extremes(all);
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        lo = fminf(lo, x[e]);
-        hi = fmaxf(hi, x[e]);
-        odd |= (__float_as_uint(x[e]) & 0x7F800000u) == 0x7F800000u;
-    }
-#pragma unroll
-    for (int mask = 1; mask < LANES; mask <<= 1) {
-        lo = fminf(lo, __shfl_xor_sync(0xFFFFFFFFu, lo, mask));
-        hi = fmaxf(hi, __shfl_xor_sync(0xFFFFFFFFu, hi, mask));
-    }
-    const uint32_t odds = __ballot_sync(0xFFFFFFFFu, odd);
-    const bool nan = ((odds >> (lane & ~(LANES - 1))) & ((1u << LANES) - 1u)) != 0;
-    const uint32_t s = kv4_scale_of(lo, hi);
-    const float inv = __frcp_rn(__uint_as_float(s << 16));
-    const int z = kv4_round(-lo, inv);
-    const uint32_t scale = nan ? kKv4NanScale : s | static_cast<uint32_t>(z);
+    for (int mask = 1; mask < LANES; mask <<= 1) e = max2(e, __shfl_xor_sync(0xFFFFFFFFu, e, mask));
+    float inv;
+    const uint32_t scale = kv4_group(e, inv);
+    const bool nan = scale == kKv4NanScale;
+    const int z = static_cast<int>(scale & 15u);
     uint32_t w = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const int j = (lane * E + e) & 7;
-        const int c = min(max(kv4_round(x[e], inv) + z, 0), 15);
-        w |= static_cast<uint32_t>(c) << (4 * (j >> 1) + 16 * (j & 1));
-    }
+    for (int i = 0; i < E / 2; ++i)
+        w |= (kv4_code(bf_lo(x[i]), inv, z) | kv4_code(bf_hi(x[i]), inv, z) << 16) << (4 * ((lane * (E / 2) + i) & 3));
     if (nan) w = 0;
 #pragma unroll
     for (int mask = 1; mask < WL; mask <<= 1) w |= __shfl_xor_sync(0xFFFFFFFFu, w, mask);
@@ -250,18 +226,14 @@ __device__ __forceinline__ bool put_row(const float (&x)[D / 32], int lane, uint
     return nan;
 }
 
-template <int E>
-__device__ __forceinline__ void load_row(const uint16_t* p, int lane, float (&x)[E]) {
-    if constexpr (E == 4) {
+template <int N>
+__device__ __forceinline__ void load_row(const uint16_t* p, int lane, uint32_t (&x)[N]) {
+    if constexpr (N == 2) {
         const uint2 w = __ldg(reinterpret_cast<const uint2*>(p + 4 * lane));
-        x[0] = __uint_as_float(w.x << 16);
-        x[1] = __uint_as_float(w.x & 0xFFFF0000u);
-        x[2] = __uint_as_float(w.y << 16);
-        x[3] = __uint_as_float(w.y & 0xFFFF0000u);
+        x[0] = w.x;
+        x[1] = w.y;
     } else {
-        const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(p + 2 * lane));
-        x[0] = __uint_as_float(w << 16);
-        x[1] = __uint_as_float(w & 0xFFFF0000u);
+        x[0] = __ldg(reinterpret_cast<const uint32_t*>(p + 2 * lane));
     }
 }
 
@@ -669,19 +641,21 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
                     const size_t src = ((static_cast<size_t>(w.b) * a.ntok + i) * a.Hkv + w.head) * D;
                     const size_t slot = (static_cast<size_t>(w.b) * a.Hkv + w.head) * a.lp + p;
                     uint8_t* staged = staged_row(w, i, u & 1);
-                    float x[E];
-                    load_row<E>(((u & 1) ? a.v_new : a.k_new) + src, lane, x);
+                    uint32_t x[E / 2];
+                    load_row<E / 2>(((u & 1) ? a.v_new : a.k_new) + src, lane, x);
                     if (u & 1) {
                         const bool nan = put_row<D>(x, lane, a.c.v_codes + slot * C::ROW, a.c.v_scales + slot * GR, staged);
                         if (nan && lane % (kKv4Group / E) == 0) atomicMin(&s_nan[lane / (kKv4Group / E)], i);
                     } else {
+                        const float turn = lane < 16 ? -1.f : 1.f;  // x c - y s in the first half, x c + y s in the second
 #pragma unroll
-                        for (int e = 0; e < E; ++e) {
-                            const size_t j = static_cast<size_t>(p) * (D / 2) + (lane & 15) * E + e;
-                            const float other = __shfl_xor_sync(0xFFFFFFFFu, x[e], 16);
-                            const float cs = __ldg(a.cos_tab + j), sn = __ldg(a.sin_tab + j);
-                            x[e] = round_bf16(lane < 16 ? __fsub_rn(__fmul_rn(x[e], cs), __fmul_rn(other, sn))
-                                                        : __fadd_rn(__fmul_rn(x[e], cs), __fmul_rn(other, sn)));
+                        for (int e = 0; e < E / 2; ++e) {
+                            const size_t j = static_cast<size_t>(p) * (D / 2) + (lane & 15) * E + 2 * e;
+                            const float2 cs = __ldg(reinterpret_cast<const float2*>(a.cos_tab + j));
+                            const float2 sn = __ldg(reinterpret_cast<const float2*>(a.sin_tab + j));
+                            const uint32_t y = __shfl_xor_sync(0xFFFFFFFFu, x[e], 16);
+                            x[e] = pack2(__fadd_rn(__fmul_rn(bf_lo(x[e]), cs.x), turn * __fmul_rn(bf_lo(y), sn.x)),
+                                         __fadd_rn(__fmul_rn(bf_hi(x[e]), cs.y), turn * __fmul_rn(bf_hi(y), sn.y)));
                         }
                         put_row<D>(x, lane, a.c.k_codes + slot * C::ROW, a.c.k_scales + slot * GR, staged);
                     }

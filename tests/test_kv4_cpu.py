@@ -67,6 +67,23 @@ def test_float_quotient_by_reciprocal_is_exact():
             assert (got[use] == np.array(want)[use]).all()
 
 
+def test_float_quotient_by_one_fma_is_exact():
+    """The same with the product and the first sum in one rounding, and on to the integer in one more."""
+    X = np.arange(128, 256)
+    for S in range(8, 16):
+        for k in range(-12, 5):
+            x, s = F(X) * F(2.0) ** F(k), F(S)
+            inv = F(1) / s
+            t = (x.astype(np.float64) * np.float64(inv) + 6144.0).astype(np.float32)  # exact in 64 bits before it rounds
+            got = (t + F(12582912.0 - 6144.0)) - F(12582912.0)
+            want = [round(Fraction(int(v)) * Fraction(2) ** k / S) for v in X]
+            use = np.array([w <= 15 for w in want])
+            assert (got[use] == np.array(want)[use]).all()
+            t = (-x.astype(np.float64) * np.float64(inv) + 6144.0).astype(np.float32)
+            got = (t + F(12582912.0 - 6144.0)) - F(12582912.0)
+            assert (got[use] == -np.array(want)[use]).all()
+
+
 def test_float_scale_is_exact():
     """kv4_scale_of in float against the rational definition, where (hi - lo) / 15 has 4 bits itself too."""
     r = np.random.default_rng(2)
