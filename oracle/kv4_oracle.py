@@ -1,8 +1,9 @@
 """The 4-bit KV cache in numpy float64: quantiser, packed format, RoPE and attention over it.
 
 Straight from the definition in include/attn.h (attn_kv4); shares nothing with the library.
-Float64 holds every step of the quantiser exactly: a bf16's 8 bits, sums of two of them, and
-quotients that are compared with half-integers at least 2^-10 away or met exactly.
+Float64 holds every step of the quantiser exactly: a bf16's 8 bits, sums of two of them (but for
+the range of a group whose extremes are 2^45 apart, which is compared as such), and quotients
+that are compared with half-integers at least 2^-10 away or met exactly.
 """
 from __future__ import annotations
 
@@ -42,7 +43,10 @@ def quantise(bits):
     x = np.where(finite[..., None], x, 0.0)
     lo, hi = np.minimum(x.min(-1), 0.0), np.maximum(x.max(-1), 0.0)
     m, e = np.frexp((hi - lo) / 15.0)  # m in [0.5, 1)
-    s = np.maximum(np.ldexp(np.ceil(m * 16.0), e - 4), 2.0 ** -126)
+    m = np.ceil(m * 16.0)
+    # where hi - lo drops one extreme beside the other: the larger less 15 s is exact
+    m += np.maximum(hi, -lo) - 15.0 * np.ldexp(m, e - 4) > -np.minimum(hi, -lo)
+    s = np.maximum(np.ldexp(m, e - 4), 2.0 ** -126)
     z = np.rint(-lo / s)
     c = np.clip(np.rint(x / s[..., None]) + z[..., None], 0, 15)
     scales = np.where(finite, f64_to_bf16_exact(s) | z.astype(np.uint16), np.uint16(NAN_SCALE))

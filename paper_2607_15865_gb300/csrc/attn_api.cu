@@ -709,6 +709,24 @@ size_t kv4_plain_bytes(const attn_cfg& cfg, int tokens) {
     return (static_cast<size_t>(cfg.batch) * cfg.n_kv_heads * tokens * cfg.head_dim * 2 + 255) & ~static_cast<size_t>(255);
 }
 
+int run_kv4_decode(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uint16_t* v, const int32_t* d_hist_len, int hist,
+                   int n_new, const attn_kv4* cache, uint16_t* out, attn_stream_t stream) {
+    const cudaError_t e = attn::launch_kv4_decode(c->shape, q, k, v, d_hist_len, hist, n_new, kv4_of(cache), c->d_cos,
+                                                  c->d_sin, c->d_flash_o, c->d_flash_ml, c->d_counters, out, c->d_err,
+                                                  c->num_sms, reinterpret_cast<cudaStream_t>(stream), c->wait_ns);
+    return e == cudaSuccess ? ATTN_OK : cuda_fail(e, "kv4 decode launch");
+}
+
+// Whether a short chunk goes through the decode (a pass over the packed history for each 16 (query head, token)
+// columns) or through the workspace.  Calls in a graph, 40 / 8 heads, decode against workspace: 15 columns over
+// 500 10.3 and 9.6 us, over 4000 10.7 and 14.3, over 30000 18.3 and 51.7; 30 columns over 500 12.0 and 9.5, over
+// 4000 13.9 and 14.8, over 30000 28.7 and 52.2; 45 columns over 4000 16.0 and 15.2, over 30000 38.6 and 52.7, of
+// four sequences over 4000 36.1 and 32.0.
+bool kv4_chunk_decodes(const attn_ctx* c, int hist, int chunk) {
+    const int columns = c->cfg.n_q_heads / c->cfg.n_kv_heads * chunk;
+    return chunk <= kMaxDraftTokens && (columns <= 16 || (columns <= 32 && hist >= 2048));
+}
+
 }  // namespace
 
 int attn_kv4_slots(int max_len) { return max_len < 1 || max_len > (1 << 20) ? 0 : attn::kv4_slots(max_len); }
@@ -718,6 +736,7 @@ int attn_kv4_append(attn_ctx* c, const uint16_t* k, const uint16_t* v, int hist_
     if (c == nullptr || k == nullptr || v == nullptr || !kv4_ok(cache) || !aligned16(k) || !aligned16(v))
         return ATTN_EINVAL;
     if (chunk_len < 1 || hist_len < 0 || static_cast<long>(hist_len) + chunk_len > c->cfg.max_len) return ATTN_EINVAL;
+    if (attn::kv4_append_units(c->shape, c->cfg.batch, chunk_len) > INT32_MAX - 256) return ATTN_EINVAL;
     const attn::Kv4New a{k, v, hist_len, chunk_len, c->cfg.batch};
     const cudaError_t e = attn::launch_kv4_append(c->shape, a, c->d_cos, c->d_sin, kv4_of(cache),
                                                   attn::Kv4Plain{nullptr, nullptr, 0},
@@ -745,10 +764,7 @@ int attn_kv4_decode(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uin
         (reinterpret_cast<uintptr_t>(d_hist_len) & 3u))
         return ATTN_EINVAL;
     if (n_new < 1 || n_new > kMaxDraftTokens || n_new > c->cfg.max_len) return ATTN_EINVAL;
-    const cudaError_t e = attn::launch_kv4_decode(c->shape, q, k, v, d_hist_len, n_new, kv4_of(cache), c->d_cos, c->d_sin,
-                                                  c->d_flash_o, c->d_flash_ml, c->d_counters, out, c->d_err, c->num_sms,
-                                                  reinterpret_cast<cudaStream_t>(stream), c->wait_ns);
-    return e == cudaSuccess ? ATTN_OK : cuda_fail(e, "kv4 decode launch");
+    return run_kv4_decode(c, q, k, v, d_hist_len, 0, n_new, cache, out, stream);
 }
 
 size_t attn_kv4_workspace(const attn_ctx* c, int tokens) {
@@ -766,8 +782,11 @@ int attn_kv4_prefill_kv(attn_ctx* c, const uint16_t* q, const uint16_t* k, const
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) ||
         (reinterpret_cast<uintptr_t>(workspace) & 255u))
         return ATTN_EINVAL;
+    if (attn::kv4_append_units(c->shape, c->cfg.batch, chunk_len) > INT32_MAX - 256) return ATTN_EINVAL;
     const int tokens = hist_len + chunk_len;
     if (workspace_bytes < attn_kv4_workspace(c, tokens)) return ATTN_EINVAL;
+    if (kv4_chunk_decodes(c, hist_len, chunk_len))
+        return run_kv4_decode(c, q, k, v, nullptr, hist_len, chunk_len, cache, out, stream);
     uint16_t* kp = static_cast<uint16_t*>(workspace);
     uint16_t* vp = kp + kv4_plain_bytes(c->cfg, tokens) / 2;
     attn::FlashMaps maps;

@@ -145,19 +145,23 @@ struct Kv4Plain {
     uint16_t* v;
     int rows;
 };
+// Threads of an append; a launch takes fewer than 2^31 - 256.
+inline long long kv4_append_units(const Shape& s, int batch, int chunk) {
+    return static_cast<long long>(batch) * chunk * s.n_kv_heads * (s.head_dim / 16);
+}
 // Appends the new tokens; with plain.k also writes slots [0, hist + chunk) as bf16 there (row p: slot p).
 cudaError_t launch_kv4_append(const Shape& s, const Kv4New& a, const float* cos_tab, const float* sin_tab,
                               const Kv4Cache& c, const Kv4Plain& plain, cudaStream_t st);
 // Slots first .. first + count - 1 as bf16 (row i: slot first + i).
 cudaError_t launch_kv4_read(const Shape& s, int first, int count, const Kv4Cache& c, const Kv4Plain& plain,
                             cudaStream_t st);
-// Decode over the 4-bit cache (kv4_decode.cu): ntok (1 .. 16) new tokens per sequence at positions d_hist[b] + i,
-// appended and attended to; a sequence with a position outside the cache is flagged and skipped.  part_o
+// Decode over the 4-bit cache (kv4_decode.cu): ntok (1 .. 16) new tokens per sequence at positions d_hist[b] + i (without
+// d_hist: hist + i), appended and attended to; a sequence with a position outside the cache is flagged and skipped.  part_o
 // [num_sms * 128][D] and part_ml [num_sms * 144][2] hold the parts of items that CTAs share; counters:
 // an int per item (sequence, kv head, 16 columns) of up to 128 sequences, zero before and after every launch.
 cudaError_t configure_kv4_decode();
 cudaError_t launch_kv4_decode(const Shape& s, const uint16_t* q, const uint16_t* k_new, const uint16_t* v_new,
-                              const int32_t* d_hist, int ntok, const Kv4Cache& c, const float* cos_tab,
+                              const int32_t* d_hist, int hist, int ntok, const Kv4Cache& c, const float* cos_tab,
                               const float* sin_tab, float* part_o, float* part_ml, int* counters, uint16_t* out, int* err,
                               int num_sms, cudaStream_t st, uint64_t wait_ns);
 

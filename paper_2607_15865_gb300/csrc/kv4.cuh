@@ -58,18 +58,18 @@ __device__ __forceinline__ void kv4_values(uint32_t w, uint32_t m, uint32_t (&ou
     for (int i = 0; i < 4; ++i) out[i] = mul2(sub2(((w >> (4 * i)) & 0x000F000Fu) | 0x43004300u, z), s);
 }
 
-// The scale (bits of a bf16, low four bits zero) of a group with extremes lo <= 0 <= hi.  The halves
-// are exact (what a subnormal loses is under the least scale), and (hi - lo) / 15 rounds to a number of 4 bits
-// where it is one or where the difference loses a far smaller lo or hi; hi / 2 - 7.5 s, which is exact
-// near that, tells those apart.
-__device__ __forceinline__ uint32_t kv4_scale_of(float lo, float hi) {
-    const float h = hi * 0.5f, l = lo * 0.5f;
-    uint32_t up = (__float_as_uint(__fdiv_rn(__fsub_rn(h, l), 7.5f)) + 0xFFFFFu) & 0xFFF00000u;
-    if (__fsub_rn(h, __fmul_rn(__uint_as_float(up), 7.5f)) > l) up += 0x00100000u;
+// The scale (bits of a bf16, low four bits zero) of a group with extremes -neg <= 0 <= hi: the next number of 4
+// bits from a quotient that is 1 or 2 parts in 2^22 too small is s or the one before it, and the one before where
+// it leaves 7.5 s < (hi + neg) / 2, told from the larger half less 7.5 s, which is exact where that decides.
+// (Halves, so that the sum does not overflow; what a subnormal loses by it is under the least scale.)
+__device__ __forceinline__ uint32_t kv4_scale_of(float hi, float neg) {
+    const float h = hi * 0.5f, l = neg * 0.5f;
+    uint32_t up = (__float_as_uint(__fmul_rn(__fadd_rn(h, l), 0.133333295f)) + 0xFFFFFu) & 0xFFF00000u;
+    if (__fsub_rn(fmaxf(h, l), __fmul_rn(__uint_as_float(up), 7.5f)) > -fminf(h, l)) up += 0x00100000u;
     return max(up, 0x00800000u) >> 16;
 }
 
-// rint(x / s) + 0x4B400000 for a bf16 x and the reciprocal inv of a scale: x / s (8 bits over 4) is a tie or at least
+// rint(x / s) + 0x4B400000 for a bf16 x and the reciprocal inv of a scale, good to a few parts in 2^23: x / s (8 bits over 4) is a tie or at least
 // 2^-10 away from one, so x * inv rounded to a multiple of 2^-11 (by adding 1.5 * 2^12) is the tie itself
 // or on its quotient's side of it, and adding on to 1.5 * 2^23 leaves the integer in the low bits.
 __device__ __forceinline__ int kv4_round(float x, float inv) {
@@ -87,8 +87,8 @@ __device__ __forceinline__ uint32_t kv4_extremes(const uint32_t (&w)[4]) {
 
 // The scale and zero point of a group with those extremes, and the reciprocal of the scale.
 __device__ __forceinline__ uint32_t kv4_group(uint32_t extremes, float& inv) {
-    const uint32_t s = kv4_scale_of(-bf_hi(extremes), bf_lo(extremes));
-    inv = __frcp_rn(__uint_as_float(s << 16));
+    const uint32_t s = kv4_scale_of(bf_lo(extremes), bf_hi(extremes));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(__uint_as_float(s << 16)));  // 2^-126 <= s < 2^126
     const bool odd = (extremes & 0x7F80u) == 0x7F80u || (extremes & 0x7F800000u) == 0x7F800000u;
     return odd ? kKv4NanScale : s | static_cast<uint32_t>(kv4_round(bf_hi(extremes), inv) - kKv4Round);
 }

@@ -42,19 +42,20 @@ __device__ __forceinline__ void turn(uint32_t& x, uint32_t& y, float c0, float c
 }
 
 // One thread per 16 values of k and of v (8 and their RoPE partners D / 2 further) of a (token, kv head).
+struct AppendCut {
+    FastDiv heads, chunk;
+    int units, lp, blocks;
+};
 template <int D>
-__device__ __forceinline__ void append_unit(long long u, const Kv4New& a, int Hkv, int lp, const float* cos_tab,
+__device__ __forceinline__ void append_unit(int u, const Kv4New& a, const AppendCut& cut, const float* cos_tab,
                                             const float* sin_tab, const Kv4Cache& c, const Kv4Plain& plain) {
     constexpr int PARTS = D / 16;
-    const long long n = static_cast<long long>(a.batch) * a.chunk * Hkv * PARTS;
-    const bool in = u < n;
-    if (!in) u = n - 1;  // whole warps take part in the group reductions
-    const int part = static_cast<int>(u % PARTS);
-    const long long row = u / PARTS;  // (sequence, token, head)
-    const int g = static_cast<int>(row % Hkv);
-    const int i = static_cast<int>(row / Hkv % a.chunk);
-    const int b = static_cast<int>(row / Hkv / a.chunk);
-    const bool mine = in;
+    const bool mine = u < cut.units;
+    if (!mine) u = cut.units - 1;  // whole warps take part in the group reductions
+    const int part = u % PARTS, row = u / PARTS;  // (sequence, token, head)
+    const int Hkv = static_cast<int>(cut.heads.d), lp = cut.lp;
+    const int tok = fdiv(row, cut.heads), g = row - tok * Hkv;
+    const int b = fdiv(tok, cut.chunk), i = tok - b * a.chunk;
     const int p = a.hist + i, j = 8 * part;
     const size_t src = static_cast<size_t>(row) * D + j;
     const size_t slot = (static_cast<size_t>(b) * Hkv + g) * lp + p;
@@ -125,19 +126,18 @@ __device__ __forceinline__ void read_part(int block, const ReadCut& r, const Kv4
 }
 
 template <int D>
-__global__ void __launch_bounds__(kThreads) kv4_append_kernel(Kv4New a, int Hkv, int lp,
-                                                              const float* __restrict__ cos_tab,
+__global__ void __launch_bounds__(kThreads) kv4_append_kernel(Kv4New a, AppendCut cut, const float* __restrict__ cos_tab,
                                                               const float* __restrict__ sin_tab, Kv4Cache c, Kv4Plain plain,
-                                                              int append_blocks, ReadCut history) {
+                                                              ReadCut history) {
     // A dependent launch: it reads and writes only after the stream's previous kernel, and the kernel after it
     // (flash_fwd, whose prologue reads q) may be resident by then.
     griddep_wait();
     griddep_launch_dependents();
     const int block = static_cast<int>(blockIdx.x);
-    if (block < append_blocks)
-        append_unit<D>(static_cast<long long>(block) * kThreads + threadIdx.x, a, Hkv, lp, cos_tab, sin_tab, c, plain);
+    if (block < cut.blocks)
+        append_unit<D>(block * kThreads + static_cast<int>(threadIdx.x), a, cut, cos_tab, sin_tab, c, plain);
     else  // the history in front of the chunk, to the workspace
-        read_part<D>(block - append_blocks, history, c, plain);
+        read_part<D>(block - cut.blocks, history, c, plain);
 }
 
 template <int D>
@@ -159,23 +159,25 @@ cudaLaunchConfig_t dependent(long long blocks, cudaStream_t st, cudaLaunchAttrib
     return cfg;
 }
 
-long long blocks_for(long long units) { return (units + kThreads - 1) / kThreads; }
-
 }  // namespace
 
 cudaError_t launch_kv4_append(const Shape& s, const Kv4New& a, const float* cos_tab, const float* sin_tab, const Kv4Cache& c,
                               const Kv4Plain& plain, cudaStream_t st) {
     const bool d128 = s.head_dim == 128;
-    const long long append = blocks_for(static_cast<long long>(a.batch) * a.chunk * s.n_kv_heads * (s.head_dim / 16));
+    const long long units = kv4_append_units(s, a.batch, a.chunk);
+    if (units > INT32_MAX - kThreads) return cudaErrorInvalidConfiguration;
     const int lp = kv4_slots(s.max_len);
-    const ReadCut history = d128 ? read_cut<128>(0, std::max(a.hist, 1), lp) : read_cut<64>(0, std::max(a.hist, 1), lp);
+    const AppendCut cut{make_fastdiv(s.n_kv_heads), make_fastdiv(a.chunk), static_cast<int>(units), lp,
+                        static_cast<int>((units + kThreads - 1) / kThreads)};
+    const int hist = std::max(a.hist, 1);
+    const ReadCut history = d128 ? read_cut<128>(0, hist, lp) : read_cut<64>(0, hist, lp);
     const long long read =
         plain.k == nullptr || a.hist == 0 ? 0 : 2LL * a.batch * s.n_kv_heads * static_cast<long long>(history.parts.d);
-    if (append + read > INT32_MAX) return cudaErrorInvalidConfiguration;
+    if (cut.blocks + read > INT32_MAX) return cudaErrorInvalidConfiguration;
     cudaLaunchAttribute attr;
-    const cudaLaunchConfig_t cfg = dependent(append + read, st, &attr);
-    return cudaLaunchKernelEx(&cfg, d128 ? kv4_append_kernel<128> : kv4_append_kernel<64>, a, s.n_kv_heads, lp,
-                              cos_tab, sin_tab, c, plain, static_cast<int>(append), history);
+    const cudaLaunchConfig_t cfg = dependent(cut.blocks + read, st, &attr);
+    return cudaLaunchKernelEx(&cfg, d128 ? kv4_append_kernel<128> : kv4_append_kernel<64>, a, cut, cos_tab, sin_tab, c, plain,
+                              history);
 }
 
 cudaError_t launch_kv4_read(const Shape& s, int first, int count, const Kv4Cache& c, const Kv4Plain& plain,

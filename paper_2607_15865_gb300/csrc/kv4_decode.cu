@@ -190,7 +190,7 @@ struct Args {
     int* err;
     uint64_t wait_ns;
     float scale_log2, move;  // log2 e / sqrt D in units of 2^-73, and the lead of a score that moves the maximum (2^8)
-    int batch, ntok, Hq, Hkv, max_len, lp, ncg, min_blocks;
+    int batch, ntok, Hq, Hkv, max_len, lp, ncg, min_blocks, hist;
 };
 
 // One warp: quantise the E = D / 32 values of a row that each lane holds (bf16 pairs; with E = 2 one pair), write
@@ -373,7 +373,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
     const int hc = a.Hkv * a.ncg;  // items of a sequence
     const int cta = static_cast<int>(blockIdx.x);
     auto blocks_of = [&](int b, int& h) {
-        h = a.d_hist[b];
+        h = a.d_hist != nullptr ? a.d_hist[b] : a.hist;
         const bool ok = h >= 0 && h <= a.max_len - a.ntok;
         if (!ok && cta == 0) atomicOr(a.err, kDevErrHistRange);
         return ok ? (h + a.ntok + KB - 1) / KB : 0;
@@ -981,7 +981,7 @@ cudaError_t configure_kv4_decode() {
 }
 
 cudaError_t launch_kv4_decode(const Shape& s, const uint16_t* q, const uint16_t* k_new, const uint16_t* v_new,
-                              const int32_t* d_hist, int ntok, const Kv4Cache& c, const float* cos_tab,
+                              const int32_t* d_hist, int hist, int ntok, const Kv4Cache& c, const float* cos_tab,
                               const float* sin_tab, float* part_o, float* part_ml, int* counters, uint16_t* out, int* err,
                               int num_sms, cudaStream_t st, uint64_t wait_ns) {
     const int cols = s.n_q_heads / s.n_kv_heads * ntok;
@@ -993,7 +993,8 @@ cudaError_t launch_kv4_decode(const Shape& s, const uint16_t* q, const uint16_t*
         a.out = out + tok * s.n_q_heads * D;
         a.k_new = k_new + tok * s.n_kv_heads * D;
         a.v_new = v_new + tok * s.n_kv_heads * D;
-        a.d_hist = d_hist + b0;
+        a.d_hist = d_hist == nullptr ? nullptr : d_hist + b0;
+        a.hist = hist;
         a.lp = kv4_slots(s.max_len);
         const size_t slots = heads * a.lp;
         a.c = Kv4Cache{c.k_codes + slots * (D / 2), c.k_scales + slots * (D / kKv4Group), c.v_codes + slots * (D / 2),

@@ -85,6 +85,28 @@ def test_append_of_special_values(D):
             assert ((got == want) | (np.isnan(got) & np.isnan(want))).all(), f"token {t}"
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_append_of_ranges_that_float_rounds_off(D):
+    """Groups whose range is 15 times a scale but for a far smaller value of the other sign, either way round."""
+    n, Hkv, L = 40, 1, 64
+    r = np.random.default_rng(5)
+    f = r.uniform(-0.2, 0.2, (1, n, Hkv, D // 32, 32))
+    big = 15.0 * r.integers(8, 16, (1, n, Hkv, D // 32)) * 2.0 ** r.integers(-6, 3, (1, n, Hkv, D // 32))
+    f *= big[..., None]
+    f[..., 1::2] = np.abs(f[..., 1::2])
+    for i in range(n):  # all of one sign, then one value of the other far below it (or none)
+        sign = 1.0 if i % 2 else -1.0
+        f[0, i] = sign * np.abs(f[0, i])
+        f[0, i, :, :, 7] = sign * big[0, i]
+        f[0, i, :, :, 9] = -sign * big[0, i] * 2.0 ** -(20 + i) * (i % 5 > 0)
+    v = K.f32_to_bf16(f.reshape(1, n, Hkv, D))
+    attn = context(1, Hkv, Hkv, D, L)
+    ref = K.Cache(1, Hkv, slots(L), D)
+    cache = U.to_dev(ref, L)
+    run_append(attn, cache, ref, f"round{D}", 0, n, None, v)
+    U.same_cache(cache, ref, "append")
+
+
 @pytest.mark.parametrize("B,Hkv,D,L,first,count", [
     (1, 1, 64, 1, 0, 1), (2, 3, 128, 100, 37, 63), (1, 8, 128, 2048, 0, 2048), (3, 2, 64, 130, 129, 1),
     (2, 2, 128, 65, 3, 0),

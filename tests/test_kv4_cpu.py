@@ -107,6 +107,30 @@ def test_float_scale_is_exact():
             assert Fraction(float(below)) < d
 
 
+def test_float_scale_from_a_low_quotient_is_exact():
+    """The same with a product by a constant 1 to 2 parts in 2^22 below 1 / 7.5 in place of the quotient."""
+    c = F(0.133333295)
+    assert -2.0 < (float(c) * 7.5 - 1) * 2 ** 22 < -1.0
+    r = np.random.default_rng(3)
+    hi = K.bf16_to_f64(K.f32_to_bf16(np.abs(r.normal(size=20000)) * 2.0 ** r.integers(-20, 20, 20000)))
+    lo = -K.bf16_to_f64(K.f32_to_bf16(np.abs(r.normal(size=20000)) * 2.0 ** r.integers(-20, 20, 20000)))
+    lo[:6000] = 0
+    hi[:3000] = 15 * r.integers(8, 16, 3000) * 2.0 ** r.integers(-8, 4, 3000)
+    lo[3000:6000] = -15 * r.integers(8, 16, 3000) * 2.0 ** r.integers(-8, 4, 3000)
+    lo[1500:3000] = -2.0 ** -30
+    keep = (K.bf16_to_f64(K.f32_to_bf16(hi)) == hi) & (K.bf16_to_f64(K.f32_to_bf16(lo)) == lo)
+    hi, lo = hi[keep], lo[keep]
+    up = (((F(hi) * F(0.5) - F(lo) * F(0.5)) * c).view(np.uint32) + np.uint32(0xFFFFF)) & np.uint32(0xFFF00000)
+    h, n = F(hi) * F(0.5), F(-lo) * F(0.5)
+    up += (np.maximum(h, n) - up.view(np.float32) * F(7.5) > -np.minimum(h, n)).astype(np.uint32) << np.uint32(20)
+    got = up.view(np.float32).astype(np.float64)
+    for g, h, l in zip(got, hi, lo):
+        d = (Fraction(h) - Fraction(l)) / 15
+        m, e = np.frexp(g)
+        below = np.ldexp(m * 16 - 1, e - 4) if m > 0.5 else np.ldexp(15.0, e - 5)
+        assert Fraction(g) >= d > Fraction(float(below))
+
+
 def test_refusals_without_a_context():
     from paper_2607_15865_gb300 import _lib, build
     build.build()
