@@ -191,6 +191,93 @@ def test_decode_long(B, Hq, Hkv, D, L, hist, n):
     run_decode(attn, U.history(f"long{B}{D}", B, Hkv, slots(L), D, hist), f"long{B}{D}", hist, n)
 
 
+def ramp(B, top):
+    """Lengths 0 .. top, the long ones not all at one end."""
+    return [top * ((i * 7) % B) // (B - 1) for i in range(B)]
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,D,L,hist,n", [
+    # few items, cut into pieces in proportion to the lengths
+    (6, 8, 2, 128, 1500, ramp(6, 1499), 1), (31, 2, 1, 64, 900, ramp(31, 890), 3), (1, 64, 64, 128, 200, [150], 1),
+    # more items than half the SMs: equal runs, which begin and end inside items
+    (12, 16, 8, 128, 1300, ramp(12, 1299), 1), (12, 16, 8, 64, 2500, ramp(12, 2400), 1),
+    (12, 16, 8, 128, 700, ramp(12, 690), 8), (20, 32, 8, 64, 600, ramp(20, 590), 4),
+    (40, 4, 4, 128, 400, [399 - i for i in range(40)], 1), (5, 16, 16, 64, 4000, [3999, 0, 31, 3000, 64], 1),
+    (90, 2, 1, 128, 100, ramp(90, 99), 1),
+    # several launches
+    (130, 2, 1, 64, 150, ramp(130, 149), 1), (129, 2, 2, 128, 70, ramp(129, 66), 2),
+    # column groups of one kv head
+    (3, 16, 1, 128, 300, [250, 0, 100], 5), (7, 32, 4, 64, 200, ramp(7, 180), 16),
+])
+def test_decode_cuts(B, Hq, Hkv, D, L, hist, n):
+    attn = context(B, Hq, Hkv, D, L)
+    run_decode(attn, U.history(f"cut{B}{Hkv}{D}", B, Hkv, slots(L), D, hist), f"cut{B}{Hq}{D}{n}", hist, n)
+
+
+@pytest.mark.parametrize("B,Hkv", [(3, 2), (11, 8)])
+def test_decode_with_nothing_to_do(B, Hkv):
+    """Every length outside the cache: all skipped and flagged."""
+    attn = context(B, 2 * Hkv, Hkv, 128, 64)
+    hist = [64] * B
+    out = run_decode(attn, U.history("none", B, Hkv, 64, 128, hist), "none", hist, 1)
+    assert (out == 7).all()
+
+
+def test_decode_leaves_its_counters_for_the_next_call():
+    """Shared items merged again and again, by calls of several shapes and with attn_decode between them."""
+    import torch
+    attn = context(2, 8, 2, 128, 3000)
+    hist = [2999, 1700]
+    ref = U.history("again", 2, 2, slots(3000), 128, hist)
+    kc = torch.zeros(2, 2, 3000, 128, dtype=torch.bfloat16, device="cuda")
+    q, k, v = (U.dev_bf16(x) for x in U.new_tokens("again", 2, 1, 8, 2, 128))
+    lens = torch.tensor([100, 2000], dtype=torch.int32, device="cuda")
+    for i in range(3):
+        run_decode(attn, U.copy(ref), f"again{i}", [h - i for h in hist], 1 + i)
+        attn.decode(q, k, v, lens, kc, kc.clone())
+
+
+def test_decode_in_a_graph():
+    import torch
+    attn = context(1, 8, 2, 128, 600)
+    ref = U.history("graph", 1, 2, slots(600), 128, [500])
+    cache = U.to_dev(ref, 600)
+    q, k, v = U.new_tokens("graph", 1, 1, 8, 2, 128)
+    dq, dk, dv = (U.dev_bf16(x) for x in (q, k, v))
+    lens = torch.tensor([500], dtype=torch.int32, device="cuda")
+    out = torch.empty_like(dq)
+    attn.kv4_decode(dq, dk, dv, lens, cache, out=out)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        attn.kv4_decode(dq, dk, dv, lens, cache, out=out)
+    tab = K.tables(600, 128, attn.rope_theta)
+    for step in range(3):
+        out.zero_()
+        lens.fill_(500 + step)
+        g.replay()
+        torch.cuda.synchronize()
+        pos = np.array([500 + step])
+        ref.write(0, pos, K.rope(k[0], pos, tab), v[0])
+        U.close(out[0], *K.attend(K.rope(q[0], pos, tab), pos, ref, 0), f"replay {step}")
+    U.same_cache(cache, ref, "graph")
+
+
+def test_decode_wait_that_runs_out():
+    """With a limit of 1 ns the wait for the new tokens' rows may run out: the call returns and says so at most, and
+    the next one, with the default limit, is right."""
+    attn = context(1, 8, 2, 128, 300)
+    ref = U.history("limit", 1, 2, slots(300), 128, [250])
+    import torch
+    q, k, v = (U.dev_bf16(x) for x in U.new_tokens("limit", 1, 16, 8, 2, 128))
+    lens = torch.tensor([250], dtype=torch.int32, device="cuda")
+    attn.set_wait_limit(1)
+    attn.kv4_decode(q, k, v, lens, U.to_dev(ref, 300))
+    assert attn.device_error() in (0, 2)
+    attn.set_wait_limit(0)
+    run_decode(attn, ref, "limit", [250], 16)
+
+
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("n", [1, 3])
 def test_decode_skips_and_flags_lengths_outside(D, n):
@@ -276,6 +363,9 @@ def run_prefill(attn, cache, ref, tag, hist, n, workspace=None, what="prefill"):
 @pytest.mark.parametrize("B,Hq,Hkv,D,L,hist,n", [
     (1, 4, 2, 64, 32, 0, 16), (1, 4, 2, 64, 32, 16, 8), (1, 1, 1, 128, 1, 0, 1), (2, 14, 2, 128, 300, 77, 130),
     (1, 16, 1, 64, 700, 500, 77), (3, 5, 5, 128, 260, 1, 259), (1, 28, 4, 128, 512, 0, 300),
+    # short chunks, through the decode and (33 columns, and 32 over a short history) the workspace
+    (2, 8, 2, 128, 2200, 2100, 4), (2, 8, 2, 128, 2200, 2100, 8), (1, 6, 2, 64, 2200, 2150, 11), (1, 8, 2, 128, 300, 280, 8),
+    (3, 4, 1, 64, 64, 0, 4), (12, 8, 8, 128, 100, 99, 1),
 ])
 def test_prefill(B, Hq, Hkv, D, L, hist, n):
     attn = context(B, Hq, Hkv, D, L)
