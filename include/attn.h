@@ -430,7 +430,7 @@ int attn_w4bf16_rows_per_launch(int K);
  * Whatever attends to a token sees the values its slot stands for, the token itself included, so
  * a prompt's outputs do not depend on how it is cut into chunks (up to the order of float sums).  Slots past
  * the tokens written may hold anything.  The calls enqueue on `stream`, allocate nothing and use the
- * context's scratch as the other stages do.
+ * context's scratch as the other stages do; their kernels are not in attn_timing_read but for flash_fwd.
  */
 typedef struct attn_kv4 {
     uint8_t* k_codes;
@@ -445,7 +445,7 @@ int attn_kv4_slots(int max_len);
 
 /* Quantise chunk_len new tokens (k, v [batch][chunk_len][n_kv_heads][head_dim], k before RoPE) into slots
  * hist_len .. hist_len + chunk_len - 1 of every sequence; no other slot is written.  hist_len >= 0, chunk_len
- * >= 1, hist_len + chunk_len <= max_len.  Returns ATTN_OK, ATTN_EINVAL or ATTN_ECUDA. */
+ * >= 1, hist_len + chunk_len <= max_len, batch * chunk_len * n_kv_heads * head_dim / 16 below 2^31 - 256.  Returns ATTN_OK, ATTN_EINVAL or ATTN_ECUDA. */
 int attn_kv4_append(attn_ctx* ctx, const uint16_t* k, const uint16_t* v, int hist_len, int chunk_len,
                     const attn_kv4* cache, attn_stream_t stream);
 
@@ -455,16 +455,20 @@ int attn_kv4_read(attn_ctx* ctx, const attn_kv4* cache, int first, int count, ui
                   attn_stream_t stream);
 
 /* attn_decode_multi over a 4-bit cache: n_new (1 .. 16) tokens per sequence at positions d_hist_len[b] + i are
- * quantised into their slots and attend to slots [0, d_hist_len[b] + i].  A sequence with a position
- * outside [0, max_len - 1] is skipped (cache and out not written) and sets ATTN_DEVERR_HIST_RANGE.  The other
- * arguments and the errors are those of attn_decode_multi. */
+ * quantised into their slots and attend to slots [0, d_hist_len[b] + i], at either head_dim and any n_new of
+ * those.  A sequence with a position outside [0, max_len - 1] is skipped (cache and out not written) and sets
+ * ATTN_DEVERR_HIST_RANGE.  The products take the values 2^-73 as large, in bf16: a group of scale 2^67 or more
+ * (values from about 2^67) comes out infinite or NaN, and one under 2^-53 loses bits below 2^-60.  The other arguments
+ * and the errors are those of attn_decode_multi. */
 int attn_kv4_decode(attn_ctx* ctx, const uint16_t* q, const uint16_t* k, const uint16_t* v,
                     const int32_t* d_hist_len, int n_new, const attn_kv4* cache, uint16_t* out, attn_stream_t stream);
 
 /* attn_prefill_kv over a 4-bit cache (hist_len = 0: a prefill): the chunk is quantised into its slots and attends
  * causally to slots [0, hist_len + i].  workspace: device memory of at least attn_kv4_workspace(ctx,
  * hist_len + chunk_len) bytes, 256-byte aligned, which holds the bf16 values of those slots during the call
- * (one workspace serves every layer).  The other arguments and the errors are those of attn_prefill_kv. */
+ * (one workspace serves every layer).  A chunk of a few tokens goes through attn_kv4_decode's kernel where that is
+ * the faster (with that call's range of values), and leaves the workspace alone.  batch * chunk_len * n_kv_heads *
+ * head_dim / 16 below 2^31 - 256.  The other arguments and the errors are those of attn_prefill_kv. */
 size_t attn_kv4_workspace(const attn_ctx* ctx, int tokens);
 int attn_kv4_prefill_kv(attn_ctx* ctx, const uint16_t* q, const uint16_t* k, const uint16_t* v, int hist_len,
                         int chunk_len, const attn_kv4* cache, uint16_t* out, void* workspace, size_t workspace_bytes,
