@@ -445,7 +445,8 @@ int attn_kv4_slots(int max_len);
 
 /* Quantise chunk_len new tokens (k, v [batch][chunk_len][n_kv_heads][head_dim], k before RoPE) into slots
  * hist_len .. hist_len + chunk_len - 1 of every sequence; no other slot is written.  hist_len >= 0, chunk_len
- * >= 1, hist_len + chunk_len <= max_len, batch * chunk_len * n_kv_heads * head_dim / 16 below 2^31 - 256.  Returns ATTN_OK, ATTN_EINVAL or ATTN_ECUDA. */
+ * >= 1, hist_len + chunk_len <= max_len, batch * chunk_len * n_kv_heads * head_dim / 16 below 2^31 - 256.
+ * Returns ATTN_OK, ATTN_EINVAL or ATTN_ECUDA. */
 int attn_kv4_append(attn_ctx* ctx, const uint16_t* k, const uint16_t* v, int hist_len, int chunk_len,
                     const attn_kv4* cache, attn_stream_t stream);
 
@@ -467,8 +468,10 @@ int attn_kv4_decode(attn_ctx* ctx, const uint16_t* q, const uint16_t* k, const u
  * causally to slots [0, hist_len + i].  workspace: device memory of at least attn_kv4_workspace(ctx,
  * hist_len + chunk_len) bytes, 256-byte aligned, which holds the bf16 values of those slots during the call
  * (one workspace serves every layer).  A chunk of a few tokens goes through attn_kv4_decode's kernel where that is
- * the faster (with that call's range of values), and leaves the workspace alone.  batch * chunk_len * n_kv_heads *
- * head_dim / 16 below 2^31 - 256.  The other arguments and the errors are those of attn_prefill_kv. */
+ * the faster (with that call's range of values), and leaves the workspace alone.  Otherwise a NaN or an infinity
+ * in a token's v makes its values NaN for the tokens of the chunk just before it (those of its tile) too, as in
+ * attn_prefill_kv.  batch * chunk_len * n_kv_heads * head_dim / 16 below 2^31 - 256.  The other arguments and the
+ * errors are those of attn_prefill_kv. */
 size_t attn_kv4_workspace(const attn_ctx* ctx, int tokens);
 int attn_kv4_prefill_kv(attn_ctx* ctx, const uint16_t* q, const uint16_t* k, const uint16_t* v, int hist_len,
                         int chunk_len, const attn_kv4* cache, uint16_t* out, void* workspace, size_t workspace_bytes,

@@ -309,7 +309,12 @@ __device__ __forceinline__ int search(const int* sums, int batch, int hc, int r)
     return lo;
 }
 
-// The merge of up to N parts (m, l, o[4]) with a running (m, l, o[4]); parts of weight 0 are left out.
+// The maximum that a part is merged by: NaN where its sum is (then its scores may be NaN throughout, and m -inf as if
+// it had none).  -inf: no slot of the part is seen.
+__device__ __forceinline__ float mark(float m, float l) { return l != l ? l : m; }
+
+// The merge of up to N parts (m, l, o[4]) with a running (m, l, o[4]); parts without a slot are left out, those of weight
+// 0 are not (0 times a NaN).
 struct Merged {
     float m = -INFINITY, l = 0.f, o[4] = {};
     template <int N>
@@ -324,8 +329,8 @@ struct Merged {
         for (int e = 0; e < 4; ++e) o[e] *= f0;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
+            if (ml[i].x == -INFINITY) continue;
             const float f = exp2_fast(ml[i].x - mu);
-            if (f == 0.f) continue;
             l += f * ml[i].y;
             o[0] += f * x[i].x;
             o[1] += f * x[i].y;
@@ -604,7 +609,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
             if (subs > 1) {
                 if (sub > 0 && sub < subs) {
                     s_x[tid] = make_float4(acc.o[0], acc.o[1], acc.o[2], acc.o[3]);
-                    s_y[tid] = make_float2(acc.m, acc.l);
+                    s_y[tid] = make_float2(mark(acc.m, acc.l), acc.l);
                     if (nan < kNone) atomicMin(&s_nan[d / kKv4Group], nan);
                 }
                 __syncthreads();
@@ -859,7 +864,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
                         *reinterpret_cast<float4*>(dst + 4 * i) =
                             make_float4(o[n][2 * i][e], o[n][2 * i][2 + e], o[n][2 * i + 1][e], o[n][2 * i + 1][2 + e]);
                 }
-                if (g == 0) s_ml[col] = make_float2(m[n][e] * a.scale_log2, sum[n][e]);
+                if (g == 0) s_ml[col] = make_float2(mark(m[n][e] * a.scale_log2, sum[n][e]), sum[n][e]);
             }
         w = now;
         final_turn = !following(w.b, w.item, w.T, w.base, w.hi);
@@ -885,8 +890,8 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
             const float mu = mx == -INFINITY ? 0.f : mx;
 #pragma unroll
             for (int w = 0; w < W; ++w) {
+                if (f[w] == -INFINITY) continue;  // a warp without blocks wrote nothing else
                 f[w] = exp2_fast(f[w] - mu);
-                if (f[w] == 0.f) continue;  // a warp without blocks wrote nothing else
                 l += f[w] * s_ml[w * C::COLS + col].y;
                 const float* x = s_o + (w * C::COLS + col) * C::OS + d;
 #pragma unroll
@@ -904,7 +909,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
                 float* dst = a.part_o + (static_cast<size_t>(part) * 16 + col) * D + d;
 #pragma unroll
                 for (int e = 0; e < V; e += 2) *reinterpret_cast<float2*>(dst + e) = make_float2(acc[e], acc[e + 1]);
-                if (d == 0) reinterpret_cast<float2*>(a.part_ml)[part * 16 + col] = make_float2(mx, l);
+                if (d == 0) reinterpret_cast<float2*>(a.part_ml)[part * 16 + col] = make_float2(mark(mx, l), l);
             }
         }
         if (j0 != j1 && tid < 4) a.part_nan[4 * part + tid] = s_nan[tid];

@@ -330,6 +330,42 @@ def test_decode_nan_in_the_history(D):
 
 
 @pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hkv,hist", [
+    (2, [400, 300]),
+    (2, [5000, 700]),      # parts of several CTAs
+    (64, [400, 1500, 5]),  # runs over items
+])
+@pytest.mark.parametrize("n", [1, 9])
+def test_decode_nan_in_many_neighbouring_keys(D, Hkv, hist, n):
+    """Stretches of the history in which every key is NaN, one that a whole part consists of among them."""
+    L, B = max(hist) + 20, len(hist)
+    attn = context(B, 2 * Hkv, Hkv, D, L)
+    ref = U.history(f"nans{D}", B, Hkv, slots(L), D, hist)
+    ref.scales[0][0, 0, 64:128] = K.NAN_SCALE
+    ref.scales[0][0, Hkv - 1, :hist[0] // 2] = K.NAN_SCALE
+    out = run_decode(attn, ref, f"nans{D}", hist, n)
+    assert out[0, :, :2].isnan().all() and out[0, :, -2:].isnan().all() and not out[1:].isnan().any()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hkv,hist", [(1, 100), (1, 5000), (80, 700)])
+def test_decode_nan_of_a_value_whose_weight_is_next_to_nothing(D, Hkv, hist):
+    """A NaN v is seen whatever its weight: the new key is so near to the first head's q that all others weigh less
+    than 2^-150 there (what they add to the other values is less than a float holds, and is not compared)."""
+    import torch
+    attn = context(1, 2 * Hkv, Hkv, D, hist + 1)
+    tag = f"faint{D}"
+    ref = U.history(tag, 1, Hkv, slots(hist + 1), D, [hist])
+    ref.scales[1][0, :, 3, 0] = K.NAN_SCALE
+    q, k, v = U.new_tokens(tag, 1, 1, 2 * Hkv, Hkv, D)
+    k = K.f32_to_bf16(20.0 * K.bf16_to_f64(q)[:, :, ::2])
+    lens = torch.tensor([hist], dtype=torch.int32, device="cuda")
+    out = attn.kv4_decode(U.dev_bf16(q), U.dev_bf16(k), U.dev_bf16(v), lens, U.to_dev(ref, hist + 1))
+    assert out[..., :32].isnan().all() and not out[..., 32:].isnan().any()
+    assert attn.device_error() == 0
+
+
+@pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("Hq,n", [(2, 4), (8, 5)])
 def test_decode_nan_in_a_new_token_reaches_only_later_ones(D, Hq, n):
     """Token 2's infinite k and NaN v are seen by tokens 2 .. n - 1 and not by 0 and 1."""
