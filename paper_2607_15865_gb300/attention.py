@@ -57,6 +57,15 @@ def _stream(stream) -> int:
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
+def _empty(shape, dtype, like, stream) -> torch.Tensor:
+    """Memory that the allocator holds for `stream`, on which a call given one uses it: from the current stream's
+    pool it could still be in use there, or be handed out again while the call runs."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
 def _is_len(t, batch: int) -> bool:
     return (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == torch.int32 and t.is_contiguous()
             and t.shape == (batch,))
@@ -271,7 +280,7 @@ class Attention:
         ref = self._kv4(cache)
         shape = (self.batch, self.n_kv_heads, max(count, 0), self.head_dim)
         if out is None:
-            out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=cache.k_codes.device) for _ in range(2))
+            out = tuple(_empty(shape, torch.bfloat16, cache.k_codes, stream) for _ in range(2))
         k, v = out
         rc = self.lib.attn_kv4_read(self._ctx, ref, int(first), count, _ptr(k, "k", shape), _ptr(v, "v", shape),
                                     _stream(stream))
@@ -287,7 +296,7 @@ class Attention:
             raise TypeError("hist_len must be a contiguous int32 CUDA tensor of shape [batch]")
         args = _ptr(q, "q", qs), _ptr(k, "k", ks), _ptr(v, "v", ks)
         if out is None:
-            out = torch.empty_like(q)
+            out = torch.empty_like(q) if stream is None else _empty(q.shape, q.dtype, q, stream)
             o = out.data_ptr()
         else:
             o = _ptr(out, "out", qs)
@@ -309,11 +318,11 @@ class Attention:
         args = (_ptr(q, "q", qs), _ptr(k, "k", ks), _ptr(v, "v", ks))
         need = self.kv4_workspace(int(hist_len) + S)
         if workspace is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            workspace = _empty(need, torch.uint8, q, stream)
         if not (isinstance(workspace, torch.Tensor) and workspace.is_cuda and workspace.dtype == torch.uint8
                 and workspace.is_contiguous() and workspace.numel() >= need):
             raise TypeError(f"workspace must be a contiguous uint8 CUDA tensor of at least {need} bytes")
-        out = self._new_out(q, out)
+        out = _empty(q.shape, q.dtype, q, stream) if out is None else out
         rc = self.lib.attn_kv4_prefill_kv(self._ctx, *args, int(hist_len), S, self._kv4(cache), _ptr(out, "out", qs),
                                           workspace.data_ptr(), workspace.numel(), _stream(stream))
         self._check(rc, "attn_kv4_prefill_kv")

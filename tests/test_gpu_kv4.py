@@ -445,6 +445,33 @@ def test_the_cache_is_the_bf16_cache_quantised():
         assert (scales[:, :, :200].cpu().numpy().view(np.uint16) == s).all(), "kv"[t]
 
 
+def test_memory_that_a_call_allocates_belongs_to_its_stream():
+    """A workspace and outputs allocated by calls on another stream are not memory that the current stream still
+    writes to."""
+    import torch
+    attn = context(1, 8, 2, 128, 1000)
+    ref = U.history("pool", 1, 2, slots(1000), 128, [500])
+    q, k, v = U.new_tokens("pool", 1, 300, 8, 2, 128)
+    dq, dk, dv = U.dev_bf16(q), U.dev_bf16(k), U.dev_bf16(v)
+    a, b = U.to_dev(ref, 1000), U.to_dev(ref, 1000)
+    want = attn.kv4_prefill_kv(dq, dk, dv, 500, a)
+    want_k, want_v = attn.kv4_read(a)
+    sizes = [attn.kv4_workspace(800), want.nbytes, want_k.nbytes, want_v.nbytes]
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    blocks = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes]
+    for cycles in (1, 200_000_000):  # 0.1 s, and then the writes (once before, to have the kernels loaded)
+        torch.cuda._sleep(cycles)
+        for x in blocks:
+            x.fill_(0x7F)
+    del blocks, x
+    out = attn.kv4_prefill_kv(dq, dk, dv, 500, b, stream=st)
+    got_k, got_v = attn.kv4_read(b, stream=st)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(got_k[:, :, :800], want_k[:, :, :800])
+    assert torch.equal(got_v[:, :, :800], want_v[:, :, :800])
+
+
 def test_calls_on_another_stream():
     import torch
     attn = context(1, 8, 2, 128, 500)
