@@ -7,11 +7,13 @@
 //                    in proportion to the lengths: CTAs of all the warps that an SM's registers hold, so that
 //                    an item has few parts to merge
 //   many             the blocks of all items, in order, in equal runs, whatever the lengths: each item counts
-//                    kItemCost blocks more than it has, for what it costs to begin and to end one.  CTAs of
-//                    four warps, several per SM: while one begins or ends an item the others walk
+//                    kItemCost blocks more than it has, for what it costs to begin and to end one; or in whole items,
+//                    where they are short or about as many as the CTAs.  CTAs of four warps, several per SM: while
+//                    one begins or ends an item the others walk
 // Within a CTA the warps take an item's blocks in turn, each through a private ring of two stages, filled by
 // cp.async (ten 16-byte copies per lane; as four bulk copies and an mbarrier a block cost 50 instructions
-// more), and with its own running maximum, sum and accumulators; they meet once per item, in shared memory.  An item that several CTAs share is merged by the last of them to finish, in a fixed order.
+// more), and with its own running maximum, sum and accumulators; they meet once per item, in shared memory.  An
+// item that several CTAs share is merged by the last of them to finish, in a fixed order.
 //
 // Per 16 slots, with mma.sync m16n8k16 (A from registers: a tcgen05 operand would have to be written
 // back to shared or tensor memory at four times the packed bytes, for products 8 or 16 columns wide):
@@ -49,7 +51,13 @@ namespace attn {
 namespace {
 
 constexpr int kMaxSeqs = 128;   // sequences of one launch (their block counts are summed in shared memory)
-constexpr int kItemCost = 16;    // blocks
+// Blocks that it costs a CTA to begin and end an item.  Calls in a graph (32 / 8 heads of 128 values, us) with 0, 8, 16, 32:
+// 16 sequences of mixed lengths 33.1, 26.6, 24.5, 25.5; of 8191 40.2, 38.4, 37.2, 38.3; of 1024 16.4, 12.7, 13.2, 14.7.
+constexpr int kItemCost = 16;
+// Blocks of a piece, unless the item is but one: a merge takes 2 us or more, a block of each warp 0.5.  One sequence of 300, 500
+// and 700 tokens 5.4, 6.2 and 7.1 us in one piece, 7.7, 8.1 and 8.2 in several; 1000 in either 8.0; with 16 columns 400
+// tokens 8.5 and 10.4.  Pieces of 8 blocks at least took 8.3 for 1000 tokens, of 2 as long as of 4.
+constexpr int kMinBlocks = 4;
 constexpr int kMaxNew = 16;     // new tokens per sequence
 constexpr int kNone = 1 << 20;  // no new token with a NaN group
 
@@ -60,6 +68,9 @@ struct Cfg {
     static constexpr int W = !WIDE ? 4 : NT == 1 ? 16 : 8;  // warps
     static constexpr int CTAS = WIDE ? 1 : NT == 1 ? 4 : D == 128 ? 2 : 3;  // per SM: what registers and shared memory allow
     static constexpr int THREADS = 32 * W;
+    static constexpr int ALONE = NT == 1 ? 24 : 16;   // pieces: an item of up to so many blocks is one (see kMinBlocks)
+    static constexpr int EXCESS = NT == 1 ? 20 : 32;  // runs: blocks that a CTA may have more than its run, where that
+    static constexpr int LONGEST = NT == 1 ? 36 : 48; // saves all merges, and the longest item of mixed ones (below)
     static constexpr int BATCH = NT == 1 ? 8 : WIDE ? 20 : D == 128 ? 16 : 12;  // parts that a merging thread loads at once
     static constexpr int KB = 32 * 128 / D;      // slots per block
     static constexpr int ROW = D / 2;            // bytes of a slot's codes
@@ -190,7 +201,7 @@ struct Args {
     int* err;
     uint64_t wait_ns;
     float scale_log2, move;  // log2 e / sqrt D in units of 2^-73, and the lead of a score that moves the maximum (2^8)
-    int batch, ntok, Hq, Hkv, max_len, lp, ncg, min_blocks, hist;
+    int batch, ntok, Hq, Hkv, max_len, lp, ncg, hist;
 };
 
 // One warp: quantise the E = D / 32 values of a row that each lane holds (bf16 pairs; with E = 2 one pair), write
@@ -267,14 +278,14 @@ __device__ __forceinline__ int small_ceil_div(int x, int y) { return small_div(x
 // least target (of 32 tried) for which the pieces are at most per for each of the hc items of a sequence.  Lane b
 // holds the blocks T of an item of sequence b (0: skipped).  The item's block 0 .. : T, hist, lo, hi; base:
 // the piece, c0: the pieces of the item (0: there is no piece `cta`).
-__device__ __forceinline__ Segment piece_of(int T, int hist, int hc, int per, int min_blocks, int cta, int lane) {
+__device__ __forceinline__ Segment piece_of(int T, int hist, int hc, int per, int alone, int cta, int lane) {
     Segment w = {};
     const uint32_t live = __ballot_sync(0xFFFFFFFFu, T > 0);
     const int items = __popc(live), sum = __reduce_add_sync(0xFFFFFFFFu, T), longest = __reduce_max_sync(0xFFFFFFFFu, T);
     if (items == 0) return w;
-    int target = max(min_blocks, small_ceil_div(longest, small_div(per, items)));  // fits
+    int target = max(kMinBlocks, small_ceil_div(longest, small_div(per, items)));  // fits
     if (longest * items != sum) {
-        const int least = max(min_blocks, (sum + per - 1) / per);  // no less fits
+        const int least = max(kMinBlocks, (sum + per - 1) / per);  // no less fits
         const int mine = least + (((target - least) * lane) >> 5);
         int pieces = 0;
         for (uint32_t rest = live; rest != 0; rest &= rest - 1)
@@ -282,7 +293,7 @@ __device__ __forceinline__ Segment piece_of(int T, int hist, int hc, int per, in
         const uint32_t fits = __ballot_sync(0xFFFFFFFFu, pieces <= per);
         if (fits != 0) target = __shfl_sync(0xFFFFFFFFu, mine, __ffs(fits) - 1);
     }
-    const int n = T > 0 ? small_ceil_div(T, target) : 0, upto = warp_scan(n, lane);
+    const int n = T <= alone ? (T > 0 ? 1 : 0) : small_ceil_div(T, target), upto = warp_scan(n, lane);
     const uint32_t past = __ballot_sync(0xFFFFFFFFu, T > 0 && upto * hc > cta);
     if (past == 0) return w;
     w.b = __ffs(past) - 1;
@@ -386,12 +397,13 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
     Segment first;
     int stop = 0, each = 0, more = 0;  // runs: CTA j has each blocks, the first `more` one more
     int n = 0;                         // pieces of an item
+    bool alone = false;                // runs of whole items
     auto hist_of = [&](int b, int T) { return T * KB - s_free[b] - a.ntok; };
     if (WIDE && a.batch > 1) {
         if (warp == 0) {
             int h = 0;
             const int T = lane < a.batch ? blocks_of(lane, h) : 0;
-            first = piece_of(T, h, hc, static_cast<int>(gridDim.x) / hc, a.min_blocks, cta, lane);
+            first = piece_of(T, h, hc, static_cast<int>(gridDim.x) / hc, C::ALONE, cta, lane);
             if (lane == 0) segs[0] = first;
         }
         __syncthreads();
@@ -401,7 +413,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
     } else if (WIDE) {
         const int T = blocks_of(0, first.hist), per = static_cast<int>(gridDim.x) / hc;
         if (T == 0) return;
-        n = small_ceil_div(T, max(a.min_blocks, small_ceil_div(T, per)));
+        n = T <= C::ALONE ? 1 : small_ceil_div(T, max(kMinBlocks, small_ceil_div(T, per)));
         first.b = 0;
         first.T = T;
         first.item = small_div(cta, n);
@@ -422,29 +434,68 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
             __syncthreads();
         }
         if (warp == 0) {
-            int sum = 0;
+            int sum = 0, most = 0;
+            uint32_t least = ~0u;
             for (int b0 = 0; b0 < a.batch; b0 += 32) {
                 int v = 0;
                 if (b0 + lane < a.batch) v = a.batch > 32 ? pre[b0 + lane + 1] : cost_of(lane);
+                most = max(most, v);
+                if (v > 0) least = min(least, static_cast<uint32_t>(v));
                 v = warp_scan(v, lane);
                 if (b0 + lane < a.batch) pre[b0 + lane + 1] = sum + v;
                 sum += __shfl_sync(0xFFFFFFFFu, v, 31);
             }
-            if (lane == 0) pre[0] = 0;
+            most = __reduce_max_sync(0xFFFFFFFFu, most);
+            least = __reduce_min_sync(0xFFFFFFFFu, least);
+            if (lane == 0) {
+                pre[0] = 0;
+                flag[0] = most;
+                flag[1] = least == static_cast<uint32_t>(most);
+            }
         }
         __syncthreads();
         const int total = pre[a.batch] * hc;
-        const int nc = min(static_cast<int>(gridDim.x), (total + a.min_blocks - 1) / a.min_blocks);
+        const int nc = min(static_cast<int>(gridDim.x), (total + kMinBlocks - 1) / kMinBlocks);
         if (cta >= nc) return;
         each = total / nc;
         more = total - each * nc;
-        const int r0 = cta * each + min(cta, more);
-        stop = r0 + each + (cta < more ? 1 : 0);
-        first.b = search(pre, a.batch, hc, r0);
-        const int whole = pre[first.b + 1] - pre[first.b], rem = r0 - pre[first.b] * hc;
-        first.T = whole - kItemCost;
-        first.item = rem / whole;
-        first.base = r0 - (rem - first.item * whole) + kItemCost;
+        // Whole items, one run's worth or so for each CTA, where the CTA with the most has little more than its run.  Even
+        // lengths (32 / 8 heads, us): 64 x 200 tokens 15.4 cut and 10.1 whole, 64 x 1000 27.6 and 23.4, 16 x 200 10.6 and
+        // 8.7; but 16 x 500, with an excess of 25, 11.5 and 12.0, and 16 x 1000 13.2 and 18.0.  Mixed lengths
+        // add up to more: 64 x 1 .. 300 14.9 and 11.3, 128 x 1 .. 600 26.5 and 25.1, 128 x 1 .. 1000 32.3 and 33.2.
+        const int most = flag[0];
+        alone = flag[1] ? small_ceil_div(each, most) * most - each <= C::EXCESS : most <= min(each + C::EXCESS, C::LONGEST);
+        // The ends of the CTA's run, one in the even lanes and one in the odd; for whole items moved to the nearer end of
+        // the item that they are in.
+        int r = cta * each + min(cta, more), b = a.batch, item = 0, rem = 0, whole = 1;
+        if (lane & 1) r += each + (cta < more ? 1 : 0);
+        if (r < total) {
+            b = search(pre, a.batch, hc, r);
+            whole = pre[b + 1] - pre[b];
+            rem = r - pre[b] * hc;
+            item = rem / whole;
+            rem -= item * whole;
+            if (alone) {
+                r -= rem;
+                if (2 * rem >= whole) {
+                    r += whole;
+                    if (++item == hc) {
+                        item = 0;
+                        do ++b;
+                        while (b < a.batch && pre[b + 1] == pre[b]);
+                        if (b < a.batch) whole = pre[b + 1] - pre[b];
+                    }
+                }
+                rem = 0;
+            }
+        }
+        stop = __shfl_sync(0xFFFFFFFFu, r, 1);
+        const int r0 = __shfl_sync(0xFFFFFFFFu, r, 0);
+        if (r0 >= stop) return;
+        first.b = __shfl_sync(0xFFFFFFFFu, b, 0);
+        first.item = __shfl_sync(0xFFFFFFFFu, item, 0);
+        first.T = __shfl_sync(0xFFFFFFFFu, whole, 0) - kItemCost;
+        first.base = r0 - __shfl_sync(0xFFFFFFFFu, rem, 0) + kItemCost;
         first.lo = max(0, r0 - first.base);
         first.hi = min(first.T, stop - first.base);
         if (first.lo >= first.hi) return;  // the run ends in what the item counts beside its blocks
@@ -876,8 +927,8 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
         }
         __syncthreads();
         if (new_from(now) < new_to(now)) new_phase ^= 1u;
-        const int j0 = WIDE ? cta - now.base : cta_of(now.base);  // the CTAs that share the item
-        const int j1 = WIDE ? j0 + n - 1 : cta_of(now.base + now.T - 1);
+        const int j0 = WIDE ? cta - now.base : alone ? cta : cta_of(now.base);  // the CTAs that share the item
+        const int j1 = WIDE ? j0 + n - 1 : alone ? cta : cta_of(now.base + now.T - 1);
         const int part = 2 * cta + (cta == j0 ? 1 : 0);
         for (int u = tid; u < now.ncol * (D / V); u += C::THREADS) {
             const int col = u / (D / V), d = u % (D / V) * V;
@@ -1020,7 +1071,6 @@ cudaError_t launch_kv4_decode(const Shape& s, const uint16_t* q, const uint16_t*
         a.Hkv = s.n_kv_heads;
         a.max_len = s.max_len;
         a.ncg = (cols + 15) / 16;
-        a.min_blocks = is_wide(a, num_sms) ? 8 : 4;
         const cudaError_t e = D == 128 ? (cols <= 8 ? launch_for<128, 1>(a, num_sms, st) : launch_for<128, 2>(a, num_sms, st))
                                        : (cols <= 8 ? launch_for<64, 1>(a, num_sms, st) : launch_for<64, 2>(a, num_sms, st));
         if (e != cudaSuccess) return e;

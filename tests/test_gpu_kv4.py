@@ -174,6 +174,22 @@ def test_decode_lengths(D, hist):
 
 
 @pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [1, 5])
+@pytest.mark.parametrize("hist", [
+    [200] * 20,                                              # one item to a CTA, some without any
+    [90] * 130,                                              # several
+    [(37 * i) % 290 for i in range(40)],                     # mixed
+    [-1, 5, 700, 900] + [60] * 20 + [900, 0, -7],            # with skipped ones, at either end
+    [(53 * i) % 600 if i % 5 else 999 for i in range(150)],
+    [-1] * 20,
+])
+def test_decode_whole_items_for_a_cta(D, n, hist):
+    """Batches whose items go whole to the CTAs, several to one, and such as are cut."""
+    attn = context(len(hist), 8, 4, D, 620)
+    run_decode(attn, U.history(f"wi{D}", len(hist), 4, slots(620), D, [min(max(h, 0), 620) for h in hist]), f"wi{D}", hist, n)
+
+
+@pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("Hq,Hkv,n", [(4, 2, 2), (8, 2, 5), (8, 1, 16), (16, 1, 16), (5, 1, 3), (7, 7, 4), (8, 4, 8),
                                       (14, 2, 11)])
 def test_decode_several_tokens(D, Hq, Hkv, n):
