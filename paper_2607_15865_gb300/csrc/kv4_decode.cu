@@ -185,6 +185,13 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t a) {
     return d;
 }
 
+// Adds to a counter after what this CTA wrote before its last barrier, and before what it reads after its next.
+__device__ __forceinline__ int add_acq_rel(int* p, int v) {
+    int old;
+    asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], %2;" : "=r"(old) : "l"(p), "r"(v) : "memory");
+    return old;
+}
+
 struct Args {
     const uint16_t* q;
     const uint16_t* k_new;
@@ -974,12 +981,10 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
         if (j0 == j1 && held.b < 0) break;
         if (tid == 0) {
             auto last = [&](const Segment& x, int parts) {
-                return atomicAdd(a.counters + static_cast<size_t>(x.b) * hc + x.item, 1) == parts - 1;
+                return add_acq_rel(a.counters + static_cast<size_t>(x.b) * hc + x.item, 1) == parts - 1;
             };
-            __threadfence();  // the parts, and then their counts
             flag[0] = held.b >= 0 && last(held, cta_of(held.base + held.T - 1) - cta_of(held.base) + 1);
             flag[1] = j0 != j1 && last(now, j1 - j0 + 1);
-            __threadfence();  // the counts, and then the others' parts
         }
         __syncthreads();
         if (flag[1]) merge(now, j0, j1);
