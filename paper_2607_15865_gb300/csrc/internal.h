@@ -156,9 +156,10 @@ cudaError_t launch_kv4_append(const Shape& s, const Kv4New& a, const float* cos_
 cudaError_t launch_kv4_read(const Shape& s, int first, int count, const Kv4Cache& c, const Kv4Plain& plain,
                             cudaStream_t st);
 // Decode over the 4-bit cache (kv4_decode.cu): ntok (1 .. 16) new tokens per sequence at positions d_hist[b] + i (without
-// d_hist: hist + i), appended and attended to; a sequence with a position outside the cache is flagged and skipped.  part_o
-// [num_sms * 128][D] and part_ml [num_sms * 144][2] hold the parts of items that CTAs share; counters:
-// an int per item (sequence, kv head, 16 columns) of up to 128 sequences, zero before and after every launch.
+// d_hist: hist + i), appended and attended to; a sequence with a position outside the cache is flagged and skipped.
+// part_o [num_sms * 128][D] and part_ml [num_sms * 144][2] hold the parts of items that CTAs share (16 rows each, two
+// per CTA, four CTAs per SM; the last 32 num_sms ints of part_ml: where NaN of v begins in a part); counters: an
+// int per item (sequence, kv head, 16 columns) of up to 128 sequences, zero before and after every launch.
 cudaError_t configure_kv4_decode();
 cudaError_t launch_kv4_decode(const Shape& s, const uint16_t* q, const uint16_t* k_new, const uint16_t* v_new,
                               const int32_t* d_hist, int hist, int ntok, const Kv4Cache& c, const float* cos_tab,

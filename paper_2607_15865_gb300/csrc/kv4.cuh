@@ -69,9 +69,9 @@ __device__ __forceinline__ uint32_t kv4_scale_of(float hi, float neg) {
     return max(up, 0x00800000u) >> 16;
 }
 
-// rint(x / s) + 0x4B400000 for a bf16 x and the reciprocal inv of a scale, good to a few parts in 2^23: x / s (8 bits over 4) is a tie or at least
-// 2^-10 away from one, so x * inv rounded to a multiple of 2^-11 (by adding 1.5 * 2^12) is the tie itself
-// or on its quotient's side of it, and adding on to 1.5 * 2^23 leaves the integer in the low bits.
+// rint(x / s) + 0x4B400000 for a bf16 x and the reciprocal inv of a scale, good to a few parts in 2^23: x / s (8 bits
+// over 4) is a tie or at least 2^-10 away from one, so x * inv rounded to a multiple of 2^-11 (by adding 1.5 * 2^12) is
+// the tie itself or on its quotient's side of it, and adding on to 1.5 * 2^23 leaves the integer in the low bits.
 __device__ __forceinline__ int kv4_round(float x, float inv) {
     return __float_as_int(__fadd_rn(__fmaf_rn(x, inv, 6144.0f), 12582912.0f - 6144.0f));
 }

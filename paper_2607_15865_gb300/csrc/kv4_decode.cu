@@ -33,6 +33,16 @@
 // what is left of two larger sums.  Rows of ones in place of V^T give the softmax sum, of the same rounded P
 // that weighs V.
 // The running maximum moves lazily: only when a score passes it by 2^8 are O and the sum rescaled.
+// Roundings: q and the new k to bf16 after RoPE, as the bf16 stages round them; a weight P to bf16 (the operand's type; its
+// sum is of the rounded ones); the output.  Scores, maxima, sums and O are floats.
+//
+// What bounds it: instructions, not the 9/8 D bytes of a slot's k or v.  16 slots of a head of 128 values with up to 8
+// columns take 294 warp instructions, 18 of them mma, and 437 cycles of a scheduler, at which the SMs walk about
+// 6 TB/s; over a whole call the ALU pipe is at 49% and the tensor pipe at 24% of the active cycles.  Around the walk a
+// call takes 5 us for one short sequence (launch, lengths, first bytes, the warps' meeting) and about 2 us more where
+// items are shared.  In a graph, 32 / 8 heads of 128 values (in brackets the bytes at 6.77 TB/s), us: 1 x 1 4.8, 1 x 1024
+// 7.4 (0.2), 16 x 1024 12.8 (2.8), 16 x 8191 37.6 (22.3), 64 x 8191 119 (89.4), 4 tokens over 8188 12.2 (1.4); 40 / 8 heads
+// 1 x 32767 14.1 (5.6).  Over the bf16 cache 1 x 1024 7.6, 16 x 8191 79, 64 x 8191 311, 1 x 32767 26.9.
 //
 // The new tokens: a CTA that holds their slots rotates and quantises them, a warp per row, before its own
 // blocks, writes them to the cache and stages them for the warp that has their block.  Slots past the last
@@ -1020,9 +1030,10 @@ cudaError_t configure() {
                                 Cfg<D, NT, WIDE>::BYTES);
 }
 
-// Pieces or runs.  Calls in a graph, 4 query heads per kv head, histories of 8000, pieces against runs: 8 items 9.1
-// and 14.8 us, 32 15.0 and 16.7, 64 21.9 and 23.7, 128 32.9 and 36.3; with mixed lengths up to 8000, which pieces
-// of whole blocks divide worse the fewer there are per item, 64 16.7 and 17.0, 128 28.3 and 24.1.
+// Pieces or runs (the lengths are not known here).  Calls in a graph, 4 query heads per kv head, histories of 8000,
+// pieces against runs: 8 items 9.1 and 14.8 us, 32 15.0 and 16.7, 64 21.9 and 23.7, 128 32.9 and 36.3; with mixed
+// lengths up to 8000, which pieces of whole blocks divide worse the fewer there are per item, 64 16.7 and 17.0,
+// 128 28.3 and 24.1.
 bool is_wide(const Args& a, int num_sms) { return a.batch <= 32 && 2 * a.batch * a.Hkv * a.ncg <= num_sms; }
 
 template <int D, int NT>
