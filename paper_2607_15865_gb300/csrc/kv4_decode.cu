@@ -9,7 +9,8 @@
 //   many             the blocks of all items, in order, in equal runs, whatever the lengths: each item counts
 //                    kItemCost blocks more than it has, for what it costs to begin and to end one; or in whole items,
 //                    where they are short or about as many as the CTAs.  CTAs of four warps, several per SM: while
-//                    one begins or ends an item the others walk
+//                    one begins or ends an item the others walk (or of eight, for up to one item per SM of more
+//                    than 8 columns)
 // Within a CTA the warps take an item's blocks in turn, each through a private ring of two stages, filled by
 // cp.async (ten 16-byte copies per lane; as four bulk copies and an mbarrier a block cost 50 instructions
 // more), and with its own running maximum, sum and accumulators; they meet once per item, in shared memory.  An
@@ -41,8 +42,8 @@
 // 6 TB/s; over a whole call the ALU pipe is at 49% and the tensor pipe at 24% of the active cycles.  Around the walk a
 // call takes 5 us for one short sequence (launch, lengths, first bytes, the warps' meeting) and about 2 us more where
 // items are shared.  In a graph, 32 / 8 heads of 128 values (in brackets the bytes at 6.77 TB/s), us: 1 x 1 4.8, 1 x 1024
-// 7.4 (0.2), 16 x 1024 12.8 (2.8), 16 x 8191 37.6 (22.3), 64 x 8191 119 (89.4), 4 tokens over 8188 12.2 (1.4); 40 / 8 heads
-// 1 x 32767 14.1 (5.6).  Over the bf16 cache 1 x 1024 7.6, 16 x 8191 79, 64 x 8191 311, 1 x 32767 26.9.
+// 6.8 (0.2), 16 x 1024 12.8 (2.8), 16 x 8191 37.6 (22.3), 64 x 8191 119 (89.4), 4 tokens over 8188 12.2 (1.4); 40 / 8 heads
+// 1 x 32767 13.9 (5.6).  Over the bf16 cache 1 x 1024 7.6, 16 x 8191 79, 64 x 8191 311, 1 x 32767 26.9.
 //
 // The new tokens: a CTA that holds their slots rotates and quantises them, a warp per row, before its own
 // blocks, writes them to the cache and stages them for the warp that has their block.  Slots past the last
@@ -64,24 +65,36 @@ constexpr int kMaxSeqs = 128;   // sequences of one launch (their block counts a
 // Blocks that it costs a CTA to begin and end an item.  Calls in a graph (32 / 8 heads of 128 values, us) with 0, 8, 16, 32:
 // 16 sequences of mixed lengths 33.1, 26.6, 24.5, 25.5; of 8191 40.2, 38.4, 37.2, 38.3; of 1024 16.4, 12.7, 13.2, 14.7.
 constexpr int kItemCost = 16;
-// Blocks of a piece, unless the item is but one: a merge takes 2 us or more, a block of each warp 0.5.  One sequence of 300, 500
-// and 700 tokens 5.4, 6.2 and 7.1 us in one piece, 7.7, 8.1 and 8.2 in several; 1000 in either 8.0; with 16 columns 400
-// tokens 8.5 and 10.4.  Pieces of 8 blocks at least took 8.3 for 1000 tokens, of 2 as long as of 4.
+// Blocks of a piece, unless the item is but one: a merge takes 2 us or more, a block of each warp 0.5.  With 16 warps, one
+// sequence of 300, 500 and 700 tokens took 5.4, 6.2 and 7.1 us in one piece, 7.7, 8.1 and 8.2 in several, 1000 tokens 8.0
+// in either, and 8.3 in pieces of 8 blocks at least; with 16 columns 400 tokens 8.5 and 10.4.
 constexpr int kMinBlocks = 4;
 constexpr int kMaxNew = 16;     // new tokens per sequence
 constexpr int kNone = 1 << 20;  // no new token with a NaN group
 
-template <int D_, int NT_, bool WIDE_>
+// How the items are cut: pieces, or runs with few items or many.
+enum Cut { kPieces, kRunsFew, kRuns };
+
+template <int D_, int NT_, Cut CUT_>
 struct Cfg {
     static constexpr int D = D_, NT = NT_;       // NT: tiles of 8 columns
-    static constexpr bool WIDE = WIDE_;          // one CTA per SM
-    static constexpr int W = !WIDE ? 4 : NT == 1 ? 16 : 8;  // warps
-    static constexpr int CTAS = WIDE ? 1 : NT == 1 ? 4 : D == 128 ? 2 : 3;  // per SM: what registers and shared memory allow
+    static constexpr bool WIDE = CUT_ == kPieces;
+    // Warps, and CTAs per SM: what registers and shared memory allow.  Pieces of 8 columns with 16, 12 and 8 warps (head_dim
+    // 128, us): 1 x 2000 tokens 7.7, 7.0, 6.5, 1 x 32767 14.4, 14.5, 15.1, 4 x 8000 14.7, 14.8, 15.9; head_dim 64 with
+    // 16 and 12: 4 x 8000 10.7 and 10.8.  Many runs with 4, 3 and 2 CTAs, the last of 8 warps: 16 x 8191 37.8, 36.8, 39.3,
+    // 64 x 2000 38.2, 40.6, 43.9, 16 of mixed lengths 24.6, 24.0, 26.6.
+    static constexpr int W = CUT_ == kRuns ? 4 : NT == 2 ? 8 : D == 128 ? 12 : 16;
+    static constexpr int CTAS = CUT_ != kRuns ? 1 : NT == 1 ? 4 : D == 128 ? 2 : 3;
     static constexpr int THREADS = 32 * W;
     static constexpr int ALONE = NT == 1 ? 24 : 16;   // pieces: an item of up to so many blocks is one (see kMinBlocks)
-    static constexpr int EXCESS = NT == 1 ? 20 : 32;  // runs: blocks that a CTA may have more than its run, where that
-    static constexpr int LONGEST = NT == 1 ? 36 : 48; // saves all merges, and the longest item of mixed ones (below)
-    static constexpr int BATCH = NT == 1 ? 8 : WIDE ? 20 : D == 128 ? 16 : 12;  // parts that a merging thread loads at once
+    // runs: blocks that a CTA may have more than its run, where that saves all merges, and the longest item of mixed
+    // ones (with figures where the runs are cut)
+    static constexpr int EXCESS = NT == 1 ? 20 : CUT_ == kRunsFew ? 48 : 32;
+    static constexpr int LONGEST = NT == 1 ? 36 : 48;
+    // Parts that a merging thread loads at once: all of the most pieces that there are for 8 heads, if registers allow
+    // (1 x 32767: 14.4 us with 8, 13.9 with 10; 4 tokens over 8188 13.5 with 10, 12.2 with 20); few runs share an item (16
+    // sequences of 8 tokens over 4000 53.1 with 16, 51.9 with 4).
+    static constexpr int BATCH = CUT_ == kPieces ? (NT == 1 ? 10 : 20) : NT == 1 ? 8 : 4;
     static constexpr int KB = 32 * 128 / D;      // slots per block
     static constexpr int ROW = D / 2;            // bytes of a slot's codes
     static constexpr int GR = D / kKv4Group;     // groups
@@ -373,10 +386,11 @@ struct Merged {
     }
 };
 
-template <int D, int NT, bool WIDE>
-__global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::CTAS) kv4_decode_kernel(
+template <int D, int NT, Cut CUT>
+__global__ void __launch_bounds__(Cfg<D, NT, CUT>::THREADS, Cfg<D, NT, CUT>::CTAS) kv4_decode_kernel(
     const __grid_constant__ Args a) {
-    using C = Cfg<D, NT, WIDE>;
+    using C = Cfg<D, NT, CUT>;
+    constexpr bool WIDE = C::WIDE;
     constexpr int W = C::W, KB = C::KB, GR = C::GR, E = D / 32;
     constexpr int KW = D / 32;   // words of a lane's part of a k row (D / 4 values)
     constexpr int VW = D / 64;   // words of a lane's part of a v row (D / 8 values)
@@ -1007,9 +1021,9 @@ __global__ void __launch_bounds__(Cfg<D, NT, WIDE>::THREADS, Cfg<D, NT, WIDE>::C
     }
 }
 
-template <int D, int NT, bool WIDE>
+template <int D, int NT, Cut CUT>
 cudaError_t launch(const Args& a, int num_sms, cudaStream_t st) {
-    using C = Cfg<D, NT, WIDE>;
+    using C = Cfg<D, NT, CUT>;
     const long long most = static_cast<long long>(a.batch) * a.Hkv * a.ncg * ((a.max_len + C::KB - 1) / C::KB + kItemCost);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(std::min<long long>(num_sms * C::CTAS, most)));
@@ -1021,33 +1035,39 @@ cudaError_t launch(const Args& a, int num_sms, cudaStream_t st) {
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kv4_decode_kernel<D, NT, WIDE>, a);
+    return cudaLaunchKernelEx(&cfg, kv4_decode_kernel<D, NT, CUT>, a);
 }
 
-template <int D, int NT, bool WIDE>
+template <int D, int NT, Cut CUT>
 cudaError_t configure() {
-    return cudaFuncSetAttribute(kv4_decode_kernel<D, NT, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                Cfg<D, NT, WIDE>::BYTES);
+    return cudaFuncSetAttribute(kv4_decode_kernel<D, NT, CUT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                Cfg<D, NT, CUT>::BYTES);
 }
 
 // Pieces or runs (the lengths are not known here).  Calls in a graph, 4 query heads per kv head, histories of 8000,
 // pieces against runs: 8 items 9.1 and 14.8 us, 32 15.0 and 16.7, 64 21.9 and 23.7, 128 32.9 and 36.3; with mixed
 // lengths up to 8000, which pieces of whole blocks divide worse the fewer there are per item, 64 16.7 and 17.0,
 // 128 28.3 and 24.1.
-bool is_wide(const Args& a, int num_sms) { return a.batch <= 32 && 2 * a.batch * a.Hkv * a.ncg <= num_sms; }
-
+// With up to one item per SM and more than 8 columns, runs of CTAs of 8 warps, one per SM, instead of 4, two or three
+// (head_dim 128, 4 tokens for 16 sequences, 8 kv heads): over 1000 tokens 12.9 and 19.0 us, over 8000 53.3 and 56.1, mixed
+// up to 300 9.7 and 11.8, up to 4000 27.4 and 29.8.  (With up to 8 columns such runs of 12 warps take 9.5 us for 12.8
+// where 16 sequences have 1000 tokens each, but 14.5 for 11.0 with mixed lengths up to 1000, 28.3 for 24.5 up to 8183.)
 template <int D, int NT>
 cudaError_t launch_for(const Args& a, int num_sms, cudaStream_t st) {
-    const bool wide = is_wide(a, num_sms);
-    return wide ? launch<D, NT, true>(a, num_sms, st) : launch<D, NT, false>(a, num_sms, st);
+    const int items = a.batch * a.Hkv * a.ncg;
+    if (a.batch <= 32 && 2 * items <= num_sms) return launch<D, NT, kPieces>(a, num_sms, st);
+    if constexpr (NT == 2)
+        if (items <= num_sms) return launch<D, NT, kRunsFew>(a, num_sms, st);
+    return launch<D, NT, kRuns>(a, num_sms, st);
 }
 
 }  // namespace
 
 cudaError_t configure_kv4_decode() {
     cudaError_t e = cudaSuccess;
-    for (auto fn : {configure<128, 1, false>, configure<128, 1, true>, configure<128, 2, false>, configure<128, 2, true>,
-                    configure<64, 1, false>, configure<64, 1, true>, configure<64, 2, false>, configure<64, 2, true>})
+    for (auto fn : {configure<128, 1, kPieces>, configure<128, 1, kRuns>, configure<128, 2, kPieces>, configure<128, 2, kRunsFew>,
+                    configure<128, 2, kRuns>, configure<64, 1, kPieces>, configure<64, 1, kRuns>, configure<64, 2, kPieces>,
+                    configure<64, 2, kRunsFew>, configure<64, 2, kRuns>})
         if (e == cudaSuccess) e = fn();
     return e;
 }
