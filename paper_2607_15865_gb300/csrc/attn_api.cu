@@ -719,12 +719,13 @@ int run_kv4_decode(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uint
 
 // Whether a short chunk goes through the decode (a pass over the packed history for each 16 (query head, token)
 // columns) or through the workspace.  Calls in a graph, 40 / 8 heads, decode against workspace: 15 columns over
-// 500 10.3 and 9.6 us, over 4000 10.7 and 14.3, over 30000 18.3 and 51.7; 30 columns over 500 12.0 and 9.5, over
-// 4000 13.9 and 14.8, over 30000 28.7 and 52.2; 45 columns over 4000 16.0 and 15.2, over 30000 38.6 and 52.7, of
-// four sequences over 4000 36.1 and 32.0.
+// 500 8.1 and 9.6 us, over 4000 10.3 and 14.3, over 30000 17.9 and 51.7; 30 columns over 500 12.0 and 9.5, over
+// 4000 13.3 and 14.8, over 30000 28.0 and 52.2; 45 columns over 4000 15.4 and 14.9, over 8000 19.2 and 21.3, over
+// 30000 38.2 and 53.5, of four sequences over 8000 46.4 and 55.9; 60 columns over 8000 23.6 and 21.6, over 30000 53.1 and 53.9.
 bool kv4_chunk_decodes(const attn_ctx* c, int hist, int chunk) {
     const int columns = c->cfg.n_q_heads / c->cfg.n_kv_heads * chunk;
-    return chunk <= kMaxDraftTokens && (columns <= 16 || (columns <= 32 && hist >= 2048));
+    return chunk <= kMaxDraftTokens &&
+           (columns <= 16 || (columns <= 32 && hist >= 2048) || (columns <= 48 && hist >= 8000));
 }
 
 }  // namespace

@@ -425,6 +425,14 @@ def test_prefill(B, Hq, Hkv, D, L, hist, n):
     run_prefill(attn, U.to_dev(ref, L), ref, f"pre{B}{Hq}{D}", hist, n)
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,n", [(8, 2, 128, 12), (10, 2, 64, 9), (8, 2, 128, 13)])
+def test_prefill_of_up_to_48_columns_over_a_long_history(Hq, Hkv, D, n):
+    """Through the decode, and (52 columns) the workspace."""
+    attn = context(1, Hq, Hkv, D, 8200)
+    ref = U.history(f"pl{D}", 1, Hkv, slots(8200), D, [8100])
+    run_prefill(attn, U.to_dev(ref, 8200), ref, f"pl{D}{n}", 8100, n)
+
+
 def test_a_prompt_in_chunks_then_decodes_equals_its_cache():
     """Two chunks in one workspace, single and several tokens: each step is the stage over the cache so far."""
     import torch
