@@ -271,7 +271,8 @@ class Attention:
         ks = (self.batch, S, self.n_kv_heads, self.head_dim)
         rc = self.lib.attn_kv4_append(self._ctx, _ptr(k, "k", ks), _ptr(v, "v", ks), int(hist_len), S,
                                       self._kv4(cache), _stream(stream))
-        self._check(rc, "attn_kv4_append")
+        if rc:
+            self._check(rc, "attn_kv4_append")
 
     def kv4_read(self, cache, first: int = 0, count: int | None = None, out=None, stream=None):
         """The bf16 values (k, v), each [B,Hkv,count,D], of slots first .. first + count - 1 (default: all from
@@ -280,11 +281,16 @@ class Attention:
         ref = self._kv4(cache)
         shape = (self.batch, self.n_kv_heads, max(count, 0), self.head_dim)
         if out is None:
-            out = tuple(_empty(shape, torch.bfloat16, cache.k_codes, stream) for _ in range(2))
-        k, v = out
-        rc = self.lib.attn_kv4_read(self._ctx, ref, int(first), count, _ptr(k, "k", shape), _ptr(v, "v", shape),
-                                    _stream(stream))
-        self._check(rc, "attn_kv4_read")
+            k = _empty(shape, torch.bfloat16, cache.k_codes, stream)
+            v = torch.empty_like(k) if stream is None else _empty(shape, torch.bfloat16, k, stream)
+            out = (k, v)
+            ptrs = k.data_ptr(), v.data_ptr()
+        else:
+            k, v = out
+            ptrs = _ptr(k, "k", shape), _ptr(v, "v", shape)
+        rc = self.lib.attn_kv4_read(self._ctx, ref, int(first), count, *ptrs, _stream(stream))
+        if rc:
+            self._check(rc, "attn_kv4_read")
         return out
 
     def kv4_decode(self, q, k, v, hist_len: torch.Tensor, cache, out=None, stream=None) -> torch.Tensor:
