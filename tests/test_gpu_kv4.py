@@ -433,6 +433,18 @@ def test_prefill_of_up_to_48_columns_over_a_long_history(Hq, Hkv, D, n):
     run_prefill(attn, U.to_dev(ref, 8200), ref, f"pl{D}{n}", 8100, n)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_prefill_nan_in_the_history(D):
+    """Stretches of NaN keys, and a NaN group of a value."""
+    attn = context(1, 4, 4, D, 800)
+    ref = U.history(f"prenan{D}", 1, 4, slots(800), D, [600])
+    ref.scales[0][0, 0, :400] = K.NAN_SCALE
+    ref.scales[0][0, 1, 128:256] = K.NAN_SCALE
+    ref.scales[1][0, 2, 77, 1] = K.NAN_SCALE
+    out = run_prefill(attn, U.to_dev(ref, 800), ref, f"prenan{D}", 600, 150)
+    assert out[0, :, :2].isnan().all() and out[0, :, 2, 32:64].isnan().all() and not out[0, :, 3].isnan().any()
+
+
 def test_a_prompt_in_chunks_then_decodes_equals_its_cache():
     """Two chunks in one workspace, single and several tokens: each step is the stage over the cache so far."""
     import torch
