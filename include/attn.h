@@ -458,7 +458,8 @@ int attn_kv4_read(attn_ctx* ctx, const attn_kv4* cache, int first, int count, ui
 /* attn_decode_multi over a 4-bit cache: n_new (1 .. 16) tokens per sequence at positions d_hist_len[b] + i are
  * quantised into their slots and attend to slots [0, d_hist_len[b] + i], at either head_dim and any n_new of
  * those.  A sequence with a position outside [0, max_len - 1] is skipped (cache and out not written) and sets
- * ATTN_DEVERR_HIST_RANGE.  The products take the values 2^-73 as large, in bf16: a group of scale 2^67 or more
+ * ATTN_DEVERR_HIST_RANGE.  As over the bf16 cache, a softmax weight is rounded to bf16 (by up to 2^-8 of it) at head_dim 128
+ * and held closer (to 2^-16) at 64.  The products take the values 2^-73 as large, in bf16: a group of scale 2^67 or more
  * (values from about 2^67) comes out infinite or NaN, and one under 2^-53 loses bits below 2^-60.  The other arguments
  * and the errors are those of attn_decode_multi. */
 int attn_kv4_decode(attn_ctx* ctx, const uint16_t* q, const uint16_t* k, const uint16_t* v,

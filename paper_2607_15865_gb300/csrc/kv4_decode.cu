@@ -31,11 +31,14 @@
 // least float.  For k the zero points go as a product of their own, one further mma:
 //   S -= sum over groups of (z s) (sum of q over the group), those sums in three bf16 parts.
 // For v it is one fma with - z s instead of the product: a v that is small beside its group must not be
-// what is left of two larger sums.  Rows of ones in place of V^T give the softmax sum, of the same rounded P
-// that weighs V.
+// what is left of two larger sums.  At head_dim 128 rows of ones in place of V^T give the softmax sum, of the same
+// rounded P that weighs V; at 64 the lanes add P up in float.
 // The running maximum moves lazily: only when a score passes it by 2^8 are O and the sum rescaled.
-// Roundings: q and the new k to bf16 after RoPE, as the bf16 stages round them; a weight P to bf16 (the operand's type; its
-// sum is of the rounded ones); the output.  Scores, maxima, sums and O are floats.
+// Roundings: q and the new k to bf16 after RoPE, as the bf16 stages round them; a weight P, as over the bf16 cache, at
+// head_dim 128 to bf16 (the operand's type), and at 64, where that decode keeps it to float precision, to the sum of two
+// bf16 numbers, within 2^-16; the output.  Scores, maxima, sums and O are floats.  The second number costs a further mma per
+// V operand (calls in a graph, 32 / 8 heads of 64 values: 1 x 1024 6.2 us without and 6.5 with it, 16 x 8191 25.6 and 27.7,
+// 64 x 8191 74.4 and 82.1).
 //
 // What bounds it: instructions, not the 9/8 D bytes of a slot's k or v.  16 slots of a head of 128 values with up to 8
 // columns take 294 warp instructions, 18 of them mma, and 437 cycles of a scheduler, at which the SMs walk about
@@ -79,6 +82,7 @@ template <int D_, int NT_, Cut CUT_>
 struct Cfg {
     static constexpr int D = D_, NT = NT_;       // NT: tiles of 8 columns
     static constexpr bool WIDE = CUT_ == kPieces;
+    static constexpr int PARTS = D == 64 ? 2 : 1;  // bf16 numbers that a weight is the sum of
     // Warps, and CTAs per SM: what registers and shared memory allow.  Pieces of 8 columns with 16, 12 and 8 warps (head_dim
     // 128, us): 1 x 2000 tokens 7.7, 7.0, 6.5, 1 x 32767 14.4, 14.5, 15.1, 4 x 8000 14.7, 14.8, 15.9; head_dim 64 with
     // 16 and 12: 4 x 8000 10.7 and 10.8.  Many runs with 4, 3 and 2 CTAs, the last of 8 warps: 16 x 8191 37.8, 36.8, 39.3,
@@ -882,14 +886,21 @@ __global__ void __launch_bounds__(Cfg<D, NT, CUT>::THREADS, Cfg<D, NT, CUT>::CTA
                             }
                         }
                 }
-                uint32_t pb[NT][4];
+                uint32_t pb[NT][C::PARTS][4];
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const float* x = &s[j / 2][n][2 * (j % 2)];
-                        pb[n][j] = transpose8(pack2(exp2_fast(fmaf(x[0], a.scale_log2, -ms[n][0])),
-                                                    exp2_fast(fmaf(x[1], a.scale_log2, -ms[n][1]))));
+                        const float p0 = exp2_fast(fmaf(x[0], a.scale_log2, -ms[n][0]));
+                        const float p1 = exp2_fast(fmaf(x[1], a.scale_log2, -ms[n][1]));
+                        const uint32_t hi = pack2(p0, p1);
+                        pb[n][0][j] = transpose8(hi);
+                        if constexpr (C::PARTS == 2) {
+                            pb[n][1][j] = transpose8(pack2(p0 - bf_lo(hi), p1 - bf_hi(hi)));
+                            sum[n][0] += p0;
+                            sum[n][1] += p1;
+                        }
                     }
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {  // 16 slots
@@ -912,7 +923,9 @@ __global__ void __launch_bounds__(Cfg<D, NT, CUT>::THREADS, Cfg<D, NT, CUT>::CTA
                     p01.zs ^= 0x80008000u;
                     p23.zs ^= 0x80008000u;
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) mma(sum[n], kOnes, kOnes, kOnes, kOnes, pb[n][2 * k], pb[n][2 * k + 1]);
+                    for (int n = 0; n < NT; ++n)
+                        if constexpr (C::PARTS == 1)
+                            mma(sum[n], kOnes, kOnes, kOnes, kOnes, pb[n][0][2 * k], pb[n][0][2 * k + 1]);
 #pragma unroll
                     for (int v = 0; v < VW; ++v) {
                         const uint32_t a01 = __byte_perm(w[0][v], w[1][v], 0x5410), b01 = __byte_perm(w[0][v], w[1][v], 0x7632);
@@ -923,7 +936,9 @@ __global__ void __launch_bounds__(Cfg<D, NT, CUT>::THREADS, Cfg<D, NT, CUT>::CTA
                                            x2 = value2(a23, a23 >> 8, i, p23), x3 = value2(b23, b23 >> 8, i, p23);
 #pragma unroll
                             for (int n = 0; n < NT; ++n)
-                                mma(o[n][4 * v + i], x0, x1, x2, x3, pb[n][2 * k], pb[n][2 * k + 1]);
+#pragma unroll
+                                for (int h = 0; h < C::PARTS; ++h)
+                                    mma(o[n][4 * v + i], x0, x1, x2, x3, pb[n][h][2 * k], pb[n][h][2 * k + 1]);
                         }
                     }
                 }
@@ -933,6 +948,14 @@ __global__ void __launch_bounds__(Cfg<D, NT, CUT>::THREADS, Cfg<D, NT, CUT>::CTA
             st_off = C::STAGE - st_off;
         }
 
+        if constexpr (C::PARTS == 2) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int mask = 4; mask <= 16; mask <<= 1) sum[n][e] += __shfl_xor_sync(0xFFFFFFFFu, sum[n][e], mask);
+        }
         // The warps' parts meet.  Lane (g, t) holds columns 2 t, 2 t + 1 (+ 8 n) of values D/8 g .. D/8 g + D/8 - 1.
 #pragma unroll
         for (int n = 0; n < NT; ++n)
