@@ -460,8 +460,8 @@ int attn_kv4_read(attn_ctx* ctx, const attn_kv4* cache, int first, int count, ui
  * those.  A sequence with a position outside [0, max_len - 1] is skipped (cache and out not written) and sets
  * ATTN_DEVERR_HIST_RANGE.  As over the bf16 cache, a softmax weight is rounded to bf16 (by up to 2^-8 of it) at head_dim 128
  * and held closer (to 2^-16) at 64.  The products take the values 2^-73 as large, in bf16: a group of scale 2^67 or more
- * (values from about 2^67) comes out infinite or NaN, and one under 2^-53 loses bits below 2^-60.  The other arguments
- * and the errors are those of attn_decode_multi. */
+ * (values from about 2^67) comes out infinite or NaN, for the tokens that see it, and one under 2^-53 loses bits below
+ * 2^-60.  The other arguments and the errors are those of attn_decode_multi. */
 int attn_kv4_decode(attn_ctx* ctx, const uint16_t* q, const uint16_t* k, const uint16_t* v,
                     const int32_t* d_hist_len, int n_new, const attn_kv4* cache, uint16_t* out, attn_stream_t stream);
 

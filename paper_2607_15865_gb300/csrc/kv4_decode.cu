@@ -50,8 +50,9 @@
 //
 // The new tokens: a CTA that holds their slots rotates and quantises them, a warp per row, before its own
 // blocks, writes them to the cache and stages them for the warp that has their block.  Slots past the last
-// one are masked by position and by a scale of 0; a NaN group of a new token's v counts from that token on, so its
-// scale is taken as 0 too and the columns that see it are set to NaN when they are written.
+// one are masked by position and by a scale of 0; a group of a new token's v that is NaN, or that the products would make
+// so (a scale of 2^68 or more), counts from that token on, so its scale is taken as 0 too and the columns that see it are
+// set to NaN when they are written.
 // The only wait on other warps that is not a barrier, for the staged rows, is bounded: on expiry the warp records
 // kDevErrTimeout and goes on with what it has.
 #include <algorithm>
@@ -156,6 +157,7 @@ constexpr uint32_t kOnes = 0x3F803F80u;                       // 1
 constexpr uint32_t kUp = 0x5D805D80u, kSixteenth = 0x3D803D80u;  // 2^60, 2^-4
 constexpr float kUnit = 9.44473296573929e21f;                // 2^73
 constexpr float kLift = 60.f;                                // P is 2^60 times the weights
+constexpr uint32_t kTooLarge = 0x6180u;                      // scales from 2^68 on: times 2^60 they are infinite
 
 // The scales of a pair of values, for codes in the low and in the high four bits of a byte, and z s (in
 // units of 2^-73).
@@ -240,7 +242,7 @@ struct Args {
 
 // One warp: quantise the E = D / 32 values of a row that each lane holds (bf16 pairs; with E = 2 one pair), write
 // the row's codes and scales to the cache and to a staged row (codes, then scales).  Returns whether the lane's
-// group is NaN.
+// group is NaN, or NaN to the products.
 template <int D>
 __device__ __forceinline__ bool put_row(const uint32_t (&x)[D / 64], int lane, uint8_t* codes, uint16_t* scales,
                                         uint8_t* staged) {
@@ -268,7 +270,7 @@ __device__ __forceinline__ bool put_row(const uint32_t (&x)[D / 64], int lane, u
         scales[lane / LANES] = static_cast<uint16_t>(scale);
         reinterpret_cast<uint16_t*>(staged + D / 2)[lane / LANES] = static_cast<uint16_t>(scale);
     }
-    return nan;
+    return scale >= kTooLarge;
 }
 
 template <int N>
@@ -916,7 +918,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, CUT>::THREADS, Cfg<D, NT, CUT>::CTA
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const int row = key + (e & 1) + 8 * (e >> 1);
-                            if (row > last || (sc[e] == kKv4NanScale && k0 + row > hist)) sc[e] = 0;
+                            if (row > last || (sc[e] >= kTooLarge && k0 + row > hist)) sc[e] = 0;
                         }
                     }
                     Pair p01 = pair_of(__byte_perm(sc[0], sc[1], 0x5410)), p23 = pair_of(__byte_perm(sc[2], sc[3], 0x5410));
