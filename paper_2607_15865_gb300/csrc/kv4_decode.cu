@@ -54,7 +54,7 @@
 // so (a scale of 2^68 or more), counts from that token on, so its scale is taken as 0 too and the columns that see it are
 // set to NaN when they are written.
 // The only wait on other warps that is not a barrier, for the staged rows, is bounded: on expiry the warp records
-// kDevErrTimeout and goes on with what it has.
+// kDevErrTimeout and the item's outputs are not written.
 #include <algorithm>
 #include <cmath>
 
@@ -119,8 +119,9 @@ struct Cfg {
     static constexpr int OFF_FREE = OFF_PRE + (kMaxSeqs + 1) * 4;  // uint8 [kMaxSeqs]: slots of the last block past the last token
     static constexpr int OFF_BAR = (OFF_FREE + kMaxSeqs + 7) & ~7;  // mbarrier: the staged rows
     static constexpr int OFF_NAN = OFF_BAR + 8;                 // int [4]: first new token with a NaN group of v
-    static constexpr int OFF_FLAG = OFF_NAN + 16;               // int [2]: whether this CTA merges its first, its last item
-    static constexpr int OFF_SEG = OFF_FLAG + 8;                // Segment [2]: of this turn, and a held one
+    // int [3]: whether this CTA merges its first, its last item; whether the wait for the staged rows ran out
+    static constexpr int OFF_FLAG = OFF_NAN + 16;
+    static constexpr int OFF_SEG = OFF_FLAG + 12;               // Segment [2]: of this turn, and a held one
     static constexpr int BYTES = OFF_SEG + 2 * 40;
     static_assert(CODES == 2048 && SCALES == 256 && NEW % 4 == 0 && 2 * kMaxNew * NEW <= O_BYTES, "layout");
     static_assert(BYTES <= 232448 && CTAS * (BYTES + 1024) <= 233472, "shared memory");
@@ -357,8 +358,9 @@ __device__ __forceinline__ int search(const int* sums, int batch, int hc, int r)
 }
 
 // The maximum that a part is merged by: NaN where its sum is (then its scores may be NaN throughout, and m -inf as if
-// it had none).  -inf: no slot of the part is seen.
-__device__ __forceinline__ float mark(float m, float l) { return l != l ? l : m; }
+// it had none) or a score is past the largest float.  -inf: no slot of the part is seen.  inf, which mark does not return: a
+// wait ran out in the part, and the item is not to be written.
+__device__ __forceinline__ float mark(float m, float l) { return l != l || m == INFINITY ? NAN : m; }
 
 // The merge of up to N parts (m, l, o[4]) with a running (m, l, o[4]); parts without a slot are left out, those of weight
 // 0 are not (0 times a NaN).
@@ -697,7 +699,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, CUT>::THREADS, Cfg<D, NT, CUT>::CTA
             if (subs > 1) {
                 if (sub > 0 && sub < subs) {
                     s_x[tid] = make_float4(acc.o[0], acc.o[1], acc.o[2], acc.o[3]);
-                    s_y[tid] = make_float2(mark(acc.m, acc.l), acc.l);
+                    s_y[tid] = make_float2(acc.m == INFINITY ? acc.m : mark(acc.m, acc.l), acc.l);
                     if (nan < kNone) atomicMin(&s_nan[d / kKv4Group], nan);
                 }
                 __syncthreads();
@@ -709,7 +711,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, CUT>::THREADS, Cfg<D, NT, CUT>::CTA
                     }
                 nan = min(nan, s_nan[d / kKv4Group]);
             }
-            if (sub == 0 && u < vals)
+            if (sub == 0 && u < vals && acc.m != INFINITY)
                 *reinterpret_cast<uint2*>(a.out + row_of(w, col) * D + d) = acc.result(nan > 0 && nan <= token(w, col));
         }
     };
@@ -721,7 +723,10 @@ __global__ void __launch_bounds__(Cfg<D, NT, CUT>::THREADS, Cfg<D, NT, CUT>::CTA
         __syncthreads();  // the buffers of the item before are free
         store_q();
         if (tid < 4) s_nan[tid] = kNone;
-        if (tid == 0) segs[0] = w;
+        if (tid == 0) {
+            segs[0] = w;
+            flag[2] = 0;
+        }
         __syncthreads();
         if (first_turn) issue(s_warp + C::STAGE);
         const Segment& now = segs[0];  // what the walk needs no more is read again after it
@@ -808,7 +813,10 @@ __global__ void __launch_bounds__(Cfg<D, NT, CUT>::THREADS, Cfg<D, NT, CUT>::CTA
             __syncwarp();
             const bool tail = k0 + KB > hist;  // the block holds slots of new tokens, or none at all
             if (tail) {  // the staged rows into the block
-                if (!mbar_wait(new_full, new_phase, nullptr, a.wait_ns)) record_dev_err(a.err, kDevErrTimeout);
+                if (!mbar_wait(new_full, new_phase, nullptr, a.wait_ns)) {
+                    record_dev_err(a.err, kDevErrTimeout);
+                    flag[2] = 1;
+                }
                 const int lo = max(k0, hist), hi = min(k0 + KB, hist + a.ntok);
                 for (int p = lo; p < hi; ++p)
 #pragma unroll
@@ -986,7 +994,9 @@ __global__ void __launch_bounds__(Cfg<D, NT, CUT>::THREADS, Cfg<D, NT, CUT>::CTA
         const int j0 = WIDE ? cta - now.base : alone ? cta : cta_of(now.base);  // the CTAs that share the item
         const int j1 = WIDE ? j0 + n - 1 : alone ? cta : cta_of(now.base + now.T - 1);
         const int part = 2 * cta + (cta == j0 ? 1 : 0);
-        for (int u = tid; u < now.ncol * (D / V); u += C::THREADS) {
+        const bool gave_up = flag[2] != 0;
+        const int vals = gave_up && j0 == j1 ? 0 : now.ncol * (D / V);
+        for (int u = tid; u < vals; u += C::THREADS) {
             const int col = u / (D / V), d = u % (D / V) * V;
             float f[W], mx = -INFINITY, l = 0.f, acc[V] = {};
 #pragma unroll
@@ -1016,7 +1026,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, CUT>::THREADS, Cfg<D, NT, CUT>::CTA
                 float* dst = a.part_o + (static_cast<size_t>(part) * 16 + col) * D + d;
 #pragma unroll
                 for (int e = 0; e < V; e += 2) *reinterpret_cast<float2*>(dst + e) = make_float2(acc[e], acc[e + 1]);
-                if (d == 0) reinterpret_cast<float2*>(a.part_ml)[part * 16 + col] = make_float2(mark(mx, l), l);
+                if (d == 0) reinterpret_cast<float2*>(a.part_ml)[part * 16 + col] = make_float2(gave_up ? INFINITY : mark(mx, l), l);
             }
         }
         if (j0 != j1 && tid < 4) a.part_nan[4 * part + tid] = s_nan[tid];
