@@ -466,14 +466,16 @@ int attn_kv4_decode(attn_ctx* ctx, const uint16_t* q, const uint16_t* k, const u
                     const int32_t* d_hist_len, int n_new, const attn_kv4* cache, uint16_t* out, attn_stream_t stream);
 
 /* attn_prefill_kv over a 4-bit cache (hist_len = 0: a prefill): the chunk is quantised into its slots and attends
- * causally to slots [0, hist_len + i].  workspace: device memory of at least attn_kv4_workspace(ctx,
- * hist_len + chunk_len) bytes, 256-byte aligned, which holds the bf16 values of those slots during the call
+ * causally to slots [0, hist_len + i].  workspace: device memory of at least attn_kv4_prefill_workspace(ctx,
+ * hist_len, chunk_len) bytes, 256-byte aligned, which holds the bf16 values of those slots during the call
  * (one workspace serves every layer).  A chunk of a few tokens goes through attn_kv4_decode's kernel where that is
- * the faster (with that call's range of values), and leaves the workspace alone.  Otherwise a NaN or an infinity
- * in a token's v makes its values NaN for the tokens of the chunk just before it (those of its tile) too, as in
+ * the faster (with that call's range of values): it needs 0 bytes, and workspace may be NULL.
+ * attn_kv4_workspace(ctx, tokens) bytes are enough for any chunk with hist_len + chunk_len <= tokens; both return 0
+ * for lengths outside the cache (host only).  A chunk that needs a workspace: a NaN or an infinity in a token's v makes its values NaN for the tokens of the chunk just before it (those of its tile) too, as in
  * attn_prefill_kv.  batch * chunk_len * n_kv_heads * head_dim / 16 below 2^31 - 256.  The other arguments and the
  * errors are those of attn_prefill_kv. */
 size_t attn_kv4_workspace(const attn_ctx* ctx, int tokens);
+size_t attn_kv4_prefill_workspace(const attn_ctx* ctx, int hist_len, int chunk_len);
 int attn_kv4_prefill_kv(attn_ctx* ctx, const uint16_t* q, const uint16_t* k, const uint16_t* v, int hist_len,
                         int chunk_len, const attn_kv4* cache, uint16_t* out, void* workspace, size_t workspace_bytes,
                         attn_stream_t stream);

@@ -23,7 +23,8 @@ EXPORTED = ("attn_create", "attn_destroy", "attn_prefill", "attn_prefill_kv", "a
             "attn_strerror", "attn_last_cuda_error_string", "attn_decode_noalloc", "attn_w4bf16_gemv",
             "attn_w4bf16_rows_per_launch", "attn_w4bf16_gemv_fused", "attn_decode_layer",
             "attn_w4bf16_gemm", "attn_prefill_layer", "attn_prefill_layer_workspace", "attn_kv4_slots",
-            "attn_kv4_append", "attn_kv4_read", "attn_kv4_decode", "attn_kv4_workspace", "attn_kv4_prefill_kv")
+            "attn_kv4_append", "attn_kv4_read", "attn_kv4_decode", "attn_kv4_workspace", "attn_kv4_prefill_workspace",
+            "attn_kv4_prefill_kv")
 NOALLOC_SCRATCH_FLOATS = 1 << 20
 # attn_timing_read's slots; no kernel runs as decode_combine (the decode merges itself): it reads 0
 KERNELS = ("rope_append", "flash_fwd", "decode_split", "decode_combine")
@@ -117,6 +118,8 @@ def load(path: str = LIB_PATH):
     lib.attn_kv4_decode.restype = i32
     lib.attn_kv4_workspace.argtypes = [vp, i32]
     lib.attn_kv4_workspace.restype = ctypes.c_size_t
+    lib.attn_kv4_prefill_workspace.argtypes = [vp, i32, i32]
+    lib.attn_kv4_prefill_workspace.restype = ctypes.c_size_t
     lib.attn_kv4_prefill_kv.argtypes = [vp, u16p, u16p, u16p, i32, i32, kv4, u16p, vp, ctypes.c_size_t, vp]
     lib.attn_kv4_prefill_kv.restype = i32
     lib.attn_strerror.argtypes = [i32]

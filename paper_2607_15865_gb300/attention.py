@@ -312,22 +312,27 @@ class Attention:
         return out
 
     def kv4_workspace(self, tokens: int) -> int:
-        """Bytes of device workspace kv4_prefill_kv needs for hist_len + chunk = tokens (host only)."""
+        """Bytes of device workspace that do for every kv4_prefill_kv with hist_len + chunk <= tokens (host only)."""
         return int(self.lib.attn_kv4_workspace(self._ctx, int(tokens)))
+
+    def kv4_prefill_workspace(self, hist_len: int, chunk: int) -> int:
+        """Bytes of device workspace that a kv4_prefill_kv of these lengths uses; 0 for few tokens (host only)."""
+        return int(self.lib.attn_kv4_prefill_workspace(self._ctx, int(hist_len), int(chunk)))
 
     def kv4_prefill_kv(self, q, k, v, hist_len: int, cache, workspace=None, out=None, stream=None) -> torch.Tensor:
         """prefill_kv (hist_len = 0: prefill) over a 4-bit cache.  workspace: a uint8 CUDA tensor of at least
-        kv4_workspace(hist_len + S) bytes (allocated here when None)."""
+        kv4_workspace(hist_len + S) bytes; when None, what the call uses is allocated here."""
         S = q.shape[1]
         qs = (self.batch, S, self.n_q_heads, self.head_dim)
         ks = (self.batch, S, self.n_kv_heads, self.head_dim)
         args = (_ptr(q, "q", qs), _ptr(k, "k", ks), _ptr(v, "v", ks))
-        need = self.kv4_workspace(int(hist_len) + S)
         if workspace is None:
-            workspace = _empty(need, torch.uint8, q, stream)
-        if not (isinstance(workspace, torch.Tensor) and workspace.is_cuda and workspace.dtype == torch.uint8
-                and workspace.is_contiguous() and workspace.numel() >= need):
-            raise TypeError(f"workspace must be a contiguous uint8 CUDA tensor of at least {need} bytes")
+            workspace = _empty(self.kv4_prefill_workspace(hist_len, S), torch.uint8, q, stream)
+        else:
+            need = self.kv4_workspace(int(hist_len) + S)
+            if not (isinstance(workspace, torch.Tensor) and workspace.is_cuda and workspace.dtype == torch.uint8
+                    and workspace.is_contiguous() and workspace.numel() >= need):
+                raise TypeError(f"workspace must be a contiguous uint8 CUDA tensor of at least {need} bytes")
         out = _empty(q.shape, q.dtype, q, stream) if out is None else out
         rc = self.lib.attn_kv4_prefill_kv(self._ctx, *args, int(hist_len), S, self._kv4(cache), _ptr(out, "out", qs),
                                           workspace.data_ptr(), workspace.numel(), _stream(stream))

@@ -773,11 +773,15 @@ size_t attn_kv4_workspace(const attn_ctx* c, int tokens) {
     return 2 * kv4_plain_bytes(c->cfg, tokens);
 }
 
+size_t attn_kv4_prefill_workspace(const attn_ctx* c, int hist_len, int chunk_len) {
+    if (c == nullptr || chunk_len < 1 || hist_len < 0 || static_cast<long>(hist_len) + chunk_len > c->cfg.max_len) return 0;
+    return kv4_chunk_decodes(c, hist_len, chunk_len) ? 0 : attn_kv4_workspace(c, hist_len + chunk_len);
+}
+
 int attn_kv4_prefill_kv(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uint16_t* v, int hist_len,
                         int chunk_len, const attn_kv4* cache, uint16_t* out, void* workspace, size_t workspace_bytes,
                         attn_stream_t stream) {
-    if (c == nullptr || q == nullptr || k == nullptr || v == nullptr || out == nullptr || workspace == nullptr ||
-        !kv4_ok(cache))
+    if (c == nullptr || q == nullptr || k == nullptr || v == nullptr || out == nullptr || !kv4_ok(cache))
         return ATTN_EINVAL;
     if (chunk_len < 1 || hist_len < 0 || static_cast<long>(hist_len) + chunk_len > c->cfg.max_len) return ATTN_EINVAL;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) ||
@@ -785,7 +789,8 @@ int attn_kv4_prefill_kv(attn_ctx* c, const uint16_t* q, const uint16_t* k, const
         return ATTN_EINVAL;
     if (attn::kv4_append_units(c->shape, c->cfg.batch, chunk_len) > INT32_MAX - 256) return ATTN_EINVAL;
     const int tokens = hist_len + chunk_len;
-    if (workspace_bytes < attn_kv4_workspace(c, tokens)) return ATTN_EINVAL;
+    const size_t need = attn_kv4_prefill_workspace(c, hist_len, chunk_len);
+    if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return ATTN_EINVAL;
     if (kv4_chunk_decodes(c, hist_len, chunk_len))
         return run_kv4_decode(c, q, k, v, nullptr, hist_len, chunk_len, cache, out, stream);
     uint16_t* kp = static_cast<uint16_t*>(workspace);
