@@ -18,7 +18,13 @@ GROUP = 32
 class Kv4Cache:
     """The four tensors of a cache of max_len slots, Lp = attn_kv4_slots(max_len):
     k_codes, v_codes uint8 [B, Hkv, Lp, D / 2]; k_scales, v_scales int16 (or uint16, bfloat16) bit patterns
-    [B, Hkv, Lp, D / 32].  The tensors stay the caller's and are updated in place."""
+    [B, Hkv, Lp, D / 32], all on one device.  The tensors stay the caller's and are updated in place; the attributes
+    that hold them cannot be set, as the calls go by their addresses: other tensors are another cache."""
+
+    k_codes = property(lambda self: self._tensors[0])
+    k_scales = property(lambda self: self._tensors[1])
+    v_codes = property(lambda self: self._tensors[2])
+    v_scales = property(lambda self: self._tensors[3])
 
     def __init__(self, max_len: int, k_codes, k_scales, v_codes, v_scales):
         slots = _lib.load().attn_kv4_slots(int(max_len))
@@ -30,6 +36,8 @@ class Kv4Cache:
                 raise TypeError(f"{name} must hold {'uint8 codes' if codes else '16-bit scales'}")
             if t.dim() != 4 or not t.is_contiguous():
                 raise ValueError(f"{name} must be a contiguous tensor of 4 dimensions")
+            if t.device != k_codes.device:
+                raise ValueError(f"{name} is on {t.device}, k_codes on {k_codes.device}")
         B, H, Lp, half = k_codes.shape
         want = {"codes": (B, H, slots, half), "scales": (B, H, slots, 2 * half // GROUP)}
         for t, name in ((k_codes, "k_codes"), (v_codes, "v_codes"), (k_scales, "k_scales"), (v_scales, "v_scales")):
@@ -37,9 +45,9 @@ class Kv4Cache:
             if slots == 0 or half not in (32, 64) or tuple(t.shape) != shape:
                 raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape} (head_dim 64 or 128)")
         self.max_len = int(max_len)
-        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+        self._tensors = (k_codes, k_scales, v_codes, v_scales)
         self.shape = (B, H, self.max_len, 2 * half)
-        self.struct = _lib.AttnKv4(*(t.data_ptr() for t in (k_codes, k_scales, v_codes, v_scales)))
+        self.struct = _lib.AttnKv4(*(t.data_ptr() for t in self._tensors))
         self.ref = ctypes.pointer(self.struct)
 
     @classmethod
