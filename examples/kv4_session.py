@@ -138,14 +138,19 @@ def main(argv=None):
     size = sum(t.numel() * t.element_size() for c in packed for t in (c.k_codes, c.k_scales, c.v_codes, c.v_scales))
     size16 = sum(t.numel() * 2 for c in plain for t in c)
     rel = lambda x, y: float((x.float() - y.float()).norm() / y.float().norm())  # noqa: E731
-    k, v = attn.kv4_read(packed[0], 0, a.prompt)  # the first layer's keys do not depend on the caches before
+    # the first layer's keys and values do not depend on the caches before, but for those of the decoded tokens: the
+    # first of them comes of the prompt's last state
+    k, v = attn.kv4_read(packed[0], 0, a.prompt + 1)
+    slots, first = slice(0, a.prompt), slice(a.prompt, a.prompt + 1)
     result = {"bytes": size, "bytes_bf16": size16, "us_per_token": us4, "us_per_token_bf16": us16,
-              "prompt": rel(s4[0], s16[0]), "k": rel(k, plain[0][0][:, :, :a.prompt]),
-              "v": rel(v, plain[0][1][:, :, :a.prompt])}
+              "prompt": rel(s4[0], s16[0]), "k": rel(k[:, :, slots], plain[0][0][:, :, slots]),
+              "v": rel(v[:, :, slots], plain[0][1][:, :, slots]), "token": rel(s4[1], s16[1]), "drafts": rel(s4[-1], s16[-1]),
+              "token_k": rel(k[:, :, first], plain[0][0][:, :, first]), "token_v": rel(v[:, :, first], plain[0][1][:, :, first])}
     print(f"caches: {size / 1e6:.1f} MB in 4 bits, {size16 / 1e6:.1f} MB in bf16")
     print(f"a decoded token: {us4:.1f} us through {a.layers} blocks, {us16:.1f} us with bf16 caches")
     print(f"first layer's cache against bf16: k {result['k']:.3f}, v {result['v']:.3f} (relative)")
-    print(f"hidden states of the prompt's last chunk against bf16: {result['prompt']:.4f} (relative)")
+    print(f"hidden states against bf16: {result['prompt']:.4f} of the prompt's last chunk, {result['token']:.4f} of the first "
+          f"decoded token, {result['drafts']:.4f} of the drafted ones (relative)")
     return result
 
 
