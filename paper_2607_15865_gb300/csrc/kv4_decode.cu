@@ -4,7 +4,7 @@
 // A (sequence, kv head) has G query heads x ntok new tokens = columns, taken 16 at a time (an item).
 // An item's slots are cut into blocks of 32 (head_dim 128) or 64 slots; the lengths are read on the device.
 //   few items        (up to half the SMs) each item's blocks in equal pieces, one per CTA, as many as the SMs allow and
-//                    in proportion to the lengths: CTAs of all the warps that an SM's registers hold, so that
+//                    in proportion to the lengths: one CTA of 12 (more than 8 columns: 8) warps per SM, so that
 //                    an item has few parts to merge
 //   many             the blocks of all items, in order, in equal runs, whatever the lengths: each item counts
 //                    kItemCost blocks more than it has, for what it costs to begin and to end one; or in whole items,
@@ -37,8 +37,8 @@
 // Roundings: q and the new k to bf16 after RoPE, as the bf16 stages round them; a weight P, as over the bf16 cache, at
 // head_dim 128 to bf16 (the operand's type), and at 64, where that decode keeps it to float precision, to the sum of two
 // bf16 numbers, within 2^-16; the output.  Scores, maxima, sums and O are floats.  The second number costs a further mma per
-// V operand (calls in a graph, 32 / 8 heads of 64 values: 1 x 1024 6.2 us without and 6.5 with it, 16 x 8191 25.6 and 27.7,
-// 64 x 8191 74.4 and 82.1).
+// V operand (calls in a graph, 32 / 8 heads of 64 values: 16 x 8191 25.6 us without and 27.7 with it, 64 x 8191 74.4 and
+// 82.1).
 //
 // What bounds it: instructions, not the 9/8 D bytes of a slot's k or v.  16 slots of a head of 128 values with up to 8
 // columns take 294 warp instructions, 18 of them mma, and 437 cycles of a scheduler, at which the SMs walk about
@@ -86,9 +86,10 @@ struct Cfg {
     static constexpr int PARTS = D == 64 ? 2 : 1;  // bf16 numbers that a weight is the sum of
     // Warps, and CTAs per SM: what registers and shared memory allow.  Pieces of 8 columns with 16, 12 and 8 warps (head_dim
     // 128, us): 1 x 2000 tokens 7.7, 7.0, 6.5, 1 x 32767 14.4, 14.5, 15.1, 4 x 8000 14.7, 14.8, 15.9; head_dim 64 with
-    // 16 and 12: 4 x 8000 10.7 and 10.8.  Many runs with 4, 3 and 2 CTAs, the last of 8 warps: 16 x 8191 37.8, 36.8, 39.3,
-    // 64 x 2000 38.2, 40.6, 43.9, 16 of mixed lengths 24.6, 24.0, 26.6.
-    static constexpr int W = CUT_ == kRuns ? 4 : NT == 2 ? 8 : D == 128 ? 12 : 16;
+    // 16 and 12: 1 x 1024 6.5 and 6.1, 1 x 8191 7.95 and 7.5, 1 x 30000 10.5 and 10.65, 4 x 8000 11.05 and 11.25.  Many
+    // runs with 4, 3 and 2 CTAs, the last of 8 warps: 16 x 8191 37.8, 36.8, 39.3, 64 x 2000 38.2, 40.6, 43.9, 16 of mixed
+    // lengths 24.6, 24.0, 26.6.
+    static constexpr int W = CUT_ == kRuns ? 4 : NT == 2 ? 8 : 12;
     static constexpr int CTAS = CUT_ != kRuns ? 1 : NT == 1 ? 4 : D == 128 ? 2 : 3;
     static constexpr int THREADS = 32 * W;
     static constexpr int ALONE = NT == 1 ? 24 : 16;   // pieces: an item of up to so many blocks is one (see kMinBlocks)
