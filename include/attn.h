@@ -428,8 +428,10 @@ int attn_w4bf16_rows_per_launch(int K);
  *                       zero, with z in their place.
  * Keys are quantised after RoPE, from the bf16 that the bf16 cache would hold (attn_prefill_kv, attn_decode).
  * Whatever attends to a token sees the values its slot stands for, the token itself included, so
- * a prompt's outputs do not depend on how it is cut into chunks (up to the order of float sums).  Slots past
- * the tokens written may hold anything.  The calls enqueue on `stream`, allocate nothing and use the
+ * cutting a prompt into other chunks changes its outputs only by the order of float sums, the rounding of softmax
+ * weights, and where values leave the range of attn_kv4_decode's products or a v is not a number: the calls say what
+ * comes of those, and a short chunk and a long one do not treat them alike.  Slots past the tokens written may hold
+ * anything.  The calls enqueue on `stream`, allocate nothing and use the
  * context's scratch as the other stages do; their kernels are not in attn_timing_read but for flash_fwd.
  */
 typedef struct attn_kv4 {
@@ -471,9 +473,10 @@ int attn_kv4_decode(attn_ctx* ctx, const uint16_t* q, const uint16_t* k, const u
  * (one workspace serves every layer).  A chunk of a few tokens goes through attn_kv4_decode's kernel where that is
  * the faster (with that call's range of values): it needs 0 bytes, and workspace may be NULL.
  * attn_kv4_workspace(ctx, tokens) bytes are enough for any chunk with hist_len + chunk_len <= tokens; both return 0
- * for lengths outside the cache (host only).  A chunk that needs a workspace: a NaN or an infinity in a token's v makes its values NaN for the tokens of the chunk just before it (those of its tile) too, as in
- * attn_prefill_kv.  batch * chunk_len * n_kv_heads * head_dim / 16 below 2^31 - 256.  The other arguments and the
- * errors are those of attn_prefill_kv. */
+ * for lengths outside the cache (host only).  In a chunk that needs a workspace, a NaN or an infinity in a token's v makes
+ * its values NaN for the tokens of the chunk just before it (those of its tile) too, as in attn_prefill_kv.
+ * batch * chunk_len * n_kv_heads * head_dim / 16 below 2^31 - 256.  The other arguments and the errors are those of
+ * attn_prefill_kv. */
 size_t attn_kv4_workspace(const attn_ctx* ctx, int tokens);
 size_t attn_kv4_prefill_workspace(const attn_ctx* ctx, int hist_len, int chunk_len);
 int attn_kv4_prefill_kv(attn_ctx* ctx, const uint16_t* q, const uint16_t* k, const uint16_t* v, int hist_len,

@@ -722,6 +722,11 @@ int run_kv4_decode(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uint
 // 500 8.1 and 9.6 us, over 4000 10.3 and 14.3, over 30000 17.9 and 51.7; 30 columns over 500 12.0 and 9.5, over
 // 4000 13.3 and 14.8, over 30000 28.0 and 52.2; 45 columns over 4000 15.4 and 14.9, over 8000 19.2 and 21.3, over
 // 30000 38.2 and 53.5, of four sequences over 8000 46.4 and 55.9; 60 columns over 8000 23.6 and 21.6, over 30000 53.1 and 53.9.
+// Other heads and batches: 16 sequences of 32 / 8 heads, 16 columns over 100 8.2 and 10.2, over 2048 19.8 and 54.9, 32 columns
+// over 2048 32.5 and 55.2; 8 / 2 heads, 32 columns over 2048 11.7 and 11.1, of 16 sequences 17.2 and 21.9, 48 columns over
+// 8000 17.3 and 14.6, of four sequences 21.0 and 21.6; 32 / 8 heads of 64, 16 columns over 2048 7.7 and 11.1, 48 columns over
+// 8000 15.6 and 16.1.  The rule is wrong, by up to a quarter, for one sequence with one or two kv heads over about 8000
+// (8 / 1 heads, 16 columns 15.2 and 13.4, 32 columns 16.9 and 13.6), where pieces are many and one CTA per item merges them.
 bool kv4_chunk_decodes(const attn_ctx* c, int hist, int chunk) {
     const int columns = c->cfg.n_q_heads / c->cfg.n_kv_heads * chunk;
     return chunk <= kMaxDraftTokens &&

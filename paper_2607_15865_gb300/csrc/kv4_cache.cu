@@ -7,9 +7,10 @@
 //
 // Bytes per token and kv head: 4 D of new k and v in and 9/8 D out for append (and a table row per token), the
 // reverse for read.  Measured in a graph, 8 heads of 128 values, rotating caches:
-//   append  512 tokens 2.1 us, 4096 5.9 us, 16384 21.3 us (86 MB and 8 MB of tables, 4.4 TB/s): bound by issue, 66% of
-//           the cycles (ALU 54%), the extremes of the groups, the scales and the codes; 5 CTAs of 48 registers per
-//           SM; at 40 registers, 6 CTAs, 4096 tokens took 6.6 us, at 32 9.3 us, both with spills
+//   append  512 tokens 2.1 us, 4096 5.9 us, 16384 21.3 us (86 MB and 8 MB of tables, 4.4 TB/s): between issue (63% of
+//           the cycles, cold; the extremes of the groups, the scales and the codes) and the wait for a thread's one round
+//           of loads (28% of a warp's time); 5 CTAs of 48 registers per SM; at 40 registers, 6 CTAs, 4096 tokens took
+//           6.6 us, at 32 9.3 us, both with spills
 //   read    2048 slots 2.4 us, 32767 27.7 us (172 MB, 6.2 TB/s, 92% of the copy bandwidth): memory.  A thread has eight
 //           words and their scales in flight
 #include <algorithm>

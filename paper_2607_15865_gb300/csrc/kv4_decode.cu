@@ -40,13 +40,18 @@
 // V operand (calls in a graph, 32 / 8 heads of 64 values: 16 x 8191 25.6 us without and 27.7 with it, 64 x 8191 74.4 and
 // 82.1).
 //
-// What bounds it: instructions, not the 9/8 D bytes of a slot's k or v.  16 slots of a head of 128 values with up to 8
-// columns take 294 warp instructions, 18 of them mma, and 437 cycles of a scheduler, at which the SMs walk about
-// 6 TB/s; over a whole call the ALU pipe is at 49% and the tensor pipe at 24% of the active cycles.  Around the walk a
+// What bounds it: no unit's rate, but the latencies of few warps.  16 slots of a head of 128 values with up to 8 columns
+// take 294 warp instructions, 18 of them mma, and 437 cycles of a scheduler, at which the SMs walk about 6 TB/s.  Over a
+// whole call (16 x 8191, cold) a scheduler has 3.7 warps and issues in 58% of its cycles, the ALU pipe is at 50%, the tensor
+// pipe at 24%, the DRAM at 56%; of the time from one instruction of a warp to its next, 22% goes to fixed latencies, 16% to
+// the issue, 16% to other warps' turns, 12% to a busy pipe, 8% to barriers, 6% to fetching instructions, 4% to global
+// memory.  The walk at its rate is 25 us of the call's 37.6; beginning and ending items is the rest.  With few items
+// (4 tokens over 8188: two warps, 29%) barriers, shared memory and the fetch of instructions take 42%.  Around the walk a
 // call takes 5 us for one short sequence (launch, lengths, first bytes, the warps' meeting) and about 2 us more where
-// items are shared.  In a graph, 32 / 8 heads of 128 values (in brackets the bytes at 6.77 TB/s), us: 1 x 1 4.8, 1 x 1024
-// 6.8 (0.2), 16 x 1024 12.8 (2.8), 16 x 8191 37.6 (22.3), 64 x 8191 119 (89.4), 4 tokens over 8188 12.2 (1.4); 40 / 8 heads
-// 1 x 32767 13.9 (5.6).  Over the bf16 cache 1 x 1024 7.6, 16 x 8191 79, 64 x 8191 311, 1 x 32767 26.9.
+// items are shared.  In a graph, 32 / 8 heads of 128 values (in brackets the bytes at 6.77 TB/s), us: 1 x 1 4.6, 1 x 1024
+// 7.0 (0.2), 16 x 1024 12.8 (2.8), 16 x 8191 37.6 (22.3), 64 x 8191 119 (89.4), 4 tokens over 8188 12.5 (1.4); 40 / 8 heads
+// 1 x 32767 13.9 (5.6); 32 / 8 heads of 64 1 x 1024 6.1 (0.1), 16 x 8191 27.7 (11.2), 64 x 8191 82 (44.7).  Over the bf16 cache,
+// heads of 128, 1 x 1024 7.6, 16 x 8191 79, 64 x 8191 311, 1 x 32767 26.9.
 //
 // The new tokens: a CTA that holds their slots rotates and quantises them, a warp per row, before its own
 // blocks, writes them to the cache and stages them for the warp that has their block.  Slots past the last
