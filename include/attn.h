@@ -77,6 +77,7 @@ extern "C" {
 
 /* Bits of the device error word. */
 #define ATTN_DEVERR_HIST_RANGE 1 /* a decode hist_len[b] was outside [0, max_len - 1] */
+#define ATTN_DEVERR_TREE 4       /* a drafted token's parent, or an accepted token, was none (attn_tree_decode, _accept) */
 #define ATTN_DEVERR_TIMEOUT 2    /* a pipeline wait inside a kernel exceeded its time limit (about 1 s);
                                     the affected outputs are not written */
 
@@ -482,6 +483,59 @@ size_t attn_kv4_prefill_workspace(const attn_ctx* ctx, int hist_len, int chunk_l
 int attn_kv4_prefill_kv(attn_ctx* ctx, const uint16_t* q, const uint16_t* k, const uint16_t* v, int hist_len,
                         int chunk_len, const attn_kv4* cache, uint16_t* out, void* workspace, size_t workspace_bytes,
                         attn_stream_t stream);
+
+/*
+ * Attention with a sliding window (no counterpart in the paper, whose models attend to everything).  A query at position p
+ * sees the slots s <= p with p - s < window or s < sinks: the last `window` positions, its own among them, and the first
+ * `sinks` ones, which stay visible.  The caches are those of the other stages, whole; slots that nobody sees are not read
+ * but for those that share a tile of 128 with one that somebody sees, and what they hold (NaN too) reaches no output.
+ * window >= 1, sinks >= 0 (both may exceed max_len).  These calls want the context's device to be the current one
+ * (ATTN_EINVAL otherwise).
+ *
+ * attn_window_prefill_kv is attn_prefill_kv (hist_len = 0: attn_prefill) under a window; the other arguments and the errors
+ * are those of that call.  attn_window_decode is attn_decode (n_new = 1) and attn_decode_multi under one: n_new (1 ..
+ * ATTN_TREE_TOKENS) tokens per sequence at positions d_hist_len[b] + i, causal among themselves, at either head_dim.  A
+ * sequence with a position outside [0, max_len - 1] is skipped (cache and out not written) and sets
+ * ATTN_DEVERR_HIST_RANGE; the other arguments and the errors are those of attn_decode_multi.
+ */
+#define ATTN_TREE_TOKENS 64
+int attn_window_prefill_kv(attn_ctx* ctx, const uint16_t* q, const uint16_t* k, const uint16_t* v, int hist_len,
+                           int chunk_len, int window, int sinks, uint16_t* k_cache, uint16_t* v_cache, uint16_t* out,
+                           attn_stream_t stream);
+int attn_window_decode(attn_ctx* ctx, const uint16_t* q, const uint16_t* k, const uint16_t* v, const int32_t* d_hist_len,
+                       int n_new, int window, int sinks, uint16_t* k_cache, uint16_t* v_cache, uint16_t* out,
+                       attn_stream_t stream);
+
+/*
+ * Attention of a tree of drafted tokens (speculative decoding with several candidates for a position, which the paper
+ * names as future work, Section 6): n_new (1 .. ATTN_TREE_TOKENS) tokens per sequence.
+ *   d_parents  device int32 [batch][n_new]: the index, below i, of token i's parent in the tree; -1: it follows the history
+ *              (there may be several of those); -2: there is no token i, nothing is its child, and its row of out and its
+ *              slot are left as they were.
+ * Token i is written to slot d_hist_len[b] + i.  It is at position d_hist_len[b] + depth (0 without a parent, one more than
+ * its parent's with one), for RoPE and the window, and sees the history, its ancestors and itself.  window 0: all of
+ * those; otherwise those that the window of attn_window_decode allows, by their positions.  A sequence whose last token's
+ * slot would be past max_len - 1, or whose length is outside [0, max_len], is skipped (cache and out not written) and sets
+ * ATTN_DEVERR_HIST_RANGE; one with a parent that is not a token before its child is skipped and sets
+ * ATTN_DEVERR_TREE.  q, k, v, out and the caches: as in attn_decode_multi.
+ */
+int attn_tree_decode(attn_ctx* ctx, const uint16_t* q, const uint16_t* k, const uint16_t* v, const int32_t* d_hist_len,
+                     const int32_t* d_parents, int n_new, int window, int sinks, uint16_t* k_cache, uint16_t* v_cache,
+                     uint16_t* out, attn_stream_t stream);
+
+/*
+ * What follows the verification of a tree: token d_leaf[b] (device int32 [batch], -1: none) and its ancestors are accepted.
+ * Their k and v move, in order, to the slots from d_hist_len[b] on, where a history has them (their positions are those
+ * that k was rotated for), in the caches of every layer: k_caches and v_caches are host arrays of n_layers device
+ * pointers, which are read before the call returns.  d_new_len (NULL, or device int32 [batch], not overlapping
+ * d_hist_len): the lengths after that.  Slots past d_new_len[b] hold what they held.  A sequence that attn_tree_decode would
+ * skip, or whose d_leaf[b] is no token of the tree, keeps its cache and its length, and sets the same bits.
+ * Device arrays are 4-byte aligned, caches 16-byte; a cache may be in the list once.  Returns ATTN_OK, ATTN_EINVAL
+ * or ATTN_ECUDA.
+ */
+int attn_tree_accept(attn_ctx* ctx, const int32_t* d_hist_len, const int32_t* d_parents, const int32_t* d_leaf, int n_new,
+                     uint16_t* const* k_caches, uint16_t* const* v_caches, int n_layers, int32_t* d_new_len,
+                     attn_stream_t stream);
 
 /* Static text for an ATTN_* code. */
 const char* attn_strerror(int code);

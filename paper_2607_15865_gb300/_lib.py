@@ -15,7 +15,8 @@ LIB_PATH = os.path.join(_PKG, "libattn_gb300.so")
 
 ATTN_OK, ATTN_EINVAL, ATTN_EARCH, ATTN_ECUDA, ATTN_ENOMEM, ATTN_EDEVICE = 0, -1, -2, -3, -4, -5
 W4_WEIGHTS_STATIC = 1
-DEVERR_HIST_RANGE, DEVERR_TIMEOUT = 1, 2
+DEVERR_HIST_RANGE, DEVERR_TIMEOUT, DEVERR_TREE = 1, 2, 4
+TREE_TOKENS = 64
 
 EXPORTED = ("attn_create", "attn_destroy", "attn_prefill", "attn_prefill_kv", "attn_decode",
             "attn_decode_multi", "attn_prompt", "attn_decode_steps", "attn_device_error", "attn_set_wait_limit",
@@ -24,7 +25,7 @@ EXPORTED = ("attn_create", "attn_destroy", "attn_prefill", "attn_prefill_kv", "a
             "attn_w4bf16_rows_per_launch", "attn_w4bf16_gemv_fused", "attn_decode_layer",
             "attn_w4bf16_gemm", "attn_prefill_layer", "attn_prefill_layer_workspace", "attn_kv4_slots",
             "attn_kv4_append", "attn_kv4_read", "attn_kv4_decode", "attn_kv4_workspace", "attn_kv4_prefill_workspace",
-            "attn_kv4_prefill_kv")
+            "attn_kv4_prefill_kv", "attn_window_prefill_kv", "attn_window_decode", "attn_tree_decode", "attn_tree_accept")
 NOALLOC_SCRATCH_FLOATS = 1 << 20
 # attn_timing_read's slots; no kernel runs as decode_combine (the decode merges itself): it reads 0
 KERNELS = ("rope_append", "flash_fwd", "decode_split", "decode_combine")
@@ -122,6 +123,14 @@ def load(path: str = LIB_PATH):
     lib.attn_kv4_prefill_workspace.restype = ctypes.c_size_t
     lib.attn_kv4_prefill_kv.argtypes = [vp, u16p, u16p, u16p, i32, i32, kv4, u16p, vp, ctypes.c_size_t, vp]
     lib.attn_kv4_prefill_kv.restype = i32
+    lib.attn_window_prefill_kv.argtypes = [vp, u16p, u16p, u16p, i32, i32, i32, i32, u16p, u16p, u16p, vp]
+    lib.attn_window_prefill_kv.restype = i32
+    lib.attn_window_decode.argtypes = [vp, u16p, u16p, u16p, vp, i32, i32, i32, u16p, u16p, u16p, vp]
+    lib.attn_window_decode.restype = i32
+    lib.attn_tree_decode.argtypes = [vp, u16p, u16p, u16p, vp, vp, i32, i32, i32, u16p, u16p, u16p, vp]
+    lib.attn_tree_decode.restype = i32
+    lib.attn_tree_accept.argtypes = [vp, vp, vp, vp, i32, ctypes.POINTER(vp), ctypes.POINTER(vp), i32, vp, vp]
+    lib.attn_tree_accept.restype = i32
     lib.attn_strerror.argtypes = [i32]
     lib.attn_strerror.restype = ctypes.c_char_p
     lib.attn_last_cuda_error_string.argtypes = []

@@ -12,6 +12,9 @@ and the stage driver of Sections 4.1 and 4.5:
   prompt        a prompt of any length in segments: 1 prefill (or prefill_kv) + N prefill_kv
   decode_steps  n decode steps in a row, step t at positions hist_len + t (step-major inputs)
 
+the stages under a sliding window, window_prefill_kv and window_decode; a tree of drafted tokens, tree_decode (attention) and
+tree_accept (the accepted ones move to the end of the history);
+
 and the stages over a cache held in 4 bits (kv4.Kv4Cache): kv4_append, kv4_read, kv4_decode, kv4_prefill_kv.
 
 Caches are [B,Hkv,L,D] bf16 tensors owned by the caller and updated in place.
@@ -69,6 +72,12 @@ def _empty(shape, dtype, like, stream) -> torch.Tensor:
 def _is_len(t, batch: int) -> bool:
     return (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == torch.int32 and t.is_contiguous()
             and t.shape == (batch,))
+
+
+def _int32(x) -> int:
+    """A window or a number of sinks for the C call: one past the largest int means the same as that, and a negative one is
+    refused there whichever it is."""
+    return max(min(int(x), 2 ** 31 - 1), -1)
 
 
 class Attention:
@@ -338,6 +347,84 @@ class Attention:
                                           workspace.data_ptr(), workspace.numel(), _stream(stream))
         self._check(rc, "attn_kv4_prefill_kv")
         return out
+
+    def window_prefill_kv(self, q, k, v, hist_len: int, window: int, k_cache, v_cache, sinks: int = 0, out=None,
+                          stream=None) -> torch.Tensor:
+        """prefill_kv (hist_len = 0: prefill) where position p sees the last `window` positions, its own among them, and
+        the first `sinks`."""
+        S = q.shape[1]
+        qs = (self.batch, S, self.n_q_heads, self.head_dim)
+        ks = (self.batch, S, self.n_kv_heads, self.head_dim)
+        args = (_ptr(q, "q", qs), _ptr(k, "k", ks), _ptr(v, "v", ks))
+        out = _empty(q.shape, q.dtype, q, stream) if out is None else out
+        rc = self.lib.attn_window_prefill_kv(self._ctx, *args, int(hist_len), S, _int32(window), _int32(sinks),
+                                             _ptr(k_cache, "k_cache", self._cache), _ptr(v_cache, "v_cache", self._cache),
+                                             _ptr(out, "out", qs), _stream(stream))
+        if rc:
+            self._check(rc, "attn_window_prefill_kv")
+        return out
+
+    def window_decode(self, q, k, v, hist_len: torch.Tensor, window: int, k_cache, v_cache, sinks: int = 0, out=None,
+                      stream=None) -> torch.Tensor:
+        """decode / decode_multi under the window of window_prefill_kv: n = q.shape[1] (1 .. 64) new tokens per sequence."""
+        args, tail, out = self._few(q, k, v, hist_len, k_cache, v_cache, out, stream)
+        rc = self.lib.attn_window_decode(self._ctx, *args, hist_len.data_ptr(), q.shape[1], _int32(window), _int32(sinks), *tail)
+        if rc:
+            self._check(rc, "attn_window_decode")
+        return out
+
+    def tree_decode(self, q, k, v, hist_len: torch.Tensor, parents: torch.Tensor, k_cache, v_cache, window: int = 0,
+                    sinks: int = 0, out=None, stream=None) -> torch.Tensor:
+        """Attention of a tree of n = q.shape[1] (1 .. 64) drafted tokens per sequence.  parents: int32 [B, n] on the device,
+        the index (below i) of token i's parent, -1 where it follows the history, -2 where there is no token i (its row of
+        `out` and its slot are left as they were).  Token i goes to slot hist_len + i; it is at position hist_len + its depth
+        and sees the history, its ancestors and itself, under the window of window_prefill_kv unless window is 0."""
+        if not self._is_tree(parents, q.shape[1]):
+            raise TypeError("parents must be a contiguous int32 CUDA tensor of shape [batch, n]")
+        args, tail, out = self._few(q, k, v, hist_len, k_cache, v_cache, out, stream)
+        rc = self.lib.attn_tree_decode(self._ctx, *args, hist_len.data_ptr(), parents.data_ptr(), q.shape[1], _int32(window),
+                                       _int32(sinks), *tail)
+        if rc:
+            self._check(rc, "attn_tree_decode")
+        return out
+
+    def _is_tree(self, t, n: int) -> bool:
+        return (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == torch.int32 and t.is_contiguous()
+                and t.shape == (self.batch, n))
+
+    def _few(self, q, k, v, hist_len, k_cache, v_cache, out, stream):
+        n = q.shape[1]
+        qs = (self.batch, n, self.n_q_heads, self.head_dim)
+        ks = (self.batch, n, self.n_kv_heads, self.head_dim)
+        if not _is_len(hist_len, self.batch):
+            raise TypeError("hist_len must be a contiguous int32 CUDA tensor of shape [batch]")
+        args = _ptr(q, "q", qs), _ptr(k, "k", ks), _ptr(v, "v", ks)
+        cache = _ptr(k_cache, "k_cache", self._cache), _ptr(v_cache, "v_cache", self._cache)
+        out = _empty(q.shape, q.dtype, q, stream) if out is None else out
+        return args, (*cache, _ptr(out, "out", qs), _stream(stream)), out
+
+    def tree_accept(self, hist_len: torch.Tensor, parents: torch.Tensor, leaf: torch.Tensor, caches, new_len=None,
+                    stream=None) -> torch.Tensor:
+        """Accept token leaf[b] (-1: none) of each tree of tree_decode and its ancestors: their k and v move, in order, to the
+        slots from hist_len[b] on.  caches: the (k_cache, v_cache) of every layer.  Returns the new lengths (new_len, or a
+        tensor allocated here; not hist_len itself)."""
+        if not _is_len(hist_len, self.batch) or not _is_len(leaf, self.batch):
+            raise TypeError("hist_len and leaf must be contiguous int32 CUDA tensors of shape [batch]")
+        if not isinstance(parents, torch.Tensor) or parents.dim() != 2 or not self._is_tree(parents, parents.shape[1]):
+            raise TypeError("parents must be a contiguous int32 CUDA tensor of shape [batch, n]")
+        ks = [_ptr(k, "k_cache", self._cache) for k, _ in caches]
+        vs = [_ptr(v, "v_cache", self._cache) for _, v in caches]
+        if len(set(ks + vs)) != len(ks) + len(vs):
+            raise ValueError("a cache is in the list twice")
+        new_len = _empty(hist_len.shape, torch.int32, hist_len, stream) if new_len is None else new_len
+        if not _is_len(new_len, self.batch):
+            raise TypeError("new_len must be a contiguous int32 CUDA tensor of shape [batch]")
+        ptrs = ctypes.c_void_p * max(len(ks), 1)
+        rc = self.lib.attn_tree_accept(self._ctx, hist_len.data_ptr(), parents.data_ptr(), leaf.data_ptr(), parents.shape[1],
+                                       ptrs(*ks), ptrs(*vs), len(ks), new_len.data_ptr(), _stream(stream))
+        if rc:
+            self._check(rc, "attn_tree_accept")
+        return new_len
 
     def timing_enable(self, max_launches: int):
         """Record CUDA events around every kernel of the following calls (0 disables)."""

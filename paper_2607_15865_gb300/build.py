@@ -21,8 +21,9 @@ LIB = os.path.join(PKG, "libattn_gb300.so")
 SOURCES = [("attn_api.cu", "attn_api", []), ("rope_append.cu", "rope_append", []),
            ("decode_tc.cu", "decode_tc", []), ("flash_fwd.cu", "flash_fwd", []),
            ("decode_noalloc.cu", "decode_noalloc", []), ("w4_gemv.cu", "w4_gemv", []), ("w4_gemm.cu", "w4_gemm", []),
-           ("kv4_cache.cu", "kv4_cache", []), ("kv4_decode.cu", "kv4_decode", [])]
-HEADERS = ["internal.h", "sm100_ptx.cuh", "flash_rows.h", "kv4.cuh"]
+           ("kv4_cache.cu", "kv4_cache", []), ("kv4_decode.cu", "kv4_decode", []),
+           ("tree_decode.cu", "tree_decode", [])]
+HEADERS = ["internal.h", "sm100_ptx.cuh", "flash_rows.h", "kv4.cuh", "tree.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -811,6 +811,90 @@ int attn_kv4_prefill_kv(attn_ctx* c, const uint16_t* q, const uint16_t* k, const
     return run_flash(c, maps, hist_len, chunk_len, chunk_len, out, st);
 }
 
+// ------------------------------------------------------------------ windows and trees
+
+namespace {
+
+// Whether the calling thread's current device is the context's (the calls below are refused otherwise).
+bool on_device(const attn_ctx* c) {
+    int dev = -1;
+    return cudaGetDevice(&dev) == cudaSuccess && dev == c->device;
+}
+
+int run_tree(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uint16_t* v, const int32_t* d_hist_len,
+             const int32_t* d_parents, int n_new, int window, int sinks, uint16_t* k_cache, uint16_t* v_cache, uint16_t* out,
+             attn_stream_t stream) {
+    if (q == nullptr || k == nullptr || v == nullptr || d_hist_len == nullptr || k_cache == nullptr || v_cache == nullptr ||
+        out == nullptr)
+        return ATTN_EINVAL;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out) ||
+        (reinterpret_cast<uintptr_t>(d_hist_len) & 3u) || (reinterpret_cast<uintptr_t>(d_parents) & 3u))
+        return ATTN_EINVAL;
+    if (n_new < 1 || n_new > ATTN_TREE_TOKENS || n_new > c->cfg.max_len || sinks < 0 || !on_device(c)) return ATTN_EINVAL;
+    const attn::TreeCall t{q, k, v, d_hist_len, d_parents, 0, n_new, std::min(window, c->cfg.max_len),
+                           std::min(sinks, c->cfg.max_len), k_cache, v_cache, c->d_cos, c->d_sin, out, c->d_err};
+    const cudaError_t e = attn::launch_tree_decode(c->shape, t, reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? ATTN_OK : cuda_fail(e, "tree decode launch");
+}
+
+}  // namespace
+
+int attn_window_prefill_kv(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uint16_t* v, int hist_len, int chunk_len,
+                           int window, int sinks, uint16_t* k_cache, uint16_t* v_cache, uint16_t* out, attn_stream_t stream) {
+    if (c == nullptr || q == nullptr || k == nullptr || v == nullptr || k_cache == nullptr || v_cache == nullptr ||
+        out == nullptr)
+        return ATTN_EINVAL;
+    if (chunk_len < 1 || hist_len < 0 || static_cast<long>(hist_len) + chunk_len > c->cfg.max_len) return ATTN_EINVAL;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out))
+        return ATTN_EINVAL;
+    if (window < 1 || sinks < 0 || !on_device(c)) return ATTN_EINVAL;
+    const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    cudaError_t e = timed(c, ATTN_KERNEL_ROPE_APPEND, st, [&](int*) {
+        return attn::launch_rope_append(c->shape, k, v, hist_len, nullptr, chunk_len, chunk_len, c->d_cos, c->d_sin, c->d_cos_t,
+                                        c->d_sin_t, k_cache, v_cache, c->d_err, st);
+    });
+    if (e != cudaSuccess) return cuda_fail(e, "rope_append launch");
+    const attn::TreeCall t{q, k, v, nullptr, nullptr, hist_len, chunk_len, std::min(window, c->cfg.max_len),
+                           std::min(sinks, c->cfg.max_len), k_cache, v_cache, c->d_cos, c->d_sin, out, c->d_err};
+    e = attn::launch_tree_decode(c->shape, t, st);
+    return e == cudaSuccess ? ATTN_OK : cuda_fail(e, "window prefill launch");
+}
+
+int attn_window_decode(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uint16_t* v, const int32_t* d_hist_len,
+                       int n_new, int window, int sinks, uint16_t* k_cache, uint16_t* v_cache, uint16_t* out,
+                       attn_stream_t stream) {
+    if (c == nullptr || window < 1) return ATTN_EINVAL;
+    return run_tree(c, q, k, v, d_hist_len, nullptr, n_new, window, sinks, k_cache, v_cache, out, stream);
+}
+
+int attn_tree_decode(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uint16_t* v, const int32_t* d_hist_len,
+                     const int32_t* d_parents, int n_new, int window, int sinks, uint16_t* k_cache, uint16_t* v_cache,
+                     uint16_t* out, attn_stream_t stream) {
+    if (c == nullptr || d_parents == nullptr || window < 0) return ATTN_EINVAL;
+    return run_tree(c, q, k, v, d_hist_len, d_parents, n_new, window == 0 ? c->cfg.max_len : window, sinks, k_cache, v_cache,
+                    out, stream);
+}
+
+int attn_tree_accept(attn_ctx* c, const int32_t* d_hist_len, const int32_t* d_parents, const int32_t* d_leaf, int n_new,
+                     uint16_t* const* k_caches, uint16_t* const* v_caches, int n_layers, int32_t* d_new_len,
+                     attn_stream_t stream) {
+    if (c == nullptr || d_hist_len == nullptr || d_parents == nullptr || d_leaf == nullptr || k_caches == nullptr ||
+        v_caches == nullptr || n_layers < 1 || n_new < 1 || n_new > ATTN_TREE_TOKENS || n_new > c->cfg.max_len)
+        return ATTN_EINVAL;
+    const int32_t* ends = d_hist_len + c->cfg.batch;
+    if (d_new_len != nullptr && d_new_len < ends && d_hist_len < d_new_len + c->cfg.batch) return ATTN_EINVAL;
+    if ((reinterpret_cast<uintptr_t>(d_hist_len) | reinterpret_cast<uintptr_t>(d_parents) |
+         reinterpret_cast<uintptr_t>(d_leaf) | reinterpret_cast<uintptr_t>(d_new_len)) & 3u)
+        return ATTN_EINVAL;
+    for (int l = 0; l < n_layers; ++l)
+        if (k_caches[l] == nullptr || v_caches[l] == nullptr || !aligned16(k_caches[l]) || !aligned16(v_caches[l]))
+            return ATTN_EINVAL;
+    if (!on_device(c)) return ATTN_EINVAL;
+    const cudaError_t e = attn::launch_tree_accept(c->shape, d_hist_len, d_parents, d_leaf, n_new, k_caches, v_caches, n_layers,
+                                                   d_new_len, c->d_err, reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? ATTN_OK : cuda_fail(e, "tree accept launch");
+}
+
 // Exported for the tests, not part of attn.h: how the library cuts a call on this device (out[4] as
 // in internal.h; decode: splits per item and mode), so that a test can assert the path that it names.
 int attn_plan_prefill(const attn_ctx* c, int hist_len, int chunk_len, int* out) {

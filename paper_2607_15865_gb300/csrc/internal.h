@@ -12,6 +12,7 @@ namespace attn {
 // Error-word bits (mirrors ATTN_DEVERR_* of attn.h).
 constexpr int kDevErrHistRange = 1;
 constexpr int kDevErrTimeout = 2;
+constexpr int kDevErrTree = 4;
 // The thread's last failure text, read by attn_last_cuda_error_string (attn_api.cu).
 // record_cuda_error formats a CUDA error with the failing step and returns ATTN_ECUDA
 // (-3); record_error_text stores a plain text.
@@ -165,6 +166,30 @@ cudaError_t launch_kv4_decode(const Shape& s, const uint16_t* q, const uint16_t*
                               const int32_t* d_hist, int hist, int ntok, const Kv4Cache& c, const float* cos_tab,
                               const float* sin_tab, float* part_o, float* part_ml, int* counters, uint16_t* out, int* err,
                               int num_sms, cudaStream_t st, uint64_t wait_ns);
+
+// Attention of a few new tokens per sequence, a chain or a tree, under a window (tree_decode.cu).  n (1 .. 64) tokens per
+// sequence at d_hist[b] + their depth (tree.cuh) are appended from slot d_hist[b] on and attended to.
+// window, sinks: within [0, max_len] (a window of max_len sees everything).
+struct TreeCall {
+    const uint16_t* q;
+    const uint16_t* k;
+    const uint16_t* v;
+    const int32_t* d_hist;
+    const int32_t* parents;  // [batch][n], NULL: chains
+    int hist, n, window, sinks;
+    uint16_t* k_cache;
+    uint16_t* v_cache;
+    const float* cos_tab;
+    const float* sin_tab;
+    uint16_t* out;
+    int* err;
+};
+cudaError_t launch_tree_decode(const Shape& s, const TreeCall& c, cudaStream_t st);
+// Moves the k and v of token leaf[b] and its ancestors to the slots from d_hist[b] on in every layer's caches; new_len
+// (may be NULL): the lengths after that.
+cudaError_t launch_tree_accept(const Shape& s, const int32_t* d_hist, const int32_t* parents, const int32_t* leaf, int n,
+                               uint16_t* const* k_caches, uint16_t* const* v_caches, int layers, int32_t* new_len, int* err,
+                               cudaStream_t st);
 
 // W4BF16 GEMV (w4_gemv.cu): y[m, n] = sum_k x[m, k] (q[n, k] - z[n, k/128]) s[n, k/128] for
 // the activation rows of one launch.  tiles: the tile
