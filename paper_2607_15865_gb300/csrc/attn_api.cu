@@ -41,8 +41,8 @@ struct attn_ctx {
     uint16_t* d_lk;     // output, bf16 [B][Hq*D], [B][Hkv*D], [B][Hkv*D], [B][Hq*D]
     uint16_t* d_lv;
     uint16_t* d_lo;
-    float* d_flash_o;   // flash tail pieces: [num_sms * 256, D] partial O
-    float* d_flash_ml;  // and [num_sms * 256, 2] (m, l)
+    float* d_flash_o;   // flash tail pieces and tree_decode's parts: [num_sms * 512, D] partial O
+    float* d_flash_ml;  // and [num_sms * 512, 2] (m, l)
     int* d_err;
     PFN_cuTensorMapEncodeTiled_v12000 encode;
     // decode tensor maps of the last cache pair seen
@@ -234,6 +234,7 @@ int attn_create(const attn_cfg* cfg, attn_ctx** out) {
     e = attn::configure_flash_fwd();
     if (e == cudaSuccess) e = attn::configure_decode_tc();
     if (e == cudaSuccess) e = attn::configure_kv4_decode();
+    if (e == cudaSuccess) e = attn::configure_tree_decode();
     if (e != cudaSuccess) {
         delete c;
         return cuda_fail(e, "configure kernels");
@@ -262,7 +263,7 @@ int attn_create(const attn_cfg* cfg, attn_ctx** out) {
     oom |= cudaMalloc(&c->d_sin_t, ntab * sizeof(float)) != cudaSuccess;
     oom |= cudaMalloc(&c->d_part_o, part_rows * cfg->head_dim * sizeof(float)) != cudaSuccess;
     oom |= cudaMalloc(&c->d_part_ml, part_rows * 2 * sizeof(float)) != cudaSuccess;
-    const size_t piece_rows = static_cast<size_t>(c->num_sms) * 256;
+    const size_t piece_rows = static_cast<size_t>(c->num_sms) * 512;
     oom |= cudaMalloc(&c->d_flash_o, piece_rows * cfg->head_dim * sizeof(float)) != cudaSuccess;
     oom |= cudaMalloc(&c->d_flash_ml, piece_rows * 2 * sizeof(float)) != cudaSuccess;
     oom |= cudaMalloc(&c->d_err, sizeof(int)) != cudaSuccess;
@@ -340,6 +341,20 @@ int decode_splits(const attn_ctx* c, int ntok) {
     return std::min(attn::decode_tc_num_splits(c->shape, c->num_sms, ncg, ntok), c->nsplit_max / ntok);
 }
 
+// The tensor maps of the whole caches in c->dec_maps (kept for the pair of caches that they were last made for).
+int decode_maps(attn_ctx* c, const uint16_t* k_cache, const uint16_t* v_cache) {
+    if (k_cache == c->dec_k && v_cache == c->dec_v) return ATTN_OK;
+    const cudaError_t e = attn::make_decode_tc_maps(c->encode, c->shape, k_cache, v_cache, &c->dec_maps);
+    if (e != cudaSuccess) {
+        c->dec_k = c->dec_v = nullptr;
+        std::snprintf(g_cuda_msg, sizeof g_cuda_msg, "cuTensorMapEncodeTiled failed for the decode caches");
+        return ATTN_ECUDA;
+    }
+    c->dec_k = k_cache;
+    c->dec_v = v_cache;
+    return ATTN_OK;
+}
+
 // One decode step of ntok new tokens per sequence at positions d_hist_len[b] + hist_add + i.
 // after_decode: the previous launch on `st` was this context's decode of the same caches
 // (a decode loop).
@@ -356,16 +371,8 @@ int run_decode(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uint16_t
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(k_cache) || !aligned16(v_cache) ||
         !aligned16(out) || (reinterpret_cast<uintptr_t>(d_hist_len) & 3u))
         return ATTN_EINVAL;
-    if (k_cache != c->dec_k || v_cache != c->dec_v) {
-        const cudaError_t me = attn::make_decode_tc_maps(c->encode, c->shape, k_cache, v_cache, &c->dec_maps);
-        if (me != cudaSuccess) {
-            c->dec_k = c->dec_v = nullptr;
-            std::snprintf(g_cuda_msg, sizeof g_cuda_msg, "cuTensorMapEncodeTiled failed for the decode caches");
-            return ATTN_ECUDA;
-        }
-        c->dec_k = k_cache;
-        c->dec_v = v_cache;
-    }
+    const int rc = decode_maps(c, k_cache, v_cache);
+    if (rc != ATTN_OK) return rc;
     if (ntok < 1 || ntok > kMaxDraftTokens) return ATTN_EINVAL;
     const int ncg = attn::decode_tc_column_groups(c->cfg.n_q_heads / c->cfg.n_kv_heads, ntok);
     // grid dimensions of sequences x column groups stay within 65535
@@ -831,8 +838,11 @@ int run_tree(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uint16_t* 
         (reinterpret_cast<uintptr_t>(d_hist_len) & 3u) || (reinterpret_cast<uintptr_t>(d_parents) & 3u))
         return ATTN_EINVAL;
     if (n_new < 1 || n_new > ATTN_TREE_TOKENS || n_new > c->cfg.max_len || sinks < 0 || !on_device(c)) return ATTN_EINVAL;
+    const int rc = decode_maps(c, k_cache, v_cache);
+    if (rc != ATTN_OK) return rc;
     const attn::TreeCall t{q, k, v, d_hist_len, d_parents, 0, n_new, std::min(window, c->cfg.max_len),
-                           std::min(sinks, c->cfg.max_len), k_cache, v_cache, c->d_cos, c->d_sin, out, c->d_err};
+                           std::min(sinks, c->cfg.max_len), k_cache, v_cache, c->d_cos, c->d_sin, out, c->d_err,
+                           &c->dec_maps, c->d_flash_o, c->d_flash_ml, c->d_counters, c->num_sms, c->wait_ns};
     const cudaError_t e = attn::launch_tree_decode(c->shape, t, reinterpret_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? ATTN_OK : cuda_fail(e, "tree decode launch");
 }
@@ -855,7 +865,8 @@ int attn_window_prefill_kv(attn_ctx* c, const uint16_t* q, const uint16_t* k, co
     });
     if (e != cudaSuccess) return cuda_fail(e, "rope_append launch");
     const attn::TreeCall t{q, k, v, nullptr, nullptr, hist_len, chunk_len, std::min(window, c->cfg.max_len),
-                           std::min(sinks, c->cfg.max_len), k_cache, v_cache, c->d_cos, c->d_sin, out, c->d_err};
+                           std::min(sinks, c->cfg.max_len), k_cache, v_cache, c->d_cos, c->d_sin, out, c->d_err,
+                           nullptr, nullptr, nullptr, nullptr, 0, 0};
     e = attn::launch_tree_decode(c->shape, t, st);
     return e == cudaSuccess ? ATTN_OK : cuda_fail(e, "window prefill launch");
 }

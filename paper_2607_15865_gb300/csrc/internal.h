@@ -183,7 +183,14 @@ struct TreeCall {
     const float* sin_tab;
     uint16_t* out;
     int* err;
+    const DecodeMaps* maps;  // of the caches
+    float* part_o;           // num_sms * 512 rows of head_dim floats, and of 2: the parts of items that CTAs share
+    float* part_ml;
+    int* counters;  // an int per (sequence, kv head, 256 rows), zero before and after every launch
+    int num_sms;
+    uint64_t wait_ns;
 };
+cudaError_t configure_tree_decode();
 cudaError_t launch_tree_decode(const Shape& s, const TreeCall& c, cudaStream_t st);
 // Moves the k and v of token leaf[b] and its ancestors to the slots from d_hist[b] on in every layer's caches; new_len
 // (may be NULL): the lengths after that.
