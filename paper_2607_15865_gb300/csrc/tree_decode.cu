@@ -45,7 +45,7 @@ constexpr int kMaxSeqs = 128;  // sequences of one launch (their tiles are summe
 constexpr uint32_t kTmemCols = 512;  // S [0, 256): two of 128; O [256, 256 + 2 D): two
 constexpr uint32_t kTmO = 2 * BN;
 constexpr int kFlags = 8;
-constexpr int kMinRun = 2;  // tiles of a run, where there are few
+constexpr int kLonger = 4;  // tiles that a piece may be longer than a run
 // Registers with three warpgroups (NT = 2): 168 a thread at launch, of which the producer's group leaves 72 to the others.
 constexpr int kLaunchRegs = 168;
 constexpr uint32_t kRegsLow = 96, kRegsHigh = 200;
@@ -73,7 +73,8 @@ struct Cfg {
     // int [kFlags]: the segment, from 1, with a value that is not finite in a masked tile; the guards are at most NS / 2 + 1
     // segments ahead of the softmax
     static constexpr int OFF_FLAG = OFF_ABORT + 4;
-    static constexpr int BYTES = OFF_FLAG + kFlags * 4;
+    static constexpr int OFF_CUT = OFF_FLAG + kFlags * 4;  // int [2]: tiles of a run (0: pieces), of a piece
+    static constexpr int BYTES = OFF_CUT + 8;
     static_assert(NS / 2 + 1 < kFlags, "flags");
     static constexpr int ALLOC = BYTES + 1024;  // slack to align the base to 1024 bytes
     static_assert(ALLOC <= 232448, "shared memory budget of one CTA");
@@ -122,43 +123,66 @@ __device__ __forceinline__ Span span_of(int hist, const Args& a) {
     return s;
 }
 
-// A run's part of an item: its tiles lo .. hi - 1 of nt; first: the item's tile 0 in the order that runs are cut from.
+// A CTA's part of an item: its tiles lo .. hi - 1 of nt, in part r_mine - r_first of `parts`.
 struct Seg {
-    int b, h, hist, ns, skip, lo, hi, nt, first;
+    int b, h, hist, ns, skip, lo, hi, nt, first;  // first: the item's tile 0 in the order that runs are cut from
+    int r_first, parts;                           // the item's first run or piece, and how many have a part of it
     __device__ __forceinline__ int key(int v) const { return (v < ns ? v : v + skip) * BN; }  // first slot of tile v
     __device__ __forceinline__ bool whole() const { return lo == 0 && hi == nt; }
 };
 
+// What a CTA takes.  len > 0: the tiles pos .. end - 1 of all items in order, one of the runs of len tiles.  len = 0: the
+// piece pos, the only one, of an item that is cut into pieces of at most `target` tiles.
 struct Run {
-    int pos, end, len, total;
+    int pos, end, len, target, id;
+    // The CTA's slot for its part of an item: 0 where the item began by the run's start, 1 where it began in it.
+    __device__ __forceinline__ int slot(const Seg& s, int r) const { return len == 0 || s.first <= r * len ? 0 : 1; }
 };
 
-// The run's next segment of a sequence that has tokens and is not to be skipped, a converged warp; kin: its tokens' (tree.cuh).
-__device__ __forceinline__ bool next_seg(Run& r, const Args& a, const int* pre, const int* hist_s, int lane, Seg& s,
-                                         uint64_t (&kin)[2], bool report) {
-    while (r.pos < r.end) {
-        int before = 0;
+// The run's next segment, a converged warp; false: none is left.  pre: tiles (pieces) of the items of sequences .. b.
+__device__ __forceinline__ bool next_seg(Run& r, const Args& a, const int* pre, const int* hist_s, int lane, Seg& s) {
+    if (r.pos >= r.end) return false;
+    int before = 0;
 #pragma unroll
-        for (int i = 0; i < kMaxSeqs / 32; ++i) before += 32 * i + lane < a.batch && pre[32 * i + lane] <= r.pos;
-        s.b = __reduce_add_sync(0xFFFFFFFFu, before);
-        const int start = s.b > 0 ? pre[s.b - 1] : 0;
-        s.hist = hist_s[s.b];
-        const Span p = span_of(s.hist, a);
-        s.ns = p.ns;
-        s.skip = p.skip;
-        s.nt = p.nt;
+    for (int i = 0; i < kMaxSeqs / 32; ++i) before += 32 * i + lane < a.batch && pre[32 * i + lane] <= r.pos;
+    s.b = __reduce_add_sync(0xFFFFFFFFu, before);
+    const int start = s.b > 0 ? pre[s.b - 1] : 0;
+    s.hist = hist_s[s.b];
+    const Span p = span_of(s.hist, a);
+    s.ns = p.ns;
+    s.skip = p.skip;
+    s.nt = p.nt;
+    if (r.len == 0) {
+        s.parts = (p.nt + r.target - 1) / r.target;
+        s.h = (r.pos - start) / s.parts;
+        s.r_first = start + s.h * s.parts;
+        const int i = r.pos - s.r_first;
+        s.first = 0;
+        s.lo = p.nt * i / s.parts;
+        s.hi = p.nt * (i + 1) / s.parts;
+        r.pos = r.end;
+    } else {
         s.h = (r.pos - start) / p.nt;
         s.first = start + s.h * p.nt;
         s.lo = r.pos - s.first;
         s.hi = min(p.nt, r.end - s.first);
+        s.r_first = s.first / r.len;
+        s.parts = (s.first + p.nt - 1) / r.len - s.r_first + 1;
         r.pos = s.first + s.hi;
-        const int32_t* parents = a.parents == nullptr ? nullptr : a.parents + static_cast<size_t>(a.b0 + s.b) * a.n;
-        const int count = tree_kin(parents, a.n, lane, kin);
-        const bool range = count > 0 && s.hist + count > a.max_len;
-        if (report && lane == 0 && (count < 0 || range)) atomicOr(a.err, count < 0 ? kDevErrTree : kDevErrHistRange);
-        if (count > 0 && !range) return true;
     }
-    return false;
+    return true;
+}
+
+// The kin of a segment's tokens (tree.cuh), a converged warp.  A sequence that is skipped has none: its keys are walked like any
+// other's, and nothing is written.
+__device__ __forceinline__ void kin_seg(const Seg& s, const Args& a, int lane, uint64_t (&kin)[2], bool report) {
+    const int32_t* parents = a.parents == nullptr ? nullptr : a.parents + static_cast<size_t>(a.b0 + s.b) * a.n;
+    const int count = tree_kin(parents, a.n, lane, kin);
+    const bool range = count > 0 && s.hist + count > a.max_len;
+    if (count < 0 || range) {
+        kin[0] = kin[1] = 0;
+        if (report && lane == 0) atomicOr(a.err, count < 0 ? kDevErrTree : kDevErrHistRange);
+    }
 }
 
 // Whether some row may not see some slot of the key tile from slot kb on (the same answer in every warp).
@@ -229,9 +253,11 @@ template <int D>
 struct Eight {
     uint4 xa, xb;
     float4 c[2], s[2];
-    __device__ __forceinline__ void load(const uint16_t* row, int jb, int pos, const Args& a) {
+    __device__ __forceinline__ void load(const uint16_t* row, int jb) {
         xa = __ldg(reinterpret_cast<const uint4*>(row + jb));
         xb = __ldg(reinterpret_cast<const uint4*>(row + jb + D / 2));
+    }
+    __device__ __forceinline__ void angles(int jb, int pos, const Args& a) {
         const float4* cp = reinterpret_cast<const float4*>(a.cos_tab + static_cast<size_t>(pos) * (D / 2) + jb);
         const float4* sp = reinterpret_cast<const float4*>(a.sin_tab + static_cast<size_t>(pos) * (D / 2) + jb);
         c[0] = __ldg(cp);
@@ -246,31 +272,42 @@ __device__ __forceinline__ uint64_t kin_of(const uint64_t (&kin)[2], int token) 
     return token < 32 ? k0 : k1;
 }
 
-// One warp's 32 rows (from row r0 of the sequence's (token, head) rows on) of q, rotated, into rows `at` .. of a Q tile.  Rows
-// past the last, and of no token, are left: their scores go nowhere.
-template <int D>
-__device__ __forceinline__ void stage_q(uint8_t* tile, int at, int r0, const Seg& s, const uint64_t (&kin)[2], int lane,
-                                        const Args& a) {
+// One warp's 32 rows (from row r0 of the sequence's (token, head) rows on) of q, rotated, into rows `at` .. of a Q tile, and
+// the kin of the segment's tokens.  Rows past the last, and of no token, are left: their scores go nowhere.  `empty` waits until the
+// tile may be written, after the first loads.
+template <int D, typename F>
+__device__ __forceinline__ void stage_q(uint8_t* tile, int at, int r0, const Seg& s, uint64_t (&kin)[2], int lane, const Args& a,
+                                        F&& empty) {
     constexpr int U = D / 16, BATCH = 4;  // units of a row
     const int rows = min(32, a.n * a.G - r0);
-    const int mine = min(r0 + lane, a.n * a.G - 1) / a.G;
-    const uint64_t k = kin_of(kin, mine);
-    const int depth = k == 0 ? -1 : __popcll(k) - 1;
-    for (int i0 = 0; i0 * (32 / U) < rows; i0 += BATCH) {
+    const int mine = min(max(r0 + lane, 0), a.n * a.G - 1) / a.G;
+    int depth = 0;
+    for (int i0 = 0; i0 == 0 || i0 * (32 / U) < rows; i0 += BATCH) {
         Eight<D> x[BATCH];
         int row[BATCH];
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
             const int u = (i0 + i) * 32 + lane;
             row[i] = u / U;
-            const int d = __shfl_sync(0xFFFFFFFFu, depth, row[i] & 31), token = __shfl_sync(0xFFFFFFFFu, mine, row[i] & 31);
-            if (row[i] >= rows || d < 0) {
+            const int token = __shfl_sync(0xFFFFFFFFu, mine, row[i] & 31);
+            if (row[i] >= rows)
                 row[i] = -1;
-            } else {
-                const int head = s.h * a.G + (r0 + row[i] - token * a.G);
-                x[i].load(a.q + ((static_cast<size_t>(a.b0 + s.b) * a.n + token) * a.Hq + head) * D, u % U * 8, s.hist + d, a);
-            }
+            else
+                x[i].load(a.q + ((static_cast<size_t>(a.b0 + s.b) * a.n + token) * a.Hq + s.h * a.G + (r0 + row[i] - token * a.G)) * D,
+                          u % U * 8);
         }
+        if (i0 == 0) {
+            kin_seg(s, a, lane, kin, false);
+            const uint64_t k = kin_of(kin, mine);
+            depth = k == 0 ? -1 : __popcll(k) - 1;
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int d = __shfl_sync(0xFFFFFFFFu, depth, max(row[i], 0) & 31);
+            if (d < 0) row[i] = -1;
+            if (row[i] >= 0) x[i].angles(((i0 + i) * 32 + lane) % U * 8, s.hist + d, a);
+        }
+        if (i0 == 0 && !empty()) return;
 #pragma unroll
         for (int i = 0; i < BATCH; ++i)
             if (row[i] >= 0) {
@@ -317,6 +354,7 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
     uint8_t* gbase = smem_raw + (base - raw);
     int* pre = reinterpret_cast<int*>(gbase + C::OFF_PRE);
     int* hist_s = reinterpret_cast<int*>(gbase + C::OFF_HIST);
+    int* cut = reinterpret_cast<int*>(gbase + C::OFF_CUT);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(gbase + C::OFF_ABORT);
     volatile int* odd_flag = reinterpret_cast<volatile int*>(gbase + C::OFF_FLAG);
     auto bar = [&](int i) -> uint32_t { return base + C::OFF_BAR + 8u * static_cast<uint32_t>(i); };
@@ -349,6 +387,10 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
         tma_prefetch_desc(&map_k);
         tma_prefetch_desc(&map_v);
     }
+    // parents on their way while the lengths are
+    if (a.parents != nullptr && warp >= kWarpGuard)
+        for (int i = (warp - kWarpGuard) * 32 + lane; i * 32 < a.batch * a.n; i += 64)
+            asm volatile("prefetch.global.L1 [%0];" ::"l"(a.parents + static_cast<size_t>(a.b0) * a.n + 32 * i));
     if (warp == kWarpMma) {
         tmem_alloc(base + C::OFF_TMEM, kTmemCols);
         tmem_relinquish();
@@ -358,13 +400,31 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
         int h[PER], t[PER];
 #pragma unroll
         for (int i = 0; i < PER; ++i) h[i] = PER * lane + i < a.batch ? __ldg(a.d_hist + a.b0 + PER * lane + i) : 0;
-        int sum = 0;
         bool bad = false;
+        int sum = 0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const bool here = PER * lane + i < a.batch, ok = h[i] >= 0 && h[i] <= a.max_len;
-            bad |= !ok;
-            sum += here && ok ? span_of(h[i], a).nt * a.Hkv : 0;
+            const bool here = PER * lane + i < a.batch, good = h[i] >= 0 && h[i] <= a.max_len;
+            bad |= !good;
+            t[i] = here && good ? span_of(h[i], a).nt : 0;
+            sum += t[i] * a.Hkv;
+            hist_s[PER * lane + i] = h[i];
+        }
+        const int total = __reduce_add_sync(0xFFFFFFFFu, sum);
+        // Pieces, if there are CTAs for all and they are hardly longer than the runs would be: a CTA then has but one segment.
+        const int len = max((total + a.runs - 1) / a.runs, 1);
+        int target = len;
+        for (; target <= len + kLonger; target += max(target >> 5, 1)) {
+            int pieces = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) pieces += (t[i] + target - 1) / target * a.Hkv;
+            if (__reduce_add_sync(0xFFFFFFFFu, pieces) <= a.runs) break;
+        }
+        const bool in_pieces = target <= len + kLonger;
+        sum = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            sum += (in_pieces ? (t[i] + target - 1) / target : t[i]) * a.Hkv;
             t[i] = sum;
         }
         int upto = sum;
@@ -374,9 +434,10 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
             if (lane >= d) upto += u;
         }
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            pre[PER * lane + i] = upto - sum + t[i];
-            hist_s[PER * lane + i] = h[i];
+        for (int i = 0; i < PER; ++i) pre[PER * lane + i] = upto - sum + t[i];
+        if (lane == 0) {
+            cut[0] = in_pieces ? 0 : len;
+            cut[1] = target;
         }
         if (bad && blockIdx.x == 0) atomicOr(a.err, kDevErrHistRange);
     }
@@ -386,10 +447,11 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
     const uint32_t tmem = *reinterpret_cast<const uint32_t*>(gbase + C::OFF_TMEM);
 
     Run run;
-    run.total = pre[kMaxSeqs - 1];
-    run.len = max((run.total + a.runs - 1) / a.runs, kMinRun);
-    run.pos = min(run_id * run.len, run.total);
-    run.end = min(run.pos + run.len, run.total);
+    run.id = run_id;
+    run.len = cut[0];
+    run.target = cut[1];
+    run.pos = min(run_id * max(run.len, 1), pre[kMaxSeqs - 1]);
+    run.end = min(run.pos + max(run.len, 1), pre[kMaxSeqs - 1]);
     const Run run0 = run;
     Seg s;
     uint64_t kin[2];
@@ -408,7 +470,7 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
         if (warp == kWarpTma) {
             // ------------------------------------------------------------ producer
             uint32_t seq = 0;
-            while (ok && next_seg(run, a, pre, hist_s, lane, s, kin, false)) {
+            while (ok && next_seg(run, a, pre, hist_s, lane, s)) {
                 if (lane == 0) {
                     const int n = s.hi - s.lo, head = (a.b0 + s.b) * a.Hkv + s.h;
                     for (int i = 0; i < 2 * n; ++i, ++seq) {
@@ -463,7 +525,7 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
             auto ready = [&](uint32_t at) {
                 return mbar_wait(bar(C::B_READY + at % C::NS), (at / C::NS) & 1u, abort_flag, a.wait_ns);
             };
-            while (ok && next_seg(run, a, pre, hist_s, lane, s, kin, false)) {
+            while (ok && next_seg(run, a, pre, hist_s, lane, s)) {
                 if (lane == 0) {
                     const int n = s.hi - s.lo;
                     const uint32_t qb = NT == 1 ? segs & 1u : 0u;
@@ -535,7 +597,8 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
             const int gw = warp - kWarpGuard, me = gw * 32 + lane;
             auto rows_below = [&](int row) { return row / 8 * 4 + min(max(row % 8 - 4 * gw, 0), 4); };  // of this guard's
             uint32_t seq = 0, segs = 0;
-            while (ok && next_seg(run, a, pre, hist_s, lane, s, kin, group == 0 && warp == kWarpGuard)) {
+            while (ok && next_seg(run, a, pre, hist_s, lane, s)) {
+                kin_seg(s, a, lane, kin, group == 0 && warp == kWarpGuard);
                 const int n = s.hi - s.lo;
                 const size_t head = (static_cast<size_t>(a.b0 + s.b) * a.Hkv + s.h) * a.max_len + s.hist;  // slot of token 0
                 for (int i = 0; i < 2 * n && ok; ++i, ++seq) {
@@ -568,7 +631,8 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                                     x[e].xa = __ldg(reinterpret_cast<const uint4*>(a.v_new + row + u % U * 8));
                                     x[e].xb = __ldg(reinterpret_cast<const uint4*>(a.v_new + row + u % U * 8 + D / 2));
                                 } else {
-                                    x[e].load(a.k_new + row, u % U * 8, s.hist + __popcll(k) - 1, a);
+                                    x[e].load(a.k_new + row, u % U * 8);
+                                    x[e].angles(u % U * 8, s.hist + __popcll(k) - 1, a);
                                 }
                             }
                             landed();
@@ -644,19 +708,20 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
             Seg nx;
             uint64_t nkin[2];
             Run ahead = run;
-            auto stage = [&](uint32_t seg) {  // q of segment nx
+            auto stage = [&](uint32_t seg) {  // q and kin of segment nx
                 const uint32_t qb = NT == 1 ? seg & 1u : 0u, use = NT == 1 ? seg >> 1 : seg;
-                if (use > 0)
-                    ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(C::B_QEMPTY + qb), (use - 1u) & 1u, abort_flag, a.wait_ns));
+                stage_q<D>(gbase + C::OFF_Q + (NT == 1 ? qb : static_cast<uint32_t>(t)) * C::TILE, (warp & 3) * 32, r0, nx, nkin, lane, a,
+                           [&]() {
+                               if (use > 0)
+                                   ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(C::B_QEMPTY + qb), (use - 1u) & 1u, abort_flag, a.wait_ns));
+                               return ok;
+                           });
                 if (!ok) return;
-                if (rows_on)
-                    stage_q<D>(gbase + C::OFF_Q + (NT == 1 ? qb : static_cast<uint32_t>(t)) * C::TILE, (warp & 3) * 32, r0, nx, nkin,
-                               lane, a);
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(C::B_QREADY + qb));
             };
-            bool more = next_seg(ahead, a, pre, hist_s, lane, nx, nkin, false);
+            bool more = next_seg(ahead, a, pre, hist_s, lane, nx);
             if (more) stage(0);
             while (more && ok) {
                 s = nx;
@@ -748,13 +813,13 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                 }
                 if (!ok) break;
                 // the next segment's q beside this one's last MMAs
-                more = next_seg(ahead, a, pre, hist_s, lane, nx, nkin, false);
+                more = next_seg(ahead, a, pre, hist_s, lane, nx);
                 if (more) stage(segs + 1);
                 if (!ok) break;
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(C::B_OFULL + ob), (NT == 1 ? segs >> 1 : segs) & 1u, abort_flag, a.wait_ns));
                 if (!ok) break;
                 const bool whole = s.whole();
-                const int slot = s.lo > 0 || s.first == run0.pos ? 0 : 1;  // of a part: the item began by this run's start, or in it
+                const int slot = run0.slot(s, run_id);
                 if (rows_on) {
                     tc_fence_after();
                     const bool odd = odd_flag[segs % kFlags] == static_cast<int>(segs) + 1;
@@ -814,10 +879,9 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
             }
             // ---- the merges: of the item that began by the run's start, and of the one that goes on past its end
             Run again = run0;
-            while (next_seg(again, a, pre, hist_s, lane, s, kin, false)) {
+            while (next_seg(again, a, pre, hist_s, lane, s)) {
                 if (s.whole()) continue;
-                const int slot = s.lo > 0 || s.first == run0.pos ? 0 : 1;
-                const int r_first = s.first / run0.len, r_last = (s.first + s.nt - 1) / run0.len, parts = r_last - r_first + 1;
+                const int slot = run0.slot(s, run_id), r_first = s.r_first, parts = s.parts;
                 int* counter = a.counters + (s.b * a.Hkv + s.h) * a.groups + group;
                 const int warps = 4 * live, all = parts * warps;
                 if (ok && did[slot] == 1) {
@@ -838,37 +902,69 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                     const int blk = share % blocks, part = share / blocks, of = (all - blk + blocks - 1) / blocks;
                     const int row = blk * 32 + lane, R = group * C::ROWS + row;
                     const int tok = min(R, a.n * a.G - 1) / a.G;
+                    kin_seg(s, a, lane, kin, false);
                     const uint64_t k = kin_of(kin, tok);  // (by all lanes)
                     const bool write = row < group_rows && k != 0;
                     auto slot_of = [&](int p) {  // of part p
                         const int r = r_first + p;
-                        return static_cast<size_t>(r * a.groups + group) * 2 + (s.first <= r * run0.len ? 0 : 1);
+                        return static_cast<size_t>(r * a.groups + group) * 2 + run0.slot(s, r);
                     };
                     if (write) {
+                        // a batch of parts is loaded at once: one after the other, each would wait for its loads
+                        constexpr int BATCH = 8;
+                        auto load_ml = [&](int p0, float2 (&ml)[BATCH]) {
+#pragma unroll
+                            for (int i = 0; i < BATCH; ++i)
+                                ml[i] = p0 + i < parts ? __ldcg(reinterpret_cast<const float2*>(a.part_ml + (slot_of(p0 + i) * C::ROWS + row) * 2))
+                                                       : make_float2(-INFINITY, 0.f);
+                        };
+                        float2 ml[BATCH];
                         float m = -INFINITY, l = 0.f;
-                        for (int p = 0; p < parts; ++p) {
-                            const float2 ml = __ldcg(reinterpret_cast<const float2*>(a.part_ml + (slot_of(p) * C::ROWS + row) * 2));
-                            if (ml.y != 0.f) m = fmaxf(m, ml.x);
-                        }
-                        for (int p = 0; p < parts; ++p) {
-                            const float2 ml = __ldcg(reinterpret_cast<const float2*>(a.part_ml + (slot_of(p) * C::ROWS + row) * 2));
-                            if (ml.y != 0.f) l += ml.y * fast_exp2(ml.x - m);
+                        for (int p0 = 0; p0 < parts; p0 += BATCH) {
+                            load_ml(p0, ml);
+                            float mn = m;
+#pragma unroll
+                            for (int i = 0; i < BATCH; ++i)
+                                if (ml[i].y != 0.f) mn = fmaxf(mn, ml[i].x);  // (0: a part without a slot that this row sees)
+                            l = l != 0.f ? l * fast_exp2(m - mn) : 0.f;
+#pragma unroll
+                            for (int i = 0; i < BATCH; ++i)
+                                if (ml[i].y != 0.f) l = fmaf(ml[i].y, fast_exp2(ml[i].x - mn), l);
+                            m = mn;
                         }
                         const float inv = 1.f / l;
                         uint16_t* orow = a.out + ((static_cast<size_t>(a.b0 + s.b) * a.n + tok) * a.Hq + s.h * a.G + (R - tok * a.G)) * D;
-                        for (int d = D / 4 * part / of; d < D / 4 * (part + 1) / of; ++d) {
-                            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-                            for (int p = 0; p < parts; ++p) {
-                                const float2 ml = __ldcg(reinterpret_cast<const float2*>(a.part_ml + (slot_of(p) * C::ROWS + row) * 2));
-                                if (ml.y == 0.f) continue;  // (a part without a slot that this row sees)
-                                const float w = fast_exp2(ml.x - m);
-                                const float4 o = __ldcg(reinterpret_cast<const float4*>(a.part_o + ((slot_of(p) * (D / 4) + d) * C::ROWS + row) * 4));
-                                // an infinity counts whatever its weight
-                                auto add = [&](float x, float y) { return w != 0.f ? fmaf(w, y, x) : isfinite(y) ? x : x + y; };
-                                acc = make_float4(add(acc.x, o.x), add(acc.y, o.y), add(acc.z, o.z), add(acc.w, o.w));
+                        const int d_end = D / 4 * (part + 1) / of;
+                        for (int d0 = D / 4 * part / of; d0 < d_end; d0 += 2) {
+                            float4 acc[2] = {};
+                            for (int p0 = 0; p0 < parts; p0 += BATCH) {
+                                float4 o[BATCH][2];
+                                if (parts > BATCH) load_ml(p0, ml);
+#pragma unroll
+                                for (int i = 0; i < BATCH; ++i)
+#pragma unroll
+                                    for (int e = 0; e < 2; ++e)
+                                        if (p0 + i < parts && d0 + e < d_end)
+                                            o[i][e] = __ldcg(reinterpret_cast<const float4*>(
+                                                a.part_o + ((slot_of(p0 + i) * (D / 4) + d0 + e) * C::ROWS + row) * 4));
+#pragma unroll
+                                for (int i = 0; i < BATCH; ++i) {
+                                    if (ml[i].y == 0.f) continue;
+                                    const float w = fast_exp2(ml[i].x - m);
+                                    // an infinity counts whatever its weight
+                                    auto add = [&](float x, float y) { return w != 0.f ? fmaf(w, y, x) : isfinite(y) ? x : x + y; };
+#pragma unroll
+                                    for (int e = 0; e < 2; ++e)
+                                        if (d0 + e < d_end)
+                                            acc[e] = make_float4(add(acc[e].x, o[i][e].x), add(acc[e].y, o[i][e].y),
+                                                                 add(acc[e].z, o[i][e].z), add(acc[e].w, o[i][e].w));
+                                }
                             }
-                            *reinterpret_cast<uint2*>(orow + 4 * d) =
-                                make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+#pragma unroll
+                            for (int e = 0; e < 2; ++e)
+                                if (d0 + e < d_end)
+                                    *reinterpret_cast<uint2*>(orow + 4 * (d0 + e)) =
+                                        make_uint2(pack_bf16x2(acc[e].x * inv, acc[e].y * inv), pack_bf16x2(acc[e].z * inv, acc[e].w * inv));
                         }
                     }
                     __syncwarp();
