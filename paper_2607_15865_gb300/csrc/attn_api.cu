@@ -140,7 +140,7 @@ int encode_map(const attn_ctx* c, CUtensorMap* map, const void* gaddr, cuuint32_
 // The tensor maps of flash_fwd for `chunk` queries at positions hist.. over slots [0, hist + chunk) of caches
 // with `rows` slots per (sequence, kv head); ATTN_EINVAL where the chunk's work items would not fit their counters.
 int flash_maps(const attn_ctx* c, const uint16_t* q, int hist, int chunk, int seq_stride, const uint16_t* kc,
-               const uint16_t* vc, int rows, attn::FlashMaps* maps) {
+               const uint16_t* vc, int rows, attn::FlashMaps* maps, const attn::FlashWindow& win = {}) {
     const attn::Shape& s = c->shape;
     // flash_fwd's work items (pairs of 128-row query tiles x query heads x sequences) are
     // counted in int: keep them well inside it
@@ -151,7 +151,7 @@ int flash_maps(const attn_ctx* c, const uint16_t* q, int hist, int chunk, int se
                                     static_cast<cuuint64_t>(s.batch)};
         const cuuint64_t strides[3] = {D * 2, D * 2 * s.n_q_heads,
                                        D * 2 * s.n_q_heads * static_cast<cuuint64_t>(seq_stride)};
-        const cuuint32_t heads = static_cast<cuuint32_t>(attn::flash_pack_heads(s, hist, chunk, c->num_sms));
+        const cuuint32_t heads = static_cast<cuuint32_t>(attn::flash_pack_heads(s, hist, chunk, win, c->num_sms));
         const cuuint32_t box[4] = {64, heads, 128 / heads, 1};
         const int rc = encode_map(c, &maps->q, q, 4, dims, strides, box);
         if (rc != ATTN_OK) return rc;
@@ -165,10 +165,10 @@ int flash_maps(const attn_ctx* c, const uint16_t* q, int hist, int chunk, int se
 }
 
 int run_flash(attn_ctx* c, const attn::FlashMaps& maps, int hist, int chunk, int seq_stride, uint16_t* out,
-              cudaStream_t st) {
+              cudaStream_t st, const attn::FlashWindow& win = {}) {
     const cudaError_t e = timed(c, ATTN_KERNEL_FLASH_FWD, st, [&](int* n) {
-        return attn::launch_flash_fwd(c->shape, maps, hist, chunk, seq_stride, c->d_cos_t, c->d_sin_t, out, c->d_flash_o,
-                                      c->d_flash_ml, c->d_err, c->num_sms, st, n, c->wait_ns);
+        return attn::launch_flash_fwd(c->shape, maps, hist, chunk, seq_stride, win, c->d_cos_t, c->d_sin_t, out,
+                                      c->d_flash_o, c->d_flash_ml, c->d_err, c->num_sms, st, n, c->wait_ns);
     });
     return e == cudaSuccess ? ATTN_OK : cuda_fail(e, "flash_fwd launch");
 }
@@ -177,7 +177,8 @@ int run_flash(attn_ctx* c, const attn::FlashMaps& maps, int hist, int chunk, int
 // hold `chunk` tokens of each sequence, sequence b starting at token b * seq_stride
 // (seq_stride = chunk for a dense chunk; the prompt length for a segment of a prompt).
 int run_prefill(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uint16_t* v, int hist, int chunk,
-                int seq_stride, uint16_t* kc, uint16_t* vc, uint16_t* out, cudaStream_t st) {
+                int seq_stride, uint16_t* kc, uint16_t* vc, uint16_t* out, cudaStream_t st,
+                const attn::FlashWindow& win = {}) {
     if (c == nullptr || q == nullptr || k == nullptr || v == nullptr || kc == nullptr || vc == nullptr ||
         out == nullptr)
         return ATTN_EINVAL;
@@ -187,7 +188,7 @@ int run_prefill(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uint16_
         return ATTN_EINVAL;
     const attn::Shape& s = c->shape;
     attn::FlashMaps maps;
-    const int rc = flash_maps(c, q, hist, chunk, seq_stride, kc, vc, s.max_len, &maps);
+    const int rc = flash_maps(c, q, hist, chunk, seq_stride, kc, vc, s.max_len, &maps, win);
     if (rc != ATTN_OK) return rc;
     const cudaError_t e = timed(c, ATTN_KERNEL_ROPE_APPEND, st, [&](int*) {
         return attn::launch_rope_append(s, k, v, hist, nullptr, chunk, seq_stride, c->d_cos, c->d_sin, c->d_cos_t,
@@ -195,7 +196,7 @@ int run_prefill(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uint16_
                                         st);
     });
     if (e != cudaSuccess) return cuda_fail(e, "rope_append launch");
-    return run_flash(c, maps, hist, chunk, seq_stride, out, st);
+    return run_flash(c, maps, hist, chunk, seq_stride, out, st, win);
 }
 
 }  // namespace
@@ -840,7 +841,7 @@ int run_tree(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uint16_t* 
     if (n_new < 1 || n_new > ATTN_TREE_TOKENS || n_new > c->cfg.max_len || sinks < 0 || !on_device(c)) return ATTN_EINVAL;
     const int rc = decode_maps(c, k_cache, v_cache);
     if (rc != ATTN_OK) return rc;
-    const attn::TreeCall t{q, k, v, d_hist_len, d_parents, 0, n_new, std::min(window, c->cfg.max_len),
+    const attn::TreeCall t{q, k, v, d_hist_len, d_parents, n_new, std::min(window, c->cfg.max_len),
                            std::min(sinks, c->cfg.max_len), k_cache, v_cache, c->d_cos, c->d_sin, out, c->d_err,
                            &c->dec_maps, c->d_flash_o, c->d_flash_ml, c->d_counters, c->num_sms, c->wait_ns};
     const cudaError_t e = attn::launch_tree_decode(c->shape, t, reinterpret_cast<cudaStream_t>(stream));
@@ -851,24 +852,10 @@ int run_tree(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uint16_t* 
 
 int attn_window_prefill_kv(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uint16_t* v, int hist_len, int chunk_len,
                            int window, int sinks, uint16_t* k_cache, uint16_t* v_cache, uint16_t* out, attn_stream_t stream) {
-    if (c == nullptr || q == nullptr || k == nullptr || v == nullptr || k_cache == nullptr || v_cache == nullptr ||
-        out == nullptr)
-        return ATTN_EINVAL;
-    if (chunk_len < 1 || hist_len < 0 || static_cast<long>(hist_len) + chunk_len > c->cfg.max_len) return ATTN_EINVAL;
-    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out))
-        return ATTN_EINVAL;
-    if (window < 1 || sinks < 0 || !on_device(c)) return ATTN_EINVAL;
-    const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    cudaError_t e = timed(c, ATTN_KERNEL_ROPE_APPEND, st, [&](int*) {
-        return attn::launch_rope_append(c->shape, k, v, hist_len, nullptr, chunk_len, chunk_len, c->d_cos, c->d_sin, c->d_cos_t,
-                                        c->d_sin_t, k_cache, v_cache, c->d_err, st);
-    });
-    if (e != cudaSuccess) return cuda_fail(e, "rope_append launch");
-    const attn::TreeCall t{q, k, v, nullptr, nullptr, hist_len, chunk_len, std::min(window, c->cfg.max_len),
-                           std::min(sinks, c->cfg.max_len), k_cache, v_cache, c->d_cos, c->d_sin, out, c->d_err,
-                           nullptr, nullptr, nullptr, nullptr, 0, 0};
-    e = attn::launch_tree_decode(c->shape, t, st);
-    return e == cudaSuccess ? ATTN_OK : cuda_fail(e, "window prefill launch");
+    if (c == nullptr || window < 1 || sinks < 0 || !on_device(c)) return ATTN_EINVAL;
+    const attn::FlashWindow win{true, std::min(window, c->cfg.max_len), std::min(sinks, c->cfg.max_len), v_cache};
+    return run_prefill(c, q, k, v, hist_len, chunk_len, chunk_len, k_cache, v_cache, out, reinterpret_cast<cudaStream_t>(stream),
+                       win);
 }
 
 int attn_window_decode(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uint16_t* v, const int32_t* d_hist_len,

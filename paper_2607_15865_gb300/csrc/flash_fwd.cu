@@ -78,8 +78,9 @@ enum Bar {
     B_GFULL0, B_GEMPTY0 = B_GFULL0 + GS,
     B_SFULL0 = B_GEMPTY0 + GS, B_SFULL1, B_PFULL0, B_PFULL1,
     B_OFULL0, B_OFULL1, B_OEMPTY0, B_OEMPTY1,
-    B_DRAIN, NBAR
+    B_DRAIN, B_GREADY0, NBAR = B_GREADY0 + GS
 };
+constexpr int kFlags = 4;  // units that the guards may be ahead of the epilogue (two at most), and its own
 
 template <int D>
 struct Layout {
@@ -95,7 +96,8 @@ struct Layout {
     static constexpr int OFF_BAR = OFF_STAGE + 8 * STAGE_WARP;
     static constexpr int OFF_TMEM = OFF_BAR + NBAR * 8;
     static constexpr int OFF_ABORT = OFF_TMEM + 8;
-    static constexpr int BYTES = OFF_ABORT + 8;
+    static constexpr int OFF_FLAG = OFF_ABORT + 8;  // int [kFlags]: the unit, from 1, in whose masked tiles V was not all finite
+    static constexpr int BYTES = OFF_FLAG + 4 * kFlags;
     static constexpr int ALLOC = BYTES + 1024;  // slack to align the base to 1024 bytes
     static constexpr uint32_t TM_O = 2 * BN;    // TMEM column of O_A; O_B at TM_O + D
 };
@@ -123,6 +125,7 @@ struct Item {
     int rowsa, rowsb;  // valid rows of each tile (0: tile absent)
     int nkva, nkvb;    // KV tiles each tile attends to
     int n_kv;          // KV tiles loaded for the item
+    WindowWalk w;      // WIN: which they are; tile B sits out tiles [w.off0, w.off1)
     __device__ __forceinline__ int q0(int t) const { return t ? q0b : q0a; }
     __device__ __forceinline__ int rows(int t) const { return t ? rowsb : rowsa; }
     __device__ __forceinline__ int nkv(int t) const { return t ? nkvb : nkva; }
@@ -140,6 +143,7 @@ struct Sched {
     FastDiv fd_grid, fd_hqb, fd_hq, fd_g, fd_ns, fd_pb, fd_per, fd_nb;
     int n_heads, heads, tok;
     FastDiv fd_heads;
+    int window, sinks;  // WIN: position p sees slots s <= p with p - s < window or s < sinks
 };
 
 // Item order.  By default the longest query-tile pairs come first across every (head,
@@ -150,7 +154,7 @@ struct Sched {
 // a pair together -- so the CTAs of a round walk the K/V of only those kv heads, which
 // stays in L2, and each kv head's cache is read from DRAM about once instead of once per
 // round.
-template <bool PK>
+template <bool PK, bool WIN>
 __device__ __forceinline__ Item decode_item(int lin, const Sched& sc) {
     Item it;
     int qt;
@@ -178,6 +182,11 @@ __device__ __forceinline__ Item decode_item(int lin, const Sched& sc) {
     it.rowsb = max(0, min(tok, sc.S - it.q0b));
     it.nkva = it.rowsa ? (sc.H + it.q0a + it.rowsa + BN - 1) / BN : 0;
     it.nkvb = it.rowsb ? (sc.H + it.q0b + it.rowsb + BN - 1) / BN : 0;
+    if constexpr (WIN) {
+        it.w = window_walk(sc.H + it.q0a, sc.H + it.q0b, sc.window, sc.sinks, BN);
+        it.nkva -= it.w.skip;
+        if (it.rowsb) it.nkvb -= it.w.skip;
+    }
     if constexpr (PK) {
         it.rowsa *= sc.heads;
         it.rowsb *= sc.heads;
@@ -210,10 +219,82 @@ struct Unit {
     Item it;
     int kv_lo, kv_hi;  // KV tiles [kv_lo, kv_hi) of the item
     int piece;         // index of the piece in the partial workspace, -1 for a whole item
-    __device__ __forceinline__ int cnt(int t) const { return max(0, min(kv_hi, it.nkv(t)) - kv_lo); }
+    // Whether query tile t walks KV tile j of the unit; the first that it does (if any: `has`); the end of those.
+    template <bool WIN>
+    __device__ __forceinline__ bool on(int t, int j) const {
+        return j < it.nkv(t) && !(WIN && t && j >= it.w.off0 && j < it.w.off1);
+    }
+    template <bool WIN>
+    __device__ __forceinline__ int first(int t) const {
+        return WIN && t && kv_lo >= it.w.off0 && kv_lo < it.w.off1 ? it.w.off1 : kv_lo;
+    }
+    __device__ __forceinline__ int end(int t) const { return min(kv_hi, it.nkv(t)); }
+    template <bool WIN>
+    __device__ __forceinline__ bool has(int t) const {
+        return first<WIN>(t) < end(t);
+    }
+    // The first slot of KV tile j.
+    template <bool WIN>
+    __device__ __forceinline__ int key(int j) const {
+        return (WIN && j >= it.w.ns ? j + it.w.skip : j) * BN;
+    }
+    // WIN: whether some row of query tile t may not see some slot of the tile from slot kb on, and whether that holds for a query
+    // tile that walks KV tile j (only there is V guarded).
+    __device__ __forceinline__ bool masked(int t, int kb, const Sched& sc) const {
+        const int pos = sc.H + it.q0(t);
+        return kb + BN - 1 > pos || (kb <= pos + sc.tok - 1 - sc.window && kb + BN > sc.sinks);
+    }
+    __device__ __forceinline__ bool guarded(int j, const Sched& sc) const {
+        const int kb = key<true>(j);
+        return (on<true>(0, j) && masked(0, kb, sc)) || (on<true>(1, j) && masked(1, kb, sc));
+    }
 };
 
-template <bool PK>
+// Which of the slots k0 .. k0 + 31 the row of position pos sees, a bit each.
+__device__ __forceinline__ uint32_t window_word(int k0, int pos, int window, int sinks) {
+    auto below = [&](int x) {  // bits of the slots < x
+        const int c = min(max(x - k0, 0), 32);
+        return static_cast<uint32_t>((1ull << c) - 1);
+    };
+    return below(pos + 1) & (~below(pos - window + 1) | below(sinks));
+}
+
+// Add to query tile t's O (in TMEM, this thread's row) the values of V that are not finite, which the guards took out of the
+// guarded tiles of the unit, and that the row sees.  By a whole warp.
+template <int D>
+__device__ __noinline__ void add_not_finite(uint32_t o_col, int t, int pos, Unit un, const Sched& sc,
+                                            const uint16_t* v_head) {
+    for (int c0 = 0; c0 < D; c0 += 32) {
+        uint32_t o[32];
+        tmem_ld32(o_col + c0, o);
+        tmem_wait_ld();
+        for (int j = un.first<true>(t); j < un.end(t); ++j) {
+            if (!un.on<true>(t, j) || !un.guarded(j, sc)) continue;
+            const int kb = un.key<true>(j);
+            for (int c = 0; c < BN / 32; ++c)
+                for (uint32_t w = window_word(kb + 32 * c, pos, sc.window, sc.sinks); w != 0; w &= w - 1) {
+                    const uint4* row = reinterpret_cast<const uint4*>(
+                        v_head + static_cast<size_t>(kb + 32 * c + __ffs(w) - 1) * D + c0);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const uint4 x = __ldcg(row + u);
+                        const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            if (!isfinite(bf_lo(v[e]))) o[8 * u + 2 * e] = __float_as_uint(__uint_as_float(o[8 * u + 2 * e]) + bf_lo(v[e]));
+                            if (!isfinite(bf_hi(v[e])))
+                                o[8 * u + 2 * e + 1] = __float_as_uint(__uint_as_float(o[8 * u + 2 * e + 1]) + bf_hi(v[e]));
+                        }
+                    }
+                }
+        }
+        __syncwarp();
+        tmem_st32(o_col + c0, o);
+        tmem_wait_st();
+    }
+}
+
+template <bool PK, bool WIN>
 __device__ __forceinline__ Unit decode_unit(int lin, const Sched& sc) {
     Unit u;
     u.piece = -1;
@@ -222,11 +303,11 @@ __device__ __forceinline__ Unit decode_unit(int lin, const Sched& sc) {
         const int tail = fdiv(v, sc.fd_ns);
         const int s = v - tail * sc.nsplit;
         u.piece = v;
-        u.it = decode_item<PK>(sc.head + tail, sc);
+        u.it = decode_item<PK, WIN>(sc.head + tail, sc);
         u.kv_lo = fdiv(u.it.n_kv * s, sc.fd_ns);
         u.kv_hi = fdiv(u.it.n_kv * (s + 1), sc.fd_ns);
     } else {
-        u.it = decode_item<PK>(lin, sc);
+        u.it = decode_item<PK, WIN>(lin, sc);
         u.kv_lo = 0;
         u.kv_hi = u.it.n_kv;
     }
@@ -341,11 +422,18 @@ __device__ __forceinline__ bool rope_item(uint32_t qfull, uint32_t qready, uint3
 // reads 17 MB of partials, 24.3 with this; 512 over 8000 63.7 -> 61.9.  With more pieces the
 // larger cluster and its longer exchange cost more than the merge kernel: four of 256 rows over
 // 1500 24.3 us against 22.2, of one row over 2000 15.6 against 14.0.)
-template <int D, bool CL, bool PK>
+//
+// WIN: under a window with first tokens that stay visible.  An item walks the KV tiles of the sinks and those from the
+// window of tile A's first row on; a tile is masked by words of 32 slots where some row does not see it whole.  In such a
+// tile V may hold values that are not finite where rows that do not see them would add 0 times those, so warps 10
+// and 11, the guards, look through its V before the MMAs (0 x V summed), put 0 in place of such values, and the rows
+// that see them add them to O at the end, from global memory.  Each slot of the ring is free again when the guards are
+// through with it too.
+template <int D, bool CL, bool PK, bool WIN>
 __global__ void __launch_bounds__(kThreads, 1)
     flash_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                      const __grid_constant__ CUtensorMap map_v, const Sched sc, int s_stride, int Hkv,
-                     float scale_log2, const float* __restrict__ cos_t,
+                     float scale_log2, const uint16_t* __restrict__ v_cache, const float* __restrict__ cos_t,
                      const float* __restrict__ sin_t, int tab_stride, uint16_t* __restrict__ out, float* __restrict__ ws_o,
                      float* __restrict__ ws_ml, int* __restrict__ err, uint64_t wait_ns) {
     using L = Layout<D>;
@@ -355,6 +443,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint8_t* gbase = smem_raw + (base - raw);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(gbase + L::OFF_ABORT);
     const uint32_t* tmem_holder = reinterpret_cast<const uint32_t*>(gbase + L::OFF_TMEM);
+    volatile int* odd_flag = reinterpret_cast<volatile int*>(gbase + L::OFF_FLAG);
     auto bar = [&](int i) -> uint32_t { return base + L::OFF_BAR + 8u * static_cast<uint32_t>(i); };
 
     const int warp = threadIdx.x >> 5;
@@ -371,7 +460,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_init(bar(B_QEMPTY), 1);
         for (int st = 0; st < GS; ++st) {
             mbar_init(bar(B_GFULL0 + st), 1);
-            mbar_init(bar(B_GEMPTY0 + st), 1);
+            mbar_init(bar(B_GEMPTY0 + st), WIN ? 3 : 1);  // the issuer; the guards
+            if constexpr (WIN) mbar_init(bar(B_GREADY0 + st), 2);
         }
         for (int t = 0; t < 2; ++t) {
             mbar_init(bar(B_SFULL0 + t), 1);
@@ -380,12 +470,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(bar(B_OEMPTY0 + t), BM / 32);
         }
         mbar_init(bar(B_DRAIN), 1);
+        if constexpr (WIN)
+            for (int i = 0; i < kFlags; ++i) odd_flag[i] = 0;
         fence_mbar_init();
         tma_prefetch_desc(&map_q);
         tma_prefetch_desc(&map_k);
         tma_prefetch_desc(&map_v);
         if (static_cast<int>(blockIdx.x) < n_units) {
-            const Item it = decode_unit<PK>(unit_of(blockIdx.x, sc), sc).it;
+            const Item it = decode_unit<PK, WIN>(unit_of(blockIdx.x, sc), sc).it;
             mbar_arrive_expect_tx(bar(B_QFULL), PK ? 2 * L::DCH * 128 * sc.tok * sc.heads : 2 * L::Q_TILE);
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -416,7 +508,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             bool ok = true;
             bool kv_visible = false;  // K1's cache writes complete (dependent launch)
             for (int lin = blockIdx.x; lin < n_units && ok; lin += gridDim.x) {
-                const Unit un = decode_unit<PK>(unit_of(lin, sc), sc);
+                const Unit un = decode_unit<PK, WIN>(unit_of(lin, sc), sc);
                 const Item& it = un.it;
                 if (items > 0) {  // (the first unit's q tiles were issued in the prologue)
                     if (!mbar_wait(bar(B_QEMPTY), static_cast<uint32_t>(items - 1) & 1u, abort_flag, wait_ns)) {
@@ -436,7 +528,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     // the next unit's q tiles into L2, so that their copy after this unit is short
                     const int nxt = lin + static_cast<int>(gridDim.x);
                     if (nxt < n_units) {
-                        const Item nt = decode_unit<PK>(unit_of(nxt, sc), sc).it;
+                        const Item nt = decode_unit<PK, WIN>(unit_of(nxt, sc), sc).it;
 #pragma unroll
                         for (int t = 0; t < 2; ++t)
                             if (nt.rows(t) > 0)
@@ -464,12 +556,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (has_k) {
 #pragma unroll
                         for (int c = 0; c < L::DCH; ++c)
-                            tma_load_3d(slot + c * L::CHUNK, &map_k, c * 64, j * BN, kv_row, bar(B_GFULL0 + st));
+                            tma_load_3d(slot + c * L::CHUNK, &map_k, c * 64, un.key<WIN>(j), kv_row, bar(B_GFULL0 + st));
                     }
                     if (has_v) {
 #pragma unroll
                         for (int c = 0; c < L::DCH; ++c)
-                            tma_load_3d(slot + L::KV_TILE + c * L::CHUNK, &map_v, c * 64, (j - 1) * BN, kv_row,
+                            tma_load_3d(slot + L::KV_TILE + c * L::CHUNK, &map_v, c * 64, un.key<WIN>(j - 1), kv_row,
                                         bar(B_GFULL0 + st));
                     }
                 }
@@ -527,12 +619,20 @@ __global__ void __launch_bounds__(kThreads, 1)
                 return true;
             };
             uint32_t gslot = 0;  // gc % GS
+            uint32_t ready_par = 0;  // WIN: a bit per slot, the parity of its next B_GREADY
+            // WIN: the guards are through with the group's V, which is KV tile j
+            auto wait_v = [&](const Unit& un, int j) -> bool {
+                if (!WIN || !un.guarded(j, sc)) return true;
+                if (!mbar_wait(bar(B_GREADY0 + gslot), ready_par >> gslot & 1u, abort_flag, wait_ns)) return false;
+                ready_par ^= 1u << gslot;
+                return true;
+            };
             auto next_group = [&]() {
                 ++gc;
                 gslot = gslot + 1 == GS ? 0 : gslot + 1;
             };
             for (int lin = blockIdx.x; lin < n_units && ok; lin += gridDim.x) {
-                const Unit un = decode_unit<PK>(unit_of(lin, sc), sc);
+                const Unit un = decode_unit<PK, WIN>(unit_of(lin, sc), sc);
                 const Item& it = un.it;
                 if (!mbar_wait(bar(B_QREADY), static_cast<uint32_t>(items) & 1u, abort_flag, wait_ns)) {
                     ok = false;
@@ -541,14 +641,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tc_fence_after();
                 for (int j = un.kv_lo; j < un.kv_hi && ok; ++j) {
                     // group j: K(j), and V(j-1) for the PV MMAs of the previous tile
-                    if (!mbar_wait(bar(B_GFULL0 + gslot), (gc / GS) & 1u, abort_flag, wait_ns)) {
+                    if (!mbar_wait(bar(B_GFULL0 + gslot), (gc / GS) & 1u, abort_flag, wait_ns) ||
+                        (j > un.kv_lo && !wait_v(un, j - 1))) {
                         ok = false;
                         break;
                     }
                     tc_fence_after();
-                    const bool pv_a = j > un.kv_lo && j - 1 < it.nkv(0), pv_b = j > un.kv_lo && j - 1 < it.nkv(1);
-                    const bool s_a = j < it.nkv(0), s_b = j < it.nkv(1);
-                    const bool first = j - 1 == un.kv_lo;
+                    const bool pv_a = j > un.kv_lo && un.on<WIN>(0, j - 1), pv_b = j > un.kv_lo && un.on<WIN>(1, j - 1);
+                    const bool s_a = un.on<WIN>(0, j), s_b = un.on<WIN>(1, j);
+                    const bool first = j - 1 == un.kv_lo, first_b = j - 1 == un.first<WIN>(1);
                     if (pv_a) {
                         if (!wait_p(0, first)) {
                             ok = false;
@@ -559,12 +660,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     if (s_a) issue_s(0, gslot);
                     if (pv_b) {
-                        if (!wait_p(1, first)) {
+                        if (!wait_p(1, first_b)) {
                             ok = false;
                             break;
                         }
                         tc_fence_after();
-                        issue_pv(1, first, gslot);
+                        issue_pv(1, first_b, gslot);
                     }
                     if (s_b) issue_s(1, gslot);
                     umma_commit(bar(B_GEMPTY0 + gslot));
@@ -573,24 +674,25 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (!ok) break;
                 umma_commit(bar(B_QEMPTY));  // every S MMA of the unit is issued
                 // the last group: V of the final tile
-                if (!mbar_wait(bar(B_GFULL0 + gslot), (gc / GS) & 1u, abort_flag, wait_ns)) ok = false;
+                if (!mbar_wait(bar(B_GFULL0 + gslot), (gc / GS) & 1u, abort_flag, wait_ns) || !wait_v(un, un.kv_hi - 1)) ok = false;
                 tc_fence_after();
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
-                    if (ok && un.kv_hi - 1 < it.nkv(t)) {
-                        if (!wait_p(t, un.kv_hi - 1 == un.kv_lo)) {
+                    if (ok && un.on<WIN>(t, un.kv_hi - 1)) {
+                        const bool first = un.kv_hi - 1 == un.first<WIN>(t);
+                        if (!wait_p(t, first)) {
                             ok = false;
                             break;
                         }
                         tc_fence_after();
-                        issue_pv(t, un.kv_hi - 1 == un.kv_lo, gslot);
+                        issue_pv(t, first, gslot);
                     }
                 if (!ok) break;
                 umma_commit(bar(B_GEMPTY0 + gslot));
                 next_group();
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
-                    if (un.cnt(t) > 0) {
+                    if (un.has<WIN>(t)) {
                         umma_commit(bar(B_OFULL0 + t));
                         ++o_cnt[t];
                     }
@@ -603,6 +705,56 @@ __global__ void __launch_bounds__(kThreads, 1)
             // All tensor-core work issued here must finish before TMEM is released.
             umma_commit(bar(B_DRAIN));
             mbar_wait(bar(B_DRAIN), 0, nullptr);
+        } else if (WIN && warp > kWarpMma) {
+            // ---------------------------------------------------- guards
+            const int me = (warp - kWarpMma - 1) * 32 + lane;
+            uint32_t gc = 0;
+            int units = 0;
+            bool ok = true;
+            for (int lin = blockIdx.x; lin < n_units && ok; lin += gridDim.x) {
+                const Unit un = decode_unit<PK, WIN>(unit_of(lin, sc), sc);
+                ++units;
+                for (int j = un.kv_lo; j <= un.kv_hi; ++j, ++gc) {
+                    const int st = static_cast<int>(gc % GS);
+                    ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(B_GFULL0 + st), (gc / GS) & 1u, abort_flag, wait_ns));
+                    if (!ok) break;
+                    if (j > un.kv_lo && un.guarded(j - 1, sc)) {
+                        // the products with 0 add up to 0, or to NaN
+                        uint4* v = reinterpret_cast<uint4*>(gbase + L::OFF_G + st * L::G_SLOT + L::KV_TILE);
+                        uint32_t sum[4] = {0u, 0u, 0u, 0u};
+#pragma unroll 8
+                        for (int u = me; u < L::KV_TILE / 16; u += 64) {
+                            const uint4 x = v[u];
+                            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(sum[e]) : "r"(w[e]), "r"(0u));
+                        }
+                        if (__any_sync(0xFFFFFFFFu, ((sum[0] | sum[1] | sum[2] | sum[3]) & 0x7FFF7FFFu) != 0)) {
+                            for (int u = me; u < L::KV_TILE / 16; u += 64) {
+                                uint4 x = v[u];
+                                uint32_t* w = reinterpret_cast<uint32_t*>(&x);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    if ((w[e] & 0x7F80u) == 0x7F80u) w[e] &= 0xFFFF0000u;
+                                    if ((w[e] & 0x7F800000u) == 0x7F800000u) w[e] &= 0x0000FFFFu;
+                                }
+                                v[u] = x;
+                            }
+                            odd_flag[units % kFlags] = units;
+                            fence_proxy_async_smem();
+                        }
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bar(B_GREADY0 + st));
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(B_GEMPTY0 + st));
+                }
+            }
+            if (!ok && lane == 0) {
+                *abort_flag = 1;
+                atomicOr(err, kDevErrTimeout);
+            }
+            __syncwarp();
         }
         if constexpr (CL) {  // the two cluster barriers of the merge, reached by every thread
             __syncwarp();
@@ -628,7 +780,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         int lin = blockIdx.x;
         Unit un;
         if (lin < n_units) {
-            un = decode_unit<PK>(unit_of(lin, sc), sc);
+            un = decode_unit<PK, WIN>(unit_of(lin, sc), sc);
             ok = rope_item<D, PK>(bar(B_QFULL), bar(B_QREADY), static_cast<uint32_t>(items) & 1u, abort_flag, qtile,
                                   row, row_tok, un.it.rows(t), H + un.it.q0(t), q_rows, cos_t, sin_t, tab_stride, wait_ns);
             ++items;
@@ -638,9 +790,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             float m_run = -INFINITY;  // reference max of P (log2 domain)
             float l_run = 0.f;
             const int pos_row = H + it.q0(t) + row_tok;  // last key this row may see
-            const int min_pos = H + it.q0(t);        // smallest row position of the tile
-            const int n_tiles = un.cnt(t);
-            for (int j = un.kv_lo; j < un.kv_lo + n_tiles; ++j) {
+            [[maybe_unused]] const int min_pos = H + it.q0(t);  // smallest row position of the tile
+            const int j_first = un.first<WIN>(t), j_end = un.end(t);
+            for (int j = j_first; j < j_end; ++j) {
+                if (WIN && !un.on<WIN>(t, j)) continue;
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(B_SFULL0 + t), s_cnt & 1u, abort_flag, wait_ns));
                 if (!ok) break;
                 ++s_cnt;
@@ -649,8 +802,18 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int c = 0; c < BN / 32; ++c) tmem_ld32(s_col + 32 * c, r[c]);
                 tmem_wait_ld();
-                const int kb = j * BN;
-                if (kb + BN - 1 > min_pos) {  // the tile crosses the diagonal: mask by index
+                const int kb = un.key<WIN>(j);
+                if constexpr (WIN) {
+                    if (un.masked(t, kb, sc)) {
+#pragma unroll
+                        for (int c = 0; c < BN / 32; ++c) {
+                            const uint32_t w = window_word(kb + 32 * c, pos_row, sc.window, sc.sinks);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (!(w >> e & 1u)) r[c][e] = __float_as_uint(-INFINITY);
+                        }
+                    }
+                } else if (kb + BN - 1 > min_pos) {  // the tile crosses the diagonal: mask by index
 #pragma unroll
                     for (int c = 0; c < BN / 32; ++c)
 #pragma unroll
@@ -699,7 +862,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const float2 sum2a = make_float2(sum2[0].x + sum2[1].x, sum2[0].y + sum2[1].y);
                 const float2 sum2b = make_float2(sum2[2].x + sum2[3].x, sum2[2].y + sum2[3].y);
                 const float2 sum2t = make_float2(sum2a.x + sum2b.x, sum2a.y + sum2b.y);
-                if (j > un.kv_lo && __any_sync(0xFFFFFFFFu, move)) {
+                if (j > j_first && __any_sync(0xFFFFFFFFu, move)) {
                     // O_T holds the sum through tile j-1 (PV_T(j-1) completed before S_T(j)),
                     // and PV_T(j) waits for this thread's arrive below.  Done after P, when the
                     // scores no longer hold registers.
@@ -725,7 +888,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int next = lin + static_cast<int>(gridDim.x);
             Unit nun;
             if (next < n_units) {
-                nun = decode_unit<PK>(unit_of(next, sc), sc);
+                nun = decode_unit<PK, WIN>(unit_of(next, sc), sc);
                 ok = rope_item<D, PK>(bar(B_QFULL), bar(B_QREADY), static_cast<uint32_t>(items) & 1u, abort_flag, qtile,
                                       row, row_tok, nun.it.rows(t), H + nun.it.q0(t), q_rows, cos_t, sin_t, tab_stride, wait_ns);
                 ++items;
@@ -733,11 +896,17 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             // epilogue: O_T / l -> bf16 -> out, or for a piece the unnormalised O_T and (m, l)
             const size_t prow = (static_cast<size_t>(un.piece) * 2 * BM + t * BM + row);
-            if (n_tiles > 0) {
+            if (j_first < j_end) {
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(B_OFULL0 + t), o_cnt & 1u, abort_flag, wait_ns));
                 if (!ok) break;
                 ++o_cnt;
                 tc_fence_after();
+                if constexpr (WIN) {
+                    const int unit = fdiv(lin, sc.fd_grid) + 1;
+                    if (odd_flag[unit % kFlags] == unit)
+                        add_not_finite<D>(o_col, t, row < it.rows(t) ? pos_row : -1, un, sc,
+                                          v_cache + (static_cast<size_t>(it.b) * Hkv + it.g) * tab_stride * D);
+                }
                 if constexpr (CL) {
                     cl_m = m_run;
                     cl_l = l_run;
@@ -822,7 +991,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             constexpr int W = D / 2;  // columns that a CTA finishes
             const int rank = static_cast<int>(cluster_rank()), rg = t * BM + row;
             const bool rows_on = (row & ~31) < un.it.rows(t);  // (this warp has rows of the chunk)
-            const bool tile_on = ok && un.cnt(t) > 0;
+            const bool tile_on = ok && un.has<WIN>(t);
             // the peer's columns [W][256 rows] in the group ring, its (m, l) [256 rows] in the q tiles
             const float* peer_o = reinterpret_cast<const float*>(gbase + L::OFF_G) + rg;
             const float2* peer_ml = reinterpret_cast<const float2*>(gbase + L::OFF_Q) + rg;
@@ -900,7 +1069,7 @@ __global__ void __launch_bounds__(256) flash_combine_kernel(const float* __restr
     const int head = sc.head, nsplit = sc.nsplit;
     const int item = head + static_cast<int>(blockIdx.x) / 2;
     const int t = static_cast<int>(blockIdx.x) % 2;
-    const Item it = decode_item<PK>(item, sc);
+    const Item it = decode_item<PK, false>(item, sc);  // (its rows)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int row = static_cast<int>(blockIdx.y) * 8 + warp;
     if (row < it.rows(t)) {
@@ -990,32 +1159,38 @@ int unit_of_host(int lin, int g, int n_units) {
     return r * g + (g - 1 - lin % g);
 }
 
-HostSchedule make_schedule(const Shape& s, int hist, int chunk, int num_sms) {
+HostSchedule make_schedule(const Shape& s, int hist, int chunk, const FlashWindow& win, int num_sms) {
     HostSchedule sc;
-    const int heads = sc.heads = flash_pack_heads(s, hist, chunk, num_sms);
+    const int heads = sc.heads = flash_pack_heads(s, hist, chunk, win, num_sms);
     const int tok = BM / heads;  // tokens of a tile
     const int n_qtiles = (chunk + tok - 1) / tok;
     sc.n_pairs = (n_qtiles + 1) / 2;
     const int hq = s.n_q_heads / heads;
     sc.n_items = sc.n_pairs * hq * s.batch;
     const int hq_b = hq * s.batch, G = hq / s.n_kv_heads;
-    const double head_bytes = 4.0 * (static_cast<double>(hist) + chunk) * s.head_dim;  // K/V of one kv head
+    // K/V of one kv head that the launch reads
+    const double head_bytes =
+        4.0 * (win.on ? std::min(static_cast<double>(hist), static_cast<double>(win.window) + win.sinks) + chunk
+                      : static_cast<double>(hist) + chunk) * s.head_dim;
     sc.kvb = 0;
-    if (hist >= chunk && head_bytes * s.batch * s.n_kv_heads > kKvBlockFrom) {
+    if ((hist >= chunk || (win.on && win.window <= chunk)) && head_bytes * s.batch * s.n_kv_heads > kKvBlockFrom) {
         sc.kvb = 1;
         for (int d = 1; d <= s.n_kv_heads; ++d)
             if (s.n_kv_heads % d == 0 && d * head_bytes <= kKvBlockBytes) sc.kvb = d;
     }
     auto n_kv = [&](int item) {  // KV tiles of an item (longest pairs first, in either order)
         const int qt = sc.kvb ? item % (sc.n_pairs * sc.kvb * G) / (sc.kvb * G) : item / hq_b;
-        const int pt = sc.n_pairs - 1 - qt;
-        return (hist + std::min(2 * tok * (pt + 1), chunk) + BN - 1) / BN;
+        const int pt = sc.n_pairs - 1 - qt, end = (hist + std::min(2 * tok * (pt + 1), chunk) + BN - 1) / BN;
+        if (!win.on) return end;
+        const int pos = hist + 2 * tok * pt;
+        return end - window_walk(pos, pos + tok, win.window, win.sinks, BN).skip;
     };
     // costs in KV steps of both query tiles (about 1.3 us each)
     const double c_unit = 1.6, c_split = 2.5, c_step = 1.0;
     const int full_rounds = sc.n_items / num_sms;
     const int tail = sc.n_items - full_rounds * num_sms;
-    const int nkv_min = tail > 0 ? n_kv(sc.n_items - 1) : 1;  // the tail's shortest item
+    int nkv_min = tail > 0 ? n_kv(sc.n_items - 1) : 1;  // the tail's shortest item: the last one, but under a window
+    for (int i = sc.n_items - tail; win.on && i < sc.n_items; ++i) nkv_min = std::min(nkv_min, n_kv(i));
     int best_ns = 1;
     double best = 1e300;
     std::vector<double> load;
@@ -1050,12 +1225,14 @@ HostSchedule make_schedule(const Shape& s, int hist, int chunk, int num_sms) {
     return sc;
 }
 
-template <int D>
-cudaError_t launch_d(const Shape& s, const FlashMaps& maps, int hist, int chunk, int s_stride, const float* cos_t,
-                     const float* sin_t, uint16_t* out, float* ws_o, float* ws_ml, int* err, int num_sms,
+template <int D, bool WIN>
+cudaError_t launch_d(const Shape& s, const FlashMaps& maps, int hist, int chunk, int s_stride, const FlashWindow& win,
+                     const float* cos_t, const float* sin_t, uint16_t* out, float* ws_o, float* ws_ml, int* err, int num_sms,
                      cudaStream_t st, int* n_launched, uint64_t wait_ns) {
-    const HostSchedule hs = make_schedule(s, hist, chunk, num_sms);
+    const HostSchedule hs = make_schedule(s, hist, chunk, win, num_sms);
     Sched sc;
+    sc.window = win.window;
+    sc.sinks = win.sinks;
     sc.S = chunk;
     sc.H = hist;
     sc.heads = hs.heads;
@@ -1096,10 +1273,10 @@ cudaError_t launch_d(const Shape& s, const FlashMaps& maps, int hist, int chunk,
     kcfg.attrs = kattr;
     kcfg.numAttrs = hs.cluster ? 2 : 1;
     const bool pk = hs.heads > 1;
-    const auto fwd = hs.cluster ? (pk ? flash_fwd_kernel<D, true, true> : flash_fwd_kernel<D, true, false>)
-                                : (pk ? flash_fwd_kernel<D, false, true> : flash_fwd_kernel<D, false, false>);
+    const auto fwd = hs.cluster ? (pk ? flash_fwd_kernel<D, true, true, WIN> : flash_fwd_kernel<D, true, false, WIN>)
+                                : (pk ? flash_fwd_kernel<D, false, true, WIN> : flash_fwd_kernel<D, false, false, WIN>);
     cudaError_t e = cudaLaunchKernelEx(&kcfg, fwd, maps.q, maps.k, maps.v, sc, s_stride, s.n_kv_heads,
-                                       scale_log2, cos_t, sin_t, s.max_len, out, ws_o, ws_ml, err, wait_ns);
+                                       scale_log2, win.v_cache, cos_t, sin_t, s.max_len, out, ws_o, ws_ml, err, wait_ns);
     *n_launched = 1;
     if (e != cudaSuccess || hs.nsplit == 1 || hs.cluster) return e;
     cudaLaunchConfig_t cfg = {};
@@ -1121,8 +1298,10 @@ cudaError_t launch_d(const Shape& s, const FlashMaps& maps, int hist, int chunk,
 // with exactly kLaunchRegs registers per thread: check before any launch.
 template <int D>
 cudaError_t configure_d() {
-    for (auto fn : {flash_fwd_kernel<D, false, false>, flash_fwd_kernel<D, true, false>,
-                    flash_fwd_kernel<D, false, true>, flash_fwd_kernel<D, true, true>}) {
+    for (auto fn : {flash_fwd_kernel<D, false, false, false>, flash_fwd_kernel<D, true, false, false>,
+                    flash_fwd_kernel<D, false, true, false>, flash_fwd_kernel<D, true, true, false>,
+                    flash_fwd_kernel<D, false, false, true>, flash_fwd_kernel<D, true, false, true>,
+                    flash_fwd_kernel<D, false, true, true>, flash_fwd_kernel<D, true, true, true>}) {
         cudaFuncAttributes attr;
         cudaError_t e = cudaFuncGetAttributes(&attr, fn);
         if (e != cudaSuccess) return e;
@@ -1148,10 +1327,12 @@ cudaError_t configure_d() {
 // heads, 128 over 8000: 31.8 -> 25.2 us, 128 over 20000: 61 -> 40, 16 sequences of 100 over 500:
 // 45.8 -> 32; below the line 100 over 3000 21.2 -> 21.9 and 4 sequences of 64 over 500 14.0 -> 17.0,
 // both before the merge loaded in batches).
-int flash_pack_heads(const Shape& s, int hist, int chunk, int num_sms) {
+int flash_pack_heads(const Shape& s, int hist, int chunk, const FlashWindow& win, int num_sms) {
     const int G = s.n_q_heads / s.n_kv_heads;
     if (G == 1 || chunk > BM) return 1;
-    const long long items = static_cast<long long>(s.n_q_heads) * s.batch, steps = (hist + chunk + BN - 1) / BN;
+    const long long items = static_cast<long long>(s.n_q_heads) * s.batch;
+    long long steps = (hist + chunk + BN - 1) / BN;
+    if (win.on) steps -= window_walk(hist, hist + chunk, win.window, win.sinks, BN).skip;
     if (chunk * G <= BM && (steps >= 4 || items > num_sms)) return G;
     return items >= 2LL * num_sms || items * steps >= 8LL * num_sms ? G : 1;
 }
@@ -1174,13 +1355,13 @@ cudaError_t configure_flash_fwd() {
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    e = cudaOccupancyMaxActiveClusters(&g_pairs_fit[dev], flash_fwd_kernel<128, true, false>, &cfg);
+    e = cudaOccupancyMaxActiveClusters(&g_pairs_fit[dev], flash_fwd_kernel<128, true, false, false>, &cfg);
     if (e != cudaSuccess) return e;
     return cudaSuccess;
 }
 
 void flash_plan(const Shape& s, int hist, int chunk, int num_sms, int out[4]) {
-    const HostSchedule hs = make_schedule(s, hist, chunk, num_sms);
+    const HostSchedule hs = make_schedule(s, hist, chunk, {}, num_sms);
     out[0] = hs.heads;
     out[1] = hs.nsplit;
     out[2] = hs.cluster ? 1 : 0;
@@ -1188,13 +1369,11 @@ void flash_plan(const Shape& s, int hist, int chunk, int num_sms, int out[4]) {
 }
 
 cudaError_t launch_flash_fwd(const Shape& s, const FlashMaps& maps, int hist, int chunk, int s_stride,
-                             const float* cos_t, const float* sin_t, uint16_t* out, float* ws_o, float* ws_ml, int* err,
+                             const FlashWindow& win, const float* cos_t, const float* sin_t, uint16_t* out, float* ws_o, float* ws_ml, int* err,
                              int num_sms, cudaStream_t st, int* n_launched, uint64_t wait_ns) {
-    if (s.head_dim == 128)
-        return launch_d<128>(s, maps, hist, chunk, s_stride, cos_t, sin_t, out, ws_o, ws_ml, err, num_sms, st,
-                             n_launched, wait_ns);
-    return launch_d<64>(s, maps, hist, chunk, s_stride, cos_t, sin_t, out, ws_o, ws_ml, err, num_sms, st, n_launched,
-                        wait_ns);
+    const auto launch = s.head_dim == 128 ? (win.on ? launch_d<128, true> : launch_d<128, false>)
+                                          : (win.on ? launch_d<64, true> : launch_d<64, false>);
+    return launch(s, maps, hist, chunk, s_stride, win, cos_t, sin_t, out, ws_o, ws_ml, err, num_sms, st, n_launched, wait_ns);
 }
 
 }  // namespace attn

@@ -65,8 +65,15 @@ cudaError_t launch_rope_append(const Shape& s, const uint16_t* k, const uint16_t
 // K2: causal flash attention of `chunk` new queries at positions hist.. over cache
 // slots [0, hist+chunk) (prefill: hist=0).  RoPE of q is applied in the kernel.
 
+// A window of that many positions, 1 <= window <= max_len, under which the first sinks <= max_len stay visible; v_cache: the
+// one of the map (values that are not finite are read from it).  Without one (on = false) a query sees all before it.
+struct FlashWindow {
+    bool on = false;
+    int window = 0, sinks = 0;
+    const uint16_t* v_cache = nullptr;
+};
 // Query heads that share a query tile's 128 rows: all of a kv head's, or 1.
-int flash_pack_heads(const Shape& s, int hist, int chunk, int num_sms);
+int flash_pack_heads(const Shape& s, int hist, int chunk, const FlashWindow& win, int num_sms);
 struct FlashMaps {
     CUtensorMap q;  // q [B, S, Hq, D] as 4-D {D, Hq, S, B}; box {64, heads, 128 / heads, 1} (flash_pack_heads)
     CUtensorMap k;  // k_cache as 3-D {D, hist+chunk, B*Hkv}; box {64, 128, 1}
@@ -82,7 +89,7 @@ cudaError_t configure_flash_fwd();
 // out holds `chunk` tokens of each sequence, sequence b starting at token b * s_stride (the
 // q map carries the same stride).
 cudaError_t launch_flash_fwd(const Shape& s, const FlashMaps& maps, int hist, int chunk, int s_stride,
-                             const float* cos_t, const float* sin_t, uint16_t* out, float* ws_o, float* ws_ml, int* err,
+                             const FlashWindow& win, const float* cos_t, const float* sin_t, uint16_t* out, float* ws_o, float* ws_ml, int* err,
                              int num_sms, cudaStream_t st, int* n_launched, uint64_t wait_ns = kWaitLimitNs);
 
 using PFN_encodeTiled = PFN_cuTensorMapEncodeTiled_v12000;
@@ -176,7 +183,7 @@ struct TreeCall {
     const uint16_t* v;
     const int32_t* d_hist;
     const int32_t* parents;  // [batch][n], NULL: chains
-    int hist, n, window, sinks;
+    int n, window, sinks;
     uint16_t* k_cache;
     uint16_t* v_cache;
     const float* cos_tab;

@@ -986,56 +986,6 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
     }
 }
 
-__device__ __forceinline__ float bf(uint16_t x) { return __uint_as_float(static_cast<uint32_t>(x) << 16); }
-__device__ __forceinline__ float round_bf16(float x) { return __bfloat162float(__float2bfloat16_rn(x)); }
-__device__ __forceinline__ uint16_t bits(float x) { return __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
-
-// A warp per (token, query head): the keys one by one, in two passes over the visible ones.
-template <int D>
-__global__ void window_chunk_kernel(const Args a, int hist) {
-    constexpr int E = D / 64;
-    const int i = blockIdx.x, b = blockIdx.y, lane = threadIdx.x & 31;
-    const int pos = hist + i, lo = max(0, pos - a.window + 1);
-    for (int h = threadIdx.x >> 5; h < a.Hq; h += blockDim.x >> 5) {
-        const int g = h / (a.Hq / a.Hkv);
-        const size_t row = ((static_cast<size_t>(b) * a.n + i) * a.Hq + h) * D;
-        float q[2 * E], acc[2 * E];
-        for (int e = 0; e < E; ++e) {
-            const int j = lane * E + e;
-            const float c = a.cos_tab[static_cast<size_t>(pos) * (D / 2) + j], s = a.sin_tab[static_cast<size_t>(pos) * (D / 2) + j];
-            const float x = bf(a.q[row + j]), y = bf(a.q[row + j + D / 2]);
-            q[e] = round_bf16(__fsub_rn(__fmul_rn(x, c), __fmul_rn(y, s)));
-            q[E + e] = round_bf16(__fadd_rn(__fmul_rn(y, c), __fmul_rn(x, s)));
-            acc[e] = acc[E + e] = 0.f;
-        }
-        const uint16_t* kc = a.k_cache + (static_cast<size_t>(b) * a.Hkv + g) * a.max_len * D;
-        const uint16_t* vc = a.v_cache + (static_cast<size_t>(b) * a.Hkv + g) * a.max_len * D;
-        float m = -INFINITY, l = 0.f;
-        auto key = [&](int s) {
-            float d = 0.f;
-            for (int e = 0; e < E; ++e)
-                d += q[e] * bf(kc[static_cast<size_t>(s) * D + lane * E + e]) + q[E + e] * bf(kc[static_cast<size_t>(s) * D + D / 2 + lane * E + e]);
-            for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xFFFFFFFFu, d, o);
-            d *= a.scale_log2;
-            const float mn = fmaxf(m, d), r = mn == -INFINITY ? 0.f : mn;
-            const float w = fast_exp2(m - r), p = fast_exp2(d - r);
-            l = l * w + p;
-            for (int e = 0; e < E; ++e) {
-                acc[e] = acc[e] * w + p * bf(vc[static_cast<size_t>(s) * D + lane * E + e]);
-                acc[E + e] = acc[E + e] * w + p * bf(vc[static_cast<size_t>(s) * D + D / 2 + lane * E + e]);
-            }
-            m = mn;
-        };
-        const int end = pos + 1;
-        for (int s = 0; s < min(a.sinks, min(lo, end)); ++s) key(s);
-        for (int s = lo; s < end; ++s) key(s);
-        for (int e = 0; e < E; ++e) {
-            a.out[row + lane * E + e] = bits(acc[e] / l);
-            a.out[row + D / 2 + lane * E + e] = bits(acc[E + e] / l);
-        }
-    }
-}
-
 // Layers whose caches one launch of tree_accept moves.
 constexpr int kAcceptLayers = 128;
 struct Accept {
@@ -1173,14 +1123,6 @@ cudaError_t launch_tree_decode(const Shape& s, const TreeCall& c, cudaStream_t s
     a.max_len = s.max_len;
     a.window = c.window;
     a.sinks = c.sinks;
-    if (c.d_hist == nullptr) {
-        const dim3 grid(static_cast<unsigned>(c.n), static_cast<unsigned>(s.batch));
-        if (s.head_dim == 128)
-            window_chunk_kernel<128><<<grid, 256, 0, st>>>(a, c.hist);
-        else
-            window_chunk_kernel<64><<<grid, 256, 0, st>>>(a, c.hist);
-        return cudaGetLastError();
-    }
     // a second tile of rows where one does not hold them all: it halves the passes over the keys
     const bool two = c.n * a.G > BM;
     if (s.head_dim == 128) return two ? launch<128, 2>(s, c, a, st) : launch<128, 1>(s, c, a, st);
