@@ -126,6 +126,7 @@ struct Item {
     int nkva, nkvb;    // KV tiles each tile attends to
     int n_kv;          // KV tiles loaded for the item
     WindowWalk w;      // WIN: which they are; tile B sits out tiles [w.off0, w.off1)
+    int edge, diag;    // WIN: every row sees the whole of tiles [edge, diag)
     __device__ __forceinline__ int q0(int t) const { return t ? q0b : q0a; }
     __device__ __forceinline__ int rows(int t) const { return t ? rowsb : rowsa; }
     __device__ __forceinline__ int nkv(int t) const { return t ? nkvb : nkva; }
@@ -186,6 +187,9 @@ __device__ __forceinline__ Item decode_item(int lin, const Sched& sc) {
         it.w = window_walk(sc.H + it.q0a, sc.H + it.q0b, sc.window, sc.sinks, BN);
         it.nkva -= it.w.skip;
         if (it.rowsb) it.nkvb -= it.w.skip;
+        const int before = sc.H + (it.rowsb ? it.q0b + it.rowsb : it.q0a + it.rowsa) - 1 - sc.window;  // the last row's window
+        it.edge = before < 0 ? 0 : max(before / BN + 1 - it.w.skip, 0);
+        it.diag = (sc.H + it.q0a + 1) / BN - it.w.skip;
     }
     if constexpr (PK) {
         it.rowsa *= sc.heads;
@@ -238,16 +242,13 @@ struct Unit {
     __device__ __forceinline__ int key(int j) const {
         return (WIN && j >= it.w.ns ? j + it.w.skip : j) * BN;
     }
-    // WIN: whether some row of query tile t may not see some slot of the tile from slot kb on, and whether that holds for a query
-    // tile that walks KV tile j (only there is V guarded).
+    // WIN: whether some row of query tile t may not see some slot of the tile from slot kb on.
     __device__ __forceinline__ bool masked(int t, int kb, const Sched& sc) const {
         const int pos = sc.H + it.q0(t);
         return kb + BN - 1 > pos || (kb <= pos + sc.tok - 1 - sc.window && kb + BN > sc.sinks);
     }
-    __device__ __forceinline__ bool guarded(int j, const Sched& sc) const {
-        const int kb = key<true>(j);
-        return (on<true>(0, j) && masked(0, kb, sc)) || (on<true>(1, j) && masked(1, kb, sc));
-    }
+    // WIN: whether the V of KV tile j is guarded: some row may not see it whole.
+    __device__ __forceinline__ bool guarded(int j) const { return j < it.edge || j >= it.diag; }
 };
 
 // Which of the slots k0 .. k0 + 31 the row of position pos sees, a bit each.
@@ -269,7 +270,7 @@ __device__ __noinline__ void add_not_finite(uint32_t o_col, int t, int pos, Unit
         tmem_ld32(o_col + c0, o);
         tmem_wait_ld();
         for (int j = un.first<true>(t); j < un.end(t); ++j) {
-            if (!un.on<true>(t, j) || !un.guarded(j, sc)) continue;
+            if (!un.on<true>(t, j) || !un.guarded(j)) continue;
             const int kb = un.key<true>(j);
             for (int c = 0; c < BN / 32; ++c)
                 for (uint32_t w = window_word(kb + 32 * c, pos, sc.window, sc.sinks); w != 0; w &= w - 1) {
@@ -622,7 +623,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             uint32_t ready_par = 0;  // WIN: a bit per slot, the parity of its next B_GREADY
             // WIN: the guards are through with the group's V, which is KV tile j
             auto wait_v = [&](const Unit& un, int j) -> bool {
-                if (!WIN || !un.guarded(j, sc)) return true;
+                if (!WIN || !un.guarded(j)) return true;
                 if (!mbar_wait(bar(B_GREADY0 + gslot), ready_par >> gslot & 1u, abort_flag, wait_ns)) return false;
                 ready_par ^= 1u << gslot;
                 return true;
@@ -639,6 +640,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     break;
                 }
                 tc_fence_after();
+                [[maybe_unused]] bool was_b = false;  // WIN: S_B(j - 1) was issued
                 for (int j = un.kv_lo; j < un.kv_hi && ok; ++j) {
                     // group j: K(j), and V(j-1) for the PV MMAs of the previous tile
                     if (!mbar_wait(bar(B_GFULL0 + gslot), (gc / GS) & 1u, abort_flag, wait_ns) ||
@@ -647,7 +649,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         break;
                     }
                     tc_fence_after();
-                    const bool pv_a = j > un.kv_lo && un.on<WIN>(0, j - 1), pv_b = j > un.kv_lo && un.on<WIN>(1, j - 1);
+                    const bool pv_a = j > un.kv_lo && j - 1 < it.nkv(0), pv_b = WIN ? was_b : j > un.kv_lo && j - 1 < it.nkv(1);
                     const bool s_a = un.on<WIN>(0, j), s_b = un.on<WIN>(1, j);
                     const bool first = j - 1 == un.kv_lo, first_b = j - 1 == un.first<WIN>(1);
                     if (pv_a) {
@@ -668,6 +670,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         issue_pv(1, first_b, gslot);
                     }
                     if (s_b) issue_s(1, gslot);
+                    if constexpr (WIN) was_b = s_b;
                     umma_commit(bar(B_GEMPTY0 + gslot));
                     next_group();
                 }
@@ -718,7 +721,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const int st = static_cast<int>(gc % GS);
                     ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(B_GFULL0 + st), (gc / GS) & 1u, abort_flag, wait_ns));
                     if (!ok) break;
-                    if (j > un.kv_lo && un.guarded(j - 1, sc)) {
+                    if (j > un.kv_lo && un.guarded(j - 1)) {
                         // the products with 0 add up to 0, or to NaN
                         uint4* v = reinterpret_cast<uint4*>(gbase + L::OFF_G + st * L::G_SLOT + L::KV_TILE);
                         uint32_t sum[4] = {0u, 0u, 0u, 0u};
@@ -1178,12 +1181,14 @@ HostSchedule make_schedule(const Shape& s, int hist, int chunk, const FlashWindo
         for (int d = 1; d <= s.n_kv_heads; ++d)
             if (s.n_kv_heads % d == 0 && d * head_bytes <= kKvBlockBytes) sc.kvb = d;
     }
-    auto n_kv = [&](int item) {  // KV tiles of an item (longest pairs first, in either order)
-        const int qt = sc.kvb ? item % (sc.n_pairs * sc.kvb * G) / (sc.kvb * G) : item / hq_b;
-        const int pt = sc.n_pairs - 1 - qt, end = (hist + std::min(2 * tok * (pt + 1), chunk) + BN - 1) / BN;
-        if (!win.on) return end;
-        const int pos = hist + 2 * tok * pt;
-        return end - window_walk(pos, pos + tok, win.window, win.sinks, BN).skip;
+    std::vector<int> pair_kv(sc.n_pairs);  // KV tiles of a pair, longest causal walk first
+    for (int qt = 0; qt < sc.n_pairs; ++qt) {
+        const int pt = sc.n_pairs - 1 - qt, pos = hist + 2 * tok * pt;
+        pair_kv[qt] = (hist + std::min(2 * tok * (pt + 1), chunk) + BN - 1) / BN -
+                      (win.on ? window_walk(pos, pos + tok, win.window, win.sinks, BN).skip : 0);
+    }
+    auto n_kv = [&](int item) {  // KV tiles of an item (in either order)
+        return pair_kv[sc.kvb ? item % (sc.n_pairs * sc.kvb * G) / (sc.kvb * G) : item / hq_b];
     };
     // costs in KV steps of both query tiles (about 1.3 us each)
     const double c_unit = 1.6, c_split = 2.5, c_step = 1.0;
