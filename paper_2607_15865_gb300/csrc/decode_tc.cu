@@ -54,11 +54,16 @@
 // A split that took all T tiles writes the normalised output itself.  Every wait is
 // bounded; on expiry the CTA records kDevErrTimeout, lets its copies and MMAs finish,
 // releases TMEM and still takes part in the merge (its count, or the cluster barriers).
+//
+// WIN (one new token): the token sees the slots s with p - s < window or s < sinks alone.  The tiles
+// of the sequence are then those of the sinks and those from the window on, in that order; where one
+// holds a slot that is not seen, its score is masked and its V row zeroed.
 #include <cuda_bf16.h>
 
 #include <algorithm>
 #include <cmath>
 
+#include "flash_rows.h"
 #include "internal.h"
 #include "sm100_ptx.cuh"
 
@@ -267,7 +272,20 @@ constexpr int kModeGlobal = 0, kModeCluster = 1, kModeWaves = 2;
 // of 8190 tokens 99.6 -> 67.1 us, B16 57.3 -> 46.5, B12 56.9 -> 37.1, B8 32.7 -> 28.5.
 constexpr int ctas_per_sm(int D, int ntok) { return D == 64 && ntok == 1 ? 2 : 1; }
 static_assert(2 * (Layout<64>::ALLOC + 1024) <= 233472, "shared memory of two CTAs");
-template <int D, int NHP, int MAXTOK, int MODE>
+// Key tiles of a sequence whose token range is tr; under a window (one token) w says which.
+template <bool WIN>
+__device__ __forceinline__ int tiles_of(const TokRange& tr, int window, int sinks, WindowWalk& w) {
+    const int end = (tr.hist + tr.hi + KT - 1) / KT;
+    if constexpr (!WIN) return end;
+    w = window_walk(tr.hist, tr.hist, window, sinks, KT);
+    return end - w.skip;
+}
+template <bool WIN>
+__device__ __forceinline__ int tiles_of(const TokRange& tr, int window, int sinks) {
+    WindowWalk w;
+    return tiles_of<WIN>(tr, window, sinks, w);
+}
+template <int D, int NHP, int MAXTOK, int MODE, bool WIN>
 __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, MAXTOK)) decode_tc_kernel(
     const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
     const uint16_t* __restrict__ q, const uint16_t* __restrict__ k_new, const uint16_t* __restrict__ v_new,
@@ -276,7 +294,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, MAXTOK)) decode_tc_ke
     int max_len, int nsplit,
     float scale_log2, float* __restrict__ part_o, float* __restrict__ part_ml, int* __restrict__ counters,
     uint16_t* __restrict__ out, int* __restrict__ err, int producer_early, uint64_t wait_ns, int ncg, int spec,
-    int s0) {
+    int s0, int window, int sinks) {
+    static_assert(!WIN || MAXTOK == 1, "a window of one token");
     using L = Layout<D>;
     constexpr int VST = L::VST;
     constexpr bool WAVES = MODE == kModeWaves;
@@ -318,7 +337,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, MAXTOK)) decode_tc_ke
         const int batch = static_cast<int>(gridDim.y) / ncg;
         if (warp == 0 && batch <= 32) {
             const TokRange rb = decode_tokens<D>(d_hist[min(lane, batch - 1)], hist_add, ntok, max_len);
-            const int tb = rb.hi > rb.lo ? (rb.hist + rb.hi + KT - 1) / KT : 0;
+            const int tb = rb.hi > rb.lo ? tiles_of<WIN>(rb, window, sinks) : 0;
             int rank = 0;
             for (int j = 0; j < batch; ++j) {
                 const int tj = __shfl_sync(0xFFFFFFFFu, tb, j);
@@ -370,7 +389,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, MAXTOK)) decode_tc_ke
             if (batch <= 1024) {
                 for (int bb = lane; bb < batch; bb += 32) {
                     const TokRange rb = decode_tokens<D>(d_hist[bb], hist_add, ntok, max_len);
-                    const int tb = rb.hi > rb.lo ? (rb.hist + rb.hi + KT - 1) / KT : 0;
+                    const int tb = rb.hi > rb.lo ? tiles_of<WIN>(rb, window, sinks) : 0;
                     tmax = max(tmax, tb);
                     tsum += tb;
                 }
@@ -386,7 +405,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, MAXTOK)) decode_tc_ke
                 const TokRange own = decode_tokens<D>(hist_len, hist_add, ntok, max_len);
                 if (own.hi > own.lo) {
                     if (!even || s < (spec >> 2)) t = s0 + atomicAdd(claim_ctr, 1);
-                    if (t >= (own.hist + own.hi + KT - 1) / KT) t = -1;
+                    if (t >= tiles_of<WIN>(own, window, sinks)) t = -1;
                     if (t < 0 && atomicAdd(visit_ctr, 1) == nsplit - 1) {
                         *claim_ctr = 0;
                         *slot_ctr = 0;
@@ -405,7 +424,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, MAXTOK)) decode_tc_ke
     // tile, tile s, before the length is known: the K slot's arrival is held back until the
     // producer knows whether tile s holds keys of the sequence (the copies read in-range
     // slots or the map's zero fill either way; a tile past the sequence is not used): spec & 1.
-    const bool spec_first = (spec & 1) != 0 && s < s0 && s * KT < max_len;
+    // (which tile of the cache that is depends on the length under a window)
+    const bool spec_first = !WIN && (spec & 1) != 0 && s < s0 && s * KT < max_len;
     if (warp == kWarpTma && lane == 0) {
         *abort_flag = 0;
         lastv[5] = 0;
@@ -477,7 +497,9 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, MAXTOK)) decode_tc_ke
     auto col_runs = [&](int h) { return D == 128 || runs((c0 + h) / G); };
     if (tr.hi - tr.lo < ntok && s == 0 && g == 0 && cg == 0 && tid == 0) atomicOr(err, kDevErrHistRange);
     const int nkeys = hist + tr.hi;       // slots [0, hist) and the new tokens', up to hist + hi - 1
-    const int T = (nkeys + KT - 1) / KT;  // key tiles of the sequence; tile T-1 holds the last new slot
+    WindowWalk walk;
+    const int T = tiles_of<WIN>(tr, window, sinks, walk);  // key tiles of the sequence
+    const int t_last = (nkeys - 1) / KT;  // the tile of the last new slot
     // Splits s < s0 start with tile s; every other tile is claimed from the item's counter
     // (tickets s0, s0 + 1, ...).  A split that gets no tile writes nothing.
     // Rows of column c (token c / G, head h0 + c % G), tabulated once in the prologue:
@@ -486,7 +508,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, MAXTOK)) decode_tc_ke
     // launch's repeat its last.
     const size_t* crow = reinterpret_cast<const size_t*>(gb + L::OFF_CROW);
     const size_t* orow = reinterpret_cast<const size_t*>(gb + L::OFF_OROW);
-    int* meta = reinterpret_cast<int*>(gb + L::OFF_META);  // tile index of local tile j at [j % 8]; -1 ends
+    int* meta = reinterpret_cast<int*>(gb + L::OFF_META);  // tile (of the cache) of local tile j at [j % 8]; -1 ends
     // Wait for the last use of every ring slot by nk K and nv V copies.  (A loop that ended well has
     // put its end mark in K slot nk mod KST, whose copy had landed before: its phase is past.)
     auto drain = [&](int nk, int nv, bool ended_well) {
@@ -530,7 +552,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, MAXTOK)) decode_tc_ke
                 }
             };
             for (int j = 0;; ++j) {
-                const int tile = cur < T ? cur : -1;
+                const int tile = cur >= T ? -1 : WIN && cur >= walk.ns ? cur + walk.skip : cur;
                 const int ks = j % KST, vs = j % VST;
                 if (j >= KST && !mbar_wait(bar(B_KEMPTY0 + ks), static_cast<uint32_t>(j / KST - 1) & 1u, abort_flag, wait_ns)) {
                     ok = false;
@@ -608,7 +630,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, MAXTOK)) decode_tc_ke
         // Lane l (below D / 4) handles dimensions 4l .. 4l+3 of each new token tt (slot hist + tt,
         // rotated at that position by every CTA; written by the CTA that gets the slot's tile).
         const bool has_dims = D == 128 || 4 * lane < D;
-        const int last_row = (nkeys - 1) - (T - 1) * KT;  // row of the last new slot in tile T-1
+        const int last_row = (nkeys - 1) - t_last * KT;  // row of the last new slot in its tile
         uint2 k_rot[MAXTOK], v_val[MAXTOK];
 #pragma unroll
         for (int tt = 0; tt < MAXTOK; ++tt) {
@@ -652,7 +674,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, MAXTOK)) decode_tc_ke
             const uint32_t sV = base + L::OFF_V + (jj % VST) * L::TILE;
             const int vtile = meta[jj % 8];
             if (vtile * KT + KT > hist) {
-                // the new tokens' v into their rows of this tile; in tile T-1 the rows past the
+                // the new tokens' v into their rows of this tile; in the last one the rows past the
                 // last new slot zeroed (those slots may hold anything, and 0 * NaN would poison O)
                 uint8_t* vt = gb + L::OFF_V + (jj % VST) * L::TILE;
 #pragma unroll
@@ -670,9 +692,17 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, MAXTOK)) decode_tc_ke
                         }
                         if (has_dims) *reinterpret_cast<uint2*>(vt + sw_elem(hist + tt - vtile * KT, 4 * lane, KT)) = vv;
                     }
-                if (vtile == T - 1)
+                if (vtile == t_last)
                     for (int i = (last_row + 1) * (D / 8) + lane; i < KT * (D / 8); i += 32)
                         *reinterpret_cast<uint4*>(vt + sw_elem(i / (D / 8), 8 * (i % (D / 8)), KT)) = make_uint4(0, 0, 0, 0);
+                fence_proxy_async_smem();
+            }
+            if (WIN && vtile * KT <= hist - window && vtile * KT + KT > sinks) {
+                // the rows past the sinks and before the window
+                uint8_t* vt = gb + L::OFF_V + (jj % VST) * L::TILE;
+                const int end = min(hist - window - vtile * KT + 1, KT) * (D / 8);
+                for (int i = max(sinks - vtile * KT, 0) * (D / 8) + lane; i < end; i += 32)
+                    *reinterpret_cast<uint4*>(vt + sw_elem(i / (D / 8), 8 * (i % (D / 8)), KT)) = make_uint4(0, 0, 0, 0);
                 fence_proxy_async_smem();
             }
             __syncwarp();
@@ -818,7 +848,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, MAXTOK)) decode_tc_ke
             tmem_wait_ld();
             // key tile * KT + t is visible to global column c (token c / G) iff it is <= hist + c / G,
             // i.e. iff c >= (key - hist) * G (always for a history key: key - hist < 0)
-            const int kg = (tile * KT + t - hist) * G - c0;
+            int kg = (tile * KT + t - hist) * G - c0;
+            if (WIN && tile * KT + t <= hist - window && tile * KT + t >= sinks) kg = NHP;  // (to none)
             float sc[NHP];
             bool exceed = false;
 #pragma unroll
@@ -1162,19 +1193,20 @@ constexpr int kMaxDevices = 64;
 constexpr int kMaxCluster = 16;
 int g_cluster_fit[kMaxDevices][2][kMaxCluster + 1] = {};  // [1]: two CTAs per SM
 
-#define DECODE_TC_MODES(D, NHP, MAXTOK)                                                             \
-    decode_tc_kernel<D, NHP, MAXTOK, kModeGlobal>, decode_tc_kernel<D, NHP, MAXTOK, kModeCluster>, \
-        decode_tc_kernel<D, NHP, MAXTOK, kModeWaves>
+#define DECODE_TC_MODES(D, NHP, MAXTOK, WIN)                                                              \
+    decode_tc_kernel<D, NHP, MAXTOK, kModeGlobal, WIN>, decode_tc_kernel<D, NHP, MAXTOK, kModeCluster, WIN>, \
+        decode_tc_kernel<D, NHP, MAXTOK, kModeWaves, WIN>
 
 template <int D>
 cudaError_t set_attributes() {
     cudaError_t e = cudaSuccess;
-    for (auto fn : {DECODE_TC_MODES(D, 8, 1), DECODE_TC_MODES(D, 16, 1), DECODE_TC_MODES(D, 8, kMaxTok),
-                    DECODE_TC_MODES(D, 16, kMaxTok)})
+    for (auto fn : {DECODE_TC_MODES(D, 8, 1, false), DECODE_TC_MODES(D, 16, 1, false), DECODE_TC_MODES(D, 8, kMaxTok, false),
+                    DECODE_TC_MODES(D, 16, kMaxTok, false), DECODE_TC_MODES(D, 8, 1, true), DECODE_TC_MODES(D, 16, 1, true)})
         if (e == cudaSuccess)
             e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<D>::ALLOC);
-    for (auto fn : {decode_tc_kernel<D, 8, 1, kModeCluster>, decode_tc_kernel<D, 16, 1, kModeCluster>,
-                    decode_tc_kernel<D, 8, kMaxTok, kModeCluster>, decode_tc_kernel<D, 16, kMaxTok, kModeCluster>})
+    for (auto fn : {decode_tc_kernel<D, 8, 1, kModeCluster, false>, decode_tc_kernel<D, 16, 1, kModeCluster, false>,
+                    decode_tc_kernel<D, 8, kMaxTok, kModeCluster, false>, decode_tc_kernel<D, 16, kMaxTok, kModeCluster, false>,
+                    decode_tc_kernel<D, 8, 1, kModeCluster, true>, decode_tc_kernel<D, 16, 1, kModeCluster, true>})
         if (e == cudaSuccess) e = cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     return e;
 }
@@ -1203,7 +1235,8 @@ cudaError_t configure_decode_tc() {
         cfg.numAttrs = 1;
         int n = 0;
         if (cudaOccupancyMaxActiveClusters(
-                &n, two ? decode_tc_kernel<64, 8, 1, kModeCluster> : decode_tc_kernel<128, 8, 1, kModeCluster>, &cfg) != cudaSuccess) {
+                &n, two ? decode_tc_kernel<64, 8, 1, kModeCluster, false> : decode_tc_kernel<128, 8, 1, kModeCluster, false>,
+                &cfg) != cudaSuccess) {
             n = 0;
             cudaGetLastError();  // a refused size is never used
         }
@@ -1311,7 +1344,7 @@ cudaError_t launch_decode_tc(const Shape& s, const DecodeMaps& maps, const uint1
                              uint16_t* v_cache, const float* cos_tab, const float* sin_tab, float* part_o,
                              float* part_ml, int* counters, int nsplit, uint16_t* out, int* err, bool after_decode,
                              int ntok, int seq_tok, cudaStream_t st, bool producer_early, uint64_t wait_ns,
-                             int num_sms) {
+                             int num_sms, int window, int sinks) {
     const float scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(s.head_dim)));
     const int G = s.n_q_heads / s.n_kv_heads;
     const int ncg = decode_tc_column_groups(G, ntok);
@@ -1346,19 +1379,23 @@ cudaError_t launch_decode_tc(const Shape& s, const DecodeMaps& maps, const uint1
     }
     cfg.attrs = attr;
     cfg.numAttrs = n_attr;
-    if (ntok < 1 || ntok > kMaxTok || G > NH) return cudaErrorInvalidValue;
-    using Kernel = decltype(&decode_tc_kernel<128, 8, 1, kModeGlobal>);
-    static const Kernel kernels[2][4][3] = {
-        {{DECODE_TC_MODES(128, 8, 1)},
-         {DECODE_TC_MODES(128, 16, 1)},
-         {DECODE_TC_MODES(128, 8, kMaxTok)},
-         {DECODE_TC_MODES(128, 16, kMaxTok)}},
-        {{DECODE_TC_MODES(64, 8, 1)},
-         {DECODE_TC_MODES(64, 16, 1)},
-         {DECODE_TC_MODES(64, 8, kMaxTok)},
-         {DECODE_TC_MODES(64, 16, kMaxTok)}}};
+    if (ntok < 1 || ntok > kMaxTok || G > NH || (window > 0 && ntok > 1)) return cudaErrorInvalidValue;
+    using Kernel = decltype(&decode_tc_kernel<128, 8, 1, kModeGlobal, false>);
+    static const Kernel kernels[2][6][3] = {
+        {{DECODE_TC_MODES(128, 8, 1, false)},
+         {DECODE_TC_MODES(128, 16, 1, false)},
+         {DECODE_TC_MODES(128, 8, kMaxTok, false)},
+         {DECODE_TC_MODES(128, 16, kMaxTok, false)},
+         {DECODE_TC_MODES(128, 8, 1, true)},
+         {DECODE_TC_MODES(128, 16, 1, true)}},
+        {{DECODE_TC_MODES(64, 8, 1, false)},
+         {DECODE_TC_MODES(64, 16, 1, false)},
+         {DECODE_TC_MODES(64, 8, kMaxTok, false)},
+         {DECODE_TC_MODES(64, 16, kMaxTok, false)},
+         {DECODE_TC_MODES(64, 8, 1, true)},
+         {DECODE_TC_MODES(64, 16, 1, true)}}};
     const Kernel kernel =
-        kernels[s.head_dim == 64][ntok == 1 ? (G <= 8 ? 0 : 1) : (G * ntok <= 8 ? 2 : 3)][mode];
+        kernels[s.head_dim == 64][(window > 0 ? 4 : ntok == 1 ? 0 : 2) + (G * ntok <= 8 ? 0 : 1)][mode];
     const long items = static_cast<long>(s.batch) * s.n_kv_heads * ncg;
     const bool mid = mid_items(items, slots, per_sm);
     const int spec = (after_decode ? 0 : 1) | (2 * items > slots || mid ? 2 : 0) | (mid ? nsplit - 1 : 0) << 2;
@@ -1367,7 +1404,7 @@ cudaError_t launch_decode_tc(const Shape& s, const DecodeMaps& maps, const uint1
                               s.n_q_heads,
                               s.n_kv_heads, s.max_len, nsplit, scale_log2, part_o, part_ml, counters, out, err,
                               producer_early ? 1 : 0, wait_ns, ncg,
-                              spec, s0);
+                              spec, s0, window, sinks);
 }
 
 }  // namespace attn

@@ -114,6 +114,7 @@ struct DecodeMaps {
 // are read before the grid waits on its predecessor.
 // producer_early: a dependent launch after a kernel that writes q / the new k, v (and
 // neither the caches, the lengths nor the counters); the K/V stream starts before the wait.
+// window > 0 (one new token): the token sees the slots s with p - s < window or s < sinks alone.
 cudaError_t configure_decode_tc();
 // Column groups of 16 (query head, new token) columns one launch runs for ntok new tokens
 // per sequence: ceil(G * ntok / 16); items = B * Hkv * that many.
@@ -131,7 +132,8 @@ cudaError_t launch_decode_tc(const Shape& s, const DecodeMaps& maps, const uint1
                              uint16_t* v_cache,
                              const float* cos_tab, const float* sin_tab, float* part_o, float* part_ml,
                              int* counters, int nsplit, uint16_t* out, int* err, bool after_decode, int ntok,
-                             int seq_tok, cudaStream_t st, bool producer_early, uint64_t wait_ns, int num_sms);
+                             int seq_tok, cudaStream_t st, bool producer_early, uint64_t wait_ns, int num_sms,
+                             int window = 0, int sinks = 0);
 
 // The 4-bit KV cache (format: kv4.cuh).  Slots per (sequence, kv head): whole tiles of the decode.
 inline int kv4_slots(int max_len) { return (max_len + 63) / 64 * 64; }
