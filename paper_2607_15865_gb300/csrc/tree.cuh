@@ -44,6 +44,7 @@ __device__ __forceinline__ int tree_kin(const int32_t* parents, int n, int lane,
         bad |= up[h] >= 0 && up[h] < i && !(there >> up[h] & 1);
     }
     if (__any_sync(0xFFFFFFFFu, bad)) return -1;
+#pragma unroll 1
     for (int far = 1; far < n; far *= 2) {
         uint64_t k[2];
         int u[2];

@@ -13,7 +13,7 @@
 // have a part of it, each a share of its rows and columns, once all parts are written (a cooperative launch: they wait for one
 // another, at the end of their runs).
 //
-// Warps: 4 NT softmax warps (a tile's rows), one TMA producer, one MMA issuer, two guards.
+// Warps: 4 NT softmax warps (a tile's rows), one TMA producer, one MMA issuer, two guards and, with NT = 1, four stagers.
 //   producer  K and V tiles through a ring of slots, in the order K0, K1, V0, K2, V1, ..
 //   guards    see every tile between the producer and the issuer.  In a tile that holds slots of new tokens they put those in
 //             (k rotated), and write them to the cache; in a V tile that some row does not see whole they look for values
@@ -21,8 +21,11 @@
 //             the rows that see them add them to their O at the end (a rare path, from global memory).
 //   issuer    NT = 1: S(j + 1) before P V(j), two S buffers, so that a softmax runs beside the MMAs; Q and O have two buffers
 //             each, for the segments in turn.  NT = 2: the tiles' MMAs alternate, each has one S.
-//   softmax   rotate the q rows of the next segment into shared memory, scores -> masked by words of 32 slots (in tiles that
-//             need it) -> running maximum, moved lazily (by 2^8) -> P as bf16.
+//   stagers   rotate the q rows of the next segments into shared memory, and find their kin.  While the keys stream in, a load
+//             takes two microseconds and more, and between two segments the softmax warps had several to wait for.
+//             (NT = 2 has one Q for both tiles and few segments: the softmax warps do it.)
+//   softmax   scores -> masked by words of 32 slots (in tiles that need it) -> running maximum, moved lazily (by 2^8) -> P as
+//             bf16.
 // Roundings: rotated q and k to bf16; a weight P to bf16 for its product with v (the operand's type: 2^-8 of it; the
 // sum that O is divided by takes it unrounded); the output.  Scores, maxima, sums and O are floats.
 // Every wait is bounded; on expiry the CTA records kDevErrTimeout, lets its copies and MMAs finish, releases TMEM and
@@ -41,21 +44,24 @@ namespace {
 
 constexpr int BM = 128;        // rows per tile (TMEM lanes)
 constexpr int BN = 128;        // slots per key tile
-constexpr int kMaxSeqs = 128;  // sequences of one launch (their tiles are summed in shared memory)
+constexpr int kPer = 4, kMaxSeqs = 32 * kPer;  // sequences of one launch (a lane of the planner has kPer)
 constexpr uint32_t kTmemCols = 512;  // S [0, 256): two of 128; O [256, 256 + 2 D): two
 constexpr uint32_t kTmO = 2 * BN;
 constexpr int kFlags = 8;
+constexpr int kSegs = 8;  // segments in shared memory: the producer is at most NS / 2 + 2 ahead of every reader
 constexpr int kLonger = 4;  // tiles that a piece may be longer than a run
-// Registers with three warpgroups (NT = 2): 168 a thread at launch, of which the producer's group leaves 72 to the others.
-constexpr int kLaunchRegs = 168;
-constexpr uint32_t kRegsLow = 96, kRegsHigh = 200;
-static_assert(128 * kRegsLow + 256 * kRegsHigh <= 384 * kLaunchRegs, "register split exceeds the launch total");
+constexpr int kHead = 3;    // an item's first segment takes a run about as long as this many tiles: its q, its epilogue
+constexpr int kLaunchRegs = 168;  // registers a thread at launch
 
 template <int D_, int NT_>
 struct Cfg {
     static constexpr int D = D_, NT = NT_;
-    static constexpr int SOFT = 4 * NT;  // softmax warps; then the producer, the issuer and two guards
-    static constexpr int THREADS = (SOFT + 4) * 32;
+    static constexpr int SOFT = 4 * NT;  // softmax warps; then the producer, the issuer and two guards, the stagers
+    static constexpr int THREADS = 384;
+    // Registers: the producer's warpgroup (and the stagers') leaves some to the softmax.
+    static constexpr uint32_t REGS_LOW = NT == 1 ? 120 : 96, REGS_HIGH = NT == 1 ? 232 : 200;
+    static_assert((THREADS - 32 * SOFT) * REGS_LOW + 32 * SOFT * REGS_HIGH <= THREADS * kLaunchRegs,
+                  "register split exceeds the launch total");
     static constexpr int DCH = D / 64;        // 128-byte chunks of a row
     static constexpr int CHUNK = 128 * 128;   // bytes of a chunk of 128 rows
     static constexpr int TILE = DCH * CHUNK;  // of a Q, K or V tile
@@ -63,19 +69,20 @@ struct Cfg {
     static constexpr int ROWS = NT * BM;          // rows of a group
     static constexpr int OFF_Q = 0;               // two Q tiles: of two segments, or of the two row tiles
     static constexpr int OFF_RING = 2 * TILE;
-    static constexpr int OFF_PRE = OFF_RING + NS * TILE;     // int [kMaxSeqs]: key tiles up to and with a sequence's
-    static constexpr int OFF_HIST = OFF_PRE + kMaxSeqs * 4;  // int [kMaxSeqs]
-    static constexpr int OFF_BAR = OFF_HIST + kMaxSeqs * 4;
+    static constexpr int OFF_SEG = OFF_RING + NS * TILE;         // Seg [kSegs]
+    static constexpr int OFF_SHARED = OFF_SEG + kSegs * 32;      // Shared [2]: of the parts in slots 0 and 1
+    static constexpr int OFF_KIN = OFF_SHARED + 2 * 32;  // NT = 1: uint64 [64], the kin of the tokens of the segment in hand
+    static constexpr int OFF_BAR = OFF_KIN + (NT == 1 ? 64 * 8 : 0);
     enum { B_FULL = 0, B_READY = NS, B_EMPTY = 2 * NS, B_QREADY = 3 * NS, B_QEMPTY = B_QREADY + 2, B_SFULL = B_QEMPTY + 2,
-           B_PFULL = B_SFULL + 2, B_OFULL = B_PFULL + 2, B_OEMPTY = B_OFULL + 2, B_PVDONE = B_OEMPTY + 2, B_DRAIN, NBAR };
+           B_PFULL = B_SFULL + 2, B_OFULL = B_PFULL + 2, B_OEMPTY = B_OFULL + 2, B_PVDONE = B_OEMPTY + 2, B_DRAIN, B_KINREAD, B_PLANNED,
+           B_SEG, NBAR = B_SEG + kSegs };
     static constexpr int OFF_TMEM = OFF_BAR + NBAR * 8;
     static constexpr int OFF_ABORT = OFF_TMEM + 4;
     // int [kFlags]: the segment, from 1, with a value that is not finite in a masked tile; the guards are at most NS / 2 + 1
     // segments ahead of the softmax
     static constexpr int OFF_FLAG = OFF_ABORT + 4;
-    static constexpr int OFF_CUT = OFF_FLAG + kFlags * 4;  // int [2]: tiles of a run (0: pieces), of a piece
-    static constexpr int BYTES = OFF_CUT + 8;
-    static_assert(NS / 2 + 1 < kFlags, "flags");
+    static constexpr int BYTES = OFF_FLAG + kFlags * 4;
+    static_assert(NS / 2 + 1 < kFlags && NS / 2 + 2 < kSegs, "flags and segments");
     static constexpr int ALLOC = BYTES + 1024;  // slack to align the base to 1024 bytes
     static_assert(ALLOC <= 232448, "shared memory budget of one CTA");
 };
@@ -99,7 +106,7 @@ struct Args {
     float scale_log2;
     int b0, batch;  // sequences b0 .. b0 + batch - 1 are this launch's
     int n, Hq, Hkv, G, max_len, window, sinks;
-    int groups, runs;  // row groups; runs of each
+    int groups, runs, runs_last;  // row groups; runs of each, of the last
 };
 
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
@@ -114,80 +121,183 @@ __device__ __forceinline__ uint32_t sw128_offset(int row, int col) {
 struct Span {
     int ns, skip, nt;
 };
-__device__ __forceinline__ Span span_of(int hist, const Args& a) {
-    const int lo = max(0, hist - a.window + 1), t_lo = lo / BN;  // (the first token's window is the lowest)
+__device__ __forceinline__ Span span_of(int hist, int n, int window, int sinks) {
+    const int lo = max(0, hist - window + 1), t_lo = lo / BN;  // (the first token's window is the lowest)
     Span s;
-    s.ns = min((min(a.sinks, lo) + BN - 1) / BN, t_lo);
+    s.ns = min((min(sinks, lo) + BN - 1) / BN, t_lo);
     s.skip = t_lo - s.ns;
-    s.nt = (hist + a.n + BN - 1) / BN - s.skip;
+    s.nt = (hist + n + BN - 1) / BN - s.skip;
     return s;
 }
 
-// A CTA's part of an item: its tiles lo .. hi - 1 of nt, in part r_mine - r_first of `parts`.
-struct Seg {
-    int b, h, hist, ns, skip, lo, hi, nt, first;  // first: the item's tile 0 in the order that runs are cut from
-    int r_first, parts;                           // the item's first run or piece, and how many have a part of it
+// A CTA's part of an item: its tiles lo .. hi - 1, as the planner writes it into shared memory.
+struct alignas(16) Seg {
+    int b, h, hist, lo;
+    int hi, ns, skip, part;  // part: 0 or 1, the CTA's slot for its part of an item; kWhole: a whole item; kEnd: no segment
     __device__ __forceinline__ int key(int v) const { return (v < ns ? v : v + skip) * BN; }  // first slot of tile v
-    __device__ __forceinline__ bool whole() const { return lo == 0 && hi == nt; }
+};
+constexpr int kWhole = 2, kEnd = 3;
+
+// An item that several CTAs have a part of: those of runs first .. first + count - 1 (of the item's group), in their slot 0, but
+// for the first one's part in slot `slot0`.
+struct alignas(16) Shared {
+    int b, h, first, count;
+    int slot0, has;
 };
 
-// What a CTA takes.  len > 0: the tiles pos .. end - 1 of all items in order, one of the runs of len tiles.  len = 0: the
-// piece pos, the only one, of an item that is cut into pieces of at most `target` tiles.
-struct Run {
-    int pos, end, len, target, id;
-    // The CTA's slot for its part of an item: 0 where the item began by the run's start, 1 where it began in it.
-    __device__ __forceinline__ int slot(const Seg& s, int r) const { return len == 0 || s.first <= r * len ? 0 : 1; }
-};
+// What the planner, a converged warp, knows.  Lane l has sequences 4 l .. 4 l + 3: their lengths, and `upto`, the places (pieces)
+// of the items up to and with theirs.  len > 0: the CTA takes places pos .. end - 1, one of the runs of len places, in the line
+// of all items in order, each kHead places and then its tiles.  len = 0: it takes piece pos, if there is one, of items that
+// are cut into pieces of at most `target` tiles.
+struct Plan {
+    int hist[kPer], upto[kPer];
+    int pos, end, len, target;
 
-// The run's next segment, a converged warp; false: none is left.  pre: tiles (pieces) of the items of sequences .. b.
-__device__ __forceinline__ bool next_seg(Run& r, const Args& a, const int* pre, const int* hist_s, int lane, Seg& s) {
-    if (r.pos >= r.end) return false;
-    int before = 0;
+    // The lengths' places, summed, and this CTA's: of `runs`, the run run_id.
+    __device__ __forceinline__ void init(const Args& a, int runs, int run_id, int lane, bool report) {
+        int t[kPer], tiles = 0, places = 0;
+        bool bad = false;
 #pragma unroll
-    for (int i = 0; i < kMaxSeqs / 32; ++i) before += 32 * i + lane < a.batch && pre[32 * i + lane] <= r.pos;
-    s.b = __reduce_add_sync(0xFFFFFFFFu, before);
-    const int start = s.b > 0 ? pre[s.b - 1] : 0;
-    s.hist = hist_s[s.b];
-    const Span p = span_of(s.hist, a);
-    s.ns = p.ns;
-    s.skip = p.skip;
-    s.nt = p.nt;
-    if (r.len == 0) {
-        s.parts = (p.nt + r.target - 1) / r.target;
-        s.h = (r.pos - start) / s.parts;
-        s.r_first = start + s.h * s.parts;
-        const int i = r.pos - s.r_first;
-        s.first = 0;
-        s.lo = p.nt * i / s.parts;
-        s.hi = p.nt * (i + 1) / s.parts;
-        r.pos = r.end;
-    } else {
-        s.h = (r.pos - start) / p.nt;
-        s.first = start + s.h * p.nt;
-        s.lo = r.pos - s.first;
-        s.hi = min(p.nt, r.end - s.first);
-        s.r_first = s.first / r.len;
-        s.parts = (s.first + p.nt - 1) / r.len - s.r_first + 1;
-        r.pos = s.first + s.hi;
+        for (int i = 0; i < kPer; ++i) hist[i] = kPer * lane + i < a.batch ? __ldg(a.d_hist + a.b0 + kPer * lane + i) : 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const bool here = kPer * lane + i < a.batch, good = hist[i] >= 0 && hist[i] <= a.max_len;
+            bad |= !good;
+            t[i] = here && good ? span_of(hist[i], a.n, a.window, a.sinks).nt : 0;
+            tiles += t[i] * a.Hkv;
+            places += t[i] > 0 ? (t[i] + kHead) * a.Hkv : 0;
+        }
+        if (bad && report) atomicOr(a.err, kDevErrHistRange);
+        // Pieces, if there are CTAs for all and they are hardly longer than the runs would be: a CTA then has but one segment.
+        const int least = max((__reduce_add_sync(0xFFFFFFFFu, tiles) + runs - 1) / runs, 1);
+        target = least;
+        len = 0;
+#pragma unroll 1
+        for (;; target += max(target >> 5, 1)) {
+            if (target > least + kLonger) {
+                len = max((__reduce_add_sync(0xFFFFFFFFu, places) + runs - 1) / runs, 1);
+                break;
+            }
+            int pieces = 0;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) pieces += (t[i] + target - 1) / target * a.Hkv;
+            if (__reduce_add_sync(0xFFFFFFFFu, pieces) <= runs) break;
+        }
+        int sum = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            sum += (len == 0 ? (t[i] + target - 1) / target : t[i] > 0 ? t[i] + kHead : 0) * a.Hkv;
+            upto[i] = sum;
+        }
+        int all = sum;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int u = __shfl_up_sync(0xFFFFFFFFu, all, d);
+            if (lane >= d) all += u;
+        }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) upto[i] += all - sum;
+        all = __shfl_sync(0xFFFFFFFFu, all, 31);
+        pos = min(run_id * max(len, 1), all);
+        end = min(pos + max(len, 1), all);
     }
-    return true;
+
+    // The CTA's next segment; false: none is left.  sh: where it is a part, the item's.
+    __device__ __forceinline__ bool next(const Args& a, int run_id, Seg& s, Shared& sh) {
+        if (pos >= end) return false;
+        int before = 0, start = 0, h = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (upto[i] <= pos) {
+                ++before;
+                start = upto[i];
+            }
+        s.b = __reduce_add_sync(0xFFFFFFFFu, before);
+        start = __reduce_max_sync(0xFFFFFFFFu, start);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (s.b % kPer == i) h = hist[i];
+        s.hist = __shfl_sync(0xFFFFFFFFu, h, s.b / kPer);
+        const Span p = span_of(s.hist, a.n, a.window, a.sinks);
+        s.ns = p.ns;
+        s.skip = p.skip;
+        const int per = len == 0 ? (p.nt + target - 1) / target : p.nt + kHead;  // pieces or places of an item
+        s.h = (pos - start) / per;
+        start += s.h * per;
+        sh.b = s.b;
+        sh.h = s.h;
+        sh.has = 1;
+        sh.slot0 = s.part = 0;
+        if (len == 0) {
+            const int i = pos - start;
+            s.lo = p.nt * i / per;
+            s.hi = p.nt * (i + 1) / per;
+            sh.first = start;
+            sh.count = per;
+            pos = end;
+        } else {
+            const int first = start + kHead;  // tile 0's place
+            s.lo = max(pos - first, 0);
+            s.hi = min(p.nt, end - first);
+            if (s.hi <= 0) return false;  // (the run ends before the item's tiles)
+            // Slot 0 where the item began by the run's start, 1 where it began in it.
+            sh.first = first / len;
+            sh.count = (first + p.nt - 1) / len - sh.first + 1;
+            sh.slot0 = first > sh.first * len ? 1 : 0;
+            s.part = run_id == sh.first ? sh.slot0 : 0;
+            pos = first + s.hi;
+        }
+        if (s.lo == 0 && s.hi == p.nt) s.part = kWhole;
+        return true;
+    }
+};
+
+// The kin of a sequence's tokens (tree.cuh), a converged warp.  A sequence that is skipped has none: its keys are walked like any
+// other's, and nothing is written.  err: where that is reported, or NULL.
+struct Kin {
+    uint64_t k[2];
+};
+__device__ __forceinline__ Kin kin_seq(const int32_t* parents, int n, int hist, int max_len, int* err) {
+    const int lane = threadIdx.x & 31;
+    Kin x;
+    const int count = tree_kin(parents, n, lane, x.k);
+    const bool range = count > 0 && hist + count > max_len;
+    if (count < 0 || range) {
+        x.k[0] = x.k[1] = 0;
+        if (err != nullptr && lane == 0) atomicOr(err, count < 0 ? kDevErrTree : kDevErrHistRange);
+    }
+    return x;
+}
+__device__ __forceinline__ void kin_seg(const Seg& s, const Args& a, uint64_t (&kin)[2], bool report) {
+    const int32_t* parents = a.parents == nullptr ? nullptr : a.parents + static_cast<size_t>(a.b0 + s.b) * a.n;
+    const Kin x = kin_seq(parents, a.n, s.hist, a.max_len, report ? a.err : nullptr);
+    kin[0] = x.k[0];
+    kin[1] = x.k[1];
 }
 
-// The kin of a segment's tokens (tree.cuh), a converged warp.  A sequence that is skipped has none: its keys are walked like any
-// other's, and nothing is written.
-__device__ __forceinline__ void kin_seg(const Seg& s, const Args& a, int lane, uint64_t (&kin)[2], bool report) {
-    const int32_t* parents = a.parents == nullptr ? nullptr : a.parents + static_cast<size_t>(a.b0 + s.b) * a.n;
-    const int count = tree_kin(parents, a.n, lane, kin);
-    const bool range = count > 0 && s.hist + count > a.max_len;
-    if (count < 0 || range) {
-        kin[0] = kin[1] = 0;
-        if (report && lane == 0) atomicOr(a.err, count < 0 ? kDevErrTree : kDevErrHistRange);
+// The depth of a token (-1: there is none), by a converged warp; own: the depths of tokens `lane` and `lane` + 32.
+__device__ __forceinline__ int depth_of(const int (&own)[2], int token) {
+    const int d0 = __shfl_sync(0xFFFFFFFFu, own[0], token & 31), d1 = __shfl_sync(0xFFFFFFFFu, own[1], token & 31);
+    return token < 32 ? d0 : d1;
+}
+
+// mbar_wait in fewer instructions: there are many of them in the kernel, and what is run for the first time comes from L2.
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, const volatile int* abort, uint64_t limit_ns) {
+    if (limit_ns < kMinBlockingWaitNs) return mbar_test(bar, parity);
+#pragma unroll 1
+    for (uint64_t until = 0;;) {
+        if (mbar_try_wait(bar, parity)) return true;
+        const uint64_t now = globaltimer_ns();
+        if (until == 0)
+            until = now + limit_ns;
+        else if (now > until || *abort)
+            return false;
     }
 }
 
 // Whether some row may not see some slot of the key tile from slot kb on (the same answer in every warp).
-__device__ __forceinline__ bool masked(int kb, int hist, const Args& a) {
-    return kb + BN > hist || (kb <= hist + a.n - 1 - a.window && kb + BN > a.sinks);
+__device__ __forceinline__ bool masked(int kb, int hist, int n, int window, int sinks) {
+    return kb + BN > hist || (kb <= hist + n - 1 - window && kb + BN > sinks);
 }
 
 // What a row sees: slots [lo, hist) and [0, first), and the new ones whose bit is set.
@@ -248,16 +358,19 @@ __device__ __forceinline__ void rotate8(const uint4& xa, const uint4& xb, const 
     yb = make_uint4(vb[0], vb[1], vb[2], vb[3]);
 }
 
-// Eight pairs of a row with their cosines and sines, loaded ahead of their use.
+// Eight pairs of a row, and their cosines and sines, loaded ahead of their use.
 template <int D>
 struct Eight {
     uint4 xa, xb;
-    float4 c[2], s[2];
     __device__ __forceinline__ void load(const uint16_t* row, int jb) {
         xa = __ldg(reinterpret_cast<const uint4*>(row + jb));
         xb = __ldg(reinterpret_cast<const uint4*>(row + jb + D / 2));
     }
-    __device__ __forceinline__ void angles(int jb, int pos, const Args& a) {
+};
+template <int D>
+struct Angles {
+    float4 c[2], s[2];
+    __device__ __forceinline__ void load(int jb, int pos, const Args& a) {
         const float4* cp = reinterpret_cast<const float4*>(a.cos_tab + static_cast<size_t>(pos) * (D / 2) + jb);
         const float4* sp = reinterpret_cast<const float4*>(a.sin_tab + static_cast<size_t>(pos) * (D / 2) + jb);
         c[0] = __ldg(cp);
@@ -272,69 +385,81 @@ __device__ __forceinline__ uint64_t kin_of(const uint64_t (&kin)[2], int token) 
     return token < 32 ? k0 : k1;
 }
 
-// One warp's 32 rows (from row r0 of the sequence's (token, head) rows on) of q, rotated, into rows `at` .. of a Q tile, and
-// the kin of the segment's tokens.  Rows past the last, and of no token, are left: their scores go nowhere.  `empty` waits until the
-// tile may be written, after the first loads.
-template <int D, typename F>
-__device__ __forceinline__ void stage_q(uint8_t* tile, int at, int r0, const Seg& s, uint64_t (&kin)[2], int lane, const Args& a,
-                                        F&& empty) {
-    constexpr int U = D / 16, BATCH = 4;  // units of a row
-    const int rows = min(32, a.n * a.G - r0);
-    const int mine = min(max(r0 + lane, 0), a.n * a.G - 1) / a.G;
-    int depth = 0;
-    for (int i0 = 0; i0 == 0 || i0 * (32 / U) < rows; i0 += BATCH) {
-        Eight<D> x[BATCH];
-        int row[BATCH];
+__device__ __forceinline__ void copy16(uint32_t smem, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(from) : "memory");
+}
+
+// `rows` rows of q (from row r0 of the sequence's (token, head) rows on; 32 W at most), rotated, into rows `at` .. of a Q tile,
+// and the kin of the segment's tokens, by W warps (`me`: this thread among them).  Rows of no token are not rotated: their scores
+// go nowhere.  All rows are on their way while the kin are found, so that only the angles are waited for after that.
+template <int D, int W>
+__device__ __forceinline__ void stage_q(uint32_t tile_addr, uint8_t* tile, int at, int r0, int rows, const Seg& s, uint64_t (&kin)[2],
+                                        int me, const Args& a) {
+    constexpr int U = D / 16, BATCH = 2;  // pairs of 16-byte units of a row; a thread has as many
+    const int jb = me % U * 8;
+    auto row_of = [&](int i) { return (i * 32 * W + me) / U; };
+#pragma unroll 1
+    for (int i = 0; i < U; ++i) {
+        const int row = row_of(i);
+        if (row >= rows) break;
+        const int token = (r0 + row) / a.G;
+        const uint16_t* from = a.q + ((static_cast<size_t>(a.b0 + s.b) * a.n + token) * a.Hq + s.h * a.G + (r0 + row - token * a.G)) * D + jb;
+        copy16(tile_addr + sw128_offset(at + row, jb), from);
+        copy16(tile_addr + sw128_offset(at + row, jb + D / 2), from + D / 2);
+    }
+    kin_seg(s, a, kin, false);
+    const int depth[2] = {__popcll(kin[0]) - 1, __popcll(kin[1]) - 1};
+#pragma unroll 1
+    for (int i0 = 0; i0 * 32 * W / U < rows; i0 += BATCH) {
+        Angles<D> turn[BATCH];
+        bool live[BATCH];
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
-            const int u = (i0 + i) * 32 + lane;
-            row[i] = u / U;
-            const int token = __shfl_sync(0xFFFFFFFFu, mine, row[i] & 31);
-            if (row[i] >= rows)
-                row[i] = -1;
-            else
-                x[i].load(a.q + ((static_cast<size_t>(a.b0 + s.b) * a.n + token) * a.Hq + s.h * a.G + (r0 + row[i] - token * a.G)) * D,
-                          u % U * 8);
+            const int row = row_of(i0 + i);
+            const int d = depth_of(depth, min(r0 + row, a.n * a.G - 1) / a.G);
+            live[i] = row < rows && d >= 0;
+            if (live[i]) turn[i].load(jb, s.hist + d, a);
         }
-        if (i0 == 0) {
-            kin_seg(s, a, lane, kin, false);
-            const uint64_t k = kin_of(kin, mine);
-            depth = k == 0 ? -1 : __popcll(k) - 1;
-        }
-#pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-            const int d = __shfl_sync(0xFFFFFFFFu, depth, max(row[i], 0) & 31);
-            if (d < 0) row[i] = -1;
-            if (row[i] >= 0) x[i].angles(((i0 + i) * 32 + lane) % U * 8, s.hist + d, a);
-        }
-        if (i0 == 0 && !empty()) return;
+        if (i0 == 0) asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll
         for (int i = 0; i < BATCH; ++i)
-            if (row[i] >= 0) {
-                const int jb = ((i0 + i) * 32 + lane) % U * 8;
-                rotate8(x[i].xa, x[i].xb, x[i].c, x[i].s, *reinterpret_cast<uint4*>(tile + sw128_offset(at + row[i], jb)),
-                        *reinterpret_cast<uint4*>(tile + sw128_offset(at + row[i], jb + D / 2)));
+            if (live[i]) {
+                uint4* xa = reinterpret_cast<uint4*>(tile + sw128_offset(at + row_of(i0 + i), jb));
+                uint4* xb = reinterpret_cast<uint4*>(tile + sw128_offset(at + row_of(i0 + i), jb + D / 2));
+                rotate8(*xa, *xb, turn[i].c, turn[i].s, *xa, *xb);
             }
     }
 }
 
-// Add to o (columns c0 .. c0 + 31 of a row's O) the values that are not finite of the slots that the row sees in the masked tiles.
+// Add to a row's O (in TMEM) the values that are not finite of the slots that the row sees in the masked tiles lo .. hi - 1: a
+// whole warp, a thread per row.  v_head: slot 0 of the (sequence, kv head), v_tok: its v of token 0, `stride` apart.
 template <int D>
-__device__ __noinline__ void add_not_finite(float* o, int c0, const View& view, const Seg& s, const Args& a) {
-    const size_t head = (static_cast<size_t>(a.b0 + s.b) * a.Hkv + s.h) * a.max_len;
-    for (int v = s.lo; v < s.hi; ++v) {
-        const int kb = s.key(v);
-        if (!masked(kb, s.hist, a)) continue;
-        for (int c = 0; c < BN / 32; ++c)
-            for (uint32_t w = view.word(kb + 32 * c); w != 0; w &= w - 1) {
-                const int slot = kb + 32 * c + __ffs(w) - 1;
-                const uint16_t* row = slot < s.hist ? a.v_cache + (head + slot) * D
-                                                    : a.v_new + ((static_cast<size_t>(a.b0 + s.b) * a.n + slot - s.hist) * a.Hkv + s.h) * D;
-                for (int e = 0; e < 32; ++e) {
-                    const float x = __uint_as_float(static_cast<uint32_t>(row[c0 + e]) << 16);
-                    if (!isfinite(x)) o[e] += x;
+__device__ __noinline__ void add_not_finite(uint32_t o_col, View view, int lo, int hi, int ns, int skip, int n, int window, int sinks,
+                                            const uint16_t* v_head, const uint16_t* v_tok, int stride) {
+    const int hist = view.hist;
+#pragma unroll 1
+    for (int c0 = 0; c0 < D; c0 += 32) {
+        uint32_t o[32];
+        tmem_ld32(o_col + c0, o);
+        tmem_wait_ld();
+        for (int v = lo; v < hi; ++v) {
+            const int kb = (v < ns ? v : v + skip) * BN;
+            if (!masked(kb, hist, n, window, sinks)) continue;
+            for (int c = 0; c < BN / 32; ++c)
+                for (uint32_t w = view.word(kb + 32 * c); w != 0; w &= w - 1) {
+                    const int slot = kb + 32 * c + __ffs(w) - 1;
+                    const uint16_t* row =
+                        (slot < hist ? v_head + static_cast<size_t>(slot) * D : v_tok + static_cast<size_t>(slot - hist) * stride) + c0;
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const float x = __uint_as_float(static_cast<uint32_t>(row[e]) << 16);
+                        if (!isfinite(x)) o[e] = __float_as_uint(__uint_as_float(o[e]) + x);
+                    }
                 }
-            }
+        }
+        __syncwarp();
+        tmem_st32(o_col + c0, o);
+        tmem_wait_st();
     }
 }
 
@@ -352,16 +477,20 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
     uint8_t* gbase = smem_raw + (base - raw);
-    int* pre = reinterpret_cast<int*>(gbase + C::OFF_PRE);
-    int* hist_s = reinterpret_cast<int*>(gbase + C::OFF_HIST);
-    int* cut = reinterpret_cast<int*>(gbase + C::OFF_CUT);
+    Seg* seg_s = reinterpret_cast<Seg*>(gbase + C::OFF_SEG);
+    Shared* shared_s = reinterpret_cast<Shared*>(gbase + C::OFF_SHARED);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(gbase + C::OFF_ABORT);
     volatile int* odd_flag = reinterpret_cast<volatile int*>(gbase + C::OFF_FLAG);
     auto bar = [&](int i) -> uint32_t { return base + C::OFF_BAR + 8u * static_cast<uint32_t>(i); };
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int kWarpTma = C::SOFT, kWarpMma = C::SOFT + 1, kWarpGuard = C::SOFT + 2;
-    const int group = static_cast<int>(blockIdx.x) % a.groups, run_id = static_cast<int>(blockIdx.x) / a.groups;
+    constexpr int kWarpTma = C::SOFT, kWarpMma = C::SOFT + 1, kWarpGuard = C::SOFT + 2, kWarpStage = C::SOFT + 4;
+    volatile uint64_t* kin_s = reinterpret_cast<volatile uint64_t*>(gbase + C::OFF_KIN);
+    // the groups with two tiles of rows take turns, the last group comes behind them
+    const int cta = static_cast<int>(blockIdx.x), full = a.groups - 1;
+    const bool in_last = cta >= full * a.runs;
+    const int group = in_last ? full : cta % full, run_id = in_last ? cta - full * a.runs : cta / full;
+    const int runs = in_last ? a.runs_last : a.runs;
     const int group_rows = min(C::ROWS, a.n * a.G - group * C::ROWS);
     const int live = NT == 1 || group_rows <= BM ? 1 : 2;  // tiles with rows
 
@@ -374,7 +503,7 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
             mbar_init(bar(C::B_EMPTY + i), 1);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(C::B_QREADY + i), 4 * live);
+            mbar_init(bar(C::B_QREADY + i), 4 * live);  // (NT = 1: the stagers)
             mbar_init(bar(C::B_QEMPTY + i), 1);
             mbar_init(bar(C::B_SFULL + i), 1);
             mbar_init(bar(C::B_PFULL + i), 4);
@@ -383,76 +512,62 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
         }
         mbar_init(bar(C::B_PVDONE), 1);
         mbar_init(bar(C::B_DRAIN), 1);
+        mbar_init(bar(C::B_KINREAD), 4);
+        mbar_init(bar(C::B_PLANNED), 1);
+        for (int i = 0; i < kSegs; ++i) mbar_init(bar(C::B_SEG + i), 1);
+        shared_s[0].has = shared_s[1].has = 0;
         fence_mbar_init();
         tma_prefetch_desc(&map_k);
         tma_prefetch_desc(&map_v);
     }
     // parents on their way while the lengths are
-    if (a.parents != nullptr && warp >= kWarpGuard)
+    if (a.parents != nullptr && warp >= kWarpGuard && warp < kWarpGuard + 2)
         for (int i = (warp - kWarpGuard) * 32 + lane; i * 32 < a.batch * a.n; i += 64)
             asm volatile("prefetch.global.L1 [%0];" ::"l"(a.parents + static_cast<size_t>(a.b0) * a.n + 32 * i));
     if (warp == kWarpMma) {
         tmem_alloc(base + C::OFF_TMEM, kTmemCols);
         tmem_relinquish();
     }
-    if (warp == 0) {  // the tiles of the sequences, summed: lane l has sequences 4 l .. 4 l + 3
-        constexpr int PER = kMaxSeqs / 32;
-        int h[PER], t[PER];
-#pragma unroll
-        for (int i = 0; i < PER; ++i) h[i] = PER * lane + i < a.batch ? __ldg(a.d_hist + a.b0 + PER * lane + i) : 0;
-        bool bad = false;
-        int sum = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const bool here = PER * lane + i < a.batch, good = h[i] >= 0 && h[i] <= a.max_len;
-            bad |= !good;
-            t[i] = here && good ? span_of(h[i], a).nt : 0;
-            sum += t[i] * a.Hkv;
-            hist_s[PER * lane + i] = h[i];
+    // What the segments start with, on its way into L2 before the keys are: this CTA's share of q, of the new k and v, and of the
+    // angles of the new positions.
+    {
+        auto prefetch = [](const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); };
+        const size_t lines = static_cast<size_t>(a.batch) * a.n * a.Hkv * (D / 64), first = static_cast<size_t>(a.b0) * a.n * a.Hkv * D;
+        const size_t at = static_cast<size_t>(blockIdx.x) * C::THREADS + threadIdx.x, step = static_cast<size_t>(gridDim.x) * C::THREADS;
+#pragma unroll 1
+        for (size_t i = at; i < lines * a.G; i += step) prefetch(a.q + first * a.G + 64 * i);
+#pragma unroll 1
+        for (size_t i = at; i < lines; i += step) {
+            prefetch(a.k_new + first + 64 * i);
+            prefetch(a.v_new + first + 64 * i);
         }
-        const int total = __reduce_add_sync(0xFFFFFFFFu, sum);
-        // Pieces, if there are CTAs for all and they are hardly longer than the runs would be: a CTA then has but one segment.
-        const int len = max((total + a.runs - 1) / a.runs, 1);
-        int target = len;
-        for (; target <= len + kLonger; target += max(target >> 5, 1)) {
-            int pieces = 0;
+        if (warp == 1)
+#pragma unroll 1
+            for (int p = static_cast<int>(blockIdx.x + gridDim.x * lane); p < a.batch * a.n; p += static_cast<int>(gridDim.x) * 32) {
+                const int pos = __ldg(a.d_hist + a.b0 + p / a.n) + p % a.n;
+                if (pos < 0 || pos >= a.max_len) continue;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) pieces += (t[i] + target - 1) / target * a.Hkv;
-            if (__reduce_add_sync(0xFFFFFFFFu, pieces) <= a.runs) break;
-        }
-        const bool in_pieces = target <= len + kLonger;
-        sum = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            sum += (in_pieces ? (t[i] + target - 1) / target : t[i]) * a.Hkv;
-            t[i] = sum;
-        }
-        int upto = sum;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int u = __shfl_up_sync(0xFFFFFFFFu, upto, d);
-            if (lane >= d) upto += u;
-        }
-#pragma unroll
-        for (int i = 0; i < PER; ++i) pre[PER * lane + i] = upto - sum + t[i];
-        if (lane == 0) {
-            cut[0] = in_pieces ? 0 : len;
-            cut[1] = target;
-        }
-        if (bad && blockIdx.x == 0) atomicOr(a.err, kDevErrHistRange);
+                for (int i = 0; i < D / 64; ++i) {
+                    prefetch(a.cos_tab + static_cast<size_t>(pos) * (D / 2) + 32 * i);
+                    prefetch(a.sin_tab + static_cast<size_t>(pos) * (D / 2) + 32 * i);
+                }
+            }
     }
+    Plan plan;
+    if (warp == kWarpTma) plan.init(a, runs, run_id, lane, cta == 0);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *reinterpret_cast<const uint32_t*>(gbase + C::OFF_TMEM);
 
-    Run run;
-    run.id = run_id;
-    run.len = cut[0];
-    run.target = cut[1];
-    run.pos = min(run_id * max(run.len, 1), pre[kMaxSeqs - 1]);
-    run.end = min(run.pos + max(run.len, 1), pre[kMaxSeqs - 1]);
-    const Run run0 = run;
+    auto wait = [&](uint32_t b, uint32_t parity) { return wait_for(b, parity, abort_flag, a.wait_ns); };
+    // The CTA's i-th segment; false: there is none, or the wait ran out (ok = false).
+    bool ok = true;
+    auto take = [&](uint32_t i, Seg& to) {
+        ok = __all_sync(0xFFFFFFFFu, wait(bar(C::B_SEG + i % kSegs), (i / kSegs) & 1u));
+        if (ok) to = seg_s[i % kSegs];
+        return ok && to.part != kEnd;
+    };
     Seg s;
     uint64_t kin[2];
     // The ring's order of a segment of n tiles: K0, K1, V0, K2, V1, .., V(n - 1); where K(j) and V(j) are in it.
@@ -463,19 +578,30 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
         is_v = i == 2 * n - 1 || (i > 0 && i % 2 == 0);
         return i == 2 * n - 1 ? n - 1 : is_v ? i / 2 - 1 : (i + 1) / 2;
     };
-    bool ok = true;
 
     if (warp >= C::SOFT) {
-        if constexpr (NT == 2) warpgroup_reg_dec<kRegsLow>();
+        warpgroup_reg_dec<C::REGS_LOW>();
         if (warp == kWarpTma) {
             // ------------------------------------------------------------ producer
             uint32_t seq = 0;
-            while (ok && next_seg(run, a, pre, hist_s, lane, s)) {
+            Shared sh;
+            for (uint32_t segs = 0;; ++segs) {
+                const bool some = plan.next(a, run_id, s, sh);
+                if (lane == 0) {
+                    if (!some) s.part = kEnd;
+                    if (some && s.part != kWhole) shared_s[s.part] = sh;
+                    if (ok) {  // (after a wait that ran out: the items it shares alone)
+                        seg_s[segs % kSegs] = s;
+                        mbar_arrive(bar(C::B_SEG + segs % kSegs));
+                    }
+                }
+                if (!some) break;
+                if (!ok) continue;
                 if (lane == 0) {
                     const int n = s.hi - s.lo, head = (a.b0 + s.b) * a.Hkv + s.h;
                     for (int i = 0; i < 2 * n; ++i, ++seq) {
                         const uint32_t st = seq % C::NS;
-                        if (seq >= C::NS && !mbar_wait(bar(C::B_EMPTY + st), (seq / C::NS - 1u) & 1u, abort_flag, a.wait_ns)) {
+                        if (seq >= C::NS && !wait(bar(C::B_EMPTY + st), (seq / C::NS - 1u) & 1u)) {
                             ok = false;
                             break;
                         }
@@ -494,6 +620,7 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                 }
                 ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
             }
+            if (lane == 0) mbar_arrive(bar(C::B_PLANNED));
             if (lane == 0)  // every copy issued must land before the CTA may exit
                 for (uint32_t i = seq >= C::NS ? seq - C::NS : 0; i < seq; ++i)
                     mbar_wait(bar(C::B_FULL + i % C::NS), (i / C::NS) & 1u, nullptr);
@@ -523,13 +650,13 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                               (!first || kk > 0) ? 1u : 0u);
             };
             auto ready = [&](uint32_t at) {
-                return mbar_wait(bar(C::B_READY + at % C::NS), (at / C::NS) & 1u, abort_flag, a.wait_ns);
+                return wait(bar(C::B_READY + at % C::NS), (at / C::NS) & 1u);
             };
-            while (ok && next_seg(run, a, pre, hist_s, lane, s)) {
+            while (ok && take(segs, s)) {
                 if (lane == 0) {
                     const int n = s.hi - s.lo;
                     const uint32_t qb = NT == 1 ? segs & 1u : 0u;
-                    ok = mbar_wait(bar(C::B_QREADY + qb), (NT == 1 ? segs >> 1 : segs) & 1u, abort_flag, a.wait_ns);
+                    ok = wait(bar(C::B_QREADY + qb), (NT == 1 ? segs >> 1 : segs) & 1u);
                     for (int j = 0; j <= n && ok; ++j) {
                         if constexpr (NT == 1) {
                             if (j < n) {
@@ -542,9 +669,9 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                             }
                             if (j > 0) {
                                 const uint32_t t = tiles + j - 1, at = seq + v_at(j - 1, n);
-                                ok = mbar_wait(bar(C::B_PFULL + (t & 1u)), (t >> 1) & 1u, abort_flag, a.wait_ns) && ready(at) &&
+                                ok = wait(bar(C::B_PFULL + (t & 1u)), (t >> 1) & 1u) && ready(at) &&
                                      (j > 1 || segs < 2 ||
-                                      mbar_wait(bar(C::B_OEMPTY + qb), ((segs >> 1) - 1u) & 1u, abort_flag, a.wait_ns));
+                                      wait(bar(C::B_OEMPTY + qb), ((segs >> 1) - 1u) & 1u));
                                 if (!ok) break;
                                 tc_fence_after();
                                 issue_pv(t & 1u, qb, j == 1, at % C::NS);
@@ -558,8 +685,8 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                             tc_fence_after();
                             for (int t = 0; t < live; ++t) {
                                 if (j > 0) {
-                                    ok = mbar_wait(bar(C::B_PFULL + t), (tiles + j - 1) & 1u, abort_flag, a.wait_ns) &&
-                                         (j > 1 || segs == 0 || mbar_wait(bar(C::B_OEMPTY + t), (segs - 1u) & 1u, abort_flag, a.wait_ns));
+                                    ok = wait(bar(C::B_PFULL + t), (tiles + j - 1) & 1u) &&
+                                         (j > 1 || segs == 0 || wait(bar(C::B_OEMPTY + t), (segs - 1u) & 1u));
                                     if (!ok) break;
                                     tc_fence_after();
                                     issue_pv(t, t, j == 1, va % C::NS);
@@ -583,13 +710,37 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                     }
                     tiles += n;
                     seq += 2 * n;
-                    ++segs;
                 }
+                ++segs;
                 ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
             }
             if (lane == 0) {  // all tensor-core work must finish before TMEM is released
                 umma_commit(bar(C::B_DRAIN));
                 mbar_wait(bar(C::B_DRAIN), 0, nullptr);
+            }
+        } else if (NT == 1 && warp >= kWarpStage) {
+            // ------------------------------------------------------------ stagers
+            const int me = (warp - kWarpStage) * 32 + lane, rows = min(a.n * a.G, BM);
+            uint32_t segs = 0;
+            auto wait_all = [&](int b, uint32_t parity) { return ok = __all_sync(0xFFFFFFFFu, wait(bar(b), parity)); };
+            while (take(segs, s)) {
+                const uint32_t qb = segs & 1u;
+                if (segs >= 2 && !wait_all(C::B_QEMPTY + qb, ((segs >> 1) - 1u) & 1u)) break;
+                stage_q<D, 4>(base + C::OFF_Q + qb * C::TILE, gbase + C::OFF_Q + qb * C::TILE, 0, 0, rows, s, kin, me, a);
+                // the kin of the segment before are in the softmax warps' registers
+                if (segs >= 1 && !wait_all(C::B_KINREAD, (segs - 1u) & 1u)) break;
+                if (warp == kWarpStage) {
+                    kin_s[lane] = kin[0];
+                    kin_s[lane + 32] = kin[1];
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(C::B_QREADY + qb));
+                ++segs;
+            }
+            if (!ok && lane == 0) {
+                *abort_flag = 1;
+                atomicOr(a.err, kDevErrTimeout);
             }
         } else {
             // ------------------------------------------------------------ guards
@@ -597,8 +748,9 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
             const int gw = warp - kWarpGuard, me = gw * 32 + lane;
             auto rows_below = [&](int row) { return row / 8 * 4 + min(max(row % 8 - 4 * gw, 0), 4); };  // of this guard's
             uint32_t seq = 0, segs = 0;
-            while (ok && next_seg(run, a, pre, hist_s, lane, s)) {
-                kin_seg(s, a, lane, kin, group == 0 && warp == kWarpGuard);
+            while (ok && take(segs, s)) {
+                kin_seg(s, a, kin, group == 0 && warp == kWarpGuard);
+                const int depth[2] = {__popcll(kin[0]) - 1, __popcll(kin[1]) - 1};
                 const int n = s.hi - s.lo;
                 const size_t head = (static_cast<size_t>(a.b0 + s.b) * a.Hkv + s.h) * a.max_len + s.hist;  // slot of token 0
                 for (int i = 0; i < 2 * n && ok; ++i, ++seq) {
@@ -606,11 +758,11 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                     bool is_v;
                     const int kb = s.key(s.lo + tile_at(i, n, is_v));
                     uint8_t* tile = gbase + C::OFF_RING + st * C::TILE;
-                    const bool mixed = masked(kb, s.hist, a);
+                    const bool mixed = masked(kb, s.hist, a.n, a.window, a.sinks);
                     const int t0 = max(kb - s.hist, 0), t1 = min(kb + BN - s.hist, a.n);  // new tokens of this tile
                     bool there = false;  // the tile has landed
                     auto landed = [&]() {
-                        if (!there) ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(C::B_FULL + st), (seq / C::NS) & 1u, abort_flag, a.wait_ns));
+                        if (!there) ok = __all_sync(0xFFFFFFFFu, wait(bar(C::B_FULL + st), (seq / C::NS) & 1u));
                         there = true;
                     };
                     if (t1 > t0) {
@@ -618,13 +770,14 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                         const int at0 = s.hist - kb, i0 = rows_below(at0 + t0), units = (rows_below(at0 + t1) - i0) * U;
                         for (int u0 = 0; u0 < units && ok; u0 += 32 * BATCH) {
                             Eight<D> x[BATCH];
+                            Angles<D> turn[BATCH];
                             int token[BATCH];
 #pragma unroll
                             for (int e = 0; e < BATCH; ++e) {
                                 const int u = u0 + 32 * e + lane, i_row = i0 + u / U;
                                 const int t = min(max(i_row / 4 * 8 + 4 * gw + i_row % 4 - at0, 0), a.n - 1);
-                                const uint64_t k = kin_of(kin, t);
-                                token[e] = u < units && k != 0 ? t : -1;
+                                const int d = depth_of(depth, t);
+                                token[e] = u < units && d >= 0 ? t : -1;
                                 if (token[e] < 0) continue;
                                 const size_t row = ((static_cast<size_t>(a.b0 + s.b) * a.n + t) * a.Hkv + s.h) * D;
                                 if (is_v) {  // units of k are pairs of 8, of v two times 8 as well
@@ -632,7 +785,7 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                                     x[e].xb = __ldg(reinterpret_cast<const uint4*>(a.v_new + row + u % U * 8 + D / 2));
                                 } else {
                                     x[e].load(a.k_new + row, u % U * 8);
-                                    x[e].angles(u % U * 8, s.hist + __popcll(k) - 1, a);
+                                    turn[e].load(u % U * 8, s.hist + d, a);
                                 }
                             }
                             landed();
@@ -642,7 +795,7 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                                 if (token[e] < 0) continue;
                                 const int jb = (u0 + 32 * e + lane) % U * 8, row = at0 + token[e];
                                 uint4 ya = x[e].xa, yb = x[e].xb;
-                                if (!is_v) rotate8(x[e].xa, x[e].xb, x[e].c, x[e].s, ya, yb);
+                                if (!is_v) rotate8(x[e].xa, x[e].xb, turn[e].c, turn[e].s, ya, yb);
                                 *reinterpret_cast<uint4*>(tile + sw128_offset(row, jb)) = ya;
                                 *reinterpret_cast<uint4*>(tile + sw128_offset(row, jb + D / 2)) = yb;
                                 if (group == 0) {
@@ -695,7 +848,7 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
         __syncwarp();
     } else {
         // ------------------------------------------------------------ softmax
-        if constexpr (NT == 2) warpgroup_reg_inc<kRegsHigh>();
+        warpgroup_reg_inc<C::REGS_HIGH>();
         const int t = warp >> 2;  // row tile
         const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
         const int r0 = group * C::ROWS + warp * 32;  // the warp's first row
@@ -707,34 +860,39 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
             uint32_t tiles = 0, segs = 0;
             Seg nx;
             uint64_t nkin[2];
-            Run ahead = run;
-            auto stage = [&](uint32_t seg) {  // q and kin of segment nx
-                const uint32_t qb = NT == 1 ? seg & 1u : 0u, use = NT == 1 ? seg >> 1 : seg;
-                stage_q<D>(gbase + C::OFF_Q + (NT == 1 ? qb : static_cast<uint32_t>(t)) * C::TILE, (warp & 3) * 32, r0, nx, nkin, lane, a,
-                           [&]() {
-                               if (use > 0)
-                                   ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(C::B_QEMPTY + qb), (use - 1u) & 1u, abort_flag, a.wait_ns));
-                               return ok;
-                           });
-                if (!ok) return;
+            auto stage = [&](uint32_t seg) {  // NT = 2: q and kin of segment nx
+                if constexpr (NT == 1) return;
+                if (seg > 0) {
+                    ok = __all_sync(0xFFFFFFFFu, wait(bar(C::B_QEMPTY), (seg - 1u) & 1u));
+                    if (!ok) return;
+                }
+                stage_q<D, 1>(base + C::OFF_Q + t * C::TILE, gbase + C::OFF_Q + t * C::TILE, (warp & 3) * 32, r0,
+                              min(32, a.n * a.G - r0), nx, nkin, lane, a);
                 fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(C::B_QREADY + qb));
+                if (lane == 0) mbar_arrive(bar(C::B_QREADY));
             };
-            bool more = next_seg(ahead, a, pre, hist_s, lane, nx);
+            bool more = take(0, nx);
             if (more) stage(0);
             while (more && ok) {
                 s = nx;
-                const uint64_t k = kin_of(nkin, token);
-                const bool write = row_on && k != 0;
-                const View view = view_of(row_on ? k : 0, s.hist, a);
+                uint64_t k = 0;
+                if constexpr (NT == 2) k = kin_of(nkin, token);
+                View view = {};
+                if constexpr (NT == 2) view = view_of(row_on ? k : 0, s.hist, a);
                 float m_run = -INFINITY, l_run = 0.f;  // the reference of P (log2 domain), the sum
                 const uint32_t ob = NT == 1 ? segs & 1u : static_cast<uint32_t>(t);
                 const uint32_t o_col = tmem + lane_base + kTmO + ob * D;
                 for (int v = s.lo; v < s.hi; ++v, ++tiles) {
                     const uint32_t sb = NT == 1 ? tiles & 1u : static_cast<uint32_t>(t);
-                    ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(C::B_SFULL + sb), (NT == 1 ? tiles >> 1 : tiles) & 1u, abort_flag, a.wait_ns));
+                    ok = __all_sync(0xFFFFFFFFu, wait(bar(C::B_SFULL + sb), (NT == 1 ? tiles >> 1 : tiles) & 1u));
                     if (!ok) break;
+                    if (NT == 1 && v == s.lo) {
+                        k = kin_s[token];
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bar(C::B_KINREAD));
+                        view = view_of(row_on ? k : 0, s.hist, a);
+                    }
                     if (rows_on) {
                         tc_fence_after();
                         const uint32_t s_col = tmem + lane_base + sb * BN;
@@ -743,7 +901,7 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                         for (int c = 0; c < BN / 32; ++c) tmem_ld32(s_col + 32 * c, r[c]);
                         tmem_wait_ld();
                         const int kb = s.key(v);
-                        if (masked(kb, s.hist, a)) {
+                        if (masked(kb, s.hist, a.n, a.window, a.sinks)) {
 #pragma unroll
                             for (int c = 0; c < BN / 32; ++c) {
                                 const uint32_t w = view.word(kb + 32 * c);
@@ -790,12 +948,12 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                         m_run = m_new;
                         // O is rescaled between two P V: with NT = 2 the last one ended before these scores
                         if (NT == 1 && tiles > 0) {
-                            ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(C::B_PVDONE), (tiles - 1u) & 1u, abort_flag, a.wait_ns));
+                            ok = __all_sync(0xFFFFFFFFu, wait(bar(C::B_PVDONE), (tiles - 1u) & 1u));
                             if (!ok) break;
                             tc_fence_after();
                         }
                         if (v > s.lo && __any_sync(0xFFFFFFFFu, move)) {
-#pragma unroll
+#pragma unroll 1
                             for (int c = 0; c < D / 32; ++c) {
                                 uint32_t o[32];
                                 tmem_ld32(o_col + 32 * c, o);
@@ -813,36 +971,29 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                 }
                 if (!ok) break;
                 // the next segment's q beside this one's last MMAs
-                more = next_seg(ahead, a, pre, hist_s, lane, nx);
+                more = take(segs + 1, nx);
                 if (more) stage(segs + 1);
                 if (!ok) break;
-                ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(C::B_OFULL + ob), (NT == 1 ? segs >> 1 : segs) & 1u, abort_flag, a.wait_ns));
+                ok = __all_sync(0xFFFFFFFFu, wait(bar(C::B_OFULL + ob), (NT == 1 ? segs >> 1 : segs) & 1u));
                 if (!ok) break;
-                const bool whole = s.whole();
-                const int slot = run0.slot(s, run_id);
+                const bool whole = s.part == kWhole, write = row_on && k != 0;
+                const int slot = s.part;
                 if (rows_on) {
                     tc_fence_after();
-                    const bool odd = odd_flag[segs % kFlags] == static_cast<int>(segs) + 1;
+                    if (odd_flag[segs % kFlags] == static_cast<int>(segs) + 1)
+                        add_not_finite<D>(o_col, view, s.lo, s.hi, s.ns, s.skip, a.n, a.window, a.sinks,
+                                          a.v_cache + (static_cast<size_t>(a.b0 + s.b) * a.Hkv + s.h) * a.max_len * D,
+                                          a.v_new + (static_cast<size_t>(a.b0 + s.b) * a.n * a.Hkv + s.h) * D, a.Hkv * D);
                     const float inv = 1.f / l_run;
                     const int head = s.h * a.G + (r0 + lane - token * a.G);
                     uint16_t* orow = a.out + ((static_cast<size_t>(a.b0 + s.b) * a.n + token) * a.Hq + head) * D;
                     float* part = a.part_o + ((static_cast<size_t>(blockIdx.x) * 2 + slot) * (D / 4) * C::ROWS + warp * 32 + lane) * 4;
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < D / 32; ++c) {
                         uint32_t o[32];
                         tmem_ld32(o_col + 32 * c, o);
                         tmem_wait_ld();
-                        float f[32];
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) f[e] = __uint_as_float(o[e]);
-                        if (write && odd) {
-                            float g[32];
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) g[e] = f[e];
-                            add_not_finite<D>(g, 32 * c, view, s, a);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) f[e] = g[e];
-                        }
+                        const float* f = reinterpret_cast<const float*>(o);
                         if (write && whole) {
 #pragma unroll
                             for (int e = 0; e < 32; e += 8)
@@ -857,9 +1008,9 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                         }
                         __syncwarp();
                     }
-                    if (write && !whole)
+                    if (row_on && !whole)  // (l < 0: a row of no token)
                         *reinterpret_cast<float2*>(a.part_ml + ((static_cast<size_t>(blockIdx.x) * 2 + slot) * C::ROWS + warp * 32 + lane) * 2) =
-                            make_float2(m_run, l_run);
+                            make_float2(m_run, write ? l_run : -1.f);
                     tc_fence_before();
                 }
                 __syncwarp();
@@ -878,11 +1029,13 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                 atomicOr(a.err, kDevErrTimeout);
             }
             // ---- the merges: of the item that began by the run's start, and of the one that goes on past its end
-            Run again = run0;
-            while (next_seg(again, a, pre, hist_s, lane, s)) {
-                if (s.whole()) continue;
-                const int slot = run0.slot(s, run_id), r_first = s.r_first, parts = s.parts;
-                int* counter = a.counters + (s.b * a.Hkv + s.h) * a.groups + group;
+            mbar_wait(bar(C::B_PLANNED), 0, nullptr);
+#pragma unroll 1
+            for (int slot = 0; slot < 2; ++slot) {
+                const Shared sh = shared_s[slot];
+                if (!sh.has) continue;
+                const int parts = sh.count;
+                int* counter = a.counters + (sh.b * a.Hkv + sh.h) * a.groups + group;
                 const int warps = 4 * live, all = parts * warps;
                 if (ok && did[slot] == 1) {
                     // (every CTA of the cooperative launch is resident, and none waits before its parts are counted)
@@ -898,73 +1051,80 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                     if (!ok && lane == 0) atomicOr(a.err, kDevErrTimeout);
                 }
                 if (ok && did[slot] == 1) {
-                    const int blocks = (group_rows + 31) / 32, share = (run_id - r_first) * warps + warp;
+                    const int blocks = (group_rows + 31) / 32, share = (run_id - sh.first) * warps + warp;
                     const int blk = share % blocks, part = share / blocks, of = (all - blk + blocks - 1) / blocks;
                     const int row = blk * 32 + lane, R = group * C::ROWS + row;
                     const int tok = min(R, a.n * a.G - 1) / a.G;
-                    kin_seg(s, a, lane, kin, false);
-                    const uint64_t k = kin_of(kin, tok);  // (by all lanes)
-                    const bool write = row < group_rows && k != 0;
-                    auto slot_of = [&](int p) {  // of part p
-                        const int r = r_first + p;
-                        return static_cast<size_t>(r * a.groups + group) * 2 + run0.slot(s, r);
-                    };
-                    if (write) {
-                        // a batch of parts is loaded at once: one after the other, each would wait for its loads
+                    // part p is in slot 0 of CTA `cta0` + p * step, the first one in slot sh.slot0 of cta0
+                    const int cta0 = in_last ? full * a.runs + sh.first : sh.first * full + group, step = in_last ? 1 : full;
+                    auto slot_of = [&](int p) { return static_cast<size_t>(2 * (cta0 + p * step) + (p == 0 ? sh.slot0 : 0)); };
+                    if (row < group_rows) {
+                        // Item i of this thread: part i % parts of values d0 + i / parts.  A batch of them is loaded at once, the first
+                        // one beside the (m, l) of all parts: one after the other, each load would be waited for.
                         constexpr int BATCH = 8;
-                        auto load_ml = [&](int p0, float2 (&ml)[BATCH]) {
-#pragma unroll
-                            for (int i = 0; i < BATCH; ++i)
-                                ml[i] = p0 + i < parts ? __ldcg(reinterpret_cast<const float2*>(a.part_ml + (slot_of(p0 + i) * C::ROWS + row) * 2))
-                                                       : make_float2(-INFINITY, 0.f);
-                        };
+                        const int d0 = D / 4 * part / of, items = (D / 4 * (part + 1) / of - d0) * parts;
+                        float4 o[BATCH];
                         float2 ml[BATCH];
-                        float m = -INFINITY, l = 0.f;
-                        for (int p0 = 0; p0 < parts; p0 += BATCH) {
-                            load_ml(p0, ml);
-                            float mn = m;
+                        float m = -INFINITY, l = 0.f, inv = 0.f;
+                        bool write = true;
+                        uint16_t* orow =
+                            a.out + ((static_cast<size_t>(a.b0 + sh.b) * a.n + tok) * a.Hq + sh.h * a.G + (R - tok * a.G)) * D + 4 * d0;
+                        float4 acc = {};
+                        int p_load = 0, p = 0;
+                        const float4* o_at = reinterpret_cast<const float4*>(a.part_o) + static_cast<size_t>(d0) * C::ROWS + row;
+                        const float2* ml_at = reinterpret_cast<const float2*>(a.part_ml) + row;
+#pragma unroll 1
+                        for (int i0 = 0; i0 < items; i0 += BATCH) {
 #pragma unroll
                             for (int i = 0; i < BATCH; ++i)
-                                if (ml[i].y != 0.f) mn = fmaxf(mn, ml[i].x);  // (0: a part without a slot that this row sees)
-                            l = l != 0.f ? l * fast_exp2(m - mn) : 0.f;
-#pragma unroll
-                            for (int i = 0; i < BATCH; ++i)
-                                if (ml[i].y != 0.f) l = fmaf(ml[i].y, fast_exp2(ml[i].x - mn), l);
-                            m = mn;
-                        }
-                        const float inv = 1.f / l;
-                        uint16_t* orow = a.out + ((static_cast<size_t>(a.b0 + s.b) * a.n + tok) * a.Hq + s.h * a.G + (R - tok * a.G)) * D;
-                        const int d_end = D / 4 * (part + 1) / of;
-                        for (int d0 = D / 4 * part / of; d0 < d_end; d0 += 2) {
-                            float4 acc[2] = {};
-                            for (int p0 = 0; p0 < parts; p0 += BATCH) {
-                                float4 o[BATCH][2];
-                                if (parts > BATCH) load_ml(p0, ml);
-#pragma unroll
-                                for (int i = 0; i < BATCH; ++i)
-#pragma unroll
-                                    for (int e = 0; e < 2; ++e)
-                                        if (p0 + i < parts && d0 + e < d_end)
-                                            o[i][e] = __ldcg(reinterpret_cast<const float4*>(
-                                                a.part_o + ((slot_of(p0 + i) * (D / 4) + d0 + e) * C::ROWS + row) * 4));
-#pragma unroll
-                                for (int i = 0; i < BATCH; ++i) {
-                                    if (ml[i].y == 0.f) continue;
-                                    const float w = fast_exp2(ml[i].x - m);
-                                    // an infinity counts whatever its weight
-                                    auto add = [&](float x, float y) { return w != 0.f ? fmaf(w, y, x) : isfinite(y) ? x : x + y; };
-#pragma unroll
-                                    for (int e = 0; e < 2; ++e)
-                                        if (d0 + e < d_end)
-                                            acc[e] = make_float4(add(acc[e].x, o[i][e].x), add(acc[e].y, o[i][e].y),
-                                                                 add(acc[e].z, o[i][e].z), add(acc[e].w, o[i][e].w));
+                                if (i0 + i < items) {
+                                    const size_t at = slot_of(p_load);
+                                    ml[i] = __ldcg(ml_at + at * C::ROWS);
+                                    o[i] = __ldcg(o_at + at * (D / 4) * C::ROWS);
+                                    if (++p_load == parts) {
+                                        p_load = 0;
+                                        o_at += C::ROWS;
+                                    }
                                 }
+                            if (i0 == 0) {
+#pragma unroll 1
+                                for (int p0 = 0; p0 < parts; p0 += 4) {
+                                    float2 x[4];
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i)
+                                        x[i] = p0 + i < parts ? __ldcg(ml_at + slot_of(p0 + i) * C::ROWS) : make_float2(-INFINITY, 0.f);
+                                    float mn = m;
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i)
+                                        if (x[i].y != 0.f) mn = fmaxf(mn, x[i].x);  // (0: a part without a slot that this row sees)
+                                    l = l != 0.f ? l * fast_exp2(m - mn) : 0.f;
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) {
+                                        write = write && !(x[i].y < 0.f);
+                                        if (x[i].y != 0.f) l = fmaf(x[i].y, fast_exp2(x[i].x - mn), l);
+                                    }
+                                    m = mn;
+                                }
+                                inv = 1.f / l;
                             }
 #pragma unroll
-                            for (int e = 0; e < 2; ++e)
-                                if (d0 + e < d_end)
-                                    *reinterpret_cast<uint2*>(orow + 4 * (d0 + e)) =
-                                        make_uint2(pack_bf16x2(acc[e].x * inv, acc[e].y * inv), pack_bf16x2(acc[e].z * inv, acc[e].w * inv));
+                            for (int i = 0; i < BATCH; ++i) {
+                                if (i0 + i >= items) break;
+                                if (ml[i].y != 0.f) {
+                                    // (an infinity counts whatever its weight: at least 2^-149)
+                                    const float w = fmaxf(fast_exp2(ml[i].x - m), __int_as_float(1));
+                                    acc = make_float4(fmaf(w, o[i].x, acc.x), fmaf(w, o[i].y, acc.y), fmaf(w, o[i].z, acc.z),
+                                                      fmaf(w, o[i].w, acc.w));
+                                }
+                                if (++p == parts) {
+                                    if (write)
+                                        *reinterpret_cast<uint2*>(orow) =
+                                            make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+                                    orow += 4;
+                                    acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                                    p = 0;
+                                }
+                            }
                         }
                     }
                     __syncwarp();
@@ -1057,7 +1217,7 @@ cudaError_t configure() {
     cudaError_t e = cudaFuncGetAttributes(&attr, tree_decode_kernel<D, NT>);
     if (e != cudaSuccess) return e;
     // (the register split is only safe when the kernel is launched with exactly kLaunchRegs)
-    if ((NT == 2 && attr.numRegs != kLaunchRegs) || attr.maxThreadsPerBlock < C::THREADS) return cudaErrorInvalidConfiguration;
+    if (attr.numRegs != kLaunchRegs || attr.maxThreadsPerBlock < C::THREADS) return cudaErrorInvalidConfiguration;
     return cudaFuncSetAttribute(tree_decode_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::ALLOC);
 }
 
@@ -1069,9 +1229,14 @@ cudaError_t launch(const Shape& s, const TreeCall& c, const Args& args, cudaStre
     // sequences of a launch: their tiles are counted in int
     const long long tiles = static_cast<long long>(s.n_kv_heads) * ((s.max_len + c.n + BN - 1) / BN);
     const int seqs = static_cast<int>(std::min<long long>(std::min(s.batch, kMaxSeqs), std::max((1LL << 30) / tiles, 1LL)));
-    a.runs = static_cast<int>(std::min<long long>(std::max(c.num_sms / a.groups, 1), seqs * tiles));
+    // A step of two tiles of rows takes about half as long again as one of a single one: the last group gets as many CTAs as
+    // that leaves it, if it has but one.
+    const int last_rows = c.n * a.G - (a.groups - 1) * C::ROWS, w = NT == 2 && last_rows <= BM ? 2 : 3;
+    const long long most = seqs * tiles;
+    a.runs_last = static_cast<int>(std::min<long long>(std::max(c.num_sms * w / (3 * (a.groups - 1) + w), 1), most));
+    a.runs = a.groups == 1 ? 0 : static_cast<int>(std::min<long long>(std::max((c.num_sms - a.runs_last) / (a.groups - 1), 1), most));
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(a.runs * a.groups));
+    cfg.gridDim = dim3(static_cast<unsigned>(a.runs * (a.groups - 1) + a.runs_last));
     cfg.blockDim = dim3(C::THREADS);
     cfg.dynamicSmemBytes = C::ALLOC;
     cfg.stream = st;
