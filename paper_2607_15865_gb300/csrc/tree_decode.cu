@@ -15,10 +15,11 @@
 //
 // Warps: 4 NT softmax warps (a tile's rows), one TMA producer, one MMA issuer, two guards and, with NT = 1, four stagers.
 //   producer  K and V tiles through a ring of slots, in the order K0, K1, V0, K2, V1, ..
-//   guards    see every tile between the producer and the issuer.  In a tile that holds slots of new tokens they put those in
-//             (k rotated), and write them to the cache; in a V tile that some row does not see whole they look for values
+//   guards    see the tiles that some row does not see whole between the producer and the issuer.  In one that holds slots of
+//             new tokens they put those in (k rotated), and write them to the cache; in one of V they look for values
 //             that are not finite: 0 x NaN would reach the rows that do not see them.  Those become 0 in shared memory, and
-//             the rows that see them add them to their O at the end (a rare path, from global memory).
+//             the rows that see them add them to their O at the end (a rare path, from global memory).  They follow the
+//             others too, and a slot of the ring is free when they and the MMAs are through with it.
 //   issuer    NT = 1: S(j + 1) before P V(j), two S buffers, so that a softmax runs beside the MMAs; Q and O have two buffers
 //             each, for the segments in turn.  NT = 2: the tiles' MMAs alternate, each has one S.
 //   stagers   rotate the q rows of the next segments into shared memory, and find their kin.  While the keys stream in, a load
@@ -70,7 +71,7 @@ struct Cfg {
     static constexpr int OFF_Q = 0;               // two Q tiles: of two segments, or of the two row tiles
     static constexpr int OFF_RING = 2 * TILE;
     static constexpr int OFF_SEG = OFF_RING + NS * TILE;         // Seg [kSegs]
-    static constexpr int OFF_SHARED = OFF_SEG + kSegs * 32;      // Shared [2]: of the parts in slots 0 and 1
+    static constexpr int OFF_SHARED = OFF_SEG + kSegs * 48;      // Shared [2]: of the parts in slots 0 and 1
     static constexpr int OFF_KIN = OFF_SHARED + 2 * 32;  // NT = 1: uint64 [64], the kin of the tokens of the segment in hand
     static constexpr int OFF_BAR = OFF_KIN + (NT == 1 ? 64 * 8 : 0);
     enum { B_FULL = 0, B_READY = NS, B_EMPTY = 2 * NS, B_QREADY = 3 * NS, B_QEMPTY = B_QREADY + 2, B_SFULL = B_QEMPTY + 2,
@@ -134,6 +135,8 @@ __device__ __forceinline__ Span span_of(int hist, int n, int window, int sinks) 
 struct alignas(16) Seg {
     int b, h, hist, lo;
     int hi, ns, skip, part;  // part: 0 or 1, the CTA's slot for its part of an item; kWhole: a whole item; kEnd: no segment
+    int edge, diag, pad0, pad1;  // every row sees the whole of tiles edge .. diag - 1
+    __device__ __forceinline__ bool masked(int v) const { return v < edge || v >= diag; }
     __device__ __forceinline__ int key(int v) const { return (v < ns ? v : v + skip) * BN; }  // first slot of tile v
 };
 constexpr int kWhole = 2, kEnd = 3;
@@ -221,6 +224,9 @@ struct Plan {
         const Span p = span_of(s.hist, a.n, a.window, a.sinks);
         s.ns = p.ns;
         s.skip = p.skip;
+        const int hidden = s.hist + a.n - 1 - a.window;  // the last token's window begins behind that slot
+        s.edge = hidden < 0 ? 0 : max(hidden / BN + 1 - p.skip, 0);
+        s.diag = s.hist / BN - p.skip;
         const int per = len == 0 ? (p.nt + target - 1) / target : p.nt + kHead;  // pieces or places of an item
         s.h = (pos - start) / per;
         start += s.h * per;
@@ -295,10 +301,17 @@ __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, const vo
     }
 }
 
-// Whether some row may not see some slot of the key tile from slot kb on (the same answer in every warp).
-__device__ __forceinline__ bool masked(int kb, int hist, int n, int window, int sinks) {
-    return kb + BN > hist || (kb <= hist + n - 1 - window && kb + BN > sinks);
-}
+// A place in a ring of N slots, and the parity of its phase.
+template <int N>
+struct Cursor {
+    uint32_t slot = 0, phase = 0;
+    __device__ __forceinline__ void next() {
+        if (++slot == N) {
+            slot = 0;
+            phase ^= 1u;
+        }
+    }
+};
 
 // What a row sees: slots [lo, hist) and [0, first), and the new ones whose bit is set.
 struct View {
@@ -434,7 +447,7 @@ __device__ __forceinline__ void stage_q(uint32_t tile_addr, uint8_t* tile, int a
 // Add to a row's O (in TMEM) the values that are not finite of the slots that the row sees in the masked tiles lo .. hi - 1: a
 // whole warp, a thread per row.  v_head: slot 0 of the (sequence, kv head), v_tok: its v of token 0, `stride` apart.
 template <int D>
-__device__ __noinline__ void add_not_finite(uint32_t o_col, View view, int lo, int hi, int ns, int skip, int n, int window, int sinks,
+__device__ __noinline__ void add_not_finite(uint32_t o_col, View view, int lo, int hi, int ns, int skip, int edge, int diag,
                                             const uint16_t* v_head, const uint16_t* v_tok, int stride) {
     const int hist = view.hist;
 #pragma unroll 1
@@ -444,7 +457,7 @@ __device__ __noinline__ void add_not_finite(uint32_t o_col, View view, int lo, i
         tmem_wait_ld();
         for (int v = lo; v < hi; ++v) {
             const int kb = (v < ns ? v : v + skip) * BN;
-            if (!masked(kb, hist, n, window, sinks)) continue;
+            if (v >= edge && v < diag) continue;
             for (int c = 0; c < BN / 32; ++c)
                 for (uint32_t w = view.word(kb + 32 * c); w != 0; w &= w - 1) {
                     const int slot = kb + 32 * c + __ffs(w) - 1;
@@ -500,7 +513,7 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
         for (int i = 0; i < C::NS; ++i) {
             mbar_init(bar(C::B_FULL + i), 1);
             mbar_init(bar(C::B_READY + i), 2);  // the guards
-            mbar_init(bar(C::B_EMPTY + i), 1);
+            mbar_init(bar(C::B_EMPTY + i), 3);  // the issuer; the guards
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(C::B_QREADY + i), 4 * live);  // (NT = 1: the stagers)
@@ -565,15 +578,16 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
     bool ok = true;
     auto take = [&](uint32_t i, Seg& to) {
         ok = __all_sync(0xFFFFFFFFu, wait(bar(C::B_SEG + i % kSegs), (i / kSegs) & 1u));
-        if (ok) to = seg_s[i % kSegs];
+        const int4* at = reinterpret_cast<const int4*>(seg_s + i % kSegs);
+        const int4 x = at[0], y = at[1], z = at[2];
+        to.b = x.x, to.h = x.y, to.hist = x.z, to.lo = x.w;
+        to.hi = y.x, to.ns = y.y, to.skip = y.z, to.part = y.w;
+        to.edge = z.x, to.diag = z.y;
         return ok && to.part != kEnd;
     };
     Seg s;
     uint64_t kin[2];
-    // The ring's order of a segment of n tiles: K0, K1, V0, K2, V1, .., V(n - 1); where K(j) and V(j) are in it.
-    auto k_at = [](int j) { return j == 0 ? 0 : 2 * j - 1; };
-    auto v_at = [](int j, int n) { return min(2 * j + 2, 2 * n - 1); };
-    // and what is at place i: tile j, V or not
+    // The ring's order of a segment of n tiles: K0, K1, V0, K2, V1, .., V(n - 1).  What is at place i: tile j, V or not.
     auto tile_at = [](int i, int n, bool& is_v) {
         is_v = i == 2 * n - 1 || (i > 0 && i % 2 == 0);
         return i == 2 * n - 1 ? n - 1 : is_v ? i / 2 - 1 : (i + 1) / 2;
@@ -584,14 +598,22 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
         if (warp == kWarpTma) {
             // ------------------------------------------------------------ producer
             uint32_t seq = 0;
+            Cursor<C::NS> at;
             Shared sh;
             for (uint32_t segs = 0;; ++segs) {
                 const bool some = plan.next(a, run_id, s, sh);
                 if (lane == 0) {
                     if (!some) s.part = kEnd;
-                    if (some && s.part != kWhole) shared_s[s.part] = sh;
+                    if (some && s.part != kWhole) {
+                        int4* to = reinterpret_cast<int4*>(shared_s + s.part);
+                        to[0] = make_int4(sh.b, sh.h, sh.first, sh.count);
+                        to[1] = make_int4(sh.slot0, 1, 0, 0);
+                    }
                     if (ok) {  // (after a wait that ran out: the items it shares alone)
-                        seg_s[segs % kSegs] = s;
+                        int4* to = reinterpret_cast<int4*>(seg_s + segs % kSegs);
+                        to[0] = make_int4(s.b, s.h, s.hist, s.lo);
+                        to[1] = make_int4(s.hi, s.ns, s.skip, s.part);
+                        to[2] = make_int4(s.edge, s.diag, 0, 0);
                         mbar_arrive(bar(C::B_SEG + segs % kSegs));
                     }
                 }
@@ -599,9 +621,9 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                 if (!ok) continue;
                 if (lane == 0) {
                     const int n = s.hi - s.lo, head = (a.b0 + s.b) * a.Hkv + s.h;
-                    for (int i = 0; i < 2 * n; ++i, ++seq) {
-                        const uint32_t st = seq % C::NS;
-                        if (seq >= C::NS && !wait(bar(C::B_EMPTY + st), (seq / C::NS - 1u) & 1u)) {
+                    for (int i = 0; i < 2 * n; ++i, ++seq, at.next()) {
+                        const uint32_t st = at.slot;
+                        if (!wait(bar(C::B_EMPTY + st), at.phase ^ 1u)) {  // (a phase that there was none of is past)
                             ok = false;
                             break;
                         }
@@ -632,7 +654,8 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
             const uint32_t q_lo0 = desc_lo_sw128(base + C::OFF_Q, 16);
             const uint32_t k_lo0 = desc_lo_sw128(base + C::OFF_RING, 16);
             const uint32_t v_lo0 = desc_lo_sw128(base + C::OFF_RING, C::CHUNK);
-            uint32_t seq = 0, tiles = 0, segs = 0;
+            uint32_t tiles = 0, segs = 0;
+            Cursor<C::NS> at;  // (K(j) and V(j - 1) are used one after the other, as they are in the ring)
             auto issue_s = [&](uint32_t buf, uint32_t q, uint32_t slot) {
                 const uint32_t a_lo = q_lo0 + q * (C::TILE >> 4), b_lo = k_lo0 + slot * (C::TILE >> 4);
 #pragma unroll
@@ -649,8 +672,13 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                     umma_ts_w(tmem + kTmO + o * D, tmem + buf * BN + kk * 8, b_lo + kk * ((16 * 128) >> 4), kHi, kIdPV,
                               (!first || kk > 0) ? 1u : 0u);
             };
-            auto ready = [&](uint32_t at) {
-                return wait(bar(C::B_READY + at % C::NS), (at / C::NS) & 1u);
+            uint32_t ready_par = 0;  // a bit per slot of the ring: the parity of its next B_READY
+            auto ready = [&](int v) {  // the K or V of tile v, which is the ring's next
+                if (!wait(bar(C::B_FULL + at.slot), at.phase)) return false;
+                if (!s.masked(v)) return true;
+                const bool there = wait(bar(C::B_READY + at.slot), ready_par >> at.slot & 1u);
+                ready_par ^= 1u << at.slot;
+                return there;
             };
             while (ok && take(segs, s)) {
                 if (lane == 0) {
@@ -660,42 +688,53 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                     for (int j = 0; j <= n && ok; ++j) {
                         if constexpr (NT == 1) {
                             if (j < n) {
-                                const uint32_t at = seq + k_at(j);
-                                if (!(ok = ready(at))) break;
+                                if (!(ok = ready(s.lo + j))) break;
                                 tc_fence_after();
-                                issue_s((tiles + j) & 1u, qb, at % C::NS);
-                                umma_commit(bar(C::B_EMPTY + at % C::NS));
+                                issue_s((tiles + j) & 1u, qb, at.slot);
+                                umma_commit(bar(C::B_EMPTY + at.slot));
+                                at.next();
                                 if (j == n - 1) umma_commit(bar(C::B_QEMPTY + qb));
                             }
                             if (j > 0) {
-                                const uint32_t t = tiles + j - 1, at = seq + v_at(j - 1, n);
-                                ok = wait(bar(C::B_PFULL + (t & 1u)), (t >> 1) & 1u) && ready(at) &&
+                                const uint32_t t = tiles + j - 1;
+                                ok = wait(bar(C::B_PFULL + (t & 1u)), (t >> 1) & 1u) && ready(s.lo + j - 1) &&
                                      (j > 1 || segs < 2 ||
                                       wait(bar(C::B_OEMPTY + qb), ((segs >> 1) - 1u) & 1u));
                                 if (!ok) break;
                                 tc_fence_after();
-                                issue_pv(t & 1u, qb, j == 1, at % C::NS);
+                                issue_pv(t & 1u, qb, j == 1, at.slot);
                                 umma_commit(bar(C::B_PVDONE));
-                                umma_commit(bar(C::B_EMPTY + at % C::NS));
+                                umma_commit(bar(C::B_EMPTY + at.slot));
+                                at.next();
                             }
                         } else {
-                            const uint32_t ka = seq + k_at(j), va = seq + v_at(j - 1, n);
-                            ok = (j == n || ready(ka)) && (j == 0 || ready(va));
+                            const uint32_t ka = at.slot;
+                            if (j < n) {
+                                ok = ready(s.lo + j);
+                                at.next();
+                            }
+                            const uint32_t va = at.slot;
+                            if (j > 0) {
+                                ok = ok && ready(s.lo + j - 1);
+                                at.next();
+                            }
                             if (!ok) break;
                             tc_fence_after();
-                            for (int t = 0; t < live; ++t) {
+#pragma unroll
+                            for (int t = 0; t < 2; ++t) {
+                                if (t == live) break;
                                 if (j > 0) {
                                     ok = wait(bar(C::B_PFULL + t), (tiles + j - 1) & 1u) &&
                                          (j > 1 || segs == 0 || wait(bar(C::B_OEMPTY + t), (segs - 1u) & 1u));
                                     if (!ok) break;
                                     tc_fence_after();
-                                    issue_pv(t, t, j == 1, va % C::NS);
+                                    issue_pv(t, t, j == 1, va);
                                 }
-                                if (j < n) issue_s(t, t, ka % C::NS);
+                                if (j < n) issue_s(t, t, ka);
                             }
                             if (!ok) break;
-                            if (j < n) umma_commit(bar(C::B_EMPTY + ka % C::NS));
-                            if (j > 0) umma_commit(bar(C::B_EMPTY + va % C::NS));
+                            if (j < n) umma_commit(bar(C::B_EMPTY + ka));
+                            if (j > 0) umma_commit(bar(C::B_EMPTY + va));
                             if (j == n - 1) umma_commit(bar(C::B_QEMPTY));
                         }
                     }
@@ -709,7 +748,6 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                         atomicOr(a.err, kDevErrTimeout);
                     }
                     tiles += n;
-                    seq += 2 * n;
                 }
                 ++segs;
                 ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
@@ -747,22 +785,23 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
             // A guard has the rows of a tile whose bit 2 is its number: the 16-byte units u with u % 64 in its half.
             const int gw = warp - kWarpGuard, me = gw * 32 + lane;
             auto rows_below = [&](int row) { return row / 8 * 4 + min(max(row % 8 - 4 * gw, 0), 4); };  // of this guard's
-            uint32_t seq = 0, segs = 0;
+            uint32_t segs = 0;
+            Cursor<C::NS> at;
             while (ok && take(segs, s)) {
                 kin_seg(s, a, kin, group == 0 && warp == kWarpGuard);
                 const int depth[2] = {__popcll(kin[0]) - 1, __popcll(kin[1]) - 1};
                 const int n = s.hi - s.lo;
                 const size_t head = (static_cast<size_t>(a.b0 + s.b) * a.Hkv + s.h) * a.max_len + s.hist;  // slot of token 0
-                for (int i = 0; i < 2 * n && ok; ++i, ++seq) {
-                    const uint32_t st = seq % C::NS;
+                for (int i = 0; i < 2 * n && ok; ++i, at.next()) {
+                    const uint32_t st = at.slot;
                     bool is_v;
-                    const int kb = s.key(s.lo + tile_at(i, n, is_v));
+                    const int v = s.lo + tile_at(i, n, is_v), kb = s.key(v);
                     uint8_t* tile = gbase + C::OFF_RING + st * C::TILE;
-                    const bool mixed = masked(kb, s.hist, a.n, a.window, a.sinks);
+                    const bool mixed = s.masked(v);
                     const int t0 = max(kb - s.hist, 0), t1 = min(kb + BN - s.hist, a.n);  // new tokens of this tile
                     bool there = false;  // the tile has landed
                     auto landed = [&]() {
-                        if (!there) ok = __all_sync(0xFFFFFFFFu, wait(bar(C::B_FULL + st), (seq / C::NS) & 1u));
+                        if (!there) ok = __all_sync(0xFFFFFFFFu, wait(bar(C::B_FULL + st), at.phase));
                         there = true;
                     };
                     if (t1 > t0) {
@@ -836,7 +875,10 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                     }
                     if (mixed) fence_proxy_async_smem();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(C::B_READY + st));
+                    if (lane == 0) {
+                        if (mixed) mbar_arrive(bar(C::B_READY + st));
+                        mbar_arrive(bar(C::B_EMPTY + st));
+                    }
                 }
                 ++segs;
             }
@@ -901,7 +943,7 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                         for (int c = 0; c < BN / 32; ++c) tmem_ld32(s_col + 32 * c, r[c]);
                         tmem_wait_ld();
                         const int kb = s.key(v);
-                        if (masked(kb, s.hist, a.n, a.window, a.sinks)) {
+                        if (s.masked(v)) {
 #pragma unroll
                             for (int c = 0; c < BN / 32; ++c) {
                                 const uint32_t w = view.word(kb + 32 * c);
@@ -981,7 +1023,7 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                 if (rows_on) {
                     tc_fence_after();
                     if (odd_flag[segs % kFlags] == static_cast<int>(segs) + 1)
-                        add_not_finite<D>(o_col, view, s.lo, s.hi, s.ns, s.skip, a.n, a.window, a.sinks,
+                        add_not_finite<D>(o_col, view, s.lo, s.hi, s.ns, s.skip, s.edge, s.diag,
                                           a.v_cache + (static_cast<size_t>(a.b0 + s.b) * a.Hkv + s.h) * a.max_len * D,
                                           a.v_new + (static_cast<size_t>(a.b0 + s.b) * a.n * a.Hkv + s.h) * D, a.Hkv * D);
                     const float inv = 1.f / l_run;
