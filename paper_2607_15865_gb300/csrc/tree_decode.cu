@@ -648,9 +648,11 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                     mbar_wait(bar(C::B_FULL + i % C::NS), (i / C::NS) & 1u, nullptr);
         } else if (warp == kWarpMma) {
             // ------------------------------------------------------------ issuer
+            // The warp stays converged and one elected lane issues: what the MMAs take is in uniform registers then.
             constexpr uint32_t kIdS = idesc_bf16_f32(BM, BN, false, false);
             constexpr uint32_t kIdPV = idesc_bf16_f32(BM, D, false, true);
             constexpr uint32_t kHi = desc_hi_sw128(1024);
+            const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
             const uint32_t q_lo0 = desc_lo_sw128(base + C::OFF_Q, 16);
             const uint32_t k_lo0 = desc_lo_sw128(base + C::OFF_RING, 16);
             const uint32_t v_lo0 = desc_lo_sw128(base + C::OFF_RING, C::CHUNK);
@@ -658,104 +660,110 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
             Cursor<C::NS> at;  // (K(j) and V(j - 1) are used one after the other, as they are in the ring)
             auto issue_s = [&](uint32_t buf, uint32_t q, uint32_t slot) {
                 const uint32_t a_lo = q_lo0 + q * (C::TILE >> 4), b_lo = k_lo0 + slot * (C::TILE >> 4);
+                if (elect_one()) {
 #pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk) {
-                    const uint32_t c = ((kk >> 2) * C::CHUNK + (kk & 3) * 32) >> 4;
-                    umma_ss_w(tmem + buf * BN, a_lo + c, kHi, b_lo + c, kHi, kIdS, kk > 0 ? 1u : 0u);
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        const uint32_t c = ((kk >> 2) * C::CHUNK + (kk & 3) * 32) >> 4;
+                        umma_ss_w(tm + buf * BN, a_lo + c, kHi, b_lo + c, kHi, kIdS, kk > 0 ? 1u : 0u);
+                    }
+                    umma_commit(bar(C::B_SFULL + buf));
                 }
-                umma_commit(bar(C::B_SFULL + buf));
+                __syncwarp();
             };
             auto issue_pv = [&](uint32_t buf, uint32_t o, bool first, uint32_t slot) {
                 const uint32_t b_lo = v_lo0 + slot * (C::TILE >> 4);
+                if (elect_one()) {
 #pragma unroll
-                for (int kk = 0; kk < BN / 16; ++kk)
-                    umma_ts_w(tmem + kTmO + o * D, tmem + buf * BN + kk * 8, b_lo + kk * ((16 * 128) >> 4), kHi, kIdPV,
-                              (!first || kk > 0) ? 1u : 0u);
+                    for (int kk = 0; kk < BN / 16; ++kk)
+                        umma_ts_w(tm + kTmO + o * D, tm + buf * BN + kk * 8, b_lo + kk * ((16 * 128) >> 4), kHi, kIdPV,
+                                  (!first || kk > 0) ? 1u : 0u);
+                }
+                __syncwarp();
             };
+            auto commit = [&](uint32_t b) {
+                if (elect_one()) umma_commit(bar(b));
+                __syncwarp();
+            };
+            auto wait_all = [&](uint32_t b, uint32_t parity) { return static_cast<bool>(__all_sync(0xFFFFFFFFu, wait(bar(b), parity))); };
             uint32_t ready_par = 0;  // a bit per slot of the ring: the parity of its next B_READY
             auto ready = [&](int v) {  // the K or V of tile v, which is the ring's next
-                if (!wait(bar(C::B_FULL + at.slot), at.phase)) return false;
+                if (!wait_all(C::B_FULL + at.slot, at.phase)) return false;
                 if (!s.masked(v)) return true;
-                const bool there = wait(bar(C::B_READY + at.slot), ready_par >> at.slot & 1u);
+                const bool there = wait_all(C::B_READY + at.slot, ready_par >> at.slot & 1u);
                 ready_par ^= 1u << at.slot;
                 return there;
             };
             while (ok && take(segs, s)) {
-                if (lane == 0) {
-                    const int n = s.hi - s.lo;
-                    const uint32_t qb = NT == 1 ? segs & 1u : 0u;
-                    ok = wait(bar(C::B_QREADY + qb), (NT == 1 ? segs >> 1 : segs) & 1u);
-                    for (int j = 0; j <= n && ok; ++j) {
-                        if constexpr (NT == 1) {
-                            if (j < n) {
-                                if (!(ok = ready(s.lo + j))) break;
-                                tc_fence_after();
-                                issue_s((tiles + j) & 1u, qb, at.slot);
-                                umma_commit(bar(C::B_EMPTY + at.slot));
-                                at.next();
-                                if (j == n - 1) umma_commit(bar(C::B_QEMPTY + qb));
-                            }
-                            if (j > 0) {
-                                const uint32_t t = tiles + j - 1;
-                                ok = wait(bar(C::B_PFULL + (t & 1u)), (t >> 1) & 1u) && ready(s.lo + j - 1) &&
-                                     (j > 1 || segs < 2 ||
-                                      wait(bar(C::B_OEMPTY + qb), ((segs >> 1) - 1u) & 1u));
-                                if (!ok) break;
-                                tc_fence_after();
-                                issue_pv(t & 1u, qb, j == 1, at.slot);
-                                umma_commit(bar(C::B_PVDONE));
-                                umma_commit(bar(C::B_EMPTY + at.slot));
-                                at.next();
-                            }
-                        } else {
-                            const uint32_t ka = at.slot;
-                            if (j < n) {
-                                ok = ready(s.lo + j);
-                                at.next();
-                            }
-                            const uint32_t va = at.slot;
-                            if (j > 0) {
-                                ok = ok && ready(s.lo + j - 1);
-                                at.next();
-                            }
+                const int n = s.hi - s.lo;
+                const uint32_t qb = NT == 1 ? segs & 1u : 0u;
+                ok = wait_all(C::B_QREADY + qb, (NT == 1 ? segs >> 1 : segs) & 1u);
+                for (int j = 0; j <= n && ok; ++j) {
+                    if constexpr (NT == 1) {
+                        if (j < n) {
+                            if (!(ok = ready(s.lo + j))) break;
+                            tc_fence_after();
+                            issue_s((tiles + j) & 1u, qb, at.slot);
+                            commit(C::B_EMPTY + at.slot);
+                            at.next();
+                            if (j == n - 1) commit(C::B_QEMPTY + qb);
+                        }
+                        if (j > 0) {
+                            const uint32_t t = tiles + j - 1;
+                            ok = wait_all(C::B_PFULL + (t & 1u), (t >> 1) & 1u) && ready(s.lo + j - 1) &&
+                                 (j > 1 || segs < 2 ||
+                                  wait_all(C::B_OEMPTY + qb, ((segs >> 1) - 1u) & 1u));
                             if (!ok) break;
                             tc_fence_after();
-#pragma unroll
-                            for (int t = 0; t < 2; ++t) {
-                                if (t == live) break;
-                                if (j > 0) {
-                                    ok = wait(bar(C::B_PFULL + t), (tiles + j - 1) & 1u) &&
-                                         (j > 1 || segs == 0 || wait(bar(C::B_OEMPTY + t), (segs - 1u) & 1u));
-                                    if (!ok) break;
-                                    tc_fence_after();
-                                    issue_pv(t, t, j == 1, va);
-                                }
-                                if (j < n) issue_s(t, t, ka);
-                            }
-                            if (!ok) break;
-                            if (j < n) umma_commit(bar(C::B_EMPTY + ka));
-                            if (j > 0) umma_commit(bar(C::B_EMPTY + va));
-                            if (j == n - 1) umma_commit(bar(C::B_QEMPTY));
+                            issue_pv(t & 1u, qb, j == 1, at.slot);
+                            commit(C::B_PVDONE);
+                            commit(C::B_EMPTY + at.slot);
+                            at.next();
                         }
-                    }
-                    if (ok) {
-                        if constexpr (NT == 1)
-                            umma_commit(bar(C::B_OFULL + qb));
-                        else
-                            for (int t = 0; t < live; ++t) umma_commit(bar(C::B_OFULL + t));
                     } else {
-                        *abort_flag = 1;
-                        atomicOr(a.err, kDevErrTimeout);
+                        const uint32_t ka = at.slot;
+                        if (j < n) {
+                            ok = ready(s.lo + j);
+                            at.next();
+                        }
+                        const uint32_t va = at.slot;
+                        if (j > 0) {
+                            ok = ok && ready(s.lo + j - 1);
+                            at.next();
+                        }
+                        if (!ok) break;
+                        tc_fence_after();
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) {
+                            if (t == live) break;
+                            if (j > 0) {
+                                ok = wait_all(C::B_PFULL + t, (tiles + j - 1) & 1u) &&
+                                     (j > 1 || segs == 0 || wait_all(C::B_OEMPTY + t, (segs - 1u) & 1u));
+                                if (!ok) break;
+                                tc_fence_after();
+                                issue_pv(t, t, j == 1, va);
+                            }
+                            if (j < n) issue_s(t, t, ka);
+                        }
+                        if (!ok) break;
+                        if (j < n) commit(C::B_EMPTY + ka);
+                        if (j > 0) commit(C::B_EMPTY + va);
+                        if (j == n - 1) commit(C::B_QEMPTY);
                     }
-                    tiles += n;
                 }
+                if (ok) {
+                    if constexpr (NT == 1)
+                        commit(C::B_OFULL + qb);
+                    else
+                        for (int t = 0; t < live; ++t) commit(C::B_OFULL + t);
+                } else if (lane == 0) {
+                    *abort_flag = 1;
+                    atomicOr(a.err, kDevErrTimeout);
+                }
+                tiles += n;
                 ++segs;
-                ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
             }
-            if (lane == 0) {  // all tensor-core work must finish before TMEM is released
-                umma_commit(bar(C::B_DRAIN));
-                mbar_wait(bar(C::B_DRAIN), 0, nullptr);
-            }
+            commit(C::B_DRAIN);  // all tensor-core work must finish before TMEM is released
+            mbar_wait(bar(C::B_DRAIN), 0, nullptr);
         } else if (NT == 1 && warp >= kWarpStage) {
             // ------------------------------------------------------------ stagers
             const int me = (warp - kWarpStage) * 32 + lane, rows = min(a.n * a.G, BM);
