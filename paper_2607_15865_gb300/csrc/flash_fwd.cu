@@ -576,8 +576,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (items > 0) mbar_wait(bar(B_QFULL), static_cast<uint32_t>(items - 1) & 1u, nullptr);
             for (uint32_t t = gc >= GS ? gc - GS : 0; t < gc; ++t)
                 mbar_wait(bar(B_GFULL0 + static_cast<int>(t % GS)), (t / GS) & 1u, nullptr);
-        } else if (warp == kWarpMma && lane == 0) {
+        } else if (warp == kWarpMma) {
             // ---------------------------------------------------- tcgen05 issuer
+            // The warp stays converged and one elected lane issues: what the MMAs take is in uniform registers then.
             constexpr uint32_t kIdS = idesc_bf16_f32(BM, BN, false, false);
             constexpr uint32_t kIdPV = idesc_bf16_f32(BM, D, false, true);
             uint32_t gc = 0;  // groups consumed
@@ -591,31 +592,45 @@ __global__ void __launch_bounds__(kThreads, 1)
             // V tile once for both query tiles).
             // Descriptor low words of the operand tiles; a K step adds a constant to them.
             constexpr uint32_t kHi = desc_hi_sw128(1024);
+            const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
             const uint32_t q_lo0 = desc_lo_sw128(base + L::OFF_Q, 16);
             const uint32_t k_lo0 = desc_lo_sw128(base + L::OFF_G, 16);
             const uint32_t v_lo0 = desc_lo_sw128(base + L::OFF_G + L::KV_TILE, L::CHUNK);
             auto issue_s = [&](int t, uint32_t slot) {
                 const uint32_t a_lo = q_lo0 + t * (L::Q_TILE >> 4);
                 const uint32_t b_lo = k_lo0 + slot * (L::G_SLOT >> 4);
+                if (elect_one()) {
 #pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk) {
-                    const uint32_t c = ((kk >> 2) * L::CHUNK + (kk & 3) * 32) >> 4;
-                    umma_ss_w(tmem + t * BN, a_lo + c, kHi, b_lo + c, kHi, kIdS, kk > 0 ? 1u : 0u);
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        const uint32_t c = ((kk >> 2) * L::CHUNK + (kk & 3) * 32) >> 4;
+                        umma_ss_w(tm + t * BN, a_lo + c, kHi, b_lo + c, kHi, kIdS, kk > 0 ? 1u : 0u);
+                    }
+                    umma_commit(bar(B_SFULL0 + t));
                 }
-                umma_commit(bar(B_SFULL0 + t));
+                __syncwarp();
             };
             auto issue_pv = [&](int t, bool first, uint32_t slot) {
                 const uint32_t b_lo = v_lo0 + slot * (L::G_SLOT >> 4);
+                if (elect_one()) {
 #pragma unroll
-                for (int kk = 0; kk < BN / 16; ++kk)
-                    umma_ts_w(tmem + L::TM_O + t * D, tmem + t * BN + kk * 8, b_lo + kk * ((16 * 128) >> 4), kHi, kIdPV,
-                              (!first || kk > 0) ? 1u : 0u);
+                    for (int kk = 0; kk < BN / 16; ++kk)
+                        umma_ts_w(tm + L::TM_O + t * D, tm + t * BN + kk * 8, b_lo + kk * ((16 * 128) >> 4), kHi, kIdPV,
+                                  (!first || kk > 0) ? 1u : 0u);
+                }
+                __syncwarp();
+            };
+            auto commit = [&](int b) {
+                if (elect_one()) umma_commit(bar(b));
+                __syncwarp();
+            };
+            auto wait = [&](int b, uint32_t parity) {
+                return static_cast<bool>(__all_sync(0xFFFFFFFFu, mbar_wait(bar(b), parity, abort_flag, wait_ns)));
             };
             // P_t of the previous KV tile in TMEM, and O_t free when it is the unit's first PV
             auto wait_p = [&](int t, bool first) -> bool {
-                if (!mbar_wait(bar(B_PFULL0 + t), p_cnt[t] & 1u, abort_flag, wait_ns)) return false;
+                if (!wait(B_PFULL0 + t, p_cnt[t] & 1u)) return false;
                 ++p_cnt[t];
-                if (first && o_cnt[t] > 0 && !mbar_wait(bar(B_OEMPTY0 + t), (o_cnt[t] - 1u) & 1u, abort_flag, wait_ns))
+                if (first && o_cnt[t] > 0 && !wait(B_OEMPTY0 + t, (o_cnt[t] - 1u) & 1u))
                     return false;
                 return true;
             };
@@ -624,7 +639,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             // WIN: the guards are through with the group's V, which is KV tile j
             auto wait_v = [&](const Unit& un, int j) -> bool {
                 if (!WIN || !un.guarded(j)) return true;
-                if (!mbar_wait(bar(B_GREADY0 + gslot), ready_par >> gslot & 1u, abort_flag, wait_ns)) return false;
+                if (!wait(B_GREADY0 + gslot, ready_par >> gslot & 1u)) return false;
                 ready_par ^= 1u << gslot;
                 return true;
             };
@@ -635,7 +650,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int lin = blockIdx.x; lin < n_units && ok; lin += gridDim.x) {
                 const Unit un = decode_unit<PK, WIN>(unit_of(lin, sc), sc);
                 const Item& it = un.it;
-                if (!mbar_wait(bar(B_QREADY), static_cast<uint32_t>(items) & 1u, abort_flag, wait_ns)) {
+                if (!wait(B_QREADY, static_cast<uint32_t>(items) & 1u)) {
                     ok = false;
                     break;
                 }
@@ -643,7 +658,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 [[maybe_unused]] bool was_b = false;  // WIN: S_B(j - 1) was issued
                 for (int j = un.kv_lo; j < un.kv_hi && ok; ++j) {
                     // group j: K(j), and V(j-1) for the PV MMAs of the previous tile
-                    if (!mbar_wait(bar(B_GFULL0 + gslot), (gc / GS) & 1u, abort_flag, wait_ns) ||
+                    if (!wait(B_GFULL0 + gslot, (gc / GS) & 1u) ||
                         (j > un.kv_lo && !wait_v(un, j - 1))) {
                         ok = false;
                         break;
@@ -671,13 +686,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     if (s_b) issue_s(1, gslot);
                     if constexpr (WIN) was_b = s_b;
-                    umma_commit(bar(B_GEMPTY0 + gslot));
+                    commit(B_GEMPTY0 + gslot);
                     next_group();
                 }
                 if (!ok) break;
-                umma_commit(bar(B_QEMPTY));  // every S MMA of the unit is issued
+                commit(B_QEMPTY);  // every S MMA of the unit is issued
                 // the last group: V of the final tile
-                if (!mbar_wait(bar(B_GFULL0 + gslot), (gc / GS) & 1u, abort_flag, wait_ns) || !wait_v(un, un.kv_hi - 1)) ok = false;
+                if (!wait(B_GFULL0 + gslot, (gc / GS) & 1u) || !wait_v(un, un.kv_hi - 1)) ok = false;
                 tc_fence_after();
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
@@ -691,22 +706,22 @@ __global__ void __launch_bounds__(kThreads, 1)
                         issue_pv(t, first, gslot);
                     }
                 if (!ok) break;
-                umma_commit(bar(B_GEMPTY0 + gslot));
+                commit(B_GEMPTY0 + gslot);
                 next_group();
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
                     if (un.has<WIN>(t)) {
-                        umma_commit(bar(B_OFULL0 + t));
+                        commit(B_OFULL0 + t);
                         ++o_cnt[t];
                     }
                 ++items;
             }
-            if (!ok) {
+            if (!ok && lane == 0) {
                 *abort_flag = 1;
                 atomicOr(err, kDevErrTimeout);
             }
             // All tensor-core work issued here must finish before TMEM is released.
-            umma_commit(bar(B_DRAIN));
+            commit(B_DRAIN);
             mbar_wait(bar(B_DRAIN), 0, nullptr);
         } else if (WIN && warp > kWarpMma) {
             // ---------------------------------------------------- guards
