@@ -51,6 +51,9 @@ constexpr uint32_t kTmO = 2 * BN;
 constexpr int kFlags = 8;
 constexpr int kSegs = 8;  // segments in shared memory: the producer is at most NS / 2 + 2 ahead of every reader
 constexpr int kLonger = 4;  // tiles that a piece may be longer than a run
+// Items of up to so many tiles are not shared: walking them takes no longer than meeting does (8 tokens over 200, 2 tiles: 12.1 to
+// 10.3 us; over 300, 3 tiles: 12.5, 11.4; over 400, 4 tiles: 12.2, 12.6).
+constexpr int kAlone = 3;
 constexpr int kHead = 3;    // an item's first segment takes a run about as long as this many tiles: its q, its epilogue
 constexpr int kLaunchRegs = 168;  // registers a thread at launch
 
@@ -173,7 +176,11 @@ struct Plan {
         if (bad && report) atomicOr(a.err, kDevErrHistRange);
         // Pieces, if there are CTAs for all and they are hardly longer than the runs would be: a CTA then has but one segment.
         const int least = max((__reduce_add_sync(0xFFFFFFFFu, tiles) + runs - 1) / runs, 1);
-        target = least;
+        int most = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) most = max(most, t[i]);
+        most = __reduce_max_sync(0xFFFFFFFFu, most);
+        target = most <= kAlone ? max(least, most) : least;
         len = 0;
 #pragma unroll 1
         for (;; target += max(target >> 5, 1)) {
