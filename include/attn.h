@@ -528,7 +528,7 @@ int attn_tree_decode(attn_ctx* ctx, const uint16_t* q, const uint16_t* k, const 
  * Their k and v move, in order, to the slots from d_hist_len[b] on, where a history has them (their positions are those
  * that k was rotated for), in the caches of every layer: k_caches and v_caches are host arrays of n_layers device
  * pointers, which are read before the call returns.  d_new_len (NULL, or device int32 [batch], not overlapping
- * d_hist_len): the lengths after that.  Slots past d_new_len[b] hold what they held.  A sequence that attn_tree_decode would
+ * the other arrays): the lengths after that.  Slots past d_new_len[b] hold what they held.  A sequence that attn_tree_decode would
  * skip, or whose d_leaf[b] is no token of the tree, keeps its cache and its length, and sets the same bits.
  * Device arrays are 4-byte aligned, caches 16-byte; a cache may be in the list once.  Returns ATTN_OK, ATTN_EINVAL
  * or ATTN_ECUDA.

@@ -23,6 +23,7 @@ All calls are asynchronous on the given (default: current) torch CUDA stream.
 from __future__ import annotations
 
 import ctypes
+import operator
 
 import torch
 
@@ -53,6 +54,21 @@ def _ptr_checked(t, name: str, shape) -> int:
     return t.data_ptr()
 
 
+_shape, _dtype, _is_cuda = map(operator.attrgetter, ("shape", "dtype", "is_cuda"))
+
+
+def _ptrs(tensors, name: str, shape) -> list:
+    # _ptr of many tensors of one shape, an attribute of all at a time (three quarters of the time of 64 calls of it)
+    try:
+        if (all(map(torch.Tensor.is_contiguous, tensors)) and all(map(_is_cuda, tensors))
+                and list(map(_dtype, tensors)).count(torch.bfloat16) == len(tensors)
+                and list(map(_shape, tensors)).count(shape) == len(tensors)):
+            return list(map(torch.Tensor.data_ptr, tensors))
+    except (TypeError, AttributeError):  # (not a tensor)
+        pass
+    return [_ptr(t, name, shape) for t in tensors]
+
+
 def _stream(stream) -> int:
     if stream is not None:
         return stream.cuda_stream
@@ -77,7 +93,7 @@ def _is_len(t, batch: int) -> bool:
 def _int32(x) -> int:
     """A window or a number of sinks for the C call: one past the largest int means the same as that, and a negative one is
     refused there whichever it is."""
-    return max(min(int(x), 2 ** 31 - 1), -1)
+    return x if type(x) is int and -1 <= x < 2 ** 31 else max(min(int(x), 2 ** 31 - 1), -1)
 
 
 class Attention:
@@ -412,8 +428,8 @@ class Attention:
             raise TypeError("hist_len and leaf must be contiguous int32 CUDA tensors of shape [batch]")
         if not isinstance(parents, torch.Tensor) or parents.dim() != 2 or not self._is_tree(parents, parents.shape[1]):
             raise TypeError("parents must be a contiguous int32 CUDA tensor of shape [batch, n]")
-        ks = [_ptr(k, "k_cache", self._cache) for k, _ in caches]
-        vs = [_ptr(v, "v_cache", self._cache) for _, v in caches]
+        ks = _ptrs([k for k, _ in caches], "k_cache", self._cache)
+        vs = _ptrs([v for _, v in caches], "v_cache", self._cache)
         if len(set(ks + vs)) != len(ks) + len(vs):
             raise ValueError("a cache is in the list twice")
         new_len = _empty(hist_len.shape, torch.int32, hist_len, stream) if new_len is None else new_len

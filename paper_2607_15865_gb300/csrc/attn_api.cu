@@ -890,8 +890,10 @@ int attn_tree_accept(attn_ctx* c, const int32_t* d_hist_len, const int32_t* d_pa
     if (c == nullptr || d_hist_len == nullptr || d_parents == nullptr || d_leaf == nullptr || k_caches == nullptr ||
         v_caches == nullptr || n_layers < 1 || n_new < 1 || n_new > ATTN_TREE_TOKENS || n_new > c->cfg.max_len)
         return ATTN_EINVAL;
-    const int32_t* ends = d_hist_len + c->cfg.batch;
-    if (d_new_len != nullptr && d_new_len < ends && d_hist_len < d_new_len + c->cfg.batch) return ATTN_EINVAL;
+    const int B = c->cfg.batch;
+    auto over = [&](const int32_t* x, long long count) { return d_new_len < x + count && x < d_new_len + B; };
+    if (d_new_len != nullptr && (over(d_hist_len, B) || over(d_leaf, B) || over(d_parents, static_cast<long long>(B) * n_new)))
+        return ATTN_EINVAL;
     if ((reinterpret_cast<uintptr_t>(d_hist_len) | reinterpret_cast<uintptr_t>(d_parents) |
          reinterpret_cast<uintptr_t>(d_leaf) | reinterpret_cast<uintptr_t>(d_new_len)) & 3u)
         return ATTN_EINVAL;

@@ -145,3 +145,19 @@ def test_a_run_of_drafts():
     U.close(attn.window_decode(*d, lens, W, *gpu[1], sinks=4), *U.want(one, hist, [[-1]] * B, kc[1], vc[1], L, W, 4),
             "decoded token, window")
     assert attn.device_error() == 0
+
+
+def test_new_lengths_over_an_input_are_refused():
+    """Other blocks of the launch may still read what the first one has written."""
+    import torch
+
+    from paper_2607_15865_gb300._lib import AttnError
+    attn = attention(2, 4, 2, 64, 50)
+    kv = tuple(torch.ones(2, 2, 50, 64, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    x = torch.zeros(12, dtype=torch.int32, device="cuda")
+    lens, leaf, par = x[:2], x[4:6], x[8:12].view(2, 2).fill_(-1)
+    for bad in (leaf, x[3:5], x[5:7], x[8:10], x[7:9], x[1:3]):
+        with pytest.raises(AttnError):
+            attn.tree_accept(lens, par, leaf, [kv], new_len=bad)
+    assert attn.tree_accept(lens, par, leaf, [kv], new_len=x[2:4]).tolist() == [1, 1] and attn.device_error() == 0
+    assert attn.tree_accept(lens, par, leaf, [kv], new_len=x[6:8]).tolist() == [1, 1]
