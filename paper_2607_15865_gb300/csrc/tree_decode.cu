@@ -1286,11 +1286,12 @@ cudaError_t launch(const Shape& s, const TreeCall& c, const Args& args, cudaStre
     // sequences of a launch: their tiles are counted in int
     const long long tiles = static_cast<long long>(s.n_kv_heads) * ((s.max_len + c.n + BN - 1) / BN);
     const int seqs = static_cast<int>(std::min<long long>(std::min(s.batch, kMaxSeqs), std::max((1LL << 30) / tiles, 1LL)));
-    // A step of two tiles of rows takes about half as long again as one of a single one: the last group gets as many CTAs as
-    // that leaves it, if it has but one.
-    const int last_rows = c.n * a.G - (a.groups - 1) * C::ROWS, w = NT == 2 && last_rows <= BM ? 2 : 3;
+    // A step of two tiles of rows takes about 1.4 times as long as one of a single one (the K and V are the same): the last
+    // group, if it has but one tile, gets CTAs by that.  (64 tokens over 32700, 320 rows: 84 us with as many CTAs, 76.5 so, 77.0
+    // with nine tenths of those of the other; 16 sequences over 8000: 240, 250)
+    const int last_rows = c.n * a.G - (a.groups - 1) * C::ROWS, w = NT == 2 && last_rows <= BM ? 7 : 10;
     const long long most = seqs * tiles;
-    a.runs_last = static_cast<int>(std::min<long long>(std::max(c.num_sms * w / (3 * (a.groups - 1) + w), 1), most));
+    a.runs_last = static_cast<int>(std::min<long long>(std::max(c.num_sms * w / (10 * (a.groups - 1) + w), 1), most));
     a.runs = a.groups == 1 ? 0 : static_cast<int>(std::min<long long>(std::max((c.num_sms - a.runs_last) / (a.groups - 1), 1), most));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(a.runs * (a.groups - 1) + a.runs_last));
