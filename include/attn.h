@@ -227,9 +227,9 @@ int attn_set_wait_limit(attn_ctx* ctx, long long limit_ns);
  * Kernel timing (tracing).  The attention entry points launch these kernels (the
  * W4BF16 kernels, which take no context, are not timed):
  *   ATTN_KERNEL_ROPE_APPEND     RoPE of the new keys + in-place cache append (every stage)
- *   ATTN_KERNEL_FLASH_FWD       causal flash attention (prefill, prefill_kv), with the
+ *   ATTN_KERNEL_FLASH_FWD       causal flash attention (prefill, prefill_kv, windowed or not), with the
  *                               merge kernel of its split tail when it runs one
- *   ATTN_KERNEL_DECODE_SPLIT    split-KV decode (decode); it also merges the splits and
+ *   ATTN_KERNEL_DECODE_SPLIT    split-KV decode (decode, windows and trees of new tokens); it also merges the splits and
  *                               writes out itself
  *   ATTN_KERNEL_DECODE_COMBINE  no kernel of this version (the merge is part of the decode)
  * (ATTN_KERNEL_FLASH_FWD also covers the small merge kernel that follows it when

@@ -849,7 +849,7 @@ int run_tree(attn_ctx* c, const uint16_t* q, const uint16_t* k, const uint16_t* 
                            std::min(sinks, c->cfg.max_len), k_cache, v_cache, c->d_cos, c->d_sin, out, c->d_err,
                            &c->dec_maps, c->d_flash_o, c->d_flash_ml, c->d_counters, c->num_sms, c->wait_ns};
     const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    const cudaError_t e = timed(c, ATTN_KERNEL_DECODE_SPLIT, st, [&](int*) { return attn::launch_tree_decode(c->shape, t, st); });
+    const cudaError_t e = timed(c, ATTN_KERNEL_DECODE_SPLIT, st, [&](int* n) { return attn::launch_tree_decode(c->shape, t, st, n); });
     return e == cudaSuccess ? ATTN_OK : cuda_fail(e, "tree decode launch");
 }
 
@@ -868,8 +868,8 @@ int attn_window_decode(attn_ctx* c, const uint16_t* q, const uint16_t* k, const 
                        attn_stream_t stream) {
     if (c == nullptr || window < 1) return ATTN_EINVAL;
     // One token: the heads of a kv head are the columns of a decode's MMAs and the keys their rows, which leaves less to
-    // hand over and to merge than rows of (token, head) do (1 x 8191, window 1024, 32 / 8 heads: 17.8 us as rows, 8.5 as columns; 16 of
-    // up to 8191, window 4096: 84.7, 49.6).
+    // hand over and to merge than rows of (token, head) do (1 x 8191, window 1024, 32 / 8 heads: 13.7 us as rows, 8.5 as
+    // columns; 16 of up to 8191, window 4096: 55.6, 49.7).
     if (n_new == 1 && sinks >= 0 && on_device(c))
         return run_decode(c, q, k, v, d_hist_len, 0, false, k_cache, v_cache, out, reinterpret_cast<cudaStream_t>(stream), 1,
                           false, 0, std::min(window, c->cfg.max_len), std::min(sinks, c->cfg.max_len));

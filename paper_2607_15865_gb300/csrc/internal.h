@@ -200,7 +200,7 @@ struct TreeCall {
     uint64_t wait_ns;
 };
 cudaError_t configure_tree_decode();
-cudaError_t launch_tree_decode(const Shape& s, const TreeCall& c, cudaStream_t st);
+cudaError_t launch_tree_decode(const Shape& s, const TreeCall& c, cudaStream_t st, int* launches);
 // Moves the k and v of token leaf[b] and its ancestors to the slots from d_hist[b] on in every layer's caches; new_len
 // (may be NULL): the lengths after that.
 cudaError_t launch_tree_accept(const Shape& s, const int32_t* d_hist, const int32_t* parents, const int32_t* leaf, int n,

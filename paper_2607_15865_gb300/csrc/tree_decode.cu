@@ -8,20 +8,31 @@
 // of a sequence are those of its first `sinks` slots and those from its first token's window to its last new slot; what
 // lies between is not read.
 //
-// The work: the key tiles of all (sequence, kv head) in order, cut into equal runs, one per CTA (of each row group), from
-// the lengths on the device.  A run's part of an item is a segment; an item in several runs is merged by all the CTAs that
-// have a part of it, each a share of its rows and columns, once all parts are written (a cooperative launch: they wait for one
-// another, at the end of their runs).
+// The work, cut from the lengths on the device: where there are CTAs for all, each item (sequence, kv head, row group) in
+// pieces of about equal length, one per CTA; else the key tiles of all items in order in equal runs, one per CTA, where an
+// item's beginning counts as kHead tiles.  A run's part of an item is a segment; an item in several runs is merged by all the
+// CTAs that have a part of it, each a share of its rows and columns, once all parts are written (a cooperative launch: they
+// wait for one another, at the end of their runs).
+//
+// What bounds it (32 / 8 heads, head_dim 128, in a graph, L2 flushed): many long sequences of few tokens the memory (64 x
+// 8191, one token: 2.15 GB in 321-331 us, 97-100% of the measured copy rate; 16 x up to 8180, 12 tokens: 278 MB in 71 us, 58%, of
+// which 8 us pass before the first scores and 7 in the merges).  Trees of more than 128 rows the MMAs and what passes between
+// two of them (16 x 8100, 64 tokens, 256 rows: 153 us, 2.2 us a step of four MMAs' 1.1; 64 tokens over 32700, 40 heads: 77).
+// Short calls a chain of latencies (8 tokens over 1024: 13.4 us; lengths and plan 1.7, q 2.5, first scores 0.9, softmax 1.0, P V
+// and storing the part 2.3, the merge 2.9, the launch 2), and the fetching of instructions that run but once, so that loops
+// that are not hot are rolled and what several warps need is worked out by one (unrolled and inlined the same call took 28 us).
 //
 // Warps: 4 NT softmax warps (a tile's rows), one TMA producer, one MMA issuer, two guards and, with NT = 1, four stagers.
-//   producer  K and V tiles through a ring of slots, in the order K0, K1, V0, K2, V1, ..
+//   producer  plans the CTA's segments and hands them to the others in shared memory; K and V tiles through a ring of
+//             slots, in the order K0, K1, V0, K2, V1, ..
 //   guards    see the tiles that some row does not see whole between the producer and the issuer.  In one that holds slots of
 //             new tokens they put those in (k rotated), and write them to the cache; in one of V they look for values
 //             that are not finite: 0 x NaN would reach the rows that do not see them.  Those become 0 in shared memory, and
 //             the rows that see them add them to their O at the end (a rare path, from global memory).  They follow the
 //             others too, and a slot of the ring is free when they and the MMAs are through with it.
 //   issuer    NT = 1: S(j + 1) before P V(j), two S buffers, so that a softmax runs beside the MMAs; Q and O have two buffers
-//             each, for the segments in turn.  NT = 2: the tiles' MMAs alternate, each has one S.
+//             each, for the segments in turn.  NT = 2: the tiles' MMAs alternate, each has one S.  The warp stays
+//             converged and one elected lane issues (16 x 8100, 64 tokens: 173 us from a lone lane, 153 so).
 //   stagers   rotate the q rows of the next segments into shared memory, and find their kin.  While the keys stream in, a load
 //             takes two microseconds and more, and between two segments the softmax warps had several to wait for.
 //             (NT = 2 has one Q for both tiles and few segments: the softmax warps do it.)
@@ -36,6 +47,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "flash_rows.h"
 #include "internal.h"
 #include "sm100_ptx.cuh"
 #include "tree.cuh"
@@ -126,12 +138,8 @@ struct Span {
     int ns, skip, nt;
 };
 __device__ __forceinline__ Span span_of(int hist, int n, int window, int sinks) {
-    const int lo = max(0, hist - window + 1), t_lo = lo / BN;  // (the first token's window is the lowest)
-    Span s;
-    s.ns = min((min(sinks, lo) + BN - 1) / BN, t_lo);
-    s.skip = t_lo - s.ns;
-    s.nt = (hist + n + BN - 1) / BN - s.skip;
-    return s;
+    const WindowWalk w = window_walk(hist, hist, window, sinks, BN);  // (the first token's window is the lowest)
+    return {w.ns, w.skip, (hist + n + BN - 1) / BN - w.skip};
 }
 
 // A CTA's part of an item: its tiles lo .. hi - 1, as the planner writes it into shared memory.
@@ -655,7 +663,7 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                     mbar_wait(bar(C::B_FULL + i % C::NS), (i / C::NS) & 1u, nullptr);
         } else if (warp == kWarpMma) {
             // ------------------------------------------------------------ issuer
-            // The warp stays converged and one elected lane issues: what the MMAs take is in uniform registers then.
+            // (converged: what the MMAs take is in uniform registers then)
             constexpr uint32_t kIdS = idesc_bf16_f32(BM, BN, false, false);
             constexpr uint32_t kIdPV = idesc_bf16_f32(BM, D, false, true);
             constexpr uint32_t kHi = desc_hi_sw128(1024);
@@ -1279,7 +1287,7 @@ cudaError_t configure() {
 }
 
 template <int D, int NT>
-cudaError_t launch(const Shape& s, const TreeCall& c, const Args& args, cudaStream_t st) {
+cudaError_t launch(const Shape& s, const TreeCall& c, const Args& args, cudaStream_t st, int* launches) {
     using C = Cfg<D, NT>;
     Args a = args;
     a.groups = (c.n * a.G + C::ROWS - 1) / C::ROWS;
@@ -1307,6 +1315,7 @@ cudaError_t launch(const Shape& s, const TreeCall& c, const Args& args, cudaStre
         a.batch = std::min(s.batch - a.b0, seqs);
         const cudaError_t e = cudaLaunchKernelEx(&cfg, tree_decode_kernel<D, NT>, c.maps->k, c.maps->v, a);
         if (e != cudaSuccess) return e;
+        ++*launches;
     }
     return cudaSuccess;
 }
@@ -1321,7 +1330,8 @@ cudaError_t configure_tree_decode() {
     return e;
 }
 
-cudaError_t launch_tree_decode(const Shape& s, const TreeCall& c, cudaStream_t st) {
+cudaError_t launch_tree_decode(const Shape& s, const TreeCall& c, cudaStream_t st, int* launches) {
+    *launches = 0;
     Args a = {};
     a.q = c.q;
     a.k_new = c.k;
@@ -1348,8 +1358,8 @@ cudaError_t launch_tree_decode(const Shape& s, const TreeCall& c, cudaStream_t s
     a.sinks = c.sinks;
     // a second tile of rows where one does not hold them all: it halves the passes over the keys
     const bool two = c.n * a.G > BM;
-    if (s.head_dim == 128) return two ? launch<128, 2>(s, c, a, st) : launch<128, 1>(s, c, a, st);
-    return two ? launch<64, 2>(s, c, a, st) : launch<64, 1>(s, c, a, st);
+    if (s.head_dim == 128) return two ? launch<128, 2>(s, c, a, st, launches) : launch<128, 1>(s, c, a, st, launches);
+    return two ? launch<64, 2>(s, c, a, st, launches) : launch<64, 1>(s, c, a, st, launches);
 }
 
 cudaError_t launch_tree_accept(const Shape& s, const int32_t* d_hist, const int32_t* parents, const int32_t* leaf, int n,
