@@ -60,8 +60,8 @@ _shape, _dtype, _is_cuda = map(operator.attrgetter, ("shape", "dtype", "is_cuda"
 def _ptrs(tensors, name: str, shape) -> list:
     # _ptr of many tensors of one shape, an attribute of all at a time (three quarters of the time of 64 calls of it)
     try:
-        if (all(map(torch.Tensor.is_contiguous, tensors)) and all(map(_is_cuda, tensors))
-                and list(map(_dtype, tensors)).count(torch.bfloat16) == len(tensors)
+        if (len(tensors) > 4 and all(map(torch.Tensor.is_contiguous, tensors))
+                and all(map(_is_cuda, tensors)) and list(map(_dtype, tensors)).count(torch.bfloat16) == len(tensors)
                 and list(map(_shape, tensors)).count(shape) == len(tensors)):
             return list(map(torch.Tensor.data_ptr, tensors))
     except (TypeError, AttributeError):  # (not a tensor)

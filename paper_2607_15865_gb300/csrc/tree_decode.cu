@@ -17,7 +17,7 @@
 // What bounds it (32 / 8 heads, head_dim 128, in a graph, L2 flushed): many long sequences of few tokens the memory (64 x
 // 8191, one token: 2.15 GB in 321-331 us, 97-100% of the measured copy rate; 16 x up to 8180, 12 tokens: 278 MB in 71 us, 58%, of
 // which 8 us pass before the first scores and 7 in the merges).  Trees of more than 128 rows the MMAs and what passes between
-// two of them (16 x 8100, 64 tokens, 256 rows: 153 us, 2.2 us a step of four MMAs' 1.1; 64 tokens over 32700, 40 heads: 77).
+// two of them (16 x 8100, 64 tokens, 256 rows: 141 us, 2.2 us a step whose MMAs take 1.1; 64 tokens over 32700, 40 heads: 77).
 // Short calls a chain of latencies (8 tokens over 1024: 13.4 us; lengths and plan 1.7, q 2.5, first scores 0.9, softmax 1.0, P V
 // and storing the part 2.3, the merge 2.9, the launch 2), and the fetching of instructions that run but once, so that loops
 // that are not hot are rolled and what several warps need is worked out by one (unrolled and inlined the same call took 28 us).
@@ -62,7 +62,9 @@ constexpr uint32_t kTmemCols = 512;  // S [0, 256): two of 128; O [256, 256 + 2 
 constexpr uint32_t kTmO = 2 * BN;
 constexpr int kFlags = 8;
 constexpr int kSegs = 8;  // segments in shared memory: the producer is at most NS / 2 + 2 ahead of every reader
-constexpr int kLonger = 4;  // tiles that a piece may be longer than a run
+// Tiles that a piece may be longer than a run, and one that is a whole item: runs have two segments and two merges each
+// (16 x 8100: 64 tokens 153 us in runs of 54 tiles, 142 as items of 64; 8 tokens 106, 103).
+constexpr int kLonger = 4, kWholeLonger = 10;
 // Items of up to so many tiles are not shared: walking them takes no longer than meeting does (8 tokens over 200, 2 tiles: 12.1 to
 // 10.3 us; over 300, 3 tiles: 12.5, 11.4; over 400, 4 tiles: 12.2, 12.6).
 constexpr int kAlone = 3;
@@ -192,7 +194,8 @@ struct Plan {
         len = 0;
 #pragma unroll 1
         for (;; target += max(target >> 5, 1)) {
-            if (target > least + kLonger) {
+            if (target > least + kLonger && target < most && most <= least + kWholeLonger) target = most;
+            if (target > least + kLonger && target != most) {
                 len = max((__reduce_add_sync(0xFFFFFFFFu, places) + runs - 1) / runs, 1);
                 break;
             }
