@@ -127,6 +127,9 @@ struct Args {
     int groups, runs, runs_last;  // row groups; runs of each, of the last
 };
 
+// a / b of numbers that are not negative.
+__device__ __forceinline__ int quot(int a, int b) { return static_cast<int>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)); }
+
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
@@ -185,7 +188,7 @@ struct Plan {
         }
         if (bad && report) atomicOr(a.err, kDevErrHistRange);
         // Pieces, if there are CTAs for all and they are hardly longer than the runs would be: a CTA then has but one segment.
-        const int least = max((__reduce_add_sync(0xFFFFFFFFu, tiles) + runs - 1) / runs, 1);
+        const int least = max(quot(__reduce_add_sync(0xFFFFFFFFu, tiles) + runs - 1, runs), 1);
         int most = 0;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) most = max(most, t[i]);
@@ -196,18 +199,18 @@ struct Plan {
         for (;; target += max(target >> 5, 1)) {
             if (target > least + kLonger && target < most && most <= least + kWholeLonger) target = most;
             if (target > least + kLonger && target != most) {
-                len = max((__reduce_add_sync(0xFFFFFFFFu, places) + runs - 1) / runs, 1);
+                len = max(quot(__reduce_add_sync(0xFFFFFFFFu, places) + runs - 1, runs), 1);
                 break;
             }
             int pieces = 0;
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) pieces += (t[i] + target - 1) / target * a.Hkv;
+            for (int i = 0; i < kPer; ++i) pieces += quot(t[i] + target - 1, target) * a.Hkv;
             if (__reduce_add_sync(0xFFFFFFFFu, pieces) <= runs) break;
         }
         int sum = 0;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            sum += (len == 0 ? (t[i] + target - 1) / target : t[i] > 0 ? t[i] + kHead : 0) * a.Hkv;
+            sum += (len == 0 ? quot(t[i] + target - 1, target) : t[i] > 0 ? t[i] + kHead : 0) * a.Hkv;
             upto[i] = sum;
         }
         int all = sum;
@@ -245,8 +248,8 @@ struct Plan {
         const int hidden = s.hist + a.n - 1 - a.window;  // the last token's window begins behind that slot
         s.edge = hidden < 0 ? 0 : max(hidden / BN + 1 - p.skip, 0);
         s.diag = s.hist / BN - p.skip;
-        const int per = len == 0 ? (p.nt + target - 1) / target : p.nt + kHead;  // pieces or places of an item
-        s.h = (pos - start) / per;
+        const int per = len == 0 ? quot(p.nt + target - 1, target) : p.nt + kHead;  // pieces or places of an item
+        s.h = quot(pos - start, per);
         start += s.h * per;
         sh.b = s.b;
         sh.h = s.h;
@@ -254,8 +257,8 @@ struct Plan {
         sh.slot0 = s.part = 0;
         if (len == 0) {
             const int i = pos - start;
-            s.lo = p.nt * i / per;
-            s.hi = p.nt * (i + 1) / per;
+            s.lo = quot(p.nt * i, per);
+            s.hi = quot(p.nt * (i + 1), per);
             sh.first = start;
             sh.count = per;
             pos = end;
@@ -265,8 +268,8 @@ struct Plan {
             s.hi = min(p.nt, end - first);
             if (s.hi <= 0) return false;  // (the run ends before the item's tiles)
             // Slot 0 where the item began by the run's start, 1 where it began in it.
-            sh.first = first / len;
-            sh.count = (first + p.nt - 1) / len - sh.first + 1;
+            sh.first = quot(first, len);
+            sh.count = quot(first + p.nt - 1, len) - sh.first + 1;
             sh.slot0 = first > sh.first * len ? 1 : 0;
             s.part = run_id == sh.first ? sh.slot0 : 0;
             pos = first + s.hi;
@@ -1120,7 +1123,7 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                 }
                 if (ok && did[slot] == 1) {
                     const int blocks = (group_rows + 31) / 32, share = (run_id - sh.first) * warps + warp;
-                    const int blk = share % blocks, part = share / blocks, of = (all - blk + blocks - 1) / blocks;
+                    const int part = quot(share, blocks), blk = share - part * blocks, of = quot(all - blk + blocks - 1, blocks);
                     const int row = blk * 32 + lane, R = group * C::ROWS + row;
                     const int tok = min(R, a.n * a.G - 1) / a.G;
                     // part p is in slot 0 of CTA `cta0` + p * step, the first one in slot sh.slot0 of cta0
@@ -1130,7 +1133,7 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                         // Item i of this thread: part i % parts of values d0 + i / parts.  A batch of them is loaded at once, the first
                         // one beside the (m, l) of all parts: one after the other, each load would be waited for.
                         constexpr int BATCH = 8;
-                        const int d0 = D / 4 * part / of, items = (D / 4 * (part + 1) / of - d0) * parts;
+                        const int d0 = quot(D / 4 * part, of), items = (quot(D / 4 * (part + 1), of) - d0) * parts;
                         float4 o[BATCH];
                         float2 ml[BATCH];
                         float m = -INFINITY, l = 0.f, inv = 0.f;
