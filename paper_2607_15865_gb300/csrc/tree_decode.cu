@@ -172,12 +172,18 @@ struct Plan {
     int hist[kPer], upto[kPer];
     int pos, end, len, target;
 
+    __device__ __forceinline__ void load(const Args& a, int lane) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            hist[i] = 0;
+            if (kPer * lane + i < a.batch) asm volatile("ld.global.s32 %0, [%1];" : "=r"(hist[i]) : "l"(a.d_hist + a.b0 + kPer * lane + i));
+        }
+    }
+
     // The lengths' places, summed, and this CTA's: of `runs`, the run run_id.
     __device__ __forceinline__ void init(const Args& a, int runs, int run_id, int lane, bool report) {
         int t[kPer], tiles = 0, places = 0;
         bool bad = false;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) hist[i] = kPer * lane + i < a.batch ? __ldg(a.d_hist + a.b0 + kPer * lane + i) : 0;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const bool here = kPer * lane + i < a.batch, good = hist[i] >= 0 && hist[i] <= a.max_len;
@@ -528,7 +534,10 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
     const int group_rows = min(C::ROWS, a.n * a.G - group * C::ROWS);
     const int live = NT == 1 || group_rows <= BM ? 1 : 2;  // tiles with rows
 
-    if (warp == kWarpTma && lane == 0) {
+    // Warp 0 sets up the barriers, the planner its plan, the others what is below.  (volatile: the lengths' loads come first)
+    Plan plan;
+    if (warp == kWarpTma) plan.load(a, lane);
+    if (warp == 0 && lane == 0) {
         *abort_flag = 0;
         for (int i = 0; i < kFlags; ++i) odd_flag[i] = 0;
         for (int i = 0; i < C::NS; ++i) {
@@ -564,10 +573,12 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
     }
     // What the segments start with, on its way into L2 before the keys are: this CTA's share of q, of the new k and v, and of the
     // angles of the new positions.
-    {
+    if (warp != kWarpTma) {
         auto prefetch = [](const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); };
         const size_t lines = static_cast<size_t>(a.batch) * a.n * a.Hkv * (D / 64), first = static_cast<size_t>(a.b0) * a.n * a.Hkv * D;
-        const size_t at = static_cast<size_t>(blockIdx.x) * C::THREADS + threadIdx.x, step = static_cast<size_t>(gridDim.x) * C::THREADS;
+        constexpr int THREADS = C::THREADS - 32;  // (all but the planner's)
+        const size_t at = static_cast<size_t>(blockIdx.x) * THREADS + threadIdx.x - (warp > kWarpTma ? 32 : 0),
+                     step = static_cast<size_t>(gridDim.x) * THREADS;
 #pragma unroll 1
         for (size_t i = at; i < lines * a.G; i += step) prefetch(a.q + first * a.G + 64 * i);
 #pragma unroll 1
@@ -587,7 +598,6 @@ __global__ void __launch_bounds__(Cfg<D, NT>::THREADS, 1)
                 }
             }
     }
-    Plan plan;
     if (warp == kWarpTma) plan.init(a, runs, run_id, lane, cta == 0);
     tc_fence_before();
     __syncthreads();
