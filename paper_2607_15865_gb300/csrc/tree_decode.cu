@@ -15,10 +15,10 @@
 // wait for one another, at the end of their runs).
 //
 // What bounds it (32 / 8 heads, head_dim 128, in a graph, L2 flushed): many long sequences of few tokens the memory (64 x
-// 8191, one token: 2.15 GB in 321-331 us, 97-100% of the measured copy rate; 16 x up to 8180, 12 tokens: 278 MB in 71 us, 58%, of
+// 8191, one token: 2.15 GB in 321-331 us, 97-100% of the measured copy rate; 16 x up to 8180, 12 tokens: 278 MB in 70 us, 60%, of
 // which 8 us pass before the first scores and 7 in the merges).  Trees of more than 128 rows the MMAs and what passes between
-// two of them (16 x 8100, 64 tokens, 256 rows: 141 us, 2.2 us a step whose MMAs take 1.1; 64 tokens over 32700, 40 heads: 77).
-// Short calls a chain of latencies (8 tokens over 1024: 13.4 us; lengths and plan 1.7, q 2.5, first scores 0.9, softmax 1.0, P V
+// two of them (16 x 8100, 64 tokens, 256 rows: 138 us, 2.2 us a step whose MMAs take 1.1; 64 tokens over 32700, 40 heads: 76).
+// Short calls a chain of latencies (8 tokens over 1024: 12.9 us; lengths and plan 1.5, q 2.5, first scores 0.9, softmax 1.0, P V
 // and storing the part 2.3, the merge 2.9, the launch 2), and the fetching of instructions that run but once, so that loops
 // that are not hot are rolled and what several warps need is worked out by one (unrolled and inlined the same call took 28 us).
 //
