@@ -17,7 +17,8 @@ def attention(B, Hq, Hkv, D, L):
 # many short items per CTA, among some that several share; one, two and three groups of rows, the last of them with one tile and two
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("B,Hq,Hkv,n,window", [(60, 32, 8, 2, 0), (100, 16, 8, 9, 150), (20, 32, 8, 40, 0), (30, 40, 8, 64, 0),
-                                               (12, 16, 1, 40, 400), (9, 64, 4, 24, 0), (33, 16, 16, 64, 90)])
+                                               (12, 16, 1, 40, 400), (9, 64, 4, 24, 0), (33, 16, 16, 64, 90),
+                                               (130, 10, 2, 60, 0)])
 def test_many_segments(D, B, Hq, Hkv, n, window):
     r = np.random.default_rng([D, B, n])
     L = 1500
@@ -83,3 +84,26 @@ def test_waits_that_run_out(D, B, Hq, Hkv, n, lens):
         attn.set_wait_limit(0)
     U.check(attn, new, lens, parents, 0, 0, tag + " tree after", kc=kc, vc=vc)
     U.check(attn, new, lens, None, W, 4, tag + " window after", kc=kc, vc=vc)
+
+
+def test_two_contexts_at_once():
+    """Calls of two contexts on two streams, whose CTAs wait for others of their own launch: the same as one after the other."""
+    import torch
+    runs = []
+    for i, (Hq, Hkv, n, hist) in enumerate(((32, 8, 8, 2900), (40, 8, 30, 1500))):
+        attn = attention(1, Hq, Hkv, 128, 3000)
+        args = [U.dev(x) for x in U.new_tokens(f"two{i}", 1, n, Hq, Hkv, 128)]
+        kc, vc = (U.dev(x) for x in U.history(f"two{i}", 1, Hkv, 3000, 128, [hist]))
+        lens, par = U.dev_i32([hist]), U.dev_i32([U.random_tree(i, n, 4)])
+        runs.append((attn, lambda out=None, s=None, a=attn, x=(*args, lens, par, kc, vc): a.tree_decode(*x, out=out, stream=s)))
+    alone = [call() for _, call in runs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in runs]
+    outs = [[torch.zeros_like(x) for _ in range(10)] for x in alone]
+    torch.cuda.synchronize()
+    for k in range(10):
+        for (_, call), s, out in zip(runs, streams, outs):
+            call(out[k], s)
+    torch.cuda.synchronize()
+    for (attn, _), ref, out in zip(runs, alone, outs):
+        assert attn.device_error() == 0 and all(torch.equal(x, ref) for x in out)
